@@ -255,7 +255,7 @@ def _own_append(state):
 def _own_pages(state):
     from paper_2402_11809_b200 import binding as S
     if "call" not in state:
-        state["call"] = [S.page_pool(p) for p in state["pools"]]
+        state["call"] = S.page_pools(state["pools"])
     S.space_pages_copy(state["call"], state["moves"])
     return state["pools"]
 
