@@ -59,9 +59,11 @@ enum {
   SPACE_ST_CAPACITY      = 1,  /* kv_len + (k+1)^2 exceeds the cache capacity */
   SPACE_ST_BAD_CANDIDATE = 2,  /* a candidate id outside [0, vocab): rejected */
   SPACE_ST_TIMEOUT       = 4,  /* a bounded on-chip wait expired              */
-  SPACE_ST_BAD_PAGE      = 8   /* a page-table entry outside [0, n_pages): that page is not
+  SPACE_ST_BAD_PAGE      = 8,  /* a page-table entry outside [0, n_pages): that page is not
                                   touched (attention reads zeros in its place, the commit skips
                                   the row)                                     */
+  SPACE_ST_NONFINITE     = 16  /* a row handed to the 4-bit cache (space_kvq_*) held a NaN, counted
+                                  as 0, or an infinity, counted as the largest finite bf16       */
 };
 
 typedef struct space_ctx space_ctx;   /* opaque; owns only its own workspace */
@@ -431,6 +433,129 @@ typedef struct {
 } space_sar_args;
 int space_sar_sft_transform(const space_sar_args* args, void* stream);
 
+/* ---- KV cache in 4 bits ------------------------------------------------------------------------
+ * (No counterpart in the paper: what a step costs at serving lengths is reading the cache, and a cache in
+ * 4 bits is about a quarter of the bf16 one.)  Paged like the bf16 cache: a pool of pages of
+ * SPACE_PAGE_SIZE rows behind a page table, row s of sequence b in row s % SPACE_PAGE_SIZE of page
+ * page_table[b * pages_per_seq + s / SPACE_PAGE_SIZE], K and V of a row in the same page.
+ *
+ * A row of d channels x is held as 4-bit codes u with one step and one lowest value, both bf16:
+ *   lo = min x,   step = bf16(max((max x - lo) / 15, max|x| / 4096, 2^-100)),
+ *   u = min(round((x - lo) / step), 15) (ties to even),   and stands for lo + step * u.
+ * NaN counts as 0 and an infinity as the largest finite bf16 (SPACE_ST_NONFINITE).
+ *
+ * Bytes of a page, per kv head (head_stride apart): 4 blocks of 32 rows, each
+ *   K codes  [32][d/2]: byte i of a row holds channels 2i (low four bits) and 2i + 1
+ *   V codes  [32 d / 2]: channel c = 32w + 8q + n of row r = 16a + 8e + 2t + h in byte
+ *            512w + 64n + 16t + 8a + 4e + 2h + q/2, low four bits for even q
+ *   K steps  [32] {bf16 step, bf16 lo}, V steps [32] {bf16 step, bf16 lo}
+ * i.e. 32 d + 256 bytes a block: the order in which the attention's tensor-core operands are unpacked. */
+typedef struct {
+  void*   pool;                /* device, 16-byte aligned                                          */
+  int64_t page_stride;         /* bytes, multiples of 16; several layers may share one allocation  */
+  int64_t head_stride;         /* bytes, at least 4 * (32 d + 256)                                 */
+  const int32_t* page_table;   /* device [B, pages_per_seq]                                        */
+  int32_t pages_per_seq;
+  int32_t n_pages;             /* pages in the pool                                                */
+} space_kvq_cache;
+
+/* Bytes of one page of a contiguous pool: n_kv_heads * 4 * (32 head_dim + 256); 0 for a head_dim other
+ * than 64 and 128.  Host only. */
+int64_t space_kvq_page_bytes(int32_t n_kv_heads, int32_t head_dim);
+
+/* Puts rows behind the cached ones: row g * row_step of k_new / v_new becomes cache row kv_len[b] + g for
+ * g < count[b] + count_bias (at least 0, at most what `rows` holds).  A prompt's rows or one new token:
+ * row_step = 1; the accepted rows of a step out of its block rows: row_step = k + 1, count = n_accept,
+ * count_bias = 1.  A sequence with kv_len < 0, or whose rows would not fit pages_per_seq pages, is left as
+ * it is (SPACE_ST_CAPACITY); rows of a page outside the pool are skipped (SPACE_ST_BAD_PAGE).
+ * Asynchronous on `stream`.  Errors: INVALID_ARG, ALIGNMENT, WORKSPACE (batch beyond the context's), CUDA. */
+typedef struct {
+  int32_t batch;
+  int32_t rows;                /* rows per sequence in k_new / v_new                               */
+  int32_t row_step;            /* >= 1                                                             */
+  int32_t count_bias;
+  const void* k_new;           /* device bf16, element (b, r, h, :) at b*stride_b + r*stride_r + h*stride_h */
+  const void* v_new;           /*   (elements, multiples of 8; base 16-byte aligned), d contiguous  */
+  int64_t new_stride_b, new_stride_r, new_stride_h;
+  space_kvq_cache cache;
+  const int32_t* kv_len;       /* device [B] lengths before the call                               */
+  const int32_t* count;        /* device [B], or NULL: all of `rows` (every row_step-th)           */
+  int32_t* kv_len_out;         /* device [B] lengths after, or NULL; must not be kv_len            */
+  int32_t* status;             /* device [B], OR-ed, or NULL                                       */
+} space_kvq_append_args;
+int space_kvq_append(space_ctx* ctx, const space_kvq_append_args* args, void* stream);
+
+/* Reads cache rows first[b] .. first[b] + rows - 1 back as the bf16 values nearest to what they stand for;
+ * rows below 0, at kv_len[b] and beyond, or of a page outside the pool (SPACE_ST_BAD_PAGE) are written as
+ * zeros.  Asynchronous on `stream`.  Errors: as space_kvq_append. */
+typedef struct {
+  int32_t batch;
+  int32_t rows;
+  space_kvq_cache cache;
+  const int32_t* kv_len;       /* device [B]                                                       */
+  const int32_t* first;        /* device [B], or NULL (0)                                          */
+  void* k_out;                 /* device bf16, element (b, r, h, :) at b*stride_b + r*stride_r + h*stride_h */
+  void* v_out;                 /*   (elements, multiples of 8; base 16-byte aligned), d contiguous  */
+  int64_t out_stride_b, out_stride_r, out_stride_h;
+  int32_t* status;             /* device [B], OR-ed, or NULL                                       */
+} space_kvq_read_args;
+int space_kvq_read(space_ctx* ctx, const space_kvq_read_args* args, void* stream);
+
+/* Attention of a step's block rows over a 4-bit cache: softmax(scale q k^T) v over cache rows
+ * 0 .. kv_len[b]-1 and, with k_new / v_new, over the block's own rows (bf16, not in the cache yet) as Eq. 5
+ * shows them.  k = 0 is one row per sequence, plain token-by-token decoding.  Without k_new / v_new every
+ * row sees the cache alone (a token whose row has been appended before); a row that sees nothing at all
+ * (an empty cache) gives zeros and lse = -inf, and so does every row of a sequence with kv_len outside
+ * 0 .. pages_per_seq * SPACE_PAGE_SIZE (SPACE_ST_CAPACITY).  Keys of a page outside the pool are left out
+ * (SPACE_ST_BAD_PAGE).  Hidden rows have no influence, whatever they hold; non-finite elements of k_new /
+ * v_new count as they do in space_kvq_append (without the status bit).
+ * The output is bf16: scores and sums are fp32, the weights of the second product are rounded to 11 bits.
+ * Asynchronous on `stream`, no allocation; one call at a time per context (scratch of the context).
+ * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE (batch or k beyond the context's), CUDA. */
+typedef struct {
+  int32_t batch;
+  int32_t k;                   /* 0 .. k_max; (k+1)^2 query rows                                   */
+  int32_t mask_variant;        /* SPACE_MASK_*                                                     */
+  float   scale;               /* > 0, normally 1/sqrt(d)                                          */
+  const void* q;               /* device bf16, element (b, i, h, :) at b*stride_b + i*stride_r + h*stride_h */
+  int64_t q_stride_b, q_stride_r, q_stride_h;          /* elements, multiples of 8                 */
+  const void* k_new;           /* device bf16 [B, n_q, H_kv, d] by strides, or NULL together with v_new */
+  const void* v_new;
+  int64_t new_stride_b, new_stride_r, new_stride_h;
+  space_kvq_cache cache;
+  const int32_t* kv_len;       /* device [B] rows cached                                           */
+  void*    out;                /* device bf16 [B, n_q, H_q, d]                                     */
+  float*   lse;                /* device [B, H_q, n_q] natural-log sum-exp, or NULL                */
+  int32_t* status;             /* device [B], OR-ed, or NULL                                       */
+} space_kvq_attn_args;
+int space_kvq_attn_step(space_ctx* ctx, const space_kvq_attn_args* args, void* stream);
+
+/* ---- Moving pages ------------------------------------------------------------------------------
+ * Rows 0 .. rows-1 of page src become those of page dst, for every move and in every pool (the pools of all
+ * layers, K and V, share their page numbers), in one launch per SPACE_PAGES_MAX_MOVES moves: what a fork's
+ * copy-on-write and a compaction (space_pager_make_writable, space_pager_compact) hand out.
+ * A page is `parts` pieces, part_stride apart, of rows in groups of group_rows, group_bytes each; of a
+ * group that `rows` ends in all is copied.  bf16 pool [n_pages, H_kv, 128, d]: one pool for K, one for V,
+ * parts = H_kv, group_rows = 1, group_bytes = 2 d.  4-bit pool: parts = H_kv, group_rows = 32,
+ * group_bytes = 32 d + 256.  No page may be written twice in a call, or both read and written.
+ * Both lists are host memory, read before the call returns; no context, current device, asynchronous on
+ * `stream`, no allocation on the device.
+ * Errors: INVALID_ARG (sizes, pages, overlap), ALIGNMENT (base, strides and group_bytes not multiples of 16), CUDA. */
+#define SPACE_PAGES_MAX_POOLS 256
+#define SPACE_PAGES_MAX_MOVES 1024
+typedef struct {
+  void*   base;                /* device                                                           */
+  int64_t page_stride;         /* bytes                                                            */
+  int64_t part_stride;         /* bytes                                                            */
+  int32_t parts;
+  int32_t group_rows;          /* divides SPACE_PAGE_SIZE                                          */
+  int32_t group_bytes;
+  int32_t n_pages;
+} space_page_pool;
+typedef struct { int32_t src, dst, rows; } space_page_move;
+int space_pages_copy(const space_page_pool* pools, int32_t n_pools, const space_page_move* moves, int32_t n_moves,
+                     void* stream);
+
 /* Number of kernels this context has launched so far. */
 int64_t space_launch_count(const space_ctx* ctx);
 
@@ -489,6 +614,23 @@ int32_t space_pager_free_pages(const space_pager* p);
 int32_t space_pager_rows(const space_pager* p, int32_t slot);   /* rows reserved for the slot, -1 if unused */
 int  space_pager_batch_table(const space_pager* p, const int32_t* slots, int32_t n,
                              int32_t* table_out);               /* host [n, pages_per_seq]; -1 = no page */
+
+/* Sequences that share pages.  A fork holds the pages of its parent's first n_rows rows and no copy of them;
+ * a page returns to the pool when the last slot that holds it gives it up (release, truncate).  Before a slot's rows
+ * from first_row on are written (they, and whatever the same pages hold behind them, are not kept),
+ * space_pager_make_writable gives it pages of its own for rows first_row .. first_row + n_rows - 1 where it
+ * shares them, and lists the moves that carry the rows before first_row over; the caller runs them
+ * (space_pages_copy) before the write.  The rows must have been reserved.
+ * space_pager_compact renumbers pages so that those in use come to stand at the pool's start: it takes the
+ * highest page in use to the lowest free one, at most max_moves times (*n_moves = 0: nothing left to move); batch
+ * tables have to be written anew, and the moves run before the next call on the cache.
+ * Errors: INVALID_ARG, WORKSPACE (no free slot, not enough free pages or room for the moves: nothing has changed). */
+int  space_pager_fork(space_pager* p, int32_t parent, int32_t n_rows, int32_t* slot);
+int  space_pager_make_writable(space_pager* p, int32_t slot, int32_t first_row, int32_t n_rows,
+                               space_page_move* moves, int32_t max_moves, int32_t* n_moves);
+int  space_pager_truncate(space_pager* p, int32_t slot, int32_t n_rows);  /* pages past n_rows rows are given up */
+int  space_pager_compact(space_pager* p, space_page_move* moves, int32_t max_moves, int32_t* n_moves);
+int32_t space_pager_page_refs(const space_pager* p, int32_t page);        /* slots that hold it; -1: no such page */
 
 const char* space_strerror(int code);
 

@@ -16,6 +16,7 @@ verify     Algorithm 1 verification: greedy and rejection sampling
 commit     compaction of accepted rows into the verified cache
 lmhead     output projection (hidden states x output embedding) followed by greedy
            verification: the end of the model call of Algorithm 1 and the loop after it
+kvq        the 4-bit cache: what a row is held as, where its bytes lie, attention over it
 bf16       exact bf16 <-> float conversion helpers
 
 Parity pins: every function here is pinned by a CPU test (tests/test_oracle_*.py);

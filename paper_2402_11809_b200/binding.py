@@ -22,7 +22,7 @@ MODE_GREEDY, MODE_SAMPLE = 0, 1
 RESAMPLE_RESIDUAL_POINTMASS, RESAMPLE_PAPER_LITERAL, RESAMPLE_RESIDUAL_DRAFT = 0, 1, 2
 DTYPE_BF16, DTYPE_F32 = 0, 1
 ATTN_TENSOR, ATTN_SIMT, ATTN_TENSOR_ROWS = 0, 1, 2
-ST_CAPACITY, ST_BAD_CANDIDATE, ST_TIMEOUT, ST_BAD_PAGE = 1, 2, 4, 8
+ST_CAPACITY, ST_BAD_CANDIDATE, ST_TIMEOUT, ST_BAD_PAGE, ST_NONFINITE = 1, 2, 4, 8, 16
 PAGE_SIZE = 128
 
 EXPORTS = ["space_create", "space_destroy", "space_workspace_bytes", "space_layout",
@@ -33,7 +33,10 @@ EXPORTS = ["space_create", "space_destroy", "space_workspace_bytes", "space_layo
            "space_launch_count", "space_profile_enable", "space_profile_read",
            "space_debug_philox", "space_debug_wait_timeout", "space_strerror",
            "space_pager_create", "space_pager_destroy", "space_pager_admit", "space_pager_reserve",
-           "space_pager_release", "space_pager_free_pages", "space_pager_rows", "space_pager_batch_table"]
+           "space_pager_release", "space_pager_free_pages", "space_pager_rows", "space_pager_batch_table",
+           "space_pager_fork", "space_pager_make_writable", "space_pager_truncate", "space_pager_compact",
+           "space_pager_page_refs", "space_kvq_page_bytes", "space_kvq_append", "space_kvq_read",
+           "space_kvq_attn_step", "space_pages_copy"]
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -132,6 +135,41 @@ class HostStepArgs(C.Structure):
                 ("cache_resident", C.c_int32), ("reserved", C.c_int32)]
 
 
+class KvqCache(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("page_table", C.c_void_p), ("pages_per_seq", C.c_int32), ("n_pages", C.c_int32)]
+
+
+class KvqAppendArgs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("rows", C.c_int32), ("row_step", C.c_int32), ("count_bias", C.c_int32),
+                ("k_new", C.c_void_p), ("v_new", C.c_void_p), ("new_stride_b", C.c_int64),
+                ("new_stride_r", C.c_int64), ("new_stride_h", C.c_int64), ("cache", KvqCache),
+                ("kv_len", C.c_void_p), ("count", C.c_void_p), ("kv_len_out", C.c_void_p), ("status", C.c_void_p)]
+
+
+class KvqReadArgs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("rows", C.c_int32), ("cache", KvqCache), ("kv_len", C.c_void_p),
+                ("first", C.c_void_p), ("k_out", C.c_void_p), ("v_out", C.c_void_p), ("out_stride_b", C.c_int64),
+                ("out_stride_r", C.c_int64), ("out_stride_h", C.c_int64), ("status", C.c_void_p)]
+
+
+class KvqAttnArgs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("k", C.c_int32), ("mask_variant", C.c_int32), ("scale", C.c_float),
+                ("q", C.c_void_p), ("q_stride_b", C.c_int64), ("q_stride_r", C.c_int64), ("q_stride_h", C.c_int64),
+                ("k_new", C.c_void_p), ("v_new", C.c_void_p), ("new_stride_b", C.c_int64),
+                ("new_stride_r", C.c_int64), ("new_stride_h", C.c_int64), ("cache", KvqCache),
+                ("kv_len", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("status", C.c_void_p)]
+
+
+class PagePool(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("page_stride", C.c_int64), ("part_stride", C.c_int64), ("parts", C.c_int32),
+                ("group_rows", C.c_int32), ("group_bytes", C.c_int32), ("n_pages", C.c_int32)]
+
+
+class PageMove(C.Structure):
+    _fields_ = [("src", C.c_int32), ("dst", C.c_int32), ("rows", C.c_int32)]
+
+
 lib.space_create.argtypes = [C.POINTER(C.c_void_p), C.POINTER(Config)]
 lib.space_create.restype = C.c_int
 lib.space_destroy.argtypes = [C.c_void_p]
@@ -142,7 +180,8 @@ lib.space_layout.argtypes = [C.c_int, C.c_int, C.POINTER(Layout)]
 lib.space_layout.restype = C.c_int
 for _name, _arg in (("space_attn_step", AttnArgs), ("space_verify", VerifyArgs),
                     ("space_kv_commit", CommitArgs), ("space_step_host", HostStepArgs),
-                    ("space_lmhead_verify", LmHeadArgs)):
+                    ("space_lmhead_verify", LmHeadArgs), ("space_kvq_append", KvqAppendArgs),
+                    ("space_kvq_read", KvqReadArgs), ("space_kvq_attn_step", KvqAttnArgs)):
     getattr(lib, _name).argtypes = [C.c_void_p, C.POINTER(_arg), C.c_void_p]
     getattr(lib, _name).restype = C.c_int
 lib.space_sar_sft_transform.argtypes = [C.POINTER(SarArgs), C.c_void_p]
@@ -183,6 +222,21 @@ lib.space_pager_rows.argtypes = [C.c_void_p, C.c_int32]
 lib.space_pager_rows.restype = C.c_int32
 lib.space_pager_batch_table.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
 lib.space_pager_batch_table.restype = C.c_int
+lib.space_pager_fork.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_int32)]
+lib.space_pager_fork.restype = C.c_int
+lib.space_pager_make_writable.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
+                                          C.POINTER(C.c_int32)]
+lib.space_pager_make_writable.restype = C.c_int
+lib.space_pager_truncate.argtypes = [C.c_void_p, C.c_int32, C.c_int32]
+lib.space_pager_truncate.restype = C.c_int
+lib.space_pager_compact.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(C.c_int32)]
+lib.space_pager_compact.restype = C.c_int
+lib.space_pager_page_refs.argtypes = [C.c_void_p, C.c_int32]
+lib.space_pager_page_refs.restype = C.c_int32
+lib.space_kvq_page_bytes.argtypes = [C.c_int32, C.c_int32]
+lib.space_kvq_page_bytes.restype = C.c_int64
+lib.space_pages_copy.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p]
+lib.space_pages_copy.restype = C.c_int
 
 
 class SpaceError(RuntimeError):
@@ -242,6 +296,58 @@ def space_strerror(code):
 
 def space_workspace_bytes(**cfg):
     return lib.space_workspace_bytes(C.byref(Config(**cfg)))
+
+
+def kvq_page_bytes(n_kv_heads, head_dim):
+    """Bytes of a page of the 4-bit cache: a pool is a uint8 tensor [n_pages, n_kv_heads, page_bytes(1, d)]."""
+    return lib.space_kvq_page_bytes(n_kv_heads, head_dim)
+
+
+def kvq_pool(n_pages, n_kv_heads, head_dim, device="cuda"):
+    """An empty 4-bit page pool."""
+    import torch
+    return torch.zeros(n_pages, n_kv_heads, kvq_page_bytes(1, head_dim), dtype=torch.uint8, device=device)
+
+
+def page_pool(t):
+    """Descriptor of a page pool for space_pages_copy: a 4-bit pool (uint8 [n_pages, H_kv, bytes]), or one of the two
+    pools of a bf16 cache ([n_pages, H_kv, PAGE_SIZE, d]).  Keep the tensor alive as long as the descriptor is used."""
+    import torch
+    if t.dtype == torch.uint8:
+        assert t.dim() == 3 and t.stride(2) == 1 and t.shape[2] % 4 == 0
+        return PagePool(base=_ptr(t), page_stride=t.stride(0), part_stride=t.stride(1), parts=t.shape[1], group_rows=32,
+                        group_bytes=t.shape[2] // 4, n_pages=t.shape[0])
+    assert t.dim() == 4 and t.shape[2] == PAGE_SIZE and t.stride(3) == 1 and t.stride(2) == t.shape[3]
+    e = t.element_size()
+    return PagePool(base=_ptr(t), page_stride=t.stride(0) * e, part_stride=t.stride(1) * e, parts=t.shape[1], group_rows=1,
+                    group_bytes=t.shape[3] * e, n_pages=t.shape[0])
+
+
+def page_pools(tensors):
+    """Descriptors of several pools, as space_pages_copy takes them (they keep the tensors alive)."""
+    return _keeping((PagePool * len(tensors))(*map(page_pool, tensors)), *tensors)
+
+
+def space_pages_copy(pools, moves):
+    """Rows 0 .. rows-1 of page src to page dst in every pool.  pools: what page_pools returned, all on the current
+    device; moves: int32 numpy array [n, 3] of (src, dst, rows), as Pager.make_writable and Pager.compact return it."""
+    import numpy as np
+    moves = np.ascontiguousarray(moves, dtype=np.int32).reshape(-1, 3)
+    _check(lib.space_pages_copy(pools, len(pools), moves.ctypes.data, len(moves), _stream()))
+
+
+def _keeping(args, *tensors):
+    """The struct holds addresses only: the tensors live as long as it does."""
+    args._tensors = tensors
+    return args
+
+
+def _kvq_cache(pool, page_table):
+    import torch
+    assert pool.dtype == torch.uint8 and pool.dim() == 3 and pool.stride(2) == 1
+    assert page_table.dtype == torch.int32 and page_table.is_contiguous()
+    return KvqCache(pool=_ptr(pool), page_stride=pool.stride(0), head_stride=pool.stride(1), page_table=_ptr(page_table),
+                    pages_per_seq=page_table.shape[1], n_pages=pool.shape[0])
 
 
 class Context:
@@ -362,6 +468,66 @@ class Context:
     def space_kv_commit(self, args):
         _check(lib.space_kv_commit(self._h, C.byref(args), _stream()))
 
+    # -- 4-bit cache ------------------------------------------------------
+    def _check_rows(self, k, v):
+        import torch
+        assert k.dtype == v.dtype == torch.bfloat16 and k.shape == v.shape and k.stride() == v.stride() and k.stride(3) == 1
+        assert k.shape[2] == self.cfg.n_kv_heads and k.shape[3] == self.cfg.head_dim
+
+    def _check_pool(self, pool):
+        assert pool.shape[1] == self.cfg.n_kv_heads and pool.shape[2] == kvq_page_bytes(1, self.cfg.head_dim)
+
+    def kvq_append_args(self, k_new, v_new, pool, page_table, kv_len, count=None, count_bias=0, row_step=1,
+                        kv_len_out=None, status=None):
+        """k_new / v_new [B, rows, H_kv, d] bf16 by strides.  A prompt or a token: row_step 1; the accepted rows of a
+        step's block: row_step k + 1, count n_accept, count_bias 1."""
+        self._check_rows(k_new, v_new)
+        self._check_pool(pool)
+        return _keeping(KvqAppendArgs(batch=k_new.shape[0], rows=k_new.shape[1], row_step=row_step, count_bias=count_bias,
+                                      k_new=_ptr(k_new), v_new=_ptr(v_new), new_stride_b=k_new.stride(0),
+                                      new_stride_r=k_new.stride(1), new_stride_h=k_new.stride(2),
+                                      cache=_kvq_cache(pool, page_table), kv_len=_ptr(kv_len), count=_ptr(count),
+                                      kv_len_out=_ptr(kv_len_out), status=_ptr(status)),
+                        k_new, v_new, pool, page_table, kv_len, count, kv_len_out, status)
+
+    def space_kvq_append(self, args):
+        _check(lib.space_kvq_append(self._h, C.byref(args), _stream()))
+
+    def kvq_read_args(self, pool, page_table, kv_len, k_out, v_out, first=None, status=None):
+        """k_out / v_out [B, rows, H_kv, d] bf16 by strides."""
+        self._check_rows(k_out, v_out)
+        self._check_pool(pool)
+        return _keeping(KvqReadArgs(batch=k_out.shape[0], rows=k_out.shape[1], cache=_kvq_cache(pool, page_table),
+                                    kv_len=_ptr(kv_len), first=_ptr(first), k_out=_ptr(k_out), v_out=_ptr(v_out),
+                                    out_stride_b=k_out.stride(0), out_stride_r=k_out.stride(1), out_stride_h=k_out.stride(2),
+                                    status=_ptr(status)),
+                        pool, page_table, kv_len, first, k_out, v_out, status)
+
+    def space_kvq_read(self, args):
+        _check(lib.space_kvq_read(self._h, C.byref(args), _stream()))
+
+    def kvq_attn_args(self, q, pool, page_table, kv_len, out, k, scale, k_new=None, v_new=None, lse=None, status=None,
+                      mask_variant=MASK_SAME_GROUP):
+        """q [B, (k+1)^2, H_q, d] and k_new / v_new [B, (k+1)^2, H_kv, d] bf16 by strides, out contiguous bf16."""
+        import torch
+        assert q.dtype == out.dtype == torch.bfloat16 and q.stride(3) == 1 and out.is_contiguous() and out.shape == q.shape
+        assert q.shape[1:] == ((k + 1) ** 2, self.cfg.n_q_heads, self.cfg.head_dim)
+        self._check_pool(pool)
+        sb = sr = sh = 0
+        if k_new is not None:
+            self._check_rows(k_new, v_new)
+            assert k_new.shape[:2] == q.shape[:2]
+            sb, sr, sh = k_new.stride()[:3]
+        return _keeping(KvqAttnArgs(batch=q.shape[0], k=k, mask_variant=mask_variant, scale=scale, q=_ptr(q),
+                                    q_stride_b=q.stride(0), q_stride_r=q.stride(1), q_stride_h=q.stride(2), k_new=_ptr(k_new),
+                                    v_new=_ptr(v_new), new_stride_b=sb, new_stride_r=sr, new_stride_h=sh,
+                                    cache=_kvq_cache(pool, page_table), kv_len=_ptr(kv_len), out=_ptr(out), lse=_ptr(lse),
+                                    status=_ptr(status)),
+                        q, k_new, v_new, pool, page_table, kv_len, out, lse, status)
+
+    def space_kvq_attn_step(self, args):
+        _check(lib.space_kvq_attn_step(self._h, C.byref(args), _stream()))
+
     # -- decoding loop state (Algorithm 1) ---------------------------------
     def decode_state(self, tokens, n_tokens, last_token, cand, cand_prob, kv_len, finished, block_tokens,
                      block_pos, k, mask_token_id, mask_variant=MASK_SAME_GROUP):
@@ -431,3 +597,30 @@ class Pager:
         _check(lib.space_pager_batch_table(self._h, sl.ctypes.data_as(C.c_void_p), len(sl),
                                            out.ctypes.data_as(C.c_void_p)))
         return out
+
+    # forked slots that share pages (see include/space.h)
+    def fork(self, parent, n_rows):
+        s = C.c_int32(-1)
+        _check(lib.space_pager_fork(self._h, parent, n_rows, C.byref(s)))
+        return s.value
+
+    def make_writable(self, slot, first_row, n_rows):
+        """Moves [n, 3] (n <= 1) that space_pages_copy has to run before rows first_row .. are written."""
+        return self._moves(1, lambda buf, n: lib.space_pager_make_writable(self._h, slot, first_row, n_rows, buf, 1, n))
+
+    def truncate(self, slot, n_rows):
+        _check(lib.space_pager_truncate(self._h, slot, n_rows))
+
+    def compact(self, max_moves=1024):
+        """Moves [n, 3] that space_pages_copy has to run before the next call on the cache."""
+        return self._moves(max_moves, lambda buf, n: lib.space_pager_compact(self._h, buf, max_moves, n))
+
+    def page_refs(self, page):
+        return lib.space_pager_page_refs(self._h, page)
+
+    @staticmethod
+    def _moves(cap, call):
+        import numpy as np
+        buf, n = np.empty((max(cap, 1), 3), dtype=np.int32), C.c_int32(0)
+        _check(call(buf.ctypes.data, C.byref(n)))
+        return buf[:n.value]

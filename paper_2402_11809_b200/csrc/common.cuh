@@ -160,6 +160,7 @@ struct space_ctx {
   int* counters;           // [3][max_batch] self-resetting arrival counters (two verify launches, commit), then an error word
   int* merge_cnt;          // attention, row kernel: cut descriptors, one per (sequence, kv head, row block), and owners
   int* arrived;            // attention: pieces of a cut that are stored, one per (sequence, kv head, row block)
+  int* kvq_arrived;        // the same of the attention over the 4-bit cache, per (sequence, kv head, 16 query rows)
   VerifyPartial* vpart;    // [max_batch][k_max+2][SPACE_VERIFY_MAX_CHUNKS]
   VerifyRow* vrow;         // [max_batch][k_max+1]
   VerifyPartial* vfused;   // [max_batch][SPACE_MAX_ROWS][16] single-launch greedy path
@@ -334,6 +335,11 @@ int launch_attn_tensor(space_ctx* ctx, const space_attn_args* a, const uint64_t*
                        cudaStream_t st);
 int launch_attn_rows(space_ctx* ctx, const space_attn_args* a, const uint64_t* mask_rows, cudaStream_t st);
 size_t attn_tensor_partial_floats(const space_config* cfg, int sm_count, size_t* slots);
+int launch_kvq_append(space_ctx* ctx, const space_kvq_append_args* a, cudaStream_t st);
+int launch_kvq_read(space_ctx* ctx, const space_kvq_read_args* a, cudaStream_t st);
+int launch_kvq_attn(space_ctx* ctx, const space_kvq_attn_args* a, const uint64_t* mask_rows, cudaStream_t st);
+size_t kvq_partial_floats(const space_config* cfg, int sm_count);
+size_t kvq_items(const space_config* cfg);
 int launch_philox_debug(uint64_t seed, int64_t n, const uint32_t* c0, const uint32_t* c1,
                         const uint32_t* c2, const uint32_t* c3, uint32_t* out, cudaStream_t st);
 
