@@ -1,0 +1,161 @@
+// What the two attention kernels over the 4-bit cache share (kvq_attn.cu: up to 16 query rows on mma.sync;
+// kvq_attn_tc.cu: more rows on tcgen05): parameters, addresses of query rows, the join of an item's pieces.
+#pragma once
+#include "common.cuh"
+#include "tc_common.cuh"
+#include "attn_common.cuh"
+#include "kvq_common.cuh"
+#include <cuda_fp16.h>
+#include <math_constants.h>
+
+namespace kvq {
+using namespace tc;
+
+constexpr float REF_SLACK = 8.f;                     // a row's reference moves when a score exceeds it by 2^8
+constexpr float W_LIMIT = 16384.f;                   // weights of the second product stay below this (f16 ends at 65504)
+constexpr uint64_t WAIT_NS = 1000000000ull;
+
+struct Params {
+  Cache cache;
+  int B, n_q, H_q, H_kv, G, gsh, n_rt;               // G = 1 << gsh; n_rt: items per (sequence, kv head)
+  int n_groups;                                      // thread blocks
+  int has_new;
+  float c;                                           // scale * log2(e)
+  const char* q; int64_t q_sb, q_sr, q_sh;           // bytes
+  const char* kn; const char* vn; int64_t n_sb, n_sr, n_sh;
+  const int32_t* kv_len;
+  __nv_bfloat16* out; float* lse; int32_t* status;
+  float* part;                                       // [2 * n_groups][rows * (DH + 2)]
+  int* arrived;                                      // [B * H_kv * n_rt], self-resetting
+  int* err;
+  uint64_t mask[SPACE_MAX_ROWS];                     // Eq. 5: bit j of word i: block row i sees block row j
+};
+
+// Bounded wait on an mbarrier phase, small enough to stand inline at every site (roles that run with register counts of
+// their own cannot call): after WAIT_NS, or once another wait of the block has given up, false and the abort flag.
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* err, int site) {
+  if (mbar_try(bar, parity)) return true;
+  const uint64_t t0 = global_ns();
+#pragma unroll 1
+  while (!mbar_try(bar, parity)) {
+    if (*abort_flag || global_ns() - t0 > WAIT_NS) {
+      *abort_flag = 1;
+      atomicCAS(err, 0, site);
+      return false;
+    }
+  }
+  return true;
+}
+
+__device__ __forceinline__ uint32_t pack_h(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }     // -126 <= e <= 127
+__device__ __forceinline__ float quad_sum(float v) {
+  v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+  return v + __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+}
+__device__ __forceinline__ uint32_t h2sub(uint32_t a, uint32_t b) {
+  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// Where a kv head's query row r lies: block row and head.  (G is a power of two.)
+__device__ __forceinline__ void row_of(const Params& p, int h, int r, int& i, int& hq) {
+  i = r >> p.gsh;
+  hq = (h << p.gsh) + (r & ((1 << p.gsh) - 1));
+}
+
+// The flat list of W pages over NG thread blocks: the first `rem` blocks take one page more.
+struct Cut {
+  uint32_t NG, per, rem;
+  __device__ __forceinline__ Cut(uint32_t W, uint32_t groups) {
+    NG = min(W, groups);
+    per = NG ? W / NG : 0;
+    rem = W - per * NG;
+  }
+  __device__ __forceinline__ uint32_t begin(uint32_t g) const { return g * per + min(g, rem); }
+  __device__ __forceinline__ uint32_t owner(uint32_t f) const {                // block whose share page f is in
+    const uint32_t wide = rem * (per + 1);
+    return f < wide ? f / (per + 1) : rem + (f - wide) / per;
+  }
+};
+
+template <int DH>
+__device__ __forceinline__ void store_row4(const Params& p, int b, int h, int r, int c4, float4 o, float m, float l) {
+  int i, hq;
+  row_of(p, h, r, i, hq);
+  const float rd = l > 0.f || l != l ? 1.f / l : 0.f;      // a row without keys: zeros
+  const __nv_bfloat162 x = __floats2bfloat162_rn(o.x * rd, o.y * rd), y = __floats2bfloat162_rn(o.z * rd, o.w * rd);
+  __nv_bfloat16* dst = p.out + (((int64_t)b * p.n_q + i) * p.H_q + hq) * DH + 4 * c4;
+  *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+  if (c4 == 0 && p.lse) p.lse[((int64_t)b * p.H_q + hq) * p.n_q + i] = (m + log2f(l)) * 0.6931471805599453f;
+}
+
+// The pieces of an item that was cut over several thread blocks meet, always in the same order: called by the block
+// that stored the last of them.  item_at: the item's place in the flat list; a block's share can hold the end of one cut
+// item (its first slot) and the start of another (its second one).
+template <int DH, int RT>
+__device__ __forceinline__ void join_pieces(const Params& p, const Cut& cut, int b, int h, int r0, int rows, uint32_t piece0,
+                                            int pieces, uint32_t item_at, int tid, int threads) {
+  constexpr int C4 = DH / 4, SLOT = RT * (DH + 2), BATCH = 8;
+  const float* part = p.part + (int64_t)(2 * piece0) * SLOT;
+  const int first = cut.begin(piece0) >= item_at ? 0 : SLOT;
+#pragma unroll 1
+  for (int idx = tid; idx < rows * C4; idx += threads) {
+    const int r = idx / C4, c4 = idx % C4;
+    attn::MergeAcc ma;
+    ma.clear();
+    bool nan = false;
+#pragma unroll 1
+    for (int x0 = 0; x0 < pieces; x0 += BATCH) {     // all loads of a batch are issued before any is used
+      float ms[BATCH], ls[BATCH];
+      float4 ov[BATCH];
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        ms[j] = -CUDART_INF_F; ls[j] = 0.f; ov[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (x0 + j < pieces) {
+          const float* ps = part + (x0 + j == 0 ? (int64_t)first : (int64_t)(x0 + j) * (2 * SLOT));
+          ms[j] = __ldcg(ps + RT * DH + r);
+          ls[j] = __ldcg(ps + RT * DH + RT + r);
+          ov[j] = __ldcg(reinterpret_cast<const float4*>(ps + r * DH) + c4);
+        }
+        nan |= ls[j] != ls[j];
+      }
+#pragma unroll
+      for (int g = 0; g < BATCH; g += 4) {
+        const float m4[4] = {ms[g], ms[g + 1], ms[g + 2], ms[g + 3]}, l4[4] = {ls[g], ls[g + 1], ls[g + 2], ls[g + 3]};
+        const float4 o4[4] = {ov[g], ov[g + 1], ov[g + 2], ov[g + 3]};
+        ma.add4(m4, l4, o4);
+      }
+    }
+    if (nan) ma.den = CUDART_NAN_F;
+    store_row4<DH>(p, b, h, r0 + r, c4, ma.a, ma.mx, ma.den);
+  }
+}
+
+}  // namespace kvq
+
+int launch_kvq_attn_tc(space_ctx* ctx, kvq::Params& p, cudaStream_t st);
+size_t kvq_tc_partial_floats(const space_config* cfg, int sm_count);

@@ -1,0 +1,899 @@
+// Attention of a step's block rows over the 4-bit cache (space_kvq_attn_step), items of up to 64 query rows on tcgen05.
+//
+// The mathematics is kvq_attn.cu's: products of bare codes, steps and lowest values in the softmax, weights e step
+// against a reference of their own.  So is the work: (sequence, kv head, query rows) items, one flat list of 128-key
+// pages, an equal share per thread block, cut items joined by the block that stores their last piece.
+//
+// The products are taken transposed, the 128 keys (channels) of a page on the MMA's M extent and the query rows on N:
+//   S^T = U Q^T  (128 x N),      O^T += (U - 8)^T P^T  (d x N).
+// Both first operands come from tensor memory: the codes are unpacked in registers and stored there (tcgen05.st), because
+// through shared memory the unpacked page would cost 4 d bytes written and as many read per key, more than the tensor
+// core's products take.  The cache's order is that of the 16x256b store: a lane's 16 bytes are its registers.
+//
+// Warps (20, one thread block per SM):
+//   0      bulk copies, a page of one kv head (4 (32 d + 256) contiguous bytes) per stage of the ring
+//   1, 2   issue S^T and O^T products
+//   4-7    query rows into shared memory (f16, one power of two per item); K codes -> tensor memory
+//   8-11   V codes -> tensor memory
+//   12-19  two threads per key: scores, e, its sums, weights as f16 into shared memory (second operand); O^T out
+// The block's own rows are one more page, whose K and V the code warps bring as f16 with a power of two per row instead.
+// Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT, no role leaves its loop early (the named barriers stay
+// matched), and the block drains and exits.
+#include "kvq_attn.cuh"
+
+namespace {
+using namespace kvq;
+
+constexpr int THREADS = 640;
+constexpr int TILE = SPACE_PAGE_SIZE;
+constexpr int SHARE_COST = 2;                        // fixed cost of starting an item, in pages
+constexpr int K_WARP0 = 4, V_WARP0 = 8, SOFT_WARP0 = 12;
+constexpr float W_SHIFT = 2.f;                       // weights of a new reference lie in [2^2, 2^3) (below 2^-14 f16 has fewer bits)
+constexpr float X_LIMIT = 16.f;                      // a row's reference moves when a score exceeds it by 2^16
+
+template <int DH, int NP>
+struct Smem {
+  static constexpr int N = 16 * NP;                          // query rows of an item (with padding)
+  static constexpr int STAGES = DH == 128 ? 8 : 12;
+  static constexpr int PAGE = Fmt<DH>::HEAD;
+  static constexpr int Q_BYTES = N * DH * 2;                 // DH / 64 blocks [N][64] f16, 128-byte swizzle
+  static constexpr int P_BYTES = TILE * 128;                 // [key][64 query rows] f16, 128-byte swizzle
+  static constexpr int Q_OFF = 0;                            // two buffers each
+  static constexpr int P_OFF = 2 * Q_BYTES;
+  static constexpr int RING_OFF = P_OFF + 2 * P_BYTES;
+  static constexpr int RC_OFF = RING_OFF + STAGES * PAGE;    // [N/2] {sum, sum, -m, -m} of query rows 2i, 2i + 1
+  static constexpr int VINV_OFF = RC_OFF + 32 * 16;          // [N] 2^(m - R + W_SHIFT)
+  static constexpr int MREF_OFF = VINV_OFF + 256;            // [N] m
+  static constexpr int RREF_OFF = MREF_OFF + 256;            // [N] R
+  static constexpr int FQ_OFF = RREF_OFF + 256;              // [N] factors
+  static constexpr int GO_OFF = FQ_OFF + 256;                // [N] factors
+  static constexpr int VKEY_OFF = GO_OFF + 256;              // [128] V steps of a page's keys
+  static constexpr int XQ_OFF = VKEY_OFF + 512;                // [4][64] per quarter
+  static constexpr int XZ_OFF = XQ_OFF + 1024;               // [4][64]
+  static constexpr int QSUM_OFF = XZ_OFF + 1024;             // [2][64] c * sum of a query row
+  static constexpr int QTOP_OFF = QSUM_OFF + 512;            // [2][4] largest exponents, then [2] c with the power of two undone
+  static constexpr int PAR_OFF = QTOP_OFF + 64;              // [STAGES][2][64] block rows' K and V factors
+  static constexpr int BAD_OFF = PAR_OFF + STAGES * 512;     // [STAGES] page outside the pool
+  static constexpr int BAR_OFF = (BAD_OFF + STAGES * 4 + 15) / 16 * 16;
+  static constexpr int N_BARS = 2 * STAGES + 23;
+  static constexpr int MISC_OFF = BAR_OFF + (N_BARS * 8 + 15) / 16 * 16;
+  static constexpr int TABLE_OFF = MISC_OFF + 16;            // prefix[max_batch + 1], seq_len[max_batch]
+  static constexpr int V_PITCH = DH * 2 + 16;                // bytes: the block's V rows as f16, in a stage
+  static_assert(SPACE_MAX_ROWS * V_PITCH <= PAGE, "the block's V rows fit a stage");
+  static_assert(TABLE_OFF + 129 * 4 + 128 * 4 <= 227 * 1024, "shared-memory plan too large");
+};
+
+__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ bool soft_any(bool pred) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, 1, 256, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+      : "=r"(r) : "r"((uint32_t)pred) : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void k_sync() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
+__device__ __forceinline__ void v_sync() { asm volatile("bar.sync 3, 128;" ::: "memory"); }
+template <int R> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
+template <int R> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
+
+__device__ __forceinline__ void tmem_ld8(uint32_t a, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t a, const float* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"r"(a), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]) : "memory");
+}
+// 16 lanes x 32 columns: lane (n, t) of the warp holds of every eight columns {2t, 2t + 1} of rows n and n + 8
+__device__ __forceinline__ void tmem_st_frag4(uint32_t a, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+               ::"r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+               "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// Instruction descriptor: f16 x f16 -> f32, M = 128, N = n; first operand K-major, second one K-major or (b_mn) not.
+__device__ __forceinline__ constexpr uint32_t instr_desc(int n, int b_mn) {
+  return (1u << 4) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
+}
+// Codes of pair q (bits 4q .. 4q + 3 of both halves) less 8, as f16: 1024 + u - 1032, or (1024 + 16 u) / 16 - 72.
+__device__ __forceinline__ uint32_t centred_even(uint32_t x) { return h2sub((x & 0x000F000Fu) | 0x64006400u, 0x64086408u); }
+__device__ __forceinline__ uint32_t centred_odd(uint32_t x) {
+  const uint32_t v = (x & 0x00F000F0u) | 0x64006400u, a = 0x2C002C00u, c = 0xD480D480u;   // 1/16, -72
+  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&c));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// The items of a block's share, in order: every role walks them for itself.
+struct Walk {
+  uint32_t cur, end;
+  int b, it;                                         // item h * n_rb + block of query rows
+  int L, t0, t1;                                     // pages [t0, t1) of it; cached rows (-1: the sequence does not fit)
+  bool opens;                                        // the share begins with this item
+  __device__ __forceinline__ int cached() const { return (max(L, 0) + TILE - 1) / TILE; }   // that page: the block's own rows
+  __device__ __forceinline__ int pages(int has_new) const { return max(cached() + has_new, 1); }
+  __device__ __forceinline__ bool next(const uint32_t* prefix, const int* seq_len, int has_new, uint32_t share0) {
+    while (cur < end) {
+      while (prefix[b + 1] <= cur) ++b;
+      L = seq_len[b];
+      const int Tv = pages(has_new) + SHARE_COST;
+      const uint32_t rem = cur - prefix[b];
+      it = (int)(rem / (uint32_t)Tv);
+      const int x0 = (int)rem - it * Tv, n = min(Tv - x0, (int)(end - cur));
+      opens = cur == share0;
+      cur += n;
+      t0 = max(x0 - SHARE_COST, 0); t1 = x0 + n - SHARE_COST;
+      if (t1 > t0) return true;                      // (else only the cost of starting)
+    }
+    return false;
+  }
+};
+
+template <int DH, int NP>
+__global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_constant__ Params p, int max_batch) {
+  using F = Fmt<DH>;
+  using S = Smem<DH, NP>;
+  constexpr int N = S::N, STAGES = S::STAGES;
+  extern __shared__ __align__(1024) unsigned char sm[];
+  const uint32_t base = smem_u32(sm), bar0 = base + S::BAR_OFF;
+  auto BAR = [&](int i) { return bar0 + 8u * i; };
+  constexpr int FULL = 0, EMPTY = STAGES, KTF = 2 * STAGES, KTE = KTF + 2, VTF = KTF + 4, VTE = KTF + 6, SF = KTF + 8, SE = KTF + 10,
+                PF = KTF + 12, PE = KTF + 14, QF = KTF + 16, QE = KTF + 18, BLK = KTF + 20, DRAIN = KTF + 22;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::MISC_OFF);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF + 4);
+  volatile int* last_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF + 8);
+  uint32_t* prefix = reinterpret_cast<uint32_t*>(sm + S::TABLE_OFF);
+  int* seq_len = reinterpret_cast<int*>(prefix + max_batch + 1);
+  volatile int* bad = reinterpret_cast<volatile int*>(sm + S::BAD_OFF);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  pdl_launch_dependents();
+  if (threadIdx.x == 0) {
+    *abort_flag = (base & 1023u) ? 1 : 0;            // swizzled tiles need a 1024-byte aligned base
+    for (int s = 0; s < STAGES; ++s) { mbar_init(BAR(FULL + s), 1); mbar_init(BAR(EMPTY + s), 16); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(BAR(KTF + i), 4); mbar_init(BAR(KTE + i), 1); mbar_init(BAR(VTF + i), 4); mbar_init(BAR(VTE + i), 1);
+      mbar_init(BAR(SF + i), 1); mbar_init(BAR(SE + i), 8); mbar_init(BAR(PF + i), 8); mbar_init(BAR(PE + i), 1);
+      mbar_init(BAR(QF + i), 4); mbar_init(BAR(QE + i), 2); mbar_init(BAR(BLK + i), 8);
+    }
+    mbar_init(BAR(DRAIN), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 3) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+  if (warp == 0) {
+    // the list's running sums, as in kvq_attn.cu
+    uint32_t carry = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 32) {
+      const int b = b0 + lane;
+      int L = -1;
+      uint32_t n = 0;
+      if (b < p.B) {
+        L = p.kv_len[b];
+        if (L < 0 || (int64_t)L > (int64_t)p.cache.pages_per_seq * TILE) {
+          if (blockIdx.x == 0 && p.status) atomicOr(p.status + b, SPACE_ST_CAPACITY);
+          L = -1;
+        }
+        n = (uint32_t)((max((max(L, 0) + TILE - 1) / TILE + p.has_new, 1) + SHARE_COST) * p.H_kv * p.n_rt);
+      }
+      uint32_t incl = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      if (b < p.B) { seq_len[b] = L; prefix[b] = carry + incl - n; }
+      carry += __shfl_sync(0xFFFFFFFFu, incl, 31);
+    }
+    if (lane == 0) prefix[p.B] = carry;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  // columns: S^T two buffers, O^T, two buffers each of the unpacked K and V pages
+  const uint32_t TM_S = tmem, TM_O = tmem + 128, TM_K = tmem + 192, TM_V = tmem + 320;
+  const Cut cut(prefix[p.B], p.n_groups);
+  Walk wk;
+  const bool mine = blockIdx.x < cut.NG;
+  const uint32_t share0 = mine ? cut.begin(blockIdx.x) : 0;
+  wk.b = 0; wk.cur = share0;
+  wk.end = mine ? cut.begin(blockIdx.x + 1) : 0;
+  auto next = [&] { return wk.next(prefix, seq_len, p.has_new, share0); };
+  uint32_t g = 0, items = 0;                         // pages and items so far
+  // (a failed wait leaves no loop: what waits later returns at once, and the counts of arrivals stay matched)
+  auto hold = [&](int bar, uint32_t use, int site) { return wait(BAR(bar), use & 1, abort_flag, p.err, site); };
+
+  if (warp < 4) {
+    regs_dec<32>();
+    if (warp == 0) {
+      // ================= bulk copies =========================================
+      if (elect_one()) {
+        bool ok = true;
+        while (ok && next()) {
+          const int32_t* table = p.cache.page_table + (int64_t)wk.b * p.cache.pages_per_seq;
+          const char* head = p.cache.pool + (int64_t)(wk.it / p.n_rt) * p.cache.head_stride;
+          const int Tc = wk.cached();
+          for (int t = wk.t0; t < wk.t1; ++t, ++g) {
+            const uint32_t s = g % STAGES;
+            const int pg = t < Tc ? __ldg(table + t) : -1;
+            if (g >= STAGES) ok = hold(EMPTY + s, g / STAGES - 1, 1);
+            if (!ok) break;
+            const bool good = pg >= 0 && pg < p.cache.n_pages;
+            bad[s] = !good;
+            if (good) {
+              mbar_expect_tx(BAR(FULL + s), S::PAGE);
+              asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                           ::"r"(base + S::RING_OFF + s * S::PAGE), "l"(head + (int64_t)pg * p.cache.page_stride), "r"(S::PAGE), "r"(BAR(FULL + s)) : "memory");
+            } else {
+              if (t < Tc && p.status) atomicOr(p.status + wk.b, SPACE_ST_BAD_PAGE);
+              mbar_arrive(BAR(FULL + s));
+            }
+          }
+        }
+        // every copy has landed before the block may exit
+        for (uint32_t i = g > STAGES ? g - STAGES : 0; i < g; ++i) mbar_drain_bounded(BAR(FULL + i % STAGES), (i / STAGES) & 1, WAIT_NS);
+      }
+    } else if (warp == 1) {
+      // ================= S^T products ========================================
+      if (elect_one()) {
+        const uint64_t qdesc0 = smem_desc(base + S::Q_OFF, 16, 1024);
+        bool ok = true;
+        while (ok && next()) {
+          const uint32_t qb = items & 1;
+          ok = hold(QF + qb, items >> 1, 2);
+          const uint64_t qd = qdesc0 + (uint64_t)((qb * S::Q_BYTES) >> 4);
+          for (int t = wk.t0; t < wk.t1 && ok; ++t, ++g) {
+            const uint32_t buf = g & 1;
+            ok = hold(KTF + buf, g >> 1, 3);
+            if (ok && g >= 2) ok = hold(SE + buf, (g - 2) >> 1, 4);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int kk = 0; kk < DH / 16; ++kk)
+              mma_ts(TM_S + buf * 64, TM_K + buf * 64 + kk * 8, qd + (uint64_t)(((kk >> 2) * (N * 128) + (kk & 3) * 32) >> 4), instr_desc(N, 0), kk > 0);
+            tc_commit(BAR(SF + buf));
+            tc_commit(BAR(KTE + buf));
+            if (t == wk.t1 - 1) tc_commit(BAR(QE + qb));
+          }
+          ++items;
+        }
+        tc_commit(BAR(DRAIN));                       // all products done before tensor memory is released
+        mbar_drain_bounded(BAR(DRAIN), 0, WAIT_NS);
+      }
+    } else if (warp == 2) {
+      // ================= O^T products ========================================
+      if (elect_one()) {
+        const uint64_t pdesc0 = smem_desc(base + S::P_OFF, TILE * 128, 1024);
+        bool ok = true;
+        while (ok && next()) {
+          for (int t = wk.t0; t < wk.t1 && ok; ++t, ++g) {
+            const uint32_t buf = g & 1;
+            ok = hold(VTF + buf, g >> 1, 5);
+            if (ok) ok = hold(PF + buf, g >> 1, 6);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t pd = pdesc0 + (uint64_t)((buf * S::P_BYTES) >> 4);
+#pragma unroll
+            for (int kk = 0; kk < TILE / 16; ++kk)
+              mma_ts(TM_O, TM_V + buf * 64 + kk * 8, pd + (uint64_t)((kk * 2048) >> 4), instr_desc(N, 1), (t == wk.t0 && kk == 0) ? 0u : 1u);
+            tc_commit(BAR(VTE + buf));
+            tc_commit(BAR(PE + buf));
+          }
+        }
+        // (the last of these is waited for by the softmax threads; after a wait that ran out, here)
+        if (*abort_flag) {
+          for (uint32_t i = g > 2 ? g - 2 : 0; i < g; ++i) mbar_drain_bounded(BAR(VTE + (i & 1)), (i >> 1) & 1, WAIT_NS);
+        }
+      }
+    }
+  } else if (warp < V_WARP0) {
+    regs_dec<80>();
+    // ================= query rows, K codes -> tensor memory ====================
+    const int w = warp - K_WARP0, n = lane >> 2, t4 = lane & 3;
+    float* qsum = reinterpret_cast<float*>(sm + S::QSUM_OFF);
+    uint32_t* qtop = reinterpret_cast<uint32_t*>(sm + S::QTOP_OFF);
+    float* qc = reinterpret_cast<float*>(sm + S::QTOP_OFF + 32);
+    float* par = reinterpret_cast<float*>(sm + S::PAR_OFF);
+    while (next()) {
+      const uint32_t qb = items & 1;
+      const int h = wk.it / p.n_rt, rb = wk.it - h * p.n_rt, Tc = wk.cached();
+      float c;                                       // scale, with the query rows' power of two undone
+      {
+        // (twice over the rows, in loops: what runs once per item should not push the pages' loops out of the
+        // instruction cache; the second time they come out of the first-level cache)
+        constexpr int ROWS = N / 4;                  // of this warp
+        auto row = [&](int r, bool& there) {
+          int i, hq;
+          row_of(p, h, rb * N + w * ROWS + r, i, hq);
+          there = r < ROWS && i < p.n_q;
+          return reinterpret_cast<const uint4*>(p.q + (int64_t)wk.b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh) + t4 * (DH / 32);
+        };
+        uint32_t top = 0;
+#pragma unroll 1
+        for (int r = n; r < ROWS; r += 8) {
+          bool there;
+          const uint4* src = row(r, there);
+#pragma unroll
+          for (int j = 0; j < DH / 32; ++j) {
+            const uint4 v = there ? src[j] : make_uint4(0, 0, 0, 0);
+            const uint32_t m = max_bits(v);
+            top = max(top, m);
+            if (m >= 0x7F80u) top = 0x7F80u;
+          }
+        }
+        top >>= 7;
+        if (top >= 255u) {                           // something is not finite: the largest of what is
+          top = 0;
+#pragma unroll 1
+          for (int r = n; r < ROWS; r += 8) {
+            bool there;
+            const uint16_t* src = reinterpret_cast<const uint16_t*>(row(r, there));
+#pragma unroll 1
+            for (int j = 0; j < DH / 4 && there; ++j) {
+              const uint32_t e = (src[j] >> 7) & 0xFFu;
+              if (e < 255u) top = max(top, e);
+            }
+          }
+        }
+        __syncwarp();
+        top = __reduce_max_sync(0xFFFFFFFFu, top);
+        if (items >= 2) hold(QE + qb, (items >> 1) - 1, 7);
+        if (lane == 0) qtop[qb * 4 + w] = top;
+        k_sync();
+        top = max(max(qtop[qb * 4], qtop[qb * 4 + 1]), max(qtop[qb * 4 + 2], qtop[qb * 4 + 3]));
+        const int e = top ? min(max(8 - ((int)top - 127), -100), 100) : 0;   // largest element in [2^8, 2^9)
+        const float f = pow2(e), f16th = f * 0.0625f;
+        c = p.c * pow2(-e);
+        if (threadIdx.x == K_WARP0 * 32) qc[qb] = c;
+#pragma unroll 1
+        for (int r0 = 0; r0 < ROWS; r0 += 8) {
+          bool there;
+          const uint4* src = row(r0 + n, there);
+          const int r = w * ROWS + r0 + n;
+          float sum = 0.f;
+#pragma unroll
+          for (int j = 0; j < DH / 32; ++j) {
+            const uint4 v = there ? src[j] : make_uint4(0, 0, 0, 0);
+            sum += ((bf_lo(v.x) + bf_hi(v.x)) + (bf_lo(v.y) + bf_hi(v.y))) + ((bf_lo(v.z) + bf_hi(v.z)) + (bf_lo(v.w) + bf_hi(v.w)));
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {   // k-step 2 j + half: channels 8 j + {0, 4 | 1, 5} or {2, 6 | 3, 7}
+              const int ks = 2 * j + half;
+              const uint32_t lo = half ? v.y : v.x, hi = half ? v.w : v.z;
+              const uint32_t a0 = pack_h(bf_lo(lo) * f, bf_lo(hi) * f), a1 = pack_h(bf_hi(lo) * f16th, bf_hi(hi) * f16th);
+              const uint32_t at = base + S::Q_OFF + qb * S::Q_BYTES + (ks >> 2) * (N * 128) + r * 128 + (((2 * (ks & 3) + (t4 >> 1)) ^ (r & 7)) << 4) + (t4 & 1) * 8;
+              if (r0 + n < ROWS) asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(at), "r"(a0), "r"(a1) : "memory");
+            }
+          }
+          sum = quad_sum(sum) * p.c;
+          if (t4 == 0 && r0 + n < ROWS) qsum[qb * 64 + r] = sum;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(QF + qb));
+      }
+      for (int t = wk.t0; t < wk.t1; ++t, ++g) {
+        const uint32_t s = g % STAGES, buf = g & 1;
+        hold(FULL + s, g / STAGES, 8);
+        if (g >= 2) hold(KTE + buf, (g - 2) >> 1, 9);
+        tc_fence_after();
+        const uint32_t dst = TM_K + buf * 64 + ((uint32_t)(32 * w) << 16);
+        const bool own = t >= Tc;                    // the block's own rows (or no rows at all)
+        if (!own) {
+          const uint32_t blk = base + S::RING_OFF + s * S::PAGE + w * F::BLOCK;
+#pragma unroll
+          for (int i16 = 0; i16 < 2; ++i16) {
+            uint32_t x[DH / 32], y[DH / 32];
+            const uint32_t at = blk + (16 * i16 + n) * (DH / 2) + t4 * (DH / 8);
+            if (DH == 128) {
+              const uint4 a = lds128(at), d = lds128(at + 8 * (DH / 2));
+              x[0] = a.x; x[1] = a.y; x[2 % (DH / 32)] = a.z; x[3 % (DH / 32)] = a.w;
+              y[0] = d.x; y[1] = d.y; y[2 % (DH / 32)] = d.z; y[3 % (DH / 32)] = d.w;
+            } else {
+              const uint2 a = lds64(at), d = lds64(at + 8 * (DH / 2));
+              x[0] = a.x; x[1] = a.y; y[0] = d.x; y[1] = d.y;
+            }
+#pragma unroll
+            for (int jj = 0; jj < DH / 64; ++jj) {
+              uint32_t r[16];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {          // eight columns: pairs 2 (k % 2), + 1 of word 2 jj + k / 2
+                const uint32_t a = (k & 1) ? x[2 * jj + k / 2] >> 8 : x[2 * jj + k / 2], d = (k & 1) ? y[2 * jj + k / 2] >> 8 : y[2 * jj + k / 2];
+                r[4 * k] = a & 0x000F000Fu; r[4 * k + 1] = a & 0x00F000F0u;
+                r[4 * k + 2] = d & 0x000F000Fu; r[4 * k + 3] = d & 0x00F000F0u;
+              }
+              tmem_st_frag4(dst + ((uint32_t)(16 * i16) << 16) + 32 * jj, r);
+            }
+          }
+        } else if (p.has_new && wk.L >= 0 && 32 * w < p.n_q) {
+#pragma unroll 1
+          for (int i16 = 0; i16 < 2; ++i16) {
+            uint4 raw[2][DH / 32];
+            float f[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int key = 32 * w + 16 * i16 + 8 * i + n;
+              const uint4* src = reinterpret_cast<const uint4*>(p.kn + (int64_t)wk.b * p.n_sb + (int64_t)key * p.n_sr + (int64_t)h * p.n_sh) + t4 * (DH / 32);
+              uint32_t top = 0;
+#pragma unroll
+              for (int j = 0; j < DH / 32; ++j) {
+                raw[i][j] = key < p.n_q ? src[j] : make_uint4(0, 0, 0, 0);
+                top = max(top, top_bits(raw[i][j]));
+              }
+              top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+              top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+              const int e = max(min(127 - (int)(top >> 7), 120), -126);
+              f[i] = pow2(e);
+              if (t4 == 0) par[s * 128 + key] = fminf(pow2(-e) * c, 1e38f);
+            }
+#pragma unroll
+            for (int jj = 0; jj < DH / 64; ++jj) {
+              uint32_t r[16];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                  const uint4 v = raw[i][2 * jj + k / 2];
+                  const uint32_t lo = (k & 1) ? v.y : v.x, hi = (k & 1) ? v.w : v.z;
+                  r[4 * k + 2 * i] = pack_h(bf_lo(lo) * f[i], bf_lo(hi) * f[i]);
+                  r[4 * k + 2 * i + 1] = pack_h(bf_hi(lo) * (f[i] * 16.f), bf_hi(hi) * (f[i] * 16.f));
+                }
+              }
+              tmem_st_frag4(dst + ((uint32_t)(16 * i16) << 16) + 32 * jj, r);
+            }
+          }
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(BAR(KTF + buf));
+          mbar_arrive(BAR(EMPTY + s));
+          if (own) mbar_arrive(BAR(BLK + buf));
+        }
+      }
+      ++items;
+    }
+  } else if (warp < SOFT_WARP0) {
+    regs_dec<64>();
+    // ================= V codes -> tensor memory ================================
+    const int w = warp - V_WARP0;
+    float* par = reinterpret_cast<float*>(sm + S::PAR_OFF);
+    while (next()) {
+      const int h = wk.it / p.n_rt, Tc = wk.cached();
+      for (int t = wk.t0; t < wk.t1; ++t, ++g) {
+        const uint32_t s = g % STAGES, buf = g & 1, stage = base + S::RING_OFF + s * S::PAGE;
+        hold(FULL + s, g / STAGES, 10);
+        if (g >= 2) hold(VTE + buf, (g - 2) >> 1, 11);
+        tc_fence_after();
+        const uint32_t dst = TM_V + buf * 64 + ((uint32_t)(32 * w) << 16);
+        const bool own = t >= Tc;
+        if (!own) {
+          if (32 * w < DH) {
+#pragma unroll
+            for (int r2 = 0; r2 < 2; ++r2) {         // two blocks of 32 rows, 32 columns
+              uint32_t lo[16], hi[16];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const uint4 v = lds128(stage + (2 * r2 + k) * F::BLOCK + F::CODES + 512 * w + 16 * lane);
+                const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) {      // channels n and n + 8 of each 16: pairs 0 and 1 (2 and 3)
+                    const uint32_t u = x[2 * a + e], u8 = u >> 8;
+                    lo[8 * k + 4 * a + e] = centred_even(u); lo[8 * k + 4 * a + 2 + e] = centred_odd(u);
+                    hi[8 * k + 4 * a + e] = centred_even(u8); hi[8 * k + 4 * a + 2 + e] = centred_odd(u8);
+                  }
+              }
+              tmem_st_frag4(dst + 32 * r2, lo);
+              tmem_st_frag4(dst + (16u << 16) + 32 * r2, hi);
+            }
+          }
+        } else {
+          // the block's V rows as f16, largest element of a row in [1, 2), into the stage; eight channels a lane
+          constexpr int LANES = DH / 8;
+#pragma unroll 2
+          for (int i = 0; i < 16 * LANES / 32; ++i) {
+            const int key = 16 * w + i * (32 / LANES) + lane / LANES;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (p.has_new && wk.L >= 0 && key < p.n_q)
+              v = *(reinterpret_cast<const uint4*>(p.vn + (int64_t)wk.b * p.n_sb + (int64_t)key * p.n_sr + (int64_t)h * p.n_sh) + lane % LANES);
+            uint32_t top = top_bits(v);
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+            const int e = min(max((int)(top >> 7) - 127, -110), 126);
+            const float f = pow2(-e);
+            const uint4 hv = make_uint4(pack_h(bf_lo(v.x) * f, bf_hi(v.x) * f), pack_h(bf_lo(v.y) * f, bf_hi(v.y) * f),
+                                        pack_h(bf_lo(v.z) * f, bf_hi(v.z) * f), pack_h(bf_lo(v.w) * f, bf_hi(v.w) * f));
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};"
+                         ::"r"(stage + key * S::V_PITCH + (lane % LANES) * 16), "r"(hv.x), "r"(hv.y), "r"(hv.z), "r"(hv.w) : "memory");
+            if (lane % LANES == 0) par[s * 128 + 64 + key] = pow2(e);
+          }
+          v_sync();
+          if (32 * w < DH) {
+#pragma unroll 1
+            for (int c = 0; c < 2; ++c) {            // sixteen channels
+              uint32_t r[16];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {          // sixteen keys
+                const uint32_t at = stage + (16 * k + 8 * (lane >> 4) + (lane & 7)) * S::V_PITCH + (32 * w + 16 * c) * 2 + ((lane >> 3) & 1) * 16;
+                asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(r[4 * k]), "=r"(r[4 * k + 2]), "=r"(r[4 * k + 1]), "=r"(r[4 * k + 3]) : "r"(at) : "memory");
+              }
+              tmem_st_frag4(dst + ((uint32_t)(16 * c) << 16), r);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) r[k] = 0u;                            // a page has 128 rows, the block 64 at most
+              tmem_st_frag4(dst + ((uint32_t)(16 * c) << 16) + 32, r);
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the next copy into this stage comes after
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(BAR(VTF + buf));
+          mbar_arrive(BAR(EMPTY + s));
+          if (own) mbar_arrive(BAR(BLK + buf));
+        }
+      }
+    }
+  } else {
+    regs_inc<152>();
+    // ================= softmax, output ==========================================
+    constexpr int NC = 8 * NP;                       // query rows of a thread
+    const int quarter = warp & 3, half = (warp - SOFT_WARP0) >> 2;
+    const int kl = quarter * 32 + lane;              // key of the page; channel in the epilogue
+    const int sidx = half * 128 + kl, col0 = half * NC;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    // the key's place in the order in which the unpacked V lies: 16 a + 4 t + 2 e + h within 32 rows
+    const int kp_row = (kl & 0x70) | ((kl & 6) << 1) | ((kl & 8) >> 2) | (kl & 1);
+    const uint32_t prow = base + S::P_OFF + kp_row * 128, swz = (uint32_t)(kp_row & 7);
+    const uint32_t rc_at = base + S::RC_OFF + col0 * 8, vinv_at = base + S::VINV_OFF + col0 * 4;
+    float* rcf = reinterpret_cast<float*>(sm + S::RC_OFF);
+    float* vinv = reinterpret_cast<float*>(sm + S::VINV_OFF);
+    float* mref = reinterpret_cast<float*>(sm + S::MREF_OFF);
+    float* rref = reinterpret_cast<float*>(sm + S::RREF_OFF);
+    float* fq = reinterpret_cast<float*>(sm + S::FQ_OFF);
+    float* go = reinterpret_cast<float*>(sm + S::GO_OFF);
+    float* xq = reinterpret_cast<float*>(sm + S::XQ_OFF);
+    float* xz = reinterpret_cast<float*>(sm + S::XZ_OFF);
+    float* vkey = reinterpret_cast<float*>(sm + S::VKEY_OFF);
+    float* park = reinterpret_cast<float*>(sm + S::P_OFF);   // [128][N] floats: both buffers of P^T, while they are idle
+    volatile float* vtop = reinterpret_cast<volatile float*>(sm + S::MISC_OFF + 12);   // the largest vinv
+    const float* qsum = reinterpret_cast<const float*>(sm + S::QSUM_OFF);
+    const volatile float* qc = reinterpret_cast<const volatile float*>(sm + S::QTOP_OFF + 32);
+    const float* par = reinterpret_cast<const float*>(sm + S::PAR_OFF);
+    // a query row and a quarter of the keys: what a reduction over the keys takes a thread
+    const int rcol = sidx % N, rpart = sidx / N;
+    auto over_keys = [&](auto f, float* to, float v, auto join) {
+      if (rpart < 4) {
+#pragma unroll 4
+        for (int k = 0; k < 32; ++k) v = join(v, f(park[(32 * rpart + k) * N + rcol], 32 * rpart + k));
+        to[rpart * 64 + rcol] = v;
+      }
+    };
+    auto fmax2 = [](float a, float b) { return fmaxf(a, b); };
+    auto fsum2 = [](float a, float b) { return a + b; };
+    auto store_park = [&](const float* v) {
+#pragma unroll
+      for (int i = 0; i < NC; i += 4) *reinterpret_cast<float4*>(park + kl * N + col0 + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    };
+    uint32_t blocks = 0;                             // pages of block rows so far, per buffer
+    while (next()) {
+      const uint32_t qb = items & 1;
+      const int h = wk.it / p.n_rt, rb = wk.it - h * p.n_rt, Tc = wk.cached();
+      hold(QF + qb, items >> 1, 12);
+      ++items;
+      if (sidx < N) {
+        float* r = rcf + 4 * (sidx >> 1) + (sidx & 1);
+        r[0] = qsum[qb * 64 + sidx]; r[2] = 0.f;
+        mref[sidx] = rref[sidx] = -CUDART_INF_F;
+        vinv[sidx] = 0x1p126f;
+      }
+      const float c24 = qc[qb] * 16777216.f;         // undoes the codes' 2^-24
+      uint64_t l[NC / 2], z[NC / 2];
+#pragma unroll
+      for (int i = 0; i < NC / 2; ++i) l[i] = z[i] = pack2(0.f, 0.f);
+      soft_sync();
+      if (sidx == 0) mbar_arrive(BAR(QE + qb));      // (with the last S^T product: the query buffer is free)
+      const int r0 = rb * N, rows = min(N, p.n_q * p.G - r0);
+      for (int t = wk.t0; t < wk.t1; ++t, ++g) {
+        const uint32_t s = g % STAGES, buf = g & 1;
+        const bool first = t == wk.t0, own = t >= Tc;
+        // ---- this key's step and lowest value
+        hold(FULL + s, g / STAGES, 13);
+        float k1, k0, v1, v0;
+        bool gone;
+        if (!own) {
+          const uint32_t blk = base + S::RING_OFF + s * S::PAGE + quarter * F::BLOCK + lane * 4;
+          gone = bad[s] != 0 || t * TILE + kl >= wk.L;
+          const uint32_t kp = gone ? 0u : lds32(blk + F::K_PAR), vp = gone ? 0u : lds32(blk + F::V_PAR);
+          k1 = bf_lo(kp) * c24; k0 = bf_hi(kp); v1 = bf_lo(vp); v0 = fmaf(v1, 8.f, bf_hi(vp));
+        } else {
+          hold(BLK + buf, blocks >> (16 * buf), 14);
+          blocks += 1u << (16 * buf);                // (only the low bit of each count is looked at)
+          blocks &= 0x00010001u;
+          gone = !p.has_new || wk.L < 0 || kl >= p.n_q;
+          k1 = gone ? 0.f : par[s * 128 + (kl & 63)]; k0 = 0.f; v1 = gone ? 0.f : par[s * 128 + 64 + (kl & 63)]; v0 = 0.f;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(EMPTY + s));
+        hold(SF + buf, g >> 1, 15);
+        tc_fence_after();
+        const bool plain = !own && !__any_sync(0xFFFFFFFFu, gone);     // every row sees every key of this warp
+        float x[NC];
+        uint32_t hw[NC / 2];
+        // `fresh`: the references have to come from this page; `settled`: they have
+        bool fresh = first, settled = first;
+#pragma unroll 1
+        for (;;) {
+          // ---- scores less the rows' references, for this key and its rows
+#pragma unroll
+          for (int j = 0; j < NP; ++j) tmem_ld8(TM_S + buf * 64 + lanes + col0 + 8 * j, x + 8 * j);
+          tmem_wait_ld();
+          {
+            const uint64_t k1p = pack2(k1, k1), k0p = pack2(k0, k0);
+#pragma unroll
+            for (int i = 0; i < NC / 2; ++i) {
+              uint64_t sum, ref;
+              asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(sum), "=l"(ref) : "r"(rc_at + 16 * i));
+              unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), k1p, fma2(k0p, sum, own ? 0ull : ref)), x[2 * i], x[2 * i + 1]);
+            }
+          }
+          if (own) {                                 // (rows next to the largest number: a score stays one)
+#pragma unroll
+            for (int i = 0; i < NC; ++i) x[i] = (x[i] > 1e38f ? 1e38f : x[i] < -1e38f ? -1e38f : x[i]) + rcf[4 * ((col0 + i) >> 1) + 2 + (i & 1)];
+          }
+          if (!plain) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+              bool vis = !gone;
+              if (own && vis) vis = col0 + i < rows && ((p.mask[(r0 + col0 + i) >> p.gsh] >> kl) & 1ull);
+              if (!vis) x[i] = -CUDART_INF_F;
+            }
+          }
+          if (!fresh) {
+            bool over = false;
+            if (!settled) {
+              // do scores or weights pass the limits?  (the weights by a bound: the largest score, the largest vinv)
+              float a[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+              for (int i = 4; i < NC; i += 2) a[(i >> 1) & 3] = max3(a[(i >> 1) & 3], x[i], x[i + 1]);
+              a[0] = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
+              over = a[0] > X_LIMIT || fast_exp2(a[0]) * v1 * *vtop > W_LIMIT;
+            }
+            // ---- e, and the weights e step as f16
+            const uint64_t v1p = pack2(v1, v1);
+#pragma unroll
+            for (int i = 0; i < NC / 2; ++i) {
+              x[2 * i] = fast_exp2(x[2 * i]); x[2 * i + 1] = fast_exp2(x[2 * i + 1]);
+              uint64_t vi;
+              asm volatile("ld.shared.b64 %0, [%1];" : "=l"(vi) : "r"(vinv_at + 8 * i));
+              float w0, w1;
+              unpack2(mul2(mul2(pack2(x[2 * i], x[2 * i + 1]), v1p), vi), w0, w1);
+              hw[i] = pack_h(w0, w1);
+            }
+            if (settled || !soft_any(over)) break;
+            fresh = settled = true;                  // (from the scores again: they are still in tensor memory)
+            continue;
+          }
+          // ---- new references, from this page's largest scores and weights per query row
+          fresh = false;
+          if (!first) {                              // (P^T's buffers are idle then, and the products so far there to be scaled)
+            hold(PE + ((g - 1) & 1), (g - 1) >> 1, 16);
+            tc_fence_after();
+          }
+          store_park(x);
+          if (half == 0) vkey[kl] = v1;
+          soft_sync();
+          over_keys([](float v, int) { return v; }, xq, -CUDART_INF_F, fmax2);
+          soft_sync();
+          if (sidx < N) {
+            // (relative to the reference so far, or to 0)
+            const float up = fmaxf(fmaxf(xq[sidx], xq[64 + sidx]), fmaxf(xq[128 + sidx], xq[192 + sidx]));
+            const float mo = mref[sidx], mn = fmaxf(mo, mo == -CUDART_INF_F ? up : mo + up);
+            fq[sidx] = mo == mn ? 1.f : fast_exp2(mo - mn);
+            xz[sidx] = mn == -CUDART_INF_F ? 0.f : mo == -CUDART_INF_F ? -mn : mo - mn;   // what the scores move by
+            mref[sidx] = mn;
+            rcf[4 * (sidx >> 1) + 2 + (sidx & 1)] = mn == -CUDART_INF_F ? 0.f : -mn;
+          }
+          soft_sync();
+          {
+            const float by = xz[rcol];
+            over_keys([&](float v, int k) { return fast_exp2(v + by) * vkey[k]; }, xq, 0.f, fmax2);
+          }
+          soft_sync();
+          if (sidx < N) {
+            const float tm = fmaxf(fmaxf(xq[sidx], xq[64 + sidx]), fmaxf(xq[128 + sidx], xq[192 + sidx])), m = mref[sidx];
+            float R = rref[sidx], v = R == -CUDART_INF_F ? 0x1p126f : fast_exp2(fminf(m - R + W_SHIFT, 126.f)), f = 1.f;
+            if (tm * v > W_LIMIT) {
+              const float nr = m + (float)((int)(__float_as_uint(tm) >> 23) - 127);
+              f = fast_exp2(R - nr);
+              rref[sidx] = R = nr;
+              v = fast_exp2(fminf(m - R + W_SHIFT, 126.f));
+            }
+            go[sidx] = f; vinv[sidx] = v;
+          }
+          soft_sync();
+          if (warp == SOFT_WARP0) {                  // (a row that is not a number, or has no key yet, keeps its bound: not counted)
+            float v = 0.f;
+            for (int i = lane; i < N; i += 32) v = fmaxf(v, rref[i] == -CUDART_INF_F ? 0.f : vinv[i]);
+            const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v));
+            if (lane == 0) *vtop = __uint_as_float(m);
+          }
+          if (!first) {
+#pragma unroll
+            for (int i = 0; i < NC / 2; ++i) {
+              const uint64_t f = *reinterpret_cast<const uint64_t*>(fq + col0 + 2 * i);
+              l[i] = mul2(l[i], f); z[i] = mul2(z[i], f);
+            }
+#pragma unroll 1
+            for (int j = 0; j < NP; ++j) {
+              float o[8];
+              tmem_ld8(TM_O + lanes + col0 + 8 * j, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 8; ++e) o[e] *= go[col0 + 8 * j + e];
+              tmem_st8(TM_O + lanes + col0 + 8 * j, o);
+            }
+            tmem_wait_st();
+          }
+          soft_sync();
+        }
+        // ---- S^T goes back; P^T out; sums of e and of e (lo + 8 step)
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(SE + buf));
+        if (g >= 2) hold(PE + buf, (g - 2) >> 1, 17);
+#pragma unroll
+        for (int j = 0; j < NP; ++j)
+          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};"
+                       ::"r"(prow + buf * S::P_BYTES + ((((uint32_t)(col0 >> 3) + j) ^ swz) << 4)), "r"(hw[4 * j]), "r"(hw[4 * j + 1]), "r"(hw[4 * j + 2]), "r"(hw[4 * j + 3]) : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(PF + buf));
+        {
+          const uint64_t v0p = pack2(v0, v0);
+#pragma unroll
+          for (int i = 0; i < NC / 2; ++i) {
+            const uint64_t e = pack2(x[2 * i], x[2 * i + 1]);
+            l[i] = add2(l[i], e);
+            z[i] = fma2(e, v0p, z[i]);
+          }
+        }
+      }
+      // ---- the item's (or piece's) end: sums over the keys, then O^T
+      hold(PE + ((g - 1) & 1), (g - 1) >> 1, 18);
+      tc_fence_after();
+      {
+        float v[NC];
+#pragma unroll
+        for (int i = 0; i < NC / 2; ++i) unpack2(l[i], v[2 * i], v[2 * i + 1]);
+        store_park(v);
+        soft_sync();
+        over_keys([](float a, int) { return a; }, xq, 0.f, fsum2);
+        soft_sync();
+#pragma unroll
+        for (int i = 0; i < NC / 2; ++i) unpack2(z[i], v[2 * i], v[2 * i + 1]);
+        store_park(v);
+        soft_sync();
+        over_keys([](float a, int) { return a; }, xz, 0.f, fsum2);
+        soft_sync();
+      }
+      const int T = wk.pages(p.has_new);
+      const bool whole = wk.t0 == 0 && wk.t1 == T;
+      const uint32_t at = prefix[wk.b] + (uint32_t)(wk.it * (T + SHARE_COST));   // the item's place in the list
+      uint32_t piece0 = 0;
+      int pieces = 1;
+      if (!whole) {
+        piece0 = cut.owner(at + SHARE_COST);
+        pieces = (int)(cut.owner(at + SHARE_COST + T - 1) - piece0) + 1;
+      }
+      constexpr int SLOT = N * (DH + 2);             // (a block's share can hold the end of one cut item and the start of another)
+      float* ps = p.part + (int64_t)(2 * (int)blockIdx.x + (wk.opens ? 0 : 1)) * SLOT;
+      if (sidx < N) {
+        const float ls = (xq[sidx] + xq[64 + sidx]) + (xq[128 + sidx] + xq[192 + sidx]);
+        const float zs = (xz[sidx] + xz[64 + sidx]) + (xz[128 + sidx] + xz[192 + sidx]);
+        const float m = mref[sidx], f = rref[sidx] == -CUDART_INF_F ? 1.f : fast_exp2(rref[sidx] - m - W_SHIFT);
+        const float rd = !whole ? 1.f : ls > 0.f || ls != ls ? 1.f / ls : 0.f;   // a row without keys: zeros
+        fq[sidx] = f * rd; go[sidx] = zs * rd;
+        if (sidx < rows) {
+          if (!whole) {
+            __stcg(ps + N * DH + sidx, m);
+            __stcg(ps + N * DH + N + sidx, ls);
+          } else if (p.lse) {
+            int i, hq;
+            row_of(p, h, r0 + sidx, i, hq);
+            p.lse[((int64_t)wk.b * p.H_q + hq) * p.n_q + i] = (m + log2f(ls)) * 0.6931471805599453f;
+          }
+        }
+      }
+      soft_sync();
+#pragma unroll 1
+      for (int j = 0; j < NP; ++j) {
+        float o[8];
+        tmem_ld8(TM_O + lanes + col0 + 8 * j, o);
+        tmem_wait_ld();
+        if (kl < DH) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int r = col0 + 8 * j + e;
+            const float v = fmaf(o[e], fq[r], go[r]);
+            if (r < rows) {
+              if (whole) {
+                int i, hq;
+                row_of(p, h, r0 + r, i, hq);
+                p.out[(((int64_t)wk.b * p.n_q + i) * p.H_q + hq) * DH + kl] = __float2bfloat16_rn(v);
+              } else {
+                __stcg(ps + r * DH + kl, v);
+              }
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      if (*abort_flag && p.status && sidx == 0) atomicOr(p.status + wk.b, SPACE_ST_TIMEOUT);
+      if (!whole) {
+        __threadfence();
+        soft_sync();
+        if (sidx == 0) {
+          int* arrived = p.arrived + ((wk.b * p.H_kv + h) * p.n_rt + rb);
+          const int last = atomicAdd(arrived, 1) == pieces - 1;
+          if (last) *arrived = 0;                    // ready for the next call
+          __threadfence();
+          *last_flag = last;
+        }
+        soft_sync();
+        if (*last_flag) join_pieces<DH, N>(p, cut, wk.b, h, r0, rows, piece0, pieces, at, sidx, 256);
+      }
+      soft_sync();                                   // references, factors and the flag are free for the next item
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+}
+
+template <int DH, int NP>
+size_t smem_bytes(int max_batch) { return Smem<DH, NP>::TABLE_OFF + (size_t)(max_batch + 1) * 4 + (size_t)max_batch * 4; }
+
+template <int DH, int NP>
+cudaError_t launch_width(Params& p, const space_ctx* ctx, cudaStream_t st) {
+  static unsigned long long done_mask = 0;           // devices on which the kernel may have its shared memory
+  const int max_batch = ctx->cfg.max_batch;
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev >= 64 || !((done_mask >> dev) & 1ull)) {
+    cudaFuncSetAttribute(kvq_attn_tc_kernel<DH, NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<DH, NP>(128));
+    if (dev < 64) done_mask |= 1ull << dev;
+  }
+  p.n_groups = ctx->sm_count;
+  return launch_pdl(kvq_attn_tc_kernel<DH, NP>, dim3(p.n_groups), dim3(THREADS), smem_bytes<DH, NP>(max_batch), st, p, max_batch);
+}
+
+template <int DH>
+cudaError_t launch_dim(Params& p, const space_ctx* ctx, int np, cudaStream_t st) {
+  switch (np) {
+    case 1: return launch_width<DH, 1>(p, ctx, st);
+    case 2: return launch_width<DH, 2>(p, ctx, st);
+    case 3: return launch_width<DH, 3>(p, ctx, st);
+    default: return launch_width<DH, 4>(p, ctx, st);
+  }
+}
+
+}  // namespace
+
+size_t kvq_tc_partial_floats(const space_config* c, int sm_count) { return 2 * (size_t)sm_count * 64 * (c->head_dim + 2); }
+
+// Items of equal width, as many as 64 rows each need; widths are multiples of 16.
+int launch_kvq_attn_tc(space_ctx* ctx, kvq::Params& p, cudaStream_t st) {
+  const int rows = p.n_q * p.G, blocks = (rows + 63) / 64, np = ((rows + blocks - 1) / blocks + 15) / 16;
+  p.n_rt = (rows + 16 * np - 1) / (16 * np);
+  return cuda_ok(ctx->cfg.head_dim == 128 ? launch_dim<128>(p, ctx, np, st) : launch_dim<64>(p, ctx, np, st));
+}

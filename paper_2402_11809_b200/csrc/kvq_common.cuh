@@ -46,18 +46,33 @@ __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 
 
 // A pair of bf16 with a NaN made 0 and an infinity the largest finite value.
 __device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
-  uint32_t r = w;
-#pragma unroll
-  for (int s = 0; s < 32; s += 16) {
-    const uint32_t x = (w >> s) & 0x7FFFu;
-    if (x > 0x7F80u) r &= ~(0xFFFFu << s);
-    else if (x == 0x7F80u) r -= 1u << s;
-  }
-  return r;
+  const uint32_t mag = w & 0x7FFF7FFFu, nan = __vcmpgtu2(mag, 0x7F807F80u);
+  return (__vminu2(mag, 0x7F7F7F7Fu) | (w & 0x80008000u)) & ~nan;
 }
-__device__ __forceinline__ bool any_nonfinite(const uint4& v) {
+__device__ __forceinline__ uint32_t max_bits(const uint4& v) {     // of eight magnitudes
   const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
-  return (m & 0xFFFFu) >= 0x7F80u || (m >> 16) >= 0x7F80u;
+  return max(m & 0xFFFFu, m >> 16);
+}
+__device__ __forceinline__ bool any_nonfinite(const uint4& v) { return max_bits(v) >= 0x7F80u; }
+__device__ __forceinline__ void make_finite(uint4& v) {
+  if (max_bits(v) >= 0x7F80u) v = make_uint4(finite_pair(v.x), finite_pair(v.y), finite_pair(v.z), finite_pair(v.w));
+}
+__device__ __forceinline__ uint4 scale_bf16(const uint4& v, float f) {         // f a power of two
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 y = __floats2bfloat162_rn(bf_lo(w[i]) * f, bf_hi(w[i]) * f);
+    r[i] = *reinterpret_cast<const uint32_t*>(&y);
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+// The same, with the largest magnitude's bits.
+__device__ __forceinline__ uint32_t top_bits(uint4& v) {
+  const uint32_t m = max_bits(v);
+  if (m < 0x7F80u) return m;
+  v = make_uint4(finite_pair(v.x), finite_pair(v.y), finite_pair(v.z), finite_pair(v.w));
+  return max_bits(v);
 }
 
 }  // namespace kvq
