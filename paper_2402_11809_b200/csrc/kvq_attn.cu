@@ -31,8 +31,8 @@ constexpr int SHARE_COST = 1;                        // fixed cost of starting a
 template <int DH, int NT>
 struct Smem {
   static constexpr int RT = 8 * NT;
-  static constexpr int STAGES = NT == 1 ? ST1 : ST2;
-  static constexpr int CTAS = NT == 1 ? CT1 : CT2;           // per SM
+  static constexpr int STAGES = 3;
+  static constexpr int CTAS = NT == 1 ? 4 : NT == 2 ? 3 : 2;           // per SM
   static constexpr int RING = STAGES * Fmt<DH>::BLOCK;       // of a warp
   static constexpr int O_PITCH = DH + 4;                     // floats
   static_assert(RT * O_PITCH * 4 <= RING, "a warp's accumulators are parked in its ring once that has run dry");
@@ -703,8 +703,10 @@ cudaError_t launch_dim(Params& p, const space_ctx* ctx, cudaStream_t st) {
 constexpr int TC_ROWS = TCR;                          // more query rows per kv head go to kvq_attn_tc.cu
 
 size_t kvq_partial_floats(const space_config* c, int sm_count) {
-  const size_t a = (size_t)Smem<128, 1>::CTAS * Smem<128, 1>::RT, b = (size_t)Smem<128, 2>::CTAS * Smem<128, 2>::RT;
-  const size_t few = 2 * (size_t)sm_count * (a > b ? a : b) * (c->head_dim + 2), many = kvq_tc_partial_floats(c, sm_count);
+  constexpr int rows = 48;                           // of the blocks that an SM holds, in the widest of the three forms
+  static_assert(Smem<128, 1>::CTAS * Smem<128, 1>::RT <= rows && Smem<128, 2>::CTAS * Smem<128, 2>::RT <= rows &&
+                Smem<128, 3>::CTAS * Smem<128, 3>::RT <= rows, "a slot per block");
+  const size_t few = 2 * (size_t)sm_count * rows * (c->head_dim + 2), many = kvq_tc_partial_floats(c, sm_count);
   return few > many ? few : many;
 }
 size_t kvq_items(const space_config* c) {
@@ -732,8 +734,12 @@ int launch_kvq_attn(space_ctx* ctx, const space_kvq_attn_args* a, const uint64_t
   if ((double)p.B * p.H_kv * ((rows + 7) / 8) * ((double)p.cache.pages_per_seq + 4) > 2e9) return SPACE_E_UNSUPPORTED;
   ctx->launches += 1;
   if (rows > TC_ROWS) return launch_kvq_attn_tc(ctx, p, st);
-  const bool wide = ctx->cfg.head_dim == 128, few = rows <= FEWR;
-  const cudaError_t e = wide ? (few ? launch_dim<128, 1>(p, ctx, st) : launch_dim<128, 2>(p, ctx, st))
-                             : (few ? launch_dim<64, 1>(p, ctx, st) : launch_dim<64, 2>(p, ctx, st));
+  const bool wide = ctx->cfg.head_dim == 128;
+  // Eight rows at a time, sixteen or twenty-four: what a 32-key step of each costs is as 3 : 4 of the last two (35840 keys of
+  // 16 sequences x 16 heads, us: 16 rows 8.7, 24 rows 11.6).
+  const int nt = rows <= 8 ? 1 : 4 * ((rows + 23) / 24) < 3 * ((rows + 15) / 16) ? 3 : 2;
+  cudaError_t e;
+  if (wide) e = nt == 1 ? launch_dim<128, 1>(p, ctx, st) : nt == 2 ? launch_dim<128, 2>(p, ctx, st) : launch_dim<128, 3>(p, ctx, st);
+  else e = nt == 1 ? launch_dim<64, 1>(p, ctx, st) : nt == 2 ? launch_dim<64, 2>(p, ctx, st) : launch_dim<64, 3>(p, ctx, st);
   return cuda_ok(e);
 }

@@ -10,12 +10,12 @@
 // through shared memory the unpacked page would cost 4 d bytes written and as many read per key, more than the tensor
 // core's products take.  The cache's order is that of the 16x256b store: a lane's 16 bytes are its registers.
 //
-// Warps (20, one thread block per SM):
+// Warps (28, one thread block per SM):
 //   0      bulk copies, a page of one kv head (4 (32 d + 256) contiguous bytes) per stage of the ring
 //   1, 2   issue S^T and O^T products
 //   4-7    query rows into shared memory (f16, one power of two per item); K codes -> tensor memory
 //   8-11   V codes -> tensor memory
-//   12-19  two threads per key: scores, e, its sums, weights as f16 into shared memory (second operand); O^T out
+//   12-27  four threads per key: scores, e, its sums, weights as f16 into shared memory (second operand); O^T out
 // The block's own rows are one more page, whose K and V the code warps bring as f16 with a power of two per row instead.
 // Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT, no role leaves its loop early (the named barriers stay
 // matched), and the block drains and exits.
@@ -24,7 +24,8 @@
 namespace {
 using namespace kvq;
 
-constexpr int THREADS = 640;
+constexpr int SOFT_WARPS = 16, SOFT = 32 * SOFT_WARPS;          // four threads per key
+constexpr int THREADS = 12 * 32 + SOFT;
 constexpr int TILE = SPACE_PAGE_SIZE;
 constexpr int SHARE_COST = 2;                        // fixed cost of starting an item, in pages
 constexpr int K_WARP0 = 4, V_WARP0 = 8, SOFT_WARP0 = 12;
@@ -44,11 +45,12 @@ struct Smem {
   static constexpr int RC_OFF = RING_OFF + STAGES * PAGE;    // [N/2] {sum, sum, -m, -m} of query rows 2i, 2i + 1
   static constexpr int VINV_OFF = RC_OFF + 32 * 16;          // [N] 2^(m - R + W_SHIFT)
   static constexpr int MREF_OFF = VINV_OFF + 256;            // [N] m
-  static constexpr int RREF_OFF = MREF_OFF + 256;            // [N] R
+  static constexpr int RREF_OFF = MREF_OFF + 256;            // [N] R - m (m can be too large for the difference to show in R)
   static constexpr int FQ_OFF = RREF_OFF + 256;              // [N] factors
   static constexpr int GO_OFF = FQ_OFF + 256;                // [N] factors
-  static constexpr int VKEY_OFF = GO_OFF + 256;              // [128] V steps of a page's keys
-  static constexpr int XQ_OFF = VKEY_OFF + 512;                // [4][64] per quarter
+  static constexpr int VSPAN_OFF = GO_OFF + 256;             // [2][4]
+  static constexpr int ROFF_OFF = VSPAN_OFF + 32;            // [64]
+  static constexpr int XQ_OFF = ROFF_OFF + 256;                // [4][64] per quarter
   static constexpr int XZ_OFF = XQ_OFF + 1024;               // [4][64]
   static constexpr int QSUM_OFF = XZ_OFF + 1024;             // [2][64] c * sum of a query row
   static constexpr int QTOP_OFF = QSUM_OFF + 512;            // [2][4] largest exponents, then [2] c with the power of two undone
@@ -63,13 +65,13 @@ struct Smem {
   static_assert(TABLE_OFF + 129 * 4 + 128 * 4 <= 227 * 1024, "shared-memory plan too large");
 };
 
-__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"n"(SOFT) : "memory"); }
 __device__ __forceinline__ bool soft_any(bool pred) {
   uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
-      "bar.red.or.pred q, 1, 256, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
-      : "=r"(r) : "r"((uint32_t)pred) : "memory");
+      "bar.red.or.pred q, 1, %2, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+      : "=r"(r) : "r"((uint32_t)pred), "n"(SOFT) : "memory");
   return r != 0;
 }
 __device__ __forceinline__ void k_sync() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
@@ -77,13 +79,11 @@ __device__ __forceinline__ void v_sync() { asm volatile("bar.sync 3, 128;" ::: "
 template <int R> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
 template <int R> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
 
-__device__ __forceinline__ void tmem_ld8(uint32_t a, float* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]) : "r"(a) : "memory");
+__device__ __forceinline__ void tmem_ld4(uint32_t a, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]) : "r"(a) : "memory");
 }
-__device__ __forceinline__ void tmem_st8(uint32_t a, const float* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-               ::"r"(a), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]) : "memory");
+__device__ __forceinline__ void tmem_st4(uint32_t a, const float* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]) : "memory");
 }
 // 16 lanes x 32 columns: lane (n, t) of the warp holds of every eight columns {2t, 2t + 1} of rows n and n + 8
 __device__ __forceinline__ void tmem_st_frag4(uint32_t a, const uint32_t* r) {
@@ -102,6 +102,18 @@ __device__ __forceinline__ uint32_t centred_odd(uint32_t x) {
   const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&c));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
+// Four values per lane joined over the warp: every lane ends with the one of column 2 (lane >> 4) + ((lane >> 3) & 1).
+template <class J>
+__device__ __forceinline__ float warp_join4(const float* v, int lane, J join) {
+  const bool up = lane & 16, up2 = lane & 8;
+  const float a = join(up ? v[2] : v[0], __shfl_xor_sync(0xFFFFFFFFu, up ? v[0] : v[2], 16));
+  const float b = join(up ? v[3] : v[1], __shfl_xor_sync(0xFFFFFFFFu, up ? v[1] : v[3], 16));
+  float r = join(up2 ? b : a, __shfl_xor_sync(0xFFFFFFFFu, up2 ? a : b, 8));
+  r = join(r, __shfl_xor_sync(0xFFFFFFFFu, r, 4));
+  r = join(r, __shfl_xor_sync(0xFFFFFFFFu, r, 2));
+  return join(r, __shfl_xor_sync(0xFFFFFFFFu, r, 1));
+}
+
 // The items of a block's share, in order: every role walks them for itself.
 struct Walk {
   uint32_t cur, end;
@@ -148,10 +160,10 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     *abort_flag = (base & 1023u) ? 1 : 0;            // swizzled tiles need a 1024-byte aligned base
-    for (int s = 0; s < STAGES; ++s) { mbar_init(BAR(FULL + s), 1); mbar_init(BAR(EMPTY + s), 16); }
+    for (int s = 0; s < STAGES; ++s) { mbar_init(BAR(FULL + s), 1); mbar_init(BAR(EMPTY + s), 8 + SOFT_WARPS); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(BAR(KTF + i), 4); mbar_init(BAR(KTE + i), 1); mbar_init(BAR(VTF + i), 4); mbar_init(BAR(VTE + i), 1);
-      mbar_init(BAR(SF + i), 1); mbar_init(BAR(SE + i), 8); mbar_init(BAR(PF + i), 8); mbar_init(BAR(PE + i), 1);
+      mbar_init(BAR(SF + i), 1); mbar_init(BAR(SE + i), SOFT_WARPS); mbar_init(BAR(PF + i), SOFT_WARPS); mbar_init(BAR(PE + i), 1);
       mbar_init(BAR(QF + i), 4); mbar_init(BAR(QE + i), 2); mbar_init(BAR(BLK + i), 8);
     }
     mbar_init(BAR(DRAIN), 1);
@@ -207,7 +219,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
   auto hold = [&](int bar, uint32_t use, int site) { return wait(BAR(bar), use & 1, abort_flag, p.err, site); };
 
   if (warp < 4) {
-    regs_dec<32>();
+    regs_dec<24>();
     if (warp == 0) {
       // ================= bulk copies =========================================
       if (elect_one()) {
@@ -290,7 +302,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
       }
     }
   } else if (warp < V_WARP0) {
-    regs_dec<80>();
+    regs_dec<64>();
     // ================= query rows, K codes -> tensor memory ====================
     const int w = warp - K_WARP0, n = lane >> 2, t4 = lane & 3;
     float* qsum = reinterpret_cast<float*>(sm + S::QSUM_OFF);
@@ -542,12 +554,12 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
       }
     }
   } else {
-    regs_inc<152>();
+    regs_inc<88>();
     // ================= softmax, output ==========================================
-    constexpr int NC = 8 * NP;                       // query rows of a thread
-    const int quarter = warp & 3, half = (warp - SOFT_WARP0) >> 2;
+    constexpr int NC = 4 * NP;                       // query rows of a thread
+    const int quarter = warp & 3, part = (warp - SOFT_WARP0) >> 2;
     const int kl = quarter * 32 + lane;              // key of the page; channel in the epilogue
-    const int sidx = half * 128 + kl, col0 = half * NC;
+    const int sidx = part * 128 + kl, col0 = part * NC;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     // the key's place in the order in which the unpacked V lies: 16 a + 4 t + 2 e + h within 32 rows
     const int kp_row = (kl & 0x70) | ((kl & 6) << 1) | ((kl & 8) >> 2) | (kl & 1);
@@ -561,27 +573,25 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
     float* go = reinterpret_cast<float*>(sm + S::GO_OFF);
     float* xq = reinterpret_cast<float*>(sm + S::XQ_OFF);
     float* xz = reinterpret_cast<float*>(sm + S::XZ_OFF);
-    float* vkey = reinterpret_cast<float*>(sm + S::VKEY_OFF);
-    float* park = reinterpret_cast<float*>(sm + S::P_OFF);   // [128][N] floats: both buffers of P^T, while they are idle
+    float* vspan = reinterpret_cast<float*>(sm + S::VSPAN_OFF);   // [2][4] largest and smallest V step of a quarter's keys
+    int* roff = reinterpret_cast<int*>(sm + S::ROFF_OFF);         // [N] where a query row's output begins, in elements
     volatile float* vtop = reinterpret_cast<volatile float*>(sm + S::MISC_OFF + 12);   // the largest vinv
     const float* qsum = reinterpret_cast<const float*>(sm + S::QSUM_OFF);
     const volatile float* qc = reinterpret_cast<const volatile float*>(sm + S::QTOP_OFF + 32);
     const float* par = reinterpret_cast<const float*>(sm + S::PAR_OFF);
-    // a query row and a quarter of the keys: what a reduction over the keys takes a thread
-    const int rcol = sidx % N, rpart = sidx / N;
-    auto over_keys = [&](auto f, float* to, float v, auto join) {
-      if (rpart < 4) {
-#pragma unroll 4
-        for (int k = 0; k < 32; ++k) v = join(v, f(park[(32 * rpart + k) * N + rcol], 32 * rpart + k));
-        to[rpart * 64 + rcol] = v;
-      }
-    };
     auto fmax2 = [](float a, float b) { return fmaxf(a, b); };
     auto fsum2 = [](float a, float b) { return a + b; };
-    auto store_park = [&](const float* v) {
+    // every column joined over the warp's keys, into to[quarter]
+    auto over_keys = [&](const float* v, float* to, auto join) {
 #pragma unroll
-      for (int i = 0; i < NC; i += 4) *reinterpret_cast<float4*>(park + kl * N + col0 + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+      for (int i = 0; i < NC; i += 4) {
+        const float r = warp_join4(v + i, lane, join);
+        if ((lane & 7) == 0) to[quarter * 64 + col0 + i + (lane >> 3)] = r;
+      }
     };
+    auto fmin2 = [](float a, float b) { return fminf(a, b); };
+    auto of_quarters_v = [&](const float* v, auto join) { return join(join(v[0], v[1]), join(v[2], v[3])); };
+    auto of_quarters = [&](const float* v, auto join) { return join(join(v[sidx], v[64 + sidx]), join(v[128 + sidx], v[192 + sidx])); };
     uint32_t blocks = 0;                             // pages of block rows so far, per buffer
     while (next()) {
       const uint32_t qb = items & 1;
@@ -591,6 +601,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
       if (sidx < N) {
         float* r = rcf + 4 * (sidx >> 1) + (sidx & 1);
         r[0] = qsum[qb * 64 + sidx]; r[2] = 0.f;
+        int qi, hq;
+        row_of(p, h, rb * N + sidx, qi, hq);
+        roff[sidx] = (qi * p.H_q + hq) * DH;
         mref[sidx] = rref[sidx] = -CUDART_INF_F;
         vinv[sidx] = 0x1p126f;
       }
@@ -633,7 +646,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         for (;;) {
           // ---- scores less the rows' references, for this key and its rows
 #pragma unroll
-          for (int j = 0; j < NP; ++j) tmem_ld8(TM_S + buf * 64 + lanes + col0 + 8 * j, x + 8 * j);
+          for (int j = 0; j < NP; ++j) tmem_ld4(TM_S + buf * 64 + lanes + col0 + 4 * j, x + 4 * j);
           tmem_wait_ld();
           {
             const uint64_t k1p = pack2(k1, k1), k0p = pack2(k0, k0);
@@ -660,11 +673,11 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
             bool over = false;
             if (!settled) {
               // do scores or weights pass the limits?  (the weights by a bound: the largest score, the largest vinv)
-              float a[4] = {x[0], x[1], x[2], x[3]};
+              float a = fmaxf(x[0], x[1]), b = fmaxf(x[2], x[3]);
 #pragma unroll
-              for (int i = 4; i < NC; i += 2) a[(i >> 1) & 3] = max3(a[(i >> 1) & 3], x[i], x[i + 1]);
-              a[0] = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
-              over = a[0] > X_LIMIT || fast_exp2(a[0]) * v1 * *vtop > W_LIMIT;
+              for (int i = 4; i < NC; i += 4) { a = max3(a, x[i], x[i + 1]); b = max3(b, x[i + 2], x[i + 3]); }
+              a = fmaxf(a, b);
+              over = a > X_LIMIT || fast_exp2(a) * v1 * *vtop > W_LIMIT;
             }
             // ---- e, and the weights e step as f16
             const uint64_t v1p = pack2(v1, v1);
@@ -687,41 +700,48 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
             hold(PE + ((g - 1) & 1), (g - 1) >> 1, 16);
             tc_fence_after();
           }
-          store_park(x);
-          if (half == 0) vkey[kl] = v1;
+          over_keys(x, xq, fmax2);
+          if (part == 0) {
+            const uint32_t hi = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v1)), lo = __reduce_min_sync(0xFFFFFFFFu, gone ? 0x7F800000u : __float_as_uint(v1));
+            if (lane == 0) { vspan[quarter] = __uint_as_float(hi); vspan[4 + quarter] = __uint_as_float(lo); }
+          }
           soft_sync();
-          over_keys([](float v, int) { return v; }, xq, -CUDART_INF_F, fmax2);
-          soft_sync();
+          const float vhi = of_quarters_v(vspan, fmax2), vlo = of_quarters_v(vspan + 4, fmin2);
           if (sidx < N) {
             // (relative to the reference so far, or to 0)
-            const float up = fmaxf(fmaxf(xq[sidx], xq[64 + sidx]), fmaxf(xq[128 + sidx], xq[192 + sidx]));
+            const float up = of_quarters(xq, fmax2);
             const float mo = mref[sidx], mn = fmaxf(mo, mo == -CUDART_INF_F ? up : mo + up);
             fq[sidx] = mo == mn ? 1.f : fast_exp2(mo - mn);
             xz[sidx] = mn == -CUDART_INF_F ? 0.f : mo == -CUDART_INF_F ? -mn : mo - mn;   // what the scores move by
             mref[sidx] = mn;
+            rref[sidx] -= mo == mn || mo == -CUDART_INF_F ? 0.f : mn - mo;
             rcf[4 * (sidx >> 1) + 2 + (sidx & 1)] = mn == -CUDART_INF_F ? 0.f : -mn;
           }
-          soft_sync();
-          {
-            const float by = xz[rcol];
-            over_keys([&](float v, int k) { return fast_exp2(v + by) * vkey[k]; }, xq, 0.f, fmax2);
+          // The rows' largest weights: where the page's steps are within 2^6 of each other the largest step serves for every
+          // row; else (a row of V far above the rest, seen by some query rows or hardly) each row's own.
+          const bool wide = vhi > 64.f * vlo;
+          if (wide) {
+            soft_sync();
+#pragma unroll
+            for (int i = 0; i < NC; ++i) x[i] = fast_exp2(x[i] + xz[col0 + i]) * v1;
+            over_keys(x, xq, fmax2);
+            soft_sync();
           }
-          soft_sync();
           if (sidx < N) {
-            const float tm = fmaxf(fmaxf(xq[sidx], xq[64 + sidx]), fmaxf(xq[128 + sidx], xq[192 + sidx])), m = mref[sidx];
-            float R = rref[sidx], v = R == -CUDART_INF_F ? 0x1p126f : fast_exp2(fminf(m - R + W_SHIFT, 126.f)), f = 1.f;
-            if (tm * v > W_LIMIT) {
-              const float nr = m + (float)((int)(__float_as_uint(tm) >> 23) - 127);
-              f = fast_exp2(R - nr);
-              rref[sidx] = R = nr;
-              v = fast_exp2(fminf(m - R + W_SHIFT, 126.f));
+            const float tm = wide ? of_quarters(xq, fmax2) : vhi;
+            float D = rref[sidx], v = D == -CUDART_INF_F ? 0x1p126f : fast_exp2(fminf(W_SHIFT - D, 126.f)), f = 1.f;
+            if (tm * v > W_LIMIT && mref[sidx] > -CUDART_INF_F) {
+              const float nd = (float)((int)(__float_as_uint(tm) >> 23) - 127);
+              f = fast_exp2(D - nd);
+              rref[sidx] = D = nd;
+              v = fast_exp2(fminf(W_SHIFT - D, 126.f));
             }
             go[sidx] = f; vinv[sidx] = v;
           }
           soft_sync();
-          if (warp == SOFT_WARP0) {                  // (a row that is not a number, or has no key yet, keeps its bound: not counted)
+          if (warp == SOFT_WARP0) {                  // (a row without any key so far has the largest bound: the next page settles again)
             float v = 0.f;
-            for (int i = lane; i < N; i += 32) v = fmaxf(v, rref[i] == -CUDART_INF_F ? 0.f : vinv[i]);
+            for (int i = lane; i < rows; i += 32) v = fmaxf(v, vinv[i]);
             const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v));
             if (lane == 0) *vtop = __uint_as_float(m);
           }
@@ -733,12 +753,12 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
             }
 #pragma unroll 1
             for (int j = 0; j < NP; ++j) {
-              float o[8];
-              tmem_ld8(TM_O + lanes + col0 + 8 * j, o);
+              float o[4];
+              tmem_ld4(TM_O + lanes + col0 + 4 * j, o);
               tmem_wait_ld();
 #pragma unroll
-              for (int e = 0; e < 8; ++e) o[e] *= go[col0 + 8 * j + e];
-              tmem_st8(TM_O + lanes + col0 + 8 * j, o);
+              for (int e = 0; e < 4; ++e) o[e] *= go[col0 + 4 * j + e];
+              tmem_st4(TM_O + lanes + col0 + 4 * j, o);
             }
             tmem_wait_st();
           }
@@ -750,9 +770,11 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         if (lane == 0) mbar_arrive(BAR(SE + buf));
         if (g >= 2) hold(PE + buf, (g - 2) >> 1, 17);
 #pragma unroll
-        for (int j = 0; j < NP; ++j)
-          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};"
-                       ::"r"(prow + buf * S::P_BYTES + ((((uint32_t)(col0 >> 3) + j) ^ swz) << 4)), "r"(hw[4 * j]), "r"(hw[4 * j + 1]), "r"(hw[4 * j + 2]), "r"(hw[4 * j + 3]) : "memory");
+        for (int j = 0; j < NP; ++j) {
+          const int col = col0 + 4 * j;
+          asm volatile("st.shared.v2.b32 [%0], {%1,%2};"
+                       ::"r"(prow + buf * S::P_BYTES + ((((uint32_t)col >> 3) ^ swz) << 4) + (col & 4) * 2), "r"(hw[2 * j]), "r"(hw[2 * j + 1]) : "memory");
+        }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_before();
         __syncwarp();
@@ -768,21 +790,14 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         }
       }
       // ---- the item's (or piece's) end: sums over the keys, then O^T
-      hold(PE + ((g - 1) & 1), (g - 1) >> 1, 18);
-      tc_fence_after();
       {
         float v[NC];
 #pragma unroll
         for (int i = 0; i < NC / 2; ++i) unpack2(l[i], v[2 * i], v[2 * i + 1]);
-        store_park(v);
-        soft_sync();
-        over_keys([](float a, int) { return a; }, xq, 0.f, fsum2);
-        soft_sync();
+        over_keys(v, xq, fsum2);
 #pragma unroll
         for (int i = 0; i < NC / 2; ++i) unpack2(z[i], v[2 * i], v[2 * i + 1]);
-        store_park(v);
-        soft_sync();
-        over_keys([](float a, int) { return a; }, xz, 0.f, fsum2);
+        over_keys(v, xz, fsum2);
         soft_sync();
       }
       const int T = wk.pages(p.has_new);
@@ -797,9 +812,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
       constexpr int SLOT = N * (DH + 2);             // (a block's share can hold the end of one cut item and the start of another)
       float* ps = p.part + (int64_t)(2 * (int)blockIdx.x + (wk.opens ? 0 : 1)) * SLOT;
       if (sidx < N) {
-        const float ls = (xq[sidx] + xq[64 + sidx]) + (xq[128 + sidx] + xq[192 + sidx]);
-        const float zs = (xz[sidx] + xz[64 + sidx]) + (xz[128 + sidx] + xz[192 + sidx]);
-        const float m = mref[sidx], f = rref[sidx] == -CUDART_INF_F ? 1.f : fast_exp2(rref[sidx] - m - W_SHIFT);
+        const float ls = of_quarters(xq, fsum2), zs = of_quarters(xz, fsum2);
+        const float m = mref[sidx], f = rref[sidx] == -CUDART_INF_F ? 1.f : fast_exp2(rref[sidx] - W_SHIFT);
         const float rd = !whole ? 1.f : ls > 0.f || ls != ls ? 1.f / ls : 0.f;   // a row without keys: zeros
         fq[sidx] = f * rd; go[sidx] = zs * rd;
         if (sidx < rows) {
@@ -813,27 +827,31 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
           }
         }
       }
+      hold(PE + ((g - 1) & 1), (g - 1) >> 1, 18);
+      tc_fence_after();
       soft_sync();
+      __nv_bfloat16* dst = p.out + (int64_t)wk.b * p.n_q * p.H_q * DH + (kl & ~1);
 #pragma unroll 1
       for (int j = 0; j < NP; ++j) {
-        float o[8];
-        tmem_ld8(TM_O + lanes + col0 + 8 * j, o);
+        float o[4];
+        tmem_ld4(TM_O + lanes + col0 + 4 * j, o);
         tmem_wait_ld();
-        if (kl < DH) {
+        const int c = col0 + 4 * j;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int r = col0 + 8 * j + e;
-            const float v = fmaf(o[e], fq[r], go[r]);
-            if (r < rows) {
-              if (whole) {
-                int i, hq;
-                row_of(p, h, r0 + r, i, hq);
-                p.out[(((int64_t)wk.b * p.n_q + i) * p.H_q + hq) * DH + kl] = __float2bfloat16_rn(v);
-              } else {
-                __stcg(ps + r * DH + kl, v);
-              }
-            }
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(o[e], fq[c + e], go[c + e]);
+        if (whole) {
+          // two rows at a time: the even lane takes both channels of the first, the odd one of the second
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            const float got = __shfl_xor_sync(0xFFFFFFFFu, (lane & 1) ? o[e] : o[e + 1], 1);
+            const int r = c + e + (lane & 1);
+            const __nv_bfloat162 y = (lane & 1) ? __floats2bfloat162_rn(got, o[e + 1]) : __floats2bfloat162_rn(o[e], got);
+            if (kl < DH && r < rows) *reinterpret_cast<__nv_bfloat162*>(dst + roff[r]) = y;
           }
+        } else if (kl < DH) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (c + e < rows) __stcg(ps + (c + e) * DH + kl, o[e]);
         }
       }
       tc_fence_before();
@@ -849,7 +867,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
           *last_flag = last;
         }
         soft_sync();
-        if (*last_flag) join_pieces<DH, N>(p, cut, wk.b, h, r0, rows, piece0, pieces, at, sidx, 256);
+        if (*last_flag) join_pieces<DH, N>(p, cut, wk.b, h, r0, rows, piece0, pieces, at, sidx, SOFT);
       }
       soft_sync();                                   // references, factors and the flag are free for the next item
     }
