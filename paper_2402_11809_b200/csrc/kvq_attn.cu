@@ -697,11 +697,6 @@ cudaError_t launch_dim(Params& p, const space_ctx* ctx, cudaStream_t st) {
 
 }  // namespace
 
-#ifndef TCR
-#define TCR 16
-#endif
-constexpr int TC_ROWS = TCR;                          // more query rows per kv head go to kvq_attn_tc.cu
-
 size_t kvq_partial_floats(const space_config* c, int sm_count) {
   constexpr int rows = 48;                           // of the blocks that an SM holds, in the widest of the three forms
   static_assert(Smem<128, 1>::CTAS * Smem<128, 1>::RT <= rows && Smem<128, 2>::CTAS * Smem<128, 2>::RT <= rows &&
@@ -733,7 +728,12 @@ int launch_kvq_attn(space_ctx* ctx, const space_kvq_attn_args* a, const uint64_t
   // the flat list is counted in 32 bits: items of eight rows at least, a page and the cost of starting more than a table names
   if ((double)p.B * p.H_kv * ((rows + 7) / 8) * ((double)p.cache.pages_per_seq + 4) > 2e9) return SPACE_E_UNSUPPORTED;
   ctx->launches += 1;
-  if (rows > TC_ROWS) return launch_kvq_attn_tc(ctx, p, st);
+  // More than 48 rows, and pages for every SM: the tensor-memory form.  (What a page costs there is less, what an item costs
+  // more, and there is one block per SM to hide it: 16 x 32 heads, 49 rows, us here / there: 2000 keys 208 / 188, 8000 keys
+  // 600 / 459; 8 x 8 heads, 392 rows of 8192 keys 451 / 396; but one sequence of 300 keys, 8 heads, 64 rows 15 / 26, and
+  // 36 rows of 2000 keys 149 / 172.  The lengths are on the device: the table's width stands for them.)
+  const int blocks = (rows + 63) / 64;
+  if (rows > 48 && (int64_t)p.B * p.H_kv * blocks * p.cache.pages_per_seq >= 32 * (int64_t)ctx->sm_count) return launch_kvq_attn_tc(ctx, p, st);
   const bool wide = ctx->cfg.head_dim == 128;
   // Eight rows at a time, sixteen or twenty-four: what a 32-key step of each costs is as 3 : 4 of the last two (35840 keys of
   // 16 sequences x 16 heads, us: 16 rows 8.7, 24 rows 11.6).
