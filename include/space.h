@@ -510,8 +510,11 @@ int space_kvq_read(space_ctx* ctx, const space_kvq_read_args* args, void* stream
  * (SPACE_ST_BAD_PAGE).  Hidden rows have no influence, whatever they hold; non-finite elements of k_new /
  * v_new count as they do in space_kvq_append (without the status bit).
  * The output is bf16: scores and sums are fp32, the weights of the second product are rounded to 11 bits.
+ * The products take query rows as f16, scaled by one power of two for up to 64 rows of a kv head together: elements
+ * more than 2^21 times smaller than the largest of those rows are rounded, by at most 2^-29 of it; all others are exact.
  * Asynchronous on `stream`, no allocation; one call at a time per context (scratch of the context).
- * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE (batch or k beyond the context's), CUDA. */
+ * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE (batch or k beyond the context's), UNSUPPORTED (batch * n_kv_heads *
+ * ceil(query rows of a kv head / 8) * (pages_per_seq + 4) above 2e9), CUDA. */
 typedef struct {
   int32_t batch;
   int32_t k;                   /* 0 .. k_max; (k+1)^2 query rows                                   */

@@ -183,7 +183,7 @@ __device__ __forceinline__ float load_query(const Params& p, unsigned char* sm, 
   __syncthreads();
   static_assert(WARPS == 4, "one word per warp");
   top = max(max(tops[0], tops[1]), max(tops[2], tops[3])) >> 7;
-  // largest element in [2^8, 2^9): what f16 drops lies 2^-32 below it
+  // largest element in [2^8, 2^9): what f16 drops is 2^-29 of it at most
   const int e = top ? min(max(8 - ((int)top - 127), -100), 100) : 0;
   const float f = pow2(e), f16th = f * 0.0625f;
   const int t = x / (DH / 32), j = x % (DH / 32);    // piece: code word j of the lanes t, k-steps 2 j and 2 j + 1

@@ -897,19 +897,15 @@ cudaError_t launch_width(Params& p, const space_ctx* ctx, cudaStream_t st) {
 
 template <int DH>
 cudaError_t launch_dim(Params& p, const space_ctx* ctx, int np, cudaStream_t st) {
-  switch (np) {
-    case 1: return launch_width<DH, 1>(p, ctx, st);
-    case 2: return launch_width<DH, 2>(p, ctx, st);
-    case 3: return launch_width<DH, 3>(p, ctx, st);
-    default: return launch_width<DH, 4>(p, ctx, st);
-  }
+  return np == 3 ? launch_width<DH, 3>(p, ctx, st) : launch_width<DH, 4>(p, ctx, st);
 }
 
 }  // namespace
 
 size_t kvq_tc_partial_floats(const space_config* c, int sm_count) { return 2 * (size_t)sm_count * 64 * (c->head_dim + 2); }
 
-// Items of equal width, as many as 64 rows each need; widths are multiples of 16.
+// Items of equal width, as many as 64 rows each need; widths are multiples of 16.  More than 48 rows come here, so one
+// item has 49 to 64 of them and several have 33 to 64 each: 48 or 64 wide.
 int launch_kvq_attn_tc(space_ctx* ctx, kvq::Params& p, cudaStream_t st) {
   const int rows = p.n_q * p.G, blocks = (rows + 63) / 64, np = ((rows + blocks - 1) / blocks + 15) / 16;
   p.n_rt = (rows + 16 * np - 1) / (16 * np);

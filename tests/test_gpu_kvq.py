@@ -11,6 +11,7 @@ from oracle.layout import EQ5_LITERAL, SAME_GROUP
 
 pytestmark = pytest.mark.gpu
 P = 128
+WIDE = 5000                                          # pages of a table that names enough of them for the tensor-memory form
 
 
 @pytest.fixture(scope="module")
@@ -73,7 +74,8 @@ def random_cache(rng, lens, H, d, pps, spread=1.0):
     (64, 3, 1, 1, [31, 32, 63, 0], None),
     (128, 4, 25, 5, [0, 100, 126, 380], [1, 5, 3, 4]),                   # the accepted rows of a step, k = 4
     (64, 1, 64, 8, [1, 129], [8, 2]),
-    (128, 1, 16, 1, [17, 120], [16, 9]),                                 # the most that goes by rows, and one more
+    (128, 1, 16, 1, [17, 120], [16, 9]),
+    (128, 3, 12, 1, [31, 127], [12, 11]), (64, 2, 13, 1, [31, 127], [13, 12]),   # the most that goes by rows, and one more
     (128, 2, 17, 1, [17, 120, 0], [17, 0, 9]),
     (64, 5, 300, 1, [0, 1, 31, 129, 500], [300, 299, 33, 1, 0]),         # prompts by blocks, odd everything
     (128, 2, 257, 1, [37, 0], [257, 200]),
@@ -233,11 +235,39 @@ ATTN = [
 ]
 
 
-@pytest.mark.parametrize("d,H,G,k,lens,block", ATTN)
+# more than 48 query rows in tables wide enough for the tensor-memory form
+ATTN_WIDE = [
+    (64, 1, 4, 4, [0, 1, 31, 32, 33, 127, 128, 129], True), (128, 1, 1, 6, [600, 0, 1], True),
+    (128, 2, 1, 7, [250, 3000], True), (64, 3, 2, 5, [777, 130, 0], True), (128, 2, 4, 3, [384, 50], True),
+    (128, 8, 2, 7, [1999, 37, 1200, 2048, 640], True),                   # several items and many pages per thread block
+    (64, 4, 8, 5, [1500, 0, 900], True), (128, 1, 8, 7, [4000], True), (128, 16, 1, 6, [300] * 8, True),
+    (64, 4, 2, 7, [3500, 2900, 3100], False), (128, 2, 16, 1, [5000], False), (64, 1, 16, 2, [1030, 0, 128], False),
+    (64, 2, 16, 1, [77, 0], True),
+]
+# long lists of pages: every warp's ring goes round several times, items end and begin within a thread block's share
+ATTN_LONG = [
+    (64, 32, 1, 1, [1500, 1900, 700, 2048, 1, 1300, 2000, 1111], True),  # 8 query rows at a time
+    (64, 16, 1, 3, [2000, 1501, 2048, 900, 1999, 0, 1700, 1300], True),  # 16
+    (64, 12, 4, 1, [2047, 1500, 1800, 1203, 640, 1290], False),
+    (64, 8, 1, 4, [2500, 1501, 2048, 900, 1999, 40], True),              # 24 and a last row
+    (128, 8, 4, 2, [1500, 1480, 2001], True),
+]
+
+
+@pytest.mark.parametrize("d,H,G,k,lens,block", ATTN + ATTN_LONG)
 def test_attention(B, d, H, G, k, lens, block):
+    attention_case(B, d, H, G, k, lens, block)
+
+
+@pytest.mark.parametrize("d,H,G,k,lens,block", ATTN_WIDE)
+def test_attention_in_wide_tables(B, d, H, G, k, lens, block):
+    attention_case(B, d, H, G, k, lens, block, WIDE)
+
+
+def attention_case(B, d, H, G, k, lens, block, pps=0):
     rng = np.random.default_rng(d + 100 * H + 10 * G + k)
     n, n_q, Hq = len(lens), (k + 1) ** 2, H * G
-    pps = max(1, max((L + P - 1) // P for L in lens) + 1)
+    pps = pps or max(1, max((L + P - 1) // P for L in lens) + 1)
     pool, table = random_cache(rng, lens, H, d, pps)
     qb = bits(rng, n, n_q, Hq + 1, d, scale=2.0)                         # a head more than is used: strided rows
     kb, vb = (bits(rng, n, n_q, H, d), bits(rng, n, n_q, H, d)) if block else (None, None)
@@ -276,17 +306,18 @@ def run_attention(B, q, pool, table, lens, k, kn=None, vn=None, H=1, d=64):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-def test_sequences_that_do_not_fit_and_pages_outside_the_pool(B, d):
+@pytest.mark.parametrize("k,pps", [(1, 3), (5, WIDE)])
+def test_sequences_that_do_not_fit_and_pages_outside_the_pool(B, d, k, pps):
     rng = np.random.default_rng(4)
-    lens = [300, 40, 300, 50]
-    pool, table = random_cache(rng, lens, 2, d, 3)
-    q, kn, vn = bits(rng, 4, 4, 4, d), bits(rng, 4, 4, 2, d), bits(rng, 4, 4, 2, d)
-    given = [300, -3, 385, 50]
+    lens, n_q = [300, 40, 300, 50], (k + 1) ** 2
+    pool, table = random_cache(rng, lens, 2, d, pps)
+    q, kn, vn = bits(rng, 4, n_q, 4, d), bits(rng, 4, n_q, 2, d), bits(rng, 4, n_q, 2, d)
+    given = [300, -3, pps * P + 1, 50]
     table[0, 1], table[3, 0] = pool.shape[0], -1
     for block in (True, False):
         kb, vb = (kn, vn) if block else (None, None)
-        out, lse, status = run_attention(B, q, pool, table, given, 1, kb, vb, 2, d)
-        want, want_lse = kvq.attention(bf16_bits_to_f64(q), pool, table, [300, 0, 0, 50], 1, 1 / math.sqrt(d),
+        out, lse, status = run_attention(B, q, pool, table, given, k, kb, vb, 2, d)
+        want, want_lse = kvq.attention(bf16_bits_to_f64(q), pool, table, [300, 0, 0, 50], k, 1 / math.sqrt(d),
                                        *((bf16_bits_to_f64(kb), bf16_bits_to_f64(vb)) if block else (None, None)))
         want[1:3], want_lse[1:3] = 0, -np.inf
         check(out, lse, want, want_lse, [30.0] * 4)
@@ -294,13 +325,13 @@ def test_sequences_that_do_not_fit_and_pages_outside_the_pool(B, d):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("k", [2, 5])
-def test_hidden_rows_have_no_influence(B, d, k):
+@pytest.mark.parametrize("k,pps", [(2, 2), (5, 2), (5, WIDE)])
+def test_hidden_rows_have_no_influence(B, d, k, pps):
     """What one block row holds reaches only the rows that see it, whatever it is."""
     rng = np.random.default_rng(6)
     n_q = (k + 1) ** 2
     lens = [200, 0]
-    pool, table = random_cache(rng, lens, 1, d, 2)
+    pool, table = random_cache(rng, lens, 1, d, pps)
     q, kn, vn = bits(rng, 2, n_q, 2, d), bits(rng, 2, n_q, 1, d), bits(rng, 2, n_q, 1, d)
     base, base_lse, _ = run_attention(B, q, pool, table, lens, k, kn, vn, 1, d)
     see = kvq.visible(k)
@@ -321,17 +352,18 @@ def test_hidden_rows_have_no_influence(B, d, k):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-def test_query_rows_do_not_touch_each_other(B, d):
+@pytest.mark.parametrize("k,pps", [(2, 3), (6, WIDE)])
+def test_query_rows_do_not_touch_each_other(B, d, k, pps):
     rng = np.random.default_rng(7)
-    lens = [333]
-    pool, table = random_cache(rng, lens, 1, d, 3)
-    q, kn, vn = bits(rng, 1, 9, 2, d), bits(rng, 1, 9, 1, d), bits(rng, 1, 9, 1, d)
-    base, base_lse, _ = run_attention(B, q, pool, table, lens, 2, kn, vn, 1, d)
+    lens, n_q = [333], (k + 1) ** 2
+    pool, table = random_cache(rng, lens, 1, d, pps)
+    q, kn, vn = bits(rng, 1, n_q, 2, d), bits(rng, 1, n_q, 1, d), bits(rng, 1, n_q, 1, d)
+    base, base_lse, _ = run_attention(B, q, pool, table, lens, k, kn, vn, 1, d)
     q2 = q.copy()
     q2[0, 1, 0, 3] = 0x7FC0
     q2[0, 4, 1, 9] = 0x7F80
-    out, lse, _ = run_attention(B, q2, pool, table, lens, 2, kn, vn, 1, d)
-    hit = np.zeros((9, 2), bool)
+    out, lse, _ = run_attention(B, q2, pool, table, lens, k, kn, vn, 1, d)
+    hit = np.zeros((n_q, 2), bool)
     hit[1, 0] = hit[4, 1] = True
     assert np.isnan(out[0][hit]).all() and np.isnan(lse[0].T[hit]).all()
     assert (out[0][~hit] == base[0][~hit]).all() and (lse[0].T[~hit] == base_lse[0].T[~hit]).all()
@@ -339,11 +371,12 @@ def test_query_rows_do_not_touch_each_other(B, d):
 
 @pytest.mark.parametrize("spread", [1e-6, 1e-3, 300.0, 1e6])
 @pytest.mark.parametrize("d", [64, 128])
-def test_value_scales(B, d, spread):
+@pytest.mark.parametrize("k,pps", [(1, 4), (4, WIDE)])
+def test_value_scales(B, d, spread, k, pps):
     """V rows of other magnitudes, among them rows far larger and far smaller than the rest."""
     rng = np.random.default_rng(8)
-    lens = [400, 90]
-    pool, table = random_cache(rng, lens, 1, d, 4)
+    lens, n_q = [400, 90], (k + 1) ** 2
+    pool, table = random_cache(rng, lens, 1, d, pps)
     mem = pool.reshape(pool.shape[0], 1, 4, -1)
     n = kvq.BLOCK * d
     par = mem[..., n + 128:].copy().view(np.uint16).reshape(-1, 64)
@@ -353,18 +386,19 @@ def test_value_scales(B, d, spread):
     ok = np.isfinite(val)
     par[ok] = f32_to_bf16_bits(val.astype(np.float32))[ok]
     mem[..., n + 128:] = par.view(np.uint8).reshape(mem[..., n + 128:].shape)
-    q, kn, vn = bits(rng, 2, 4, 4, d), bits(rng, 2, 4, 1, d), bits(rng, 2, 4, 1, d, scale=spread)
-    out, lse, _ = run_attention(B, q, pool, table, lens, 1, kn, vn, 1, d)
-    want, want_lse = kvq.attention(bf16_bits_to_f64(q), pool, table, lens, 1, 1 / math.sqrt(d), bf16_bits_to_f64(kn), bf16_bits_to_f64(vn))
+    q, kn, vn = bits(rng, 2, n_q, 4, d), bits(rng, 2, n_q, 1, d), bits(rng, 2, n_q, 1, d, scale=spread)
+    out, lse, _ = run_attention(B, q, pool, table, lens, k, kn, vn, 1, d)
+    want, want_lse = kvq.attention(bf16_bits_to_f64(q), pool, table, lens, k, 1 / math.sqrt(d), bf16_bits_to_f64(kn), bf16_bits_to_f64(vn))
     check(out, lse, want, want_lse, span_of(pool, table, lens, d, bf16_bits_to_f64(vn)))
 
 
 @pytest.mark.parametrize("d", [64, 128])
-def test_peaked_and_growing_scores(B, d):
+@pytest.mark.parametrize("k,pps", [(0, 12), (1, WIDE)])
+def test_peaked_and_growing_scores(B, d, k, pps):
     """Scores that grow along the sequence by far more than 2^8 between pages, and fall again."""
     rng = np.random.default_rng(11)
     L = 1500
-    pool, table = random_cache(rng, [L], 1, d, 12)
+    pool, table = random_cache(rng, [L], 1, d, pps)
     mem = pool.reshape(pool.shape[0], 1, 4, -1)
     n = kvq.BLOCK * d
     par = mem[..., n:n + 128].copy().view(np.uint16).reshape(pool.shape[0], 4, 64)
@@ -374,32 +408,33 @@ def test_peaked_and_growing_scores(B, d):
         ok = np.isfinite(v)
         par[table[0, t]][ok] = f32_to_bf16_bits(v.astype(np.float32))[ok]
     mem[..., n:n + 128] = par.view(np.uint8).reshape(mem[..., n:n + 128].shape)
-    q = bits(rng, 1, 1, 16, d, scale=4.0)
-    out, lse, _ = run_attention(B, q, pool, table, [L], 0, None, None, 1, d)
-    want, want_lse = kvq.attention(bf16_bits_to_f64(q), pool, table, [L], 0, 1 / math.sqrt(d))
+    q = bits(rng, 1, (k + 1) ** 2, 16, d, scale=4.0)
+    out, lse, _ = run_attention(B, q, pool, table, [L], k, None, None, 1, d)
+    want, want_lse = kvq.attention(bf16_bits_to_f64(q), pool, table, [L], k, 1 / math.sqrt(d))
     s = np.abs(want_lse).max()
     # weights follow scores of several hundred: an error of 128 * 2^-23 of that in the exponent
     spans = [x * (1 + 2048 * 128 * 2.0 ** -23 * s) for x in span_of(pool, table, [L], d, None)]
     check(out, lse, want, want_lse, spans, scores=4 * s)
 
 
-def test_other_layers_in_one_allocation_and_past_32_bits(B):
+@pytest.mark.parametrize("k,pps", [(0, 6), (3, WIDE)])
+def test_other_layers_in_one_allocation_and_past_32_bits(B, k, pps):
     """A pool whose pages are far apart (a layer among many), the last ones beyond 4 GB."""
-    d, H, L = 128, 2, 700
+    d, H, L, n_q = 128, 2, 700, (k + 1) ** 2
     rng = np.random.default_rng(12)
-    small, table = random_cache(rng, [L], H, d, 6)
+    small, table = random_cache(rng, [L], H, d, pps)
     head = small.shape[2]
     page_stride = 800_000_000 // 16 * 16
     big = torch.empty((small.shape[0] - 1) * page_stride + H * (head + 48), dtype=torch.uint8, device="cuda")
     pool = big.as_strided((small.shape[0], H, head), (page_stride, head + 48, 1))
     pool.copy_(dev(small))
-    q = bits(rng, 1, 1, 8, d)
+    q = bits(rng, 1, n_q, 8, d)
     ctx = B.Context(max_batch=1, n_q_heads=8, n_kv_heads=H, head_dim=d, k_max=7, vocab=8, s_cap=1 << 14)
-    out, status = torch.zeros(1, 1, 8, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
-    lse = torch.zeros(1, 8, 1, device="cuda")
+    out, status = torch.zeros(1, n_q, 8, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    lse = torch.zeros(1, 8, n_q, device="cuda")
     dt, dl, dq = dev(table), dev(np.array([L], np.int32)), dev(q)
-    ctx.space_kvq_attn_step(ctx.kvq_attn_args(dq, pool, dt, dl, out, 0, 0.1, lse=lse, status=status))
-    want, want_lse = kvq.attention(bf16_bits_to_f64(q), small, table, [L], 0, float(np.float32(0.1)))
+    ctx.space_kvq_attn_step(ctx.kvq_attn_args(dq, pool, dt, dl, out, k, 0.1, lse=lse, status=status))
+    want, want_lse = kvq.attention(bf16_bits_to_f64(q), small, table, [L], k, float(np.float32(0.1)))
     check(f64(out), f64(lse), want, want_lse, span_of(small, table, [L], d, None))
     # rows behind them, read back, and the pages copied where they stand
     new = bits(rng, 1, 20, H, d)
@@ -569,6 +604,15 @@ def test_refusals(B):
     for lib_call in (B.lib.space_kvq_attn_step, B.lib.space_kvq_append, B.lib.space_kvq_read):
         assert lib_call(None, None, None) == B.E_INVALID_ARG and lib_call(ctx._h, None, None) == B.E_INVALID_ARG
     assert ctx.launch_count == n0
+    # a list of pages that does not fit 32 bits
+    big = B.Context(max_batch=16, n_q_heads=4, n_kv_heads=4, head_dim=d, k_max=7, vocab=8, s_cap=512)
+    bq = torch.zeros(16, 64, 4, d, dtype=torch.bfloat16, device="cuda")
+    bp, bt, bl = B.kvq_pool(1, 4, d), torch.zeros(16, 1, dtype=torch.int32, device="cuda"), torch.zeros(16, dtype=torch.int32, device="cuda")
+    a = big.kvq_attn_args(bq, bp, bt, bl, torch.empty_like(bq), 7, 0.1)
+    a.cache.pages_per_seq = 1 << 23
+    with pytest.raises(B.SpaceError) as e:
+        big.space_kvq_attn_step(a)
+    assert e.value.code == B.E_UNSUPPORTED and big.launch_count == 0
     a = attn()
     a.batch = 0
     ctx.space_kvq_attn_step(a)
