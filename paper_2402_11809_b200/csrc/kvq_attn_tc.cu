@@ -57,23 +57,16 @@ struct Smem {
   static constexpr int PAR_OFF = QTOP_OFF + 64;              // [STAGES][2][64] block rows' K and V factors
   static constexpr int BAD_OFF = PAR_OFF + STAGES * 512;     // [STAGES] page outside the pool
   static constexpr int BAR_OFF = (BAD_OFF + STAGES * 4 + 15) / 16 * 16;
-  static constexpr int N_BARS = 2 * STAGES + 23;
+  static constexpr int N_BARS = 2 * STAGES + 24;
   static constexpr int MISC_OFF = BAR_OFF + (N_BARS * 8 + 15) / 16 * 16;
-  static constexpr int TABLE_OFF = MISC_OFF + 16;            // prefix[max_batch + 1], seq_len[max_batch]
+  static constexpr int OVER_OFF = MISC_OFF + 16;             // [2] the last page (of those that ask) whose scores pass a limit
+  static constexpr int TABLE_OFF = MISC_OFF + 32;            // prefix[max_batch + 1], seq_len[max_batch]
   static constexpr int V_PITCH = DH * 2 + 16;                // bytes: the block's V rows as f16, in a stage
   static_assert(SPACE_MAX_ROWS * V_PITCH <= PAGE, "the block's V rows fit a stage");
   static_assert(TABLE_OFF + 129 * 4 + 128 * 4 <= 227 * 1024, "shared-memory plan too large");
 };
 
 __device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"n"(SOFT) : "memory"); }
-__device__ __forceinline__ bool soft_any(bool pred) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
-      "bar.red.or.pred q, 1, %2, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
-      : "=r"(r) : "r"((uint32_t)pred), "n"(SOFT) : "memory");
-  return r != 0;
-}
 __device__ __forceinline__ void k_sync() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
 __device__ __forceinline__ void v_sync() { asm volatile("bar.sync 3, 128;" ::: "memory"); }
 template <int R> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
@@ -148,7 +141,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
   const uint32_t base = smem_u32(sm), bar0 = base + S::BAR_OFF;
   auto BAR = [&](int i) { return bar0 + 8u * i; };
   constexpr int FULL = 0, EMPTY = STAGES, KTF = 2 * STAGES, KTE = KTF + 2, VTF = KTF + 4, VTE = KTF + 6, SF = KTF + 8, SE = KTF + 10,
-                PF = KTF + 12, PE = KTF + 14, QF = KTF + 16, QE = KTF + 18, BLK = KTF + 20, DRAIN = KTF + 22;
+                PF = KTF + 12, PE = KTF + 14, QF = KTF + 16, QE = KTF + 18, BLK = KTF + 20, DRAIN = KTF + 22, OVER = KTF + 23;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::MISC_OFF);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF + 4);
   volatile int* last_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF + 8);
@@ -160,6 +153,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     *abort_flag = (base & 1023u) ? 1 : 0;            // swizzled tiles need a 1024-byte aligned base
+    for (int i = 0; i < 2; ++i) reinterpret_cast<volatile uint32_t*>(sm + S::OVER_OFF)[i] = 0;
     for (int s = 0; s < STAGES; ++s) { mbar_init(BAR(FULL + s), 1); mbar_init(BAR(EMPTY + s), 8 + SOFT_WARPS); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(BAR(KTF + i), 4); mbar_init(BAR(KTE + i), 1); mbar_init(BAR(VTF + i), 4); mbar_init(BAR(VTE + i), 1);
@@ -167,6 +161,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
       mbar_init(BAR(QF + i), 4); mbar_init(BAR(QE + i), 2); mbar_init(BAR(BLK + i), 8);
     }
     mbar_init(BAR(DRAIN), 1);
+    mbar_init(BAR(OVER), SOFT_WARPS);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -592,6 +587,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
     auto fmin2 = [](float a, float b) { return fminf(a, b); };
     auto of_quarters_v = [&](const float* v, auto join) { return join(join(v[0], v[1]), join(v[2], v[3])); };
     auto of_quarters = [&](const float* v, auto join) { return join(join(v[sidx], v[64 + sidx]), join(v[128 + sidx], v[192 + sidx])); };
+    uint32_t asked = 0;                              // pages whose scores were held against the limits so far
+    volatile uint32_t* over_at = reinterpret_cast<volatile uint32_t*>(sm + S::OVER_OFF);
     uint32_t blocks = 0;                             // pages of block rows so far, per buffer
     while (next()) {
       const uint32_t qb = items & 1;
@@ -670,14 +667,16 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
             }
           }
           if (!fresh) {
-            bool over = false;
             if (!settled) {
               // do scores or weights pass the limits?  (the weights by a bound: the largest score, the largest vinv)
               float a = fmaxf(x[0], x[1]), b = fmaxf(x[2], x[3]);
 #pragma unroll
               for (int i = 4; i < NC; i += 4) { a = max3(a, x[i], x[i + 1]); b = max3(b, x[i + 2], x[i + 3]); }
               a = fmaxf(a, b);
-              over = a > X_LIMIT || fast_exp2(a) * v1 * *vtop > W_LIMIT;
+              ++asked;
+              if (a > X_LIMIT || fast_exp2(a) * v1 * *vtop > W_LIMIT) over_at[asked & 1] = asked;
+              __syncwarp();
+              if (lane == 0) mbar_arrive(BAR(OVER));
             }
             // ---- e, and the weights e step as f16
             const uint64_t v1p = pack2(v1, v1);
@@ -690,7 +689,16 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
               unpack2(mul2(mul2(pack2(x[2 * i], x[2 * i + 1]), v1p), vi), w0, w1);
               hw[i] = pack_h(w0, w1);
             }
-            if (settled || !soft_any(over)) break;
+            if (settled) break;
+            // What this waits for are the other softmax warps, each of which comes here whatever its own waits gave (they are
+            // bounded, and short once one has run out).  So it does not look at the abort flag, and all read the same word.
+            if (!mbar_try(BAR(OVER), (asked - 1) & 1)) {
+              const uint64_t t0 = global_ns();
+#pragma unroll 1
+              while (!mbar_try(BAR(OVER), (asked - 1) & 1))
+                if (global_ns() - t0 > 8 * WAIT_NS) { *abort_flag = 1; break; }
+            }
+            if (over_at[asked & 1] != asked) break;
             fresh = settled = true;                  // (from the scores again: they are still in tensor memory)
             continue;
           }
