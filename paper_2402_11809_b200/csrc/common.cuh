@@ -160,7 +160,7 @@ struct space_ctx {
   int* counters;           // [3][max_batch] self-resetting arrival counters (two verify launches, commit), then an error word
   int* merge_cnt;          // attention, row kernel: cut descriptors, one per (sequence, kv head, row block), and owners
   int* arrived;            // attention: pieces of a cut that are stored, one per (sequence, kv head, row block)
-  int* kvq_arrived;        // the same of the attention over the 4-bit cache, per (sequence, kv head, 16 query rows)
+  int* kvq_arrived;        // the same of the attention over the 4-bit cache, per (sequence, kv head, 8 query rows)
   VerifyPartial* vpart;    // [max_batch][k_max+2][SPACE_VERIFY_MAX_CHUNKS]
   VerifyRow* vrow;         // [max_batch][k_max+1]
   VerifyPartial* vfused;   // [max_batch][SPACE_MAX_ROWS][16] single-launch greedy path
@@ -338,8 +338,14 @@ size_t attn_tensor_partial_floats(const space_config* cfg, int sm_count, size_t*
 int launch_kvq_append(space_ctx* ctx, const space_kvq_append_args* a, cudaStream_t st);
 int launch_kvq_read(space_ctx* ctx, const space_kvq_read_args* a, cudaStream_t st);
 int launch_kvq_attn(space_ctx* ctx, const space_kvq_attn_args* a, const uint64_t* mask_rows, cudaStream_t st);
-size_t kvq_partial_floats(const space_config* cfg, int sm_count);
-size_t kvq_items(const space_config* cfg);
+// Scratch of the attention over the 4-bit cache: two slots of partial results per thread block, of all the query rows that
+// the blocks of an SM hold; arrival counters of its items, eight query rows each at least.
+constexpr int KVQ_SM_ROWS = 64;
+inline size_t kvq_partial_floats(const space_config* c, int sm_count) { return 2 * (size_t)sm_count * KVQ_SM_ROWS * (c->head_dim + 2); }
+inline size_t kvq_items(const space_config* c) {
+  const size_t rows = (size_t)(c->k_max + 1) * (c->k_max + 1) * (c->n_q_heads / c->n_kv_heads);
+  return (size_t)c->max_batch * c->n_kv_heads * ((rows + 7) / 8);
+}
 int launch_philox_debug(uint64_t seed, int64_t n, const uint32_t* c0, const uint32_t* c1,
                         const uint32_t* c2, const uint32_t* c3, uint32_t* out, cudaStream_t st);
 

@@ -690,24 +690,13 @@ cudaError_t launch_dim(Params& p, const space_ctx* ctx, cudaStream_t st) {
     cudaFuncSetAttribute(kvq_attn_kernel<DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<DH, NT>(128));
     if (dev < 64) done_mask |= 1ull << dev;
   }
+  static_assert(Smem<DH, NT>::CTAS * 8 * NT <= KVQ_SM_ROWS, "a slot per block");
   p.n_rt = (p.n_q * p.G + 8 * NT - 1) / (8 * NT);
   p.n_groups = Smem<DH, NT>::CTAS * ctx->sm_count;
   return launch_pdl(kvq_attn_kernel<DH, NT>, dim3(p.n_groups), dim3(THREADS), smem_bytes<DH, NT>(max_batch), st, p, max_batch);
 }
 
 }  // namespace
-
-size_t kvq_partial_floats(const space_config* c, int sm_count) {
-  constexpr int rows = 48;                           // of the blocks that an SM holds, in the widest of the three forms
-  static_assert(Smem<128, 1>::CTAS * Smem<128, 1>::RT <= rows && Smem<128, 2>::CTAS * Smem<128, 2>::RT <= rows &&
-                Smem<128, 3>::CTAS * Smem<128, 3>::RT <= rows, "a slot per block");
-  const size_t few = 2 * (size_t)sm_count * rows * (c->head_dim + 2), many = kvq_tc_partial_floats(c, sm_count);
-  return few > many ? few : many;
-}
-size_t kvq_items(const space_config* c) {
-  const size_t rows = (size_t)(c->k_max + 1) * (c->k_max + 1) * (c->n_q_heads / c->n_kv_heads);
-  return (size_t)c->max_batch * c->n_kv_heads * ((rows + 7) / 8);
-}
 
 int launch_kvq_attn(space_ctx* ctx, const space_kvq_attn_args* a, const uint64_t* mask_rows, cudaStream_t st) {
   Params p;

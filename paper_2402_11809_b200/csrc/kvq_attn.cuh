@@ -158,4 +158,3 @@ __device__ __forceinline__ void join_pieces(const Params& p, const Cut& cut, int
 }  // namespace kvq
 
 int launch_kvq_attn_tc(space_ctx* ctx, kvq::Params& p, cudaStream_t st);
-size_t kvq_tc_partial_floats(const space_config* cfg, int sm_count);

@@ -899,6 +899,7 @@ cudaError_t launch_width(Params& p, const space_ctx* ctx, cudaStream_t st) {
     cudaFuncSetAttribute(kvq_attn_tc_kernel<DH, NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<DH, NP>(128));
     if (dev < 64) done_mask |= 1ull << dev;
   }
+  static_assert(16 * NP <= KVQ_SM_ROWS, "a slot per block");
   p.n_groups = ctx->sm_count;
   return launch_pdl(kvq_attn_tc_kernel<DH, NP>, dim3(p.n_groups), dim3(THREADS), smem_bytes<DH, NP>(max_batch), st, p, max_batch);
 }
@@ -909,8 +910,6 @@ cudaError_t launch_dim(Params& p, const space_ctx* ctx, int np, cudaStream_t st)
 }
 
 }  // namespace
-
-size_t kvq_tc_partial_floats(const space_config* c, int sm_count) { return 2 * (size_t)sm_count * 64 * (c->head_dim + 2); }
 
 // Items of equal width, as many as 64 rows each need; widths are multiples of 16.  More than 48 rows come here, so one
 // item has 49 to 64 of them and several have 33 to 64 each: 48 or 64 wide.
