@@ -25,12 +25,14 @@ using namespace kvq;
 using namespace tc;
 
 constexpr int WARPS = PAGE_BLOCKS, THREADS = 32 * WARPS;   // a warp per 32-row block of a page
-constexpr int SHARE_COST = 1;                        // fixed cost of starting an item, in pages
 
 // NT: query rows of an item in eights.
 template <int DH, int NT>
 struct Smem {
   static constexpr int RT = 8 * NT;
+  // Fixed cost of an item, in pages of the list (16 sequences of 512 to 4096 keys, 32 heads, 36 rows: 168 us with 1, 153
+  // with 2, 148 with 4; 16 x 8 heads, 32 rows of 1000 keys: 30.2 with 1, 27.0 with 3; eight rows: no difference).
+  static constexpr int SHARE_COST = NT == 1 ? 1 : NT == 2 ? 3 : 4;
   static constexpr int STAGES = 3;
   static constexpr int CTAS = NT == 1 ? 4 : NT == 2 ? 3 : 2;           // per SM
   static constexpr int RING = STAGES * Fmt<DH>::BLOCK;       // of a warp
@@ -202,7 +204,7 @@ template <int DH, int NT>
 __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(const __grid_constant__ Params p, int max_batch) {
   using F = Fmt<DH>;
   using S = Smem<DH, NT>;
-  constexpr int STAGES = S::STAGES, RT = S::RT;
+  constexpr int STAGES = S::STAGES, RT = S::RT, SHARE_COST = S::SHARE_COST;
   extern __shared__ __align__(128) unsigned char sm[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & 3;
   const uint32_t base = smem_u32(sm);

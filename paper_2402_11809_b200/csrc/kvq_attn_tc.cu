@@ -27,7 +27,7 @@ using namespace kvq;
 constexpr int SOFT_WARPS = 16, SOFT = 32 * SOFT_WARPS;          // four threads per key
 constexpr int THREADS = 12 * 32 + SOFT;
 constexpr int TILE = SPACE_PAGE_SIZE;
-constexpr int SHARE_COST = 2;                        // fixed cost of starting an item, in pages
+constexpr int SHARE_COST = 5;                        // fixed cost of an item, in pages (8 us against 1.6 us a page)
 constexpr int K_WARP0 = 4, V_WARP0 = 8, SOFT_WARP0 = 12;
 constexpr float W_SHIFT = 2.f;                       // weights of a new reference lie in [2^2, 2^3) (below 2^-14 f16 has fewer bits)
 constexpr float X_LIMIT = 16.f;                      // a row's reference moves when a score exceeds it by 2^16
