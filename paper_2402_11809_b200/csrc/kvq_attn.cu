@@ -671,7 +671,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
       }
       __syncthreads();
       if (*last_flag) {
-        join_pieces<DH, RT>(p, cut, b, h, r0, rows, piece0, pieces, item_at, (int)threadIdx.x, THREADS);
+        join_pieces<DH, RT, NT == 1 ? 1 : 2, NT == 1 ? 16 : 8>(p, cut, b, h, r0, rows, piece0, pieces, item_at, (int)threadIdx.x, THREADS);
       }
     }
     __syncthreads();                                 // everybody has read the rings: the next item's requests may fill them

@@ -114,44 +114,77 @@ __device__ __forceinline__ void store_row4(const Params& p, int b, int h, int r,
 }
 
 // The pieces of an item that was cut over several thread blocks meet, always in the same order: called by the block
-// that stored the last of them.  item_at: the item's place in the flat list; a block's share can hold the end of one cut
-// item (its first slot) and the start of another (its second one).
-template <int DH, int RT>
+// that stored the last of them, by whole warps.  item_at: the item's place in the flat list; a block's share can hold the
+// end of one cut item (its first slot) and the start of another (its second one).
+// A thread has four channels of U query rows; the DH / 4 threads of a row look up the references and sums of as many
+// pieces at once, one each, while BATCH pieces of the accumulators are on their way: what this costs is the latency of
+// loads that follow each other.  131072 keys, 8 kv heads of 4 rows (74 pieces a head), us: U = 1, BATCH = 4 / 8 / 16:
+// 47.5 / 45.3 / 43.5; 2048 keys, 32 heads of 36 rows (5 pieces), BATCH = 8: U = 1 / 2: 23.5 / 21.7.  (The tensor-memory
+// form has registers for U = 1, BATCH = 4.)
+template <int DH, int RT, int U, int BATCH>
 __device__ __forceinline__ void join_pieces(const Params& p, const Cut& cut, int b, int h, int r0, int rows, uint32_t piece0,
                                             int pieces, uint32_t item_at, int tid, int threads) {
-  constexpr int C4 = DH / 4, SLOT = RT * (DH + 2), BATCH = 8;
+  constexpr int C4 = DH / 4, SLOT = RT * (DH + 2);
   const float* part = p.part + (int64_t)(2 * piece0) * SLOT;
-  const int first = cut.begin(piece0) >= item_at ? 0 : SLOT;
+  const int first = cut.begin(piece0) >= item_at ? 0 : SLOT, n = rows * C4, c4 = tid % C4;
+  auto at = [&](int x) { return part + (x == 0 ? (int64_t)first : (int64_t)x * (2 * SLOT)); };
 #pragma unroll 1
-  for (int idx = tid; idx < rows * C4; idx += threads) {
-    const int r = idx / C4, c4 = idx % C4;
-    attn::MergeAcc ma;
-    ma.clear();
-    bool nan = false;
-#pragma unroll 1
-    for (int x0 = 0; x0 < pieces; x0 += BATCH) {     // all loads of a batch are issued before any is used
-      float ms[BATCH], ls[BATCH];
-      float4 ov[BATCH];
+  for (int idx = tid - tid % 32; idx < n; idx += U * threads) {               // (warps stay whole)
+    int r[U];
+    float M[U], den[U];
+    float4 o[U];
 #pragma unroll
-      for (int j = 0; j < BATCH; ++j) {
-        ms[j] = -CUDART_INF_F; ls[j] = 0.f; ov[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (x0 + j < pieces) {
-          const float* ps = part + (x0 + j == 0 ? (int64_t)first : (int64_t)(x0 + j) * (2 * SLOT));
-          ms[j] = __ldcg(ps + RT * DH + r);
-          ls[j] = __ldcg(ps + RT * DH + RT + r);
-          ov[j] = __ldcg(reinterpret_cast<const float4*>(ps + r * DH) + c4);
-        }
-        nan |= ls[j] != ls[j];
+    for (int u = 0; u < U; ++u) {
+      r[u] = min((idx + tid % 32 + u * threads) / C4, rows - 1);
+      M[u] = -CUDART_INF_F; den[u] = 0.f; o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll 1
+    for (int x0 = 0; x0 < pieces; x0 += C4) {
+      float m[U], l[U], f[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool there = x0 + c4 < pieces;
+        m[u] = there ? __ldcg(at(x0 + c4) + RT * DH + r[u]) : -CUDART_INF_F;
+        l[u] = there ? __ldcg(at(x0 + c4) + RT * DH + RT + r[u]) : 0.f;
       }
+#pragma unroll 1
+      for (int y = 0; y < C4 && x0 + y < pieces; y += BATCH) {
+        float4 v[U][BATCH];
 #pragma unroll
-      for (int g = 0; g < BATCH; g += 4) {
-        const float m4[4] = {ms[g], ms[g + 1], ms[g + 2], ms[g + 3]}, l4[4] = {ls[g], ls[g + 1], ls[g + 2], ls[g + 3]};
-        const float4 o4[4] = {ov[g], ov[g + 1], ov[g + 2], ov[g + 3]};
-        ma.add4(m4, l4, o4);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int j = 0; j < BATCH; ++j)
+            v[u][j] = x0 + y + j < pieces ? __ldcg(reinterpret_cast<const float4*>(at(x0 + y + j) + r[u] * DH) + c4) : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (y == 0) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            float top = m[u], sum;
+#pragma unroll
+            for (int k = 1; k < C4; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, k));
+            top = fmaxf(top, M[u]);
+            const float down = M[u] == top ? 1.f : fast_exp2(M[u] - top);
+            M[u] = top;
+            f[u] = m[u] == -CUDART_INF_F ? (l[u] != l[u] ? 1.f : 0.f) : fast_exp2(m[u] - top);   // (a row that is not a number keeps no reference)
+            sum = l[u] * f[u];
+#pragma unroll
+            for (int k = 1; k < C4; k <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, k);
+            den[u] = fmaf(den[u], down, sum);
+            o[u].x *= down; o[u].y *= down; o[u].z *= down; o[u].w *= down;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int j = 0; j < BATCH; ++j) {
+            const float w = __shfl_sync(0xFFFFFFFFu, f[u], y + j, C4);
+            o[u].x = fmaf(v[u][j].x, w, o[u].x); o[u].y = fmaf(v[u][j].y, w, o[u].y);
+            o[u].z = fmaf(v[u][j].z, w, o[u].z); o[u].w = fmaf(v[u][j].w, w, o[u].w);
+          }
       }
     }
-    if (nan) ma.den = CUDART_NAN_F;
-    store_row4<DH>(p, b, h, r0 + r, c4, ma.a, ma.mx, ma.den);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (idx + tid % 32 + u * threads < n) store_row4<DH>(p, b, h, r0 + r[u], c4, o[u], M[u], den[u]);
   }
 }
 

@@ -875,7 +875,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
           *last_flag = last;
         }
         soft_sync();
-        if (*last_flag) join_pieces<DH, N>(p, cut, wk.b, h, r0, rows, piece0, pieces, at, sidx, SOFT);
+        if (*last_flag) join_pieces<DH, N, 1, 4>(p, cut, wk.b, h, r0, rows, piece0, pieces, at, sidx, SOFT);
       }
       soft_sync();                                   // references, factors and the flag are free for the next item
     }
