@@ -43,7 +43,8 @@ struct Smem {
   static constexpr int P_OFF = 2 * Q_BYTES;
   static constexpr int RING_OFF = P_OFF + 2 * P_BYTES;
   static constexpr int RC_OFF = RING_OFF + STAGES * PAGE;    // [N/2] {sum, sum, -m, -m} of query rows 2i, 2i + 1
-  static constexpr int VINV_OFF = RC_OFF + 32 * 16;          // [N] 2^(m - R + W_SHIFT)
+  static constexpr int RC0_OFF = RC_OFF + 32 * 16;           // the same without references
+  static constexpr int VINV_OFF = RC0_OFF + 32 * 16;         // [N] 2^(m - R + W_SHIFT)
   static constexpr int MREF_OFF = VINV_OFF + 256;            // [N] m
   static constexpr int RREF_OFF = MREF_OFF + 256;            // [N] R - m (m can be too large for the difference to show in R)
   static constexpr int FQ_OFF = RREF_OFF + 256;              // [N] factors
@@ -597,7 +598,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
       ++items;
       if (sidx < N) {
         float* r = rcf + 4 * (sidx >> 1) + (sidx & 1);
-        r[0] = qsum[qb * 64 + sidx]; r[2] = 0.f;
+        r[0] = r[128] = qsum[qb * 64 + sidx]; r[2] = r[130] = 0.f;
         int qi, hq;
         row_of(p, h, rb * N + sidx, qi, hq);
         roff[sidx] = (qi * p.H_q + hq) * DH;
@@ -634,6 +635,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         if (lane == 0) mbar_arrive(BAR(EMPTY + s));
         hold(SF + buf, g >> 1, 15);
         tc_fence_after();
+        const uint32_t rc_page = rc_at + (own ? S::RC0_OFF - S::RC_OFF : 0);   // (block rows' references come after a clamp)
         const bool plain = !own && !__any_sync(0xFFFFFFFFu, gone);     // every row sees every key of this warp
         float x[NC];
         uint32_t hw[NC / 2];
@@ -650,8 +652,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
 #pragma unroll
             for (int i = 0; i < NC / 2; ++i) {
               uint64_t sum, ref;
-              asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(sum), "=l"(ref) : "r"(rc_at + 16 * i));
-              unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), k1p, fma2(k0p, sum, own ? 0ull : ref)), x[2 * i], x[2 * i + 1]);
+              asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(sum), "=l"(ref) : "r"(rc_page + 16 * i));
+              unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), k1p, fma2(k0p, sum, ref)), x[2 * i], x[2 * i + 1]);
             }
           }
           if (own) {                                 // (rows next to the largest number: a score stays one)
