@@ -61,7 +61,8 @@ struct Smem {
   static constexpr int N_BARS = 2 * STAGES + 24;
   static constexpr int MISC_OFF = BAR_OFF + (N_BARS * 8 + 15) / 16 * 16;
   static constexpr int OVER_OFF = MISC_OFF + 16;             // [2] the last page (of those that ask) whose scores pass a limit
-  static constexpr int TABLE_OFF = MISC_OFF + 32;            // prefix[max_batch + 1], seq_len[max_batch]
+  static constexpr int MASK_OFF = MISC_OFF + 32;             // [64] Eq. 5
+  static constexpr int TABLE_OFF = MASK_OFF + SPACE_MAX_ROWS * 8;            // prefix[max_batch + 1], seq_len[max_batch]
   static constexpr int V_PITCH = DH * 2 + 16;                // bytes: the block's V rows as f16, in a stage
   static_assert(SPACE_MAX_ROWS * V_PITCH <= PAGE, "the block's V rows fit a stage");
   static_assert(TABLE_OFF + 129 * 4 + 128 * 4 <= 227 * 1024, "shared-memory plan too large");
@@ -166,6 +167,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  if (threadIdx.x < SPACE_MAX_ROWS) reinterpret_cast<uint64_t*>(sm + S::MASK_OFF)[threadIdx.x] = p.mask[threadIdx.x];
   if (warp == 3) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -575,6 +577,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
     const float* qsum = reinterpret_cast<const float*>(sm + S::QSUM_OFF);
     const volatile float* qc = reinterpret_cast<const volatile float*>(sm + S::QTOP_OFF + 32);
     const float* par = reinterpret_cast<const float*>(sm + S::PAR_OFF);
+    const uint64_t* masks = reinterpret_cast<const uint64_t*>(sm + S::MASK_OFF);
     auto fmax2 = [](float a, float b) { return fmaxf(a, b); };
     auto fsum2 = [](float a, float b) { return a + b; };
     // every column joined over the warp's keys, into to[quarter]
@@ -657,16 +660,20 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
             }
           }
           if (own) {                                 // (rows next to the largest number: a score stays one)
-#pragma unroll
-            for (int i = 0; i < NC; ++i) x[i] = (x[i] > 1e38f ? 1e38f : x[i] < -1e38f ? -1e38f : x[i]) + rcf[4 * ((col0 + i) >> 1) + 2 + (i & 1)];
-          }
-          if (!plain) {
+            uint32_t see = 0;                        // (a loop: this code runs once an item, and is fetched for it)
+            if (!gone) {
+#pragma unroll 1
+              for (int i = 0; i < NC; ++i)
+                if (col0 + i < rows) see |= (uint32_t)((masks[(r0 + col0 + i) >> p.gsh] >> kl) & 1ull) << i;
+            }
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-              bool vis = !gone;
-              if (own && vis) vis = col0 + i < rows && ((p.mask[(r0 + col0 + i) >> p.gsh] >> kl) & 1ull);
-              if (!vis) x[i] = -CUDART_INF_F;
+              const float y = (x[i] > 1e38f ? 1e38f : x[i] < -1e38f ? -1e38f : x[i]) + rcf[4 * ((col0 + i) >> 1) + 2 + (i & 1)];
+              x[i] = (see >> i) & 1u ? y : -CUDART_INF_F;
             }
+          } else if (!plain && gone) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) x[i] = -CUDART_INF_F;
           }
           if (!fresh) {
             if (!settled) {
