@@ -85,6 +85,7 @@ struct Acc {
   float m[NT][2], R[NT][2];                          // references (log2 units) of the sums, of the accumulators
   uint64_t l[NT], z[NT];                             // sums of e, of e (lo + 8 step); pairs of rows 2t, 2t + 1
   uint64_t nref[NT], vinv[NT];                       // -m (0 while there is none), 2^(m - R + 6)
+  float vtop;                                        // the largest of those
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -94,6 +95,7 @@ struct Acc {
       l[nt] = z[nt] = nref[nt] = pack2(0.f, 0.f);
       vinv[nt] = pack2(0x1p126f, 0x1p126f);
     }
+    vtop = 0x1p126f;
   }
   __device__ __forceinline__ void scale_rows(int nt, float f0, float f1) {
 #pragma unroll
@@ -121,6 +123,13 @@ struct Acc {
 #pragma unroll
     for (int s = 0; s < 2; ++s) v[s] = R[nt][s] == -CUDART_INF_F ? 0x1p126f : fast_exp2(fminf(m[nt][s] - R[nt][s] + 6.f, 126.f));
     vinv[nt] = pack2(v[0], v[1]);
+  }
+  __device__ __forceinline__ void set_vtop() {
+    float a, b;
+    unpack2(vinv[0], a, b);
+    vtop = fmaxf(a, b);
+#pragma unroll
+    for (int nt = 1; nt < NT; ++nt) { unpack2(vinv[nt], a, b); vtop = max3(vtop, a, b); }
   }
   // The accumulators' references moved up to the rows' largest weights (relative to m), where those would pass the limit.
   __device__ __forceinline__ void set_scale(int nt, float t0, float t1) {
@@ -374,7 +383,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
       }
       // ---- steps and lowest values of keys 8 i + lane / 4; scores relative to the rows' references
       uint64_t vs[4], vz[4];
-      float mx = -CUDART_INF_F;
+      float mx = -CUDART_INF_F, vmax = 0.f;
       const float c24 = qc * 16777216.f;            // undoes the codes' 2^-24
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -385,6 +394,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
         const float k1 = bf_lo(kp) * c24, k0 = bf_hi(kp), v1 = bf_lo(vp), v0 = fmaf(v1, 8.f, bf_hi(vp));
         const uint64_t k1p = pack2(k1, k1), k0p = pack2(k0, k0);
         vs[i] = pack2(v1, v1); vz[i] = pack2(v0, v0);
+        vmax = fmaxf(vmax, v1);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float* x = &sc[i >> 1][nt][2 * (i & 1)];
@@ -414,39 +424,36 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
 #pragma unroll
           for (int i = 0; i < 4; ++i) { sc[i >> 1][nt][2 * (i & 1)] += s0; sc[i >> 1][nt][2 * (i & 1) + 1] += s1; }
         }
+        acc.set_vtop();
+        mx = fminf(mx, 0.f);                         // (none is above its reference now; one that is not a number stays out of this)
       }
-      // ---- e, its sums, and the weights e step in f16
-      float tm = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float* x = &sc[i >> 1][nt][2 * (i & 1)];
-          const uint64_t e = pack2(fast_exp2(x[0]), fast_exp2(x[1]));
-          acc.l[nt] = add2(acc.l[nt], e);
-          acc.z[nt] = fma2(e, vz[i], acc.z[nt]);
-          const uint64_t w = mul2(e, vs[i]);
-          unpack2(w, x[0], x[1]);
-          float w0, w1;
-          unpack2(mul2(w, acc.vinv[nt]), w0, w1);
-          tm = max3(tm, w0, w1);
-        }
-      if (__any_sync(0xFFFFFFFFu, tm > W_LIMIT)) {
+      // ---- could a weight pass the limit?  By a bound, the largest e times the largest step and factor of the lane; then
+      // by the weights themselves
+      if (__any_sync(0xFFFFFFFFu, fast_exp2(mx) * vmax * acc.vtop > W_LIMIT)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float t0 = 0.f, t1 = 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) { t0 = fmaxf(t0, sc[i >> 1][nt][2 * (i & 1)]); t1 = fmaxf(t1, sc[i >> 1][nt][2 * (i & 1) + 1]); }
+          for (int i = 0; i < 4; ++i) {
+            float v1, v1_;
+            unpack2(vs[i], v1, v1_);
+            t0 = fmaxf(t0, fast_exp2(sc[i >> 1][nt][2 * (i & 1)]) * v1); t1 = fmaxf(t1, fast_exp2(sc[i >> 1][nt][2 * (i & 1) + 1]) * v1);
+          }
           acc.set_scale(nt, t0, t1);
         }
+        acc.set_vtop();
       }
+      // ---- e, its sums, and the weights e step in f16
       uint32_t pb[2][NT][2];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+          const uint64_t e = pack2(fast_exp2(sc[i >> 1][nt][2 * (i & 1)]), fast_exp2(sc[i >> 1][nt][2 * (i & 1) + 1]));
+          acc.l[nt] = add2(acc.l[nt], e);
+          acc.z[nt] = fma2(e, vz[i], acc.z[nt]);
           float w0, w1;
-          unpack2(mul2(pack2(sc[i >> 1][nt][2 * (i & 1)], sc[i >> 1][nt][2 * (i & 1) + 1]), acc.vinv[nt]), w0, w1);
+          unpack2(mul2(mul2(e, vs[i]), acc.vinv[nt]), w0, w1);
           pb[i >> 1][nt][i & 1] = transpose8(pack_h(w0, w1));
         }
       // ---- O^T += (U - 8)^T P^T: channels 16 (2 wd + ct) + lane / 4 (+ 8) are the rows
