@@ -1,22 +1,33 @@
-// Attention of a step's block rows over the 4-bit cache (space_kvq_attn_step), 8 or 16 query rows at a time.
+// Attention of a step's block rows over the 4-bit cache (space_kvq_attn_step), 8, 16 or 24 query rows at a time.
 //
 // The mathematics.  A cached row stands for lo + step u, so with the codes as they lie
 //   score = c (step_k sum_c q_c u_c + lo_k sum_c q_c),     out = sum_j e_j step_j (u_j - 8) + sum_j e_j (lo_j + 8 step_j):
 // the products take bare codes, steps and lowest values are two multiply-adds per score.  A code that is masked out of
 // its 32-bit word is already an f16 number, the subnormal u 2^-24 (or u 2^-20 for the nibbles at bits 4..7), which
 // the tensor cores take at full rate; the powers of two go into the query row (first product) and into the epilogue
-// (second one, whose codes are centred by 8 first: sums of one sign would collect the tensor core's truncation).
+// (second one, whose codes are centred by 8 first: sums of one sign would collect what the tensor core cuts off; without
+// it 65536 keys in one piece with even weights were 1.4 % off, and 64 sequences took 121 us instead of 127).
 // f16 holds a bf16 query row exactly, scaled by a power of two, and the weights e step to 11 bits.  The sums of e and of
 // e (lo + 8 step) refer to the largest score so far, the weights to the largest e step of their row so far: a row of V
 // that is large and hardly seen costs the others no bits.
 //
-// The work.  Everything is bound by the cache's bytes, (d + 8) per key and head, so: the keys of all (sequence, kv head,
-// query rows) items form one flat list of 128-key pages, every thread block takes an equal share of it, and a page's
-// four blocks of 32 keys go to its four warps.  A warp streams its blocks (contiguous 32 d + 256 bytes each) into a ring of
-// its own with bulk copies and never meets another warp until the item ends: 3 blocks per SM x 4 warps x 2 blocks in
-// flight.  The cache is laid out in the order of the m16n8k16 operands, so that a lane's 16 bytes are what it feeds to
-// the tensor core: nothing is shuffled or staged.  The pieces of an item that was cut are joined by the block that
-// stores the last of them, always in the same order.
+// The work.  The cache's bytes, (d + 8) per key and head, bind up to 8 rows, unpacking, exponentials and products beyond:
+// the keys of all (sequence, kv head, query rows) items form one flat list of 128-key pages, every thread block takes an
+// equal share of it, and a page's four blocks of 32 keys go to its four warps.  A warp streams its blocks (contiguous
+// 32 d + 256 bytes each) into a ring of its own with bulk copies and never meets another warp until the item ends: two
+// of its three stages are in flight.  The products are taken transposed, keys and channels on the sixteen rows of
+// m16n8k16 and query rows on its eight columns: the codes are the first operand, in the order in which the cache holds
+// them, so a lane's 16 bytes are what it feeds to the tensor core, and nothing is padded beyond eights of query rows (with
+// the query rows on the sixteen, the first form, one token of 64 sequences took 195 us).  The second operands lie in shared
+// memory (query) or come out of the scores by an 8 x 8 transpose (weights).  Accumulators of 8, 16, 24 query rows and
+// 32 keys leave registers for 4, 3, 2 blocks per SM.  The block's own rows are bf16 products, their weights two bf16
+// terms each.  The pieces of an item that was cut are joined by the block that stores the last of them, always in the
+// same order.
+// Measured, d = 128: 64 sequences of 1024 to 16384 keys, 8 kv heads of 4 rows, 128.5 us (73 % of the copy rate: four
+// warps per scheduler issue 0.56 instructions a cycle); one sequence of 131071 keys 43 us, of which the pages are
+// 26 (91 %), the start 5 and the join of 74 pieces a head 12; 16 sequences of 512 to 4096 keys, 32 heads, 36 rows 146 us,
+// 1.7 us a page of 24 rows and block, two blocks per SM, of which the products are half and 0.37 instructions a cycle is
+// what two warps per scheduler give; an item costs 8.7 us beside its pages.
 // Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT and the block drains and exits.
 #include "kvq_attn.cuh"
 
@@ -726,16 +737,19 @@ int launch_kvq_attn(space_ctx* ctx, const space_kvq_attn_args* a, const uint64_t
   // the flat list is counted in 32 bits: items of eight rows at least, a page and the cost of starting more than a table names
   if ((double)p.B * p.H_kv * ((rows + 7) / 8) * ((double)p.cache.pages_per_seq + 4) > 2e9) return SPACE_E_UNSUPPORTED;
   ctx->launches += 1;
-  // More than 48 rows, and pages for every SM: the tensor-memory form.  (What a page costs there is less, what an item costs
-  // more, and there is one block per SM to hide it: 16 x 32 heads, 49 rows, us here / there: 2000 keys 208 / 188, 8000 keys
-  // 600 / 459; 8 x 8 heads, 392 rows of 8192 keys 451 / 396; but one sequence of 300 keys, 8 heads, 64 rows 15 / 26, and
-  // 36 rows of 2000 keys 149 / 172.  The lengths are on the device: the table's width stands for them.)
+  // Which form.  A page costs 16 rows here 3 units, 24 rows 4, and in the tensor-memory form 64 rows 9 (what its items cost
+  // beside their pages counted in; 48 rows would cost 8 and never be the cheapest); eight rows are the cheapest there are.  16 sequences x 16
+  // heads of 2000 keys, us, by 8 / 16 / 24 rows: 8 rows 29.5 / 35 / 40, 16 rows 43 / 38 / 42, 18 rows 58 / 56 / 44, 32
+  // rows 74 / 58 / 74, 36 rows 89 / 85 / 78; here / there: 50 rows 70 / 61 (1000 keys), 64 rows 109 / 85, 100 rows 170 / 149,
+  // but 72 rows (8 x 8 heads, 3000 keys) 45 / 53 and 36 rows (16 x 32, up to 4096) 145 / 160.
+  const int in16 = 3 * ((rows + 15) / 16), in24 = 4 * ((rows + 23) / 24);
+  // It has one block per SM, so it also wants pages for each: at nine pages' worth an SM 54 / 52, at five 33 / 40.  (The
+  // lengths are on the device: the table's width stands for them.)
   const int blocks = (rows + 63) / 64;
-  if (rows > 48 && (int64_t)p.B * p.H_kv * blocks * p.cache.pages_per_seq >= 32 * (int64_t)ctx->sm_count) return launch_kvq_attn_tc(ctx, p, st);
+  if (9 * blocks < min(in16, in24) && (int64_t)p.B * p.H_kv * blocks * p.cache.pages_per_seq >= 8 * (int64_t)ctx->sm_count)
+    return launch_kvq_attn_tc(ctx, p, st);
   const bool wide = ctx->cfg.head_dim == 128;
-  // Eight rows at a time, sixteen or twenty-four: what a 32-key step of each costs is as 3 : 4 of the last two (35840 keys of
-  // 16 sequences x 16 heads, us: 16 rows 8.7, 24 rows 11.6).
-  const int nt = rows <= 8 ? 1 : 4 * ((rows + 23) / 24) < 3 * ((rows + 15) / 16) ? 3 : 2;
+  const int nt = rows <= 8 ? 1 : in24 < in16 ? 3 : 2;
   cudaError_t e;
   if (wide) e = nt == 1 ? launch_dim<128, 1>(p, ctx, st) : nt == 2 ? launch_dim<128, 2>(p, ctx, st) : launch_dim<128, 3>(p, ctx, st);
   else e = nt == 1 ? launch_dim<64, 1>(p, ctx, st) : nt == 2 ? launch_dim<64, 2>(p, ctx, st) : launch_dim<64, 3>(p, ctx, st);

@@ -1,5 +1,5 @@
-// What the two attention kernels over the 4-bit cache share (kvq_attn.cu: up to 16 query rows on mma.sync;
-// kvq_attn_tc.cu: more rows on tcgen05): parameters, addresses of query rows, the join of an item's pieces.
+// What the two attention kernels over the 4-bit cache share (kvq_attn.cu: items of 8, 16 or 24 query rows on mma.sync;
+// kvq_attn_tc.cu: of 64 on tcgen05): parameters, addresses of query rows, the join of an item's pieces.
 #pragma once
 #include "common.cuh"
 #include "tc_common.cuh"

@@ -1,4 +1,4 @@
-// Attention of a step's block rows over the 4-bit cache (space_kvq_attn_step), items of up to 64 query rows on tcgen05.
+// Attention of a step's block rows over the 4-bit cache (space_kvq_attn_step), items of 64 query rows on tcgen05.
 //
 // The mathematics is kvq_attn.cu's: products of bare codes, steps and lowest values in the softmax, weights e step
 // against a reference of their own.  So is the work: (sequence, kv head, query rows) items, one flat list of 128-key
@@ -10,12 +10,21 @@
 // through shared memory the unpacked page would cost 4 d bytes written and as many read per key, more than the tensor
 // core's products take.  The cache's order is that of the 16x256b store: a lane's 16 bytes are its registers.
 //
+// What bounds it is the softmax threads' chain: a page of 64 rows takes 1.54 us, its products 0.2 us, the unpacking
+// 0.5 beside them; left out one at a time, exponentials, products, unpacking or sums change it by 5 % at most.  So: sixteen
+// softmax warps instead of eight (8 x 8 heads, 392 rows of 8192 keys: 451 us on mma.sync, 417 with eight, 396 with
+// sixteen); whether a page's scores pass the limits is asked by an mbarrier under the exponentials, not by a barrier
+// before them (349); block rows read their sums from a list of their own instead of a select per score (335).  Slower were
+// query rows on M (1.9 us a page), scores loaded or barriers asked for ahead of time, a factor common to all rows
+// instead of one each, and wider reads of tensor memory.
+//
 // Warps (28, one thread block per SM):
 //   0      bulk copies, a page of one kv head (4 (32 d + 256) contiguous bytes) per stage of the ring
 //   1, 2   issue S^T and O^T products
 //   4-7    query rows into shared memory (f16, one power of two per item); K codes -> tensor memory
 //   8-11   V codes -> tensor memory
-//   12-27  four threads per key: scores, e, its sums, weights as f16 into shared memory (second operand); O^T out
+//   12-27  four threads per key, sixteen rows each: scores, e, its sums, weights as f16 into shared memory (second
+//          operand); O^T out
 // The block's own rows are one more page, whose K and V the code warps bring as f16 with a power of two per row instead.
 // Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT, no role leaves its loop early (the named barriers stay
 // matched), and the block drains and exits.
@@ -27,12 +36,13 @@ using namespace kvq;
 constexpr int SOFT_WARPS = 16, SOFT = 32 * SOFT_WARPS;          // four threads per key
 constexpr int THREADS = 12 * 32 + SOFT;
 constexpr int TILE = SPACE_PAGE_SIZE;
+constexpr int NP = 4;                                // sixteens of query rows of an item
 constexpr int SHARE_COST = 5;                        // fixed cost of an item, in pages (8 us against 1.6 us a page)
 constexpr int K_WARP0 = 4, V_WARP0 = 8, SOFT_WARP0 = 12;
 constexpr float W_SHIFT = 2.f;                       // weights of a new reference lie in [2^2, 2^3) (below 2^-14 f16 has fewer bits)
 constexpr float X_LIMIT = 16.f;                      // a row's reference moves when a score exceeds it by 2^16
 
-template <int DH, int NP>
+template <int DH>
 struct Smem {
   static constexpr int N = 16 * NP;                          // query rows of an item (with padding)
   static constexpr int STAGES = DH == 128 ? 8 : 12;
@@ -134,10 +144,10 @@ struct Walk {
   }
 };
 
-template <int DH, int NP>
+template <int DH>
 __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_constant__ Params p, int max_batch) {
   using F = Fmt<DH>;
-  using S = Smem<DH, NP>;
+  using S = Smem<DH>;
   constexpr int N = S::N, STAGES = S::STAGES;
   extern __shared__ __align__(1024) unsigned char sm[];
   const uint32_t base = smem_u32(sm), bar0 = base + S::BAR_OFF;
@@ -895,35 +905,27 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
   if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
 }
 
-template <int DH, int NP>
-size_t smem_bytes(int max_batch) { return Smem<DH, NP>::TABLE_OFF + (size_t)(max_batch + 1) * 4 + (size_t)max_batch * 4; }
+template <int DH>
+size_t smem_bytes(int max_batch) { return Smem<DH>::TABLE_OFF + (size_t)(max_batch + 1) * 4 + (size_t)max_batch * 4; }
 
-template <int DH, int NP>
-cudaError_t launch_width(Params& p, const space_ctx* ctx, cudaStream_t st) {
+template <int DH>
+cudaError_t launch_dim(Params& p, const space_ctx* ctx, cudaStream_t st) {
   static unsigned long long done_mask = 0;           // devices on which the kernel may have its shared memory
   const int max_batch = ctx->cfg.max_batch;
   int dev = 0;
   cudaGetDevice(&dev);
   if (dev >= 64 || !((done_mask >> dev) & 1ull)) {
-    cudaFuncSetAttribute(kvq_attn_tc_kernel<DH, NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<DH, NP>(128));
+    cudaFuncSetAttribute(kvq_attn_tc_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<DH>(128));
     if (dev < 64) done_mask |= 1ull << dev;
   }
   static_assert(16 * NP <= KVQ_SM_ROWS, "a slot per block");
   p.n_groups = ctx->sm_count;
-  return launch_pdl(kvq_attn_tc_kernel<DH, NP>, dim3(p.n_groups), dim3(THREADS), smem_bytes<DH, NP>(max_batch), st, p, max_batch);
-}
-
-template <int DH>
-cudaError_t launch_dim(Params& p, const space_ctx* ctx, int np, cudaStream_t st) {
-  return np == 3 ? launch_width<DH, 3>(p, ctx, st) : launch_width<DH, 4>(p, ctx, st);
+  return launch_pdl(kvq_attn_tc_kernel<DH>, dim3(p.n_groups), dim3(THREADS), smem_bytes<DH>(max_batch), st, p, max_batch);
 }
 
 }  // namespace
 
-// Items of equal width, as many as 64 rows each need; widths are multiples of 16.  More than 48 rows come here, so one
-// item has 49 to 64 of them and several have 33 to 64 each: 48 or 64 wide.
 int launch_kvq_attn_tc(space_ctx* ctx, kvq::Params& p, cudaStream_t st) {
-  const int rows = p.n_q * p.G, blocks = (rows + 63) / 64, np = ((rows + blocks - 1) / blocks + 15) / 16;
-  p.n_rt = (rows + 16 * np - 1) / (16 * np);
-  return cuda_ok(ctx->cfg.head_dim == 128 ? launch_dim<128>(p, ctx, np, st) : launch_dim<64>(p, ctx, np, st));
+  p.n_rt = (p.n_q * p.G + 16 * NP - 1) / (16 * NP);
+  return cuda_ok(ctx->cfg.head_dim == 128 ? launch_dim<128>(p, ctx, st) : launch_dim<64>(p, ctx, st));
 }

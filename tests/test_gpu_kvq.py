@@ -11,7 +11,7 @@ from oracle.layout import EQ5_LITERAL, SAME_GROUP
 
 pytestmark = pytest.mark.gpu
 P = 128
-WIDE = 5000                                          # pages of a table that names enough of them for the tensor-memory form
+WIDE = 5000                                          # pages of a table that names enough of them for the tensor-memory form (49 to 64 rows, 97 on)
 
 
 @pytest.fixture(scope="module")
@@ -242,7 +242,7 @@ ATTN_WIDE = [
     (128, 8, 2, 7, [1999, 37, 1200, 2048, 640], True),                   # several items and many pages per thread block
     (64, 4, 8, 5, [1500, 0, 900], True), (128, 1, 8, 7, [4000], True), (128, 16, 1, 6, [300] * 8, True),
     (64, 4, 2, 7, [3500, 2900, 3100], False), (128, 2, 16, 1, [5000], False), (64, 1, 16, 2, [1030, 0, 128], False),
-    (64, 2, 16, 1, [77, 0], True),
+    (64, 2, 16, 1, [77, 0], True), (64, 3, 4, 4, [777, 130, 0], True), (128, 1, 16, 3, [2300, 0, 128], False),
 ]
 # long lists of pages: every warp's ring goes round several times, items end and begin within a thread block's share
 ATTN_LONG = [
@@ -306,7 +306,7 @@ def run_attention(B, q, pool, table, lens, k, kn=None, vn=None, H=1, d=64):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("k,pps", [(1, 3), (5, WIDE)])
+@pytest.mark.parametrize("k,pps", [(1, 3), (5, WIDE), (6, WIDE)])
 def test_sequences_that_do_not_fit_and_pages_outside_the_pool(B, d, k, pps):
     rng = np.random.default_rng(4)
     lens, n_q = [300, 40, 300, 50], (k + 1) ** 2
@@ -325,7 +325,7 @@ def test_sequences_that_do_not_fit_and_pages_outside_the_pool(B, d, k, pps):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("k,pps", [(2, 2), (5, 2), (5, WIDE)])
+@pytest.mark.parametrize("k,pps", [(2, 2), (5, 2), (5, WIDE), (6, WIDE)])
 def test_hidden_rows_have_no_influence(B, d, k, pps):
     """What one block row holds reaches only the rows that see it, whatever it is."""
     rng = np.random.default_rng(6)
