@@ -345,6 +345,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) sum[nt] = *reinterpret_cast<const uint64_t*>(qsum + 8 * nt + 2 * t);
     acc.clear();
+    bool unset = true;                               // a row has no reference yet
     for (int j = 0; j < n_blk; ++j, ++step) {
       request(j + STAGES - 1, step + STAGES - 1);
       const uint32_t s = step % STAGES, parity = (step / STAGES) & 1;
@@ -399,27 +400,36 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int key = 8 * i + (lane >> 2);
-        uint32_t kp = lds32(blk + F::K_PAR + key * 4), vp = lds32(blk + F::V_PAR + key * 4);
-        const bool gone = valid < BLOCK_ROWS && key >= valid;                  // rows past the end may hold anything
-        if (gone) kp = vp = 0;
+        const uint32_t kp = lds32(blk + F::K_PAR + key * 4), vp = lds32(blk + F::V_PAR + key * 4);
         const float k1 = bf_lo(kp) * c24, k0 = bf_hi(kp), v1 = bf_lo(vp), v0 = fmaf(v1, 8.f, bf_hi(vp));
         const uint64_t k1p = pack2(k1, k1), k0p = pack2(k0, k0);
         vs[i] = pack2(v1, v1); vz[i] = pack2(v0, v0);
-        vmax = fmaxf(vmax, v1);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float* x = &sc[i >> 1][nt][2 * (i & 1)];
-          const uint64_t y = fma2(pack2(x[0], x[1]), k1p, fma2(k0p, sum[nt], acc.nref[nt]));
-          unpack2(y, x[0], x[1]);
-          if (gone) x[0] = x[1] = -CUDART_INF_F;
-          mx = max3(mx, x[0], x[1]);
+          unpack2(fma2(pack2(x[0], x[1]), k1p, fma2(k0p, sum[nt], acc.nref[nt])), x[0], x[1]);
         }
       }
-      // the references move when a score exceeds them by 2^8
-      bool fresh = false;
+      if (valid < BLOCK_ROWS) {                      // rows past the end may hold anything
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) fresh |= acc.m[nt][0] == -CUDART_INF_F || acc.m[nt][1] == -CUDART_INF_F;
-      if (__any_sync(0xFFFFFFFFu, fresh || mx > REF_SLACK)) {
+        for (int i = 0; i < 4; ++i)
+          if (8 * i + (lane >> 2) >= valid) {
+            vs[i] = vz[i] = pack2(0.f, 0.f);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sc[i >> 1][nt][2 * (i & 1)] = sc[i >> 1][nt][2 * (i & 1) + 1] = -CUDART_INF_F;
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v1, v1_;
+        unpack2(vs[i], v1, v1_);
+        vmax = fmaxf(vmax, v1);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) mx = max3(mx, sc[i >> 1][nt][2 * (i & 1)], sc[i >> 1][nt][2 * (i & 1) + 1]);
+      }
+      // the references move when a score exceeds them by 2^8, or while a row has none
+      if (__any_sync(0xFFFFFFFFu, unset || mx > REF_SLACK)) {
+        unset = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float a0 = -CUDART_INF_F, a1 = -CUDART_INF_F, r0_, r1_, s0, s1;
@@ -430,6 +440,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
           unpack2(acc.nref[nt], r0_, r1_);
           acc.raise(nt, col_max(a0) - r0_, col_max(a1) - r1_);
           acc.set_vinv(nt);
+          unset |= acc.m[nt][0] == -CUDART_INF_F || acc.m[nt][1] == -CUDART_INF_F;
           unpack2(acc.nref[nt], s0, s1);
           s0 -= r0_; s1 -= r1_;
 #pragma unroll
