@@ -46,6 +46,7 @@ struct Smem {
   static constexpr int SHARE_COST = NT == 1 ? 1 : NT == 2 ? 3 : 4;
   static constexpr int STAGES = 3;
   static constexpr int CTAS = NT == 1 ? 4 : NT == 2 ? 3 : 2;           // per SM
+  static constexpr int JOIN = NT == 1 ? 1 : NT == 2 ? 4 : 6;           // query rows of a thread in the join
   static constexpr int RING = STAGES * Fmt<DH>::BLOCK;       // of a warp
   static constexpr int O_PITCH = DH + 4;                     // floats
   static_assert(RT * O_PITCH * 4 <= RING, "a warp's accumulators are parked in its ring once that has run dry");
@@ -165,23 +166,30 @@ struct Acc {
 // t * DH/4 ..; the pair that a code word's mask brings out at bits 0..3 (4..7) of each half is a k-step's first (second)
 // half.  f16, scaled by one power of two; returns scale with that undone.
 template <int DH, int NT>
-__device__ __forceinline__ float load_query(const Params& p, unsigned char* sm, int b, int h, int r0) {
+struct Query {
+  static constexpr int LANES = DH / 8, PER = THREADS / LANES, PASSES = (8 * NT + PER - 1) / PER;   // threads of a row, rows at a time
+  uint4 v[PASSES];
+  __device__ __forceinline__ void fetch(const Params& p, int b, int h, int r0) {
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) {
+      const int r = k * PER + threadIdx.x / LANES;
+      int i, hq;
+      row_of(p, h, r0 + r, i, hq);
+      v[k] = make_uint4(0, 0, 0, 0);
+      if (r < 8 * NT && i < p.n_q)
+        v[k] = *(reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh) + threadIdx.x % LANES);
+    }
+  }
+};
+template <int DH, int NT>
+__device__ __forceinline__ float load_query(const Params& p, unsigned char* sm, const Query<DH, NT>& query) {
   using S = Smem<DH, NT>;
-  constexpr int LANES = DH / 8, PER = THREADS / LANES, PASSES = (S::RT + PER - 1) / PER;   // threads of a row, rows at a time
+  constexpr int LANES = Query<DH, NT>::LANES, PER = Query<DH, NT>::PER, PASSES = Query<DH, NT>::PASSES;
   float* sums = reinterpret_cast<float*>(sm + S::SUM_OFF);
   uint32_t* tops = reinterpret_cast<uint32_t*>(sums + S::RT);
   const int x = threadIdx.x % LANES, lane = threadIdx.x & 31;
-  uint4 v[PASSES];
+  const uint4 (&v)[PASSES] = query.v;
   uint32_t top = 0;
-#pragma unroll
-  for (int k = 0; k < PASSES; ++k) {
-    const int r = k * PER + threadIdx.x / LANES;
-    int i, hq;
-    row_of(p, h, r0 + r, i, hq);
-    v[k] = make_uint4(0, 0, 0, 0);
-    if (r < S::RT && i < p.n_q)
-      v[k] = *(reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh) + x);
-  }
 #pragma unroll
   for (int k = 0; k < PASSES; ++k) {
     uint32_t m = max_bits(v[k]);
@@ -337,10 +345,12 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
         }
       }
     };
+    Query<DH, NT> query;
+    query.fetch(p, b, h, r0);                        // (ahead of the requests, which wait for the page table)
 #pragma unroll 1
     for (int j = 0; j < STAGES - 1; ++j) request(j, step + j);
 
-    const float qc = load_query<DH, NT>(p, sm, b, h, r0);
+    const float qc = load_query<DH, NT>(p, sm, query);
     uint64_t sum[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) sum[nt] = *reinterpret_cast<const uint64_t*>(qsum + 8 * nt + 2 * t);
@@ -690,9 +700,9 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
     }
     if (!whole) {
       const int item = (b * p.H_kv + h) * p.n_rt + rt;
-      __threadfence();
       __syncthreads();
       if (threadIdx.x == 0) {
+        __threadfence();                             // (after the barrier: for the whole block's stores)
         const int last = atomicAdd(p.arrived + item, 1) == pieces - 1;
         if (last) p.arrived[item] = 0;               // ready for the next call
         __threadfence();
@@ -700,7 +710,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
       }
       __syncthreads();
       if (*last_flag) {
-        join_pieces<DH, RT, NT == 1 ? 1 : 2, NT == 1 ? 16 : 8>(p, cut, b, h, r0, rows, piece0, pieces, item_at, (int)threadIdx.x, THREADS);
+        join_pieces<DH, RT, S::JOIN, NT == 1 ? 16 : 4>(p, cut, b, h, r0, rows, piece0, pieces, item_at, (int)threadIdx.x, THREADS);
       }
     }
     __syncthreads();                                 // everybody has read the rings: the next item's requests may fill them

@@ -119,8 +119,8 @@ __device__ __forceinline__ void store_row4(const Params& p, int b, int h, int r,
 // A thread has four channels of U query rows; the DH / 4 threads of a row look up the references and sums of as many
 // pieces at once, one each, while BATCH pieces of the accumulators are on their way: what this costs is the latency of
 // loads that follow each other.  131072 keys, 8 kv heads of 4 rows (74 pieces a head), us: U = 1, BATCH = 4 / 8 / 16:
-// 47.5 / 45.3 / 43.5; 2048 keys, 32 heads of 36 rows (5 pieces), BATCH = 8: U = 1 / 2: 23.5 / 21.7.  (The tensor-memory
-// form has registers for U = 1, BATCH = 4.)
+// 47.5 / 45.3 / 43.5; 2048 keys, 32 heads of 36 rows (5 pieces), U, BATCH = 1, 8 / 2, 8 / 6, 4: 23.0 / 21.1 / 20.3.  (The
+// tensor-memory form has registers for U = 1, BATCH = 4.)
 template <int DH, int RT, int U, int BATCH>
 __device__ __forceinline__ void join_pieces(const Params& p, const Cut& cut, int b, int h, int r0, int rows, uint32_t piece0,
                                             int pieces, uint32_t item_at, int tid, int threads) {

@@ -884,9 +884,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
       tc_fence_before();
       if (*abort_flag && p.status && sidx == 0) atomicOr(p.status + wk.b, SPACE_ST_TIMEOUT);
       if (!whole) {
-        __threadfence();
         soft_sync();
         if (sidx == 0) {
+          __threadfence();                           // (after the barrier: for all the stores)
           int* arrived = p.arrived + ((wk.b * p.H_kv + h) * p.n_rt + rb);
           const int last = atomicAdd(arrived, 1) == pieces - 1;
           if (last) *arrived = 0;                    // ready for the next call
