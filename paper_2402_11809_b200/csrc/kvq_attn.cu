@@ -23,11 +23,11 @@
 // 32 keys leave registers for 4, 3, 2 blocks per SM.  The block's own rows are bf16 products, their weights two bf16
 // terms each.  The pieces of an item that was cut are joined by the block that stores the last of them, always in the
 // same order.
-// Measured, d = 128: 64 sequences of 1024 to 16384 keys, 8 kv heads of 4 rows, 128.5 us (73 % of the copy rate: four
+// Measured, d = 128: 64 sequences of 1024 to 16384 keys, 8 kv heads of 4 rows, 127 us (72 % of the copy rate: four
 // warps per scheduler issue 0.56 instructions a cycle); one sequence of 131071 keys 43 us, of which the pages are
-// 26 (91 %), the start 5 and the join of 74 pieces a head 12; 16 sequences of 512 to 4096 keys, 32 heads, 36 rows 146 us,
+// 26 (91 %), the start 5 and the join of 74 pieces a head 12; 16 sequences of 512 to 4096 keys, 32 heads, 36 rows 142 us,
 // 1.7 us a page of 24 rows and block, two blocks per SM, of which the products are half and 0.37 instructions a cycle is
-// what two warps per scheduler give; an item costs 8.7 us beside its pages.
+// what two warps per scheduler give; an item costs 8 us beside its pages.
 // Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT and the block drains and exits.
 #include "kvq_attn.cuh"
 
