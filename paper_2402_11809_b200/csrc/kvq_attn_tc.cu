@@ -403,29 +403,20 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         const bool own = t >= Tc;                    // the block's own rows (or no rows at all)
         if (!own) {
           const uint32_t blk = base + S::RING_OFF + s * S::PAGE + w * F::BLOCK;
+#pragma unroll 1
+          for (int i = 0; i < 2 * (DH / 64); ++i) {  // sixteen keys, four k-steps
+            const int i16 = i & 1, jj = i >> 1;
+            const uint32_t at = blk + (16 * i16 + n) * (DH / 2) + t4 * (DH / 8) + 8 * jj;
+            const uint2 x = lds64(at), y = lds64(at + 8 * (DH / 2));
+            uint32_t r[16];
 #pragma unroll
-          for (int i16 = 0; i16 < 2; ++i16) {
-            uint32_t x[DH / 32], y[DH / 32];
-            const uint32_t at = blk + (16 * i16 + n) * (DH / 2) + t4 * (DH / 8);
-            if (DH == 128) {
-              const uint4 a = lds128(at), d = lds128(at + 8 * (DH / 2));
-              x[0] = a.x; x[1] = a.y; x[2 % (DH / 32)] = a.z; x[3 % (DH / 32)] = a.w;
-              y[0] = d.x; y[1] = d.y; y[2 % (DH / 32)] = d.z; y[3 % (DH / 32)] = d.w;
-            } else {
-              const uint2 a = lds64(at), d = lds64(at + 8 * (DH / 2));
-              x[0] = a.x; x[1] = a.y; y[0] = d.x; y[1] = d.y;
+            for (int k = 0; k < 4; ++k) {            // eight columns: pairs 2 (k % 2), + 1 of word k / 2
+              const uint32_t xw = k / 2 ? x.y : x.x, yw = k / 2 ? y.y : y.x;
+              const uint32_t a = (k & 1) ? xw >> 8 : xw, d = (k & 1) ? yw >> 8 : yw;
+              r[4 * k] = a & 0x000F000Fu; r[4 * k + 1] = a & 0x00F000F0u;
+              r[4 * k + 2] = d & 0x000F000Fu; r[4 * k + 3] = d & 0x00F000F0u;
             }
-#pragma unroll
-            for (int jj = 0; jj < DH / 64; ++jj) {
-              uint32_t r[16];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {          // eight columns: pairs 2 (k % 2), + 1 of word 2 jj + k / 2
-                const uint32_t a = (k & 1) ? x[2 * jj + k / 2] >> 8 : x[2 * jj + k / 2], d = (k & 1) ? y[2 * jj + k / 2] >> 8 : y[2 * jj + k / 2];
-                r[4 * k] = a & 0x000F000Fu; r[4 * k + 1] = a & 0x00F000F0u;
-                r[4 * k + 2] = d & 0x000F000Fu; r[4 * k + 3] = d & 0x00F000F0u;
-              }
-              tmem_st_frag4(dst + ((uint32_t)(16 * i16) << 16) + 32 * jj, r);
-            }
+            tmem_st_frag4(dst + ((uint32_t)(16 * i16) << 16) + 32 * jj, r);
           }
         } else if (p.has_new && wk.L >= 0 && 32 * w < p.n_q) {
 #pragma unroll 1
@@ -492,7 +483,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         const bool own = t >= Tc;
         if (!own) {
           if (32 * w < DH) {
-#pragma unroll
+#pragma unroll 1
             for (int r2 = 0; r2 < 2; ++r2) {         // two blocks of 32 rows, 32 columns
               uint32_t lo[16], hi[16];
 #pragma unroll
