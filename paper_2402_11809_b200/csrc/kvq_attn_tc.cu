@@ -71,7 +71,8 @@ struct Smem {
   static constexpr int N_BARS = 2 * STAGES + 24;
   static constexpr int MISC_OFF = BAR_OFF + (N_BARS * 8 + 15) / 16 * 16;
   static constexpr int OVER_OFF = MISC_OFF + 16;             // [2] the last page (of those that ask) whose scores pass a limit
-  static constexpr int MASK_OFF = MISC_OFF + 32;             // [64] Eq. 5
+  static constexpr int RATIO_OFF = MISC_OFF + 32;            // [2][TILE] f16: lo / step of a page's V rows, times 2^-9
+  static constexpr int MASK_OFF = RATIO_OFF + 2 * TILE * 2;             // [64] Eq. 5
   static constexpr int TABLE_OFF = MASK_OFF + SPACE_MAX_ROWS * 8;            // prefix[max_batch + 1], seq_len[max_batch]
   static constexpr int V_PITCH = DH * 2 + 16;                // bytes: the block's V rows as f16, in a stage
   static_assert(SPACE_MAX_ROWS * V_PITCH <= PAGE, "the block's V rows fit a stage");
@@ -100,13 +101,13 @@ __device__ __forceinline__ void tmem_st_frag4(uint32_t a, const uint32_t* r) {
 __device__ __forceinline__ constexpr uint32_t instr_desc(int n, int b_mn) {
   return (1u << 4) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
 }
-// Codes of pair q (bits 4q .. 4q + 3 of both halves) less 8, as f16: 1024 + u - 1032, or (1024 + 16 u) / 16 - 72.
-__device__ __forceinline__ uint32_t centred_even(uint32_t x) { return h2sub((x & 0x000F000Fu) | 0x64006400u, 0x64086408u); }
-__device__ __forceinline__ uint32_t centred_odd(uint32_t x) {
-  const uint32_t v = (x & 0x00F000F0u) | 0x64006400u, a = 0x2C002C00u, c = 0xD480D480u;   // 1/16, -72
-  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&c));
+// Masked codes as f16 (u 2^-24, or u 2^-20 for bits 4 .. 7 of each half) to (u + lo / step) 2^-9, rounded once.
+__device__ __forceinline__ uint32_t h2fma(uint32_t x, uint32_t a, uint32_t c) {
+  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&c));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
+__device__ __forceinline__ uint32_t value_even(uint32_t x, uint32_t r) { return h2fma(x & 0x000F000Fu, 0x78007800u, r); }    // 2^15
+__device__ __forceinline__ uint32_t value_odd(uint32_t x, uint32_t r) { return h2fma(x & 0x00F000F0u, 0x68006800u, r); }     // 2^11
 // Four values per lane joined over the warp: every lane ends with the one of column 2 (lane >> 4) + ((lane >> 3) & 1).
 template <class J>
 __device__ __forceinline__ float warp_join4(const float* v, int lane, J join) {
@@ -477,12 +478,20 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
       for (int t = wk.t0; t < wk.t1; ++t, ++g) {
         const uint32_t s = g % STAGES, buf = g & 1, stage = base + S::RING_OFF + s * S::PAGE;
         hold(FULL + s, g / STAGES, 10);
+        const bool own = t >= Tc;
+        __half* ratio = reinterpret_cast<__half*>(sm + S::RATIO_OFF) + buf * TILE;
+        if (!own) {
+          const uint32_t vp = lds32(stage + w * F::BLOCK + F::V_PAR + lane * 4);
+          const bool gone = bad[s] != 0 || t * TILE + 32 * w + lane >= wk.L;   // (such a row may hold anything; its weights are 0)
+          ratio[32 * w + lane] = __float2half_rn(gone ? 0.f : __fdividef(bf_hi(vp), bf_lo(vp)) * 0x1p-9f);
+          v_sync();
+        }
         if (g >= 2) hold(VTE + buf, (g - 2) >> 1, 11);
         tc_fence_after();
         const uint32_t dst = TM_V + buf * 64 + ((uint32_t)(32 * w) << 16);
-        const bool own = t >= Tc;
         if (!own) {
           if (32 * w < DH) {
+            const uint32_t rat = smem_u32(ratio) + (lane & 3) * 4;
 #pragma unroll 1
             for (int r2 = 0; r2 < 2; ++r2) {         // two blocks of 32 rows, 32 columns
               uint32_t lo[16], hi[16];
@@ -494,9 +503,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
                 for (int a = 0; a < 2; ++a)
 #pragma unroll
                   for (int e = 0; e < 2; ++e) {      // channels n and n + 8 of each 16: pairs 0 and 1 (2 and 3)
-                    const uint32_t u = x[2 * a + e], u8 = u >> 8;
-                    lo[8 * k + 4 * a + e] = centred_even(u); lo[8 * k + 4 * a + 2 + e] = centred_odd(u);
-                    hi[8 * k + 4 * a + e] = centred_even(u8); hi[8 * k + 4 * a + 2 + e] = centred_odd(u8);
+                    const uint32_t u = x[2 * a + e], u8 = u >> 8, r = lds32(rat + ((2 * r2 + k) * 32 + 16 * a + 8 * e) * 2);
+                    lo[8 * k + 4 * a + e] = value_even(u, r); lo[8 * k + 4 * a + 2 + e] = value_odd(u, r);
+                    hi[8 * k + 4 * a + e] = value_even(u8, r); hi[8 * k + 4 * a + 2 + e] = value_odd(u8, r);
                   }
               }
               tmem_st_frag4(dst + 32 * r2, lo);
@@ -521,7 +530,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
                                         pack_h(bf_lo(v.z) * f, bf_hi(v.z) * f), pack_h(bf_lo(v.w) * f, bf_hi(v.w) * f));
             asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};"
                          ::"r"(stage + key * S::V_PITCH + (lane % LANES) * 16), "r"(hv.x), "r"(hv.y), "r"(hv.z), "r"(hv.w) : "memory");
-            if (lane % LANES == 0) par[s * 128 + 64 + key] = pow2(e);
+            if (lane % LANES == 0) par[s * 128 + 64 + key] = pow2(e) * 0x1p-9f;   // (as the cache's values)
           }
           v_sync();
           if (32 * w < DH) {
@@ -610,9 +619,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         vinv[sidx] = 0x1p126f;
       }
       const float c24 = qc[qb] * 16777216.f;         // undoes the codes' 2^-24
-      uint64_t l[NC / 2], z[NC / 2];
+      uint64_t l[NC / 2];
 #pragma unroll
-      for (int i = 0; i < NC / 2; ++i) l[i] = z[i] = pack2(0.f, 0.f);
+      for (int i = 0; i < NC / 2; ++i) l[i] = pack2(0.f, 0.f);
       soft_sync();
       if (sidx == 0) mbar_arrive(BAR(QE + qb));      // (with the last S^T product: the query buffer is free)
       const int r0 = rb * N, rows = min(N, p.n_q * p.G - r0);
@@ -621,19 +630,19 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         const bool first = t == wk.t0, own = t >= Tc;
         // ---- this key's step and lowest value
         hold(FULL + s, g / STAGES, 13);
-        float k1, k0, v1, v0;
+        float k1, k0, v1;
         bool gone;
         if (!own) {
           const uint32_t blk = base + S::RING_OFF + s * S::PAGE + quarter * F::BLOCK + lane * 4;
           gone = bad[s] != 0 || t * TILE + kl >= wk.L;
           const uint32_t kp = gone ? 0u : lds32(blk + F::K_PAR), vp = gone ? 0u : lds32(blk + F::V_PAR);
-          k1 = bf_lo(kp) * c24; k0 = bf_hi(kp); v1 = bf_lo(vp); v0 = fmaf(v1, 8.f, bf_hi(vp));
+          k1 = bf_lo(kp) * c24; k0 = bf_hi(kp); v1 = bf_lo(vp);
         } else {
           hold(BLK + buf, blocks >> (16 * buf), 14);
           blocks += 1u << (16 * buf);                // (only the low bit of each count is looked at)
           blocks &= 0x00010001u;
           gone = !p.has_new || wk.L < 0 || kl >= p.n_q;
-          k1 = gone ? 0.f : par[s * 128 + (kl & 63)]; k0 = 0.f; v1 = gone ? 0.f : par[s * 128 + 64 + (kl & 63)]; v0 = 0.f;
+          k1 = gone ? 0.f : par[s * 128 + (kl & 63)]; k0 = 0.f; v1 = gone ? 0.f : par[s * 128 + 64 + (kl & 63)];
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(BAR(EMPTY + s));
@@ -767,7 +776,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
 #pragma unroll
             for (int i = 0; i < NC / 2; ++i) {
               const uint64_t f = *reinterpret_cast<const uint64_t*>(fq + col0 + 2 * i);
-              l[i] = mul2(l[i], f); z[i] = mul2(z[i], f);
+              l[i] = mul2(l[i], f);
             }
 #pragma unroll 1
             for (int j = 0; j < NP; ++j) {
@@ -782,7 +791,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
           }
           soft_sync();
         }
-        // ---- S^T goes back; P^T out; sums of e and of e (lo + 8 step)
+        // ---- S^T goes back; P^T out; sums of e
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(BAR(SE + buf));
@@ -797,15 +806,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(BAR(PF + buf));
-        {
-          const uint64_t v0p = pack2(v0, v0);
 #pragma unroll
-          for (int i = 0; i < NC / 2; ++i) {
-            const uint64_t e = pack2(x[2 * i], x[2 * i + 1]);
-            l[i] = add2(l[i], e);
-            z[i] = fma2(e, v0p, z[i]);
-          }
-        }
+        for (int i = 0; i < NC / 2; ++i) l[i] = add2(l[i], pack2(x[2 * i], x[2 * i + 1]));
       }
       // ---- the item's (or piece's) end: sums over the keys, then O^T
       {
@@ -813,9 +815,6 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
 #pragma unroll
         for (int i = 0; i < NC / 2; ++i) unpack2(l[i], v[2 * i], v[2 * i + 1]);
         over_keys(v, xq, fsum2);
-#pragma unroll
-        for (int i = 0; i < NC / 2; ++i) unpack2(z[i], v[2 * i], v[2 * i + 1]);
-        over_keys(v, xz, fsum2);
         soft_sync();
       }
       const int T = wk.pages(p.has_new);
@@ -830,10 +829,10 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
       constexpr int SLOT = N * (DH + 2);             // (a block's share can hold the end of one cut item and the start of another)
       float* ps = p.part + (int64_t)(2 * (int)blockIdx.x + (wk.opens ? 0 : 1)) * SLOT;
       if (sidx < N) {
-        const float ls = of_quarters(xq, fsum2), zs = of_quarters(xz, fsum2);
-        const float m = mref[sidx], f = rref[sidx] == -CUDART_INF_F ? 1.f : fast_exp2(rref[sidx] - W_SHIFT);
+        const float ls = of_quarters(xq, fsum2);
+        const float m = mref[sidx], f = rref[sidx] == -CUDART_INF_F ? 1.f : fast_exp2(rref[sidx] - W_SHIFT + 9.f);
         const float rd = !whole ? 1.f : ls > 0.f || ls != ls ? 1.f / ls : 0.f;   // a row without keys: zeros
-        fq[sidx] = f * rd; go[sidx] = zs * rd;
+        fq[sidx] = f * rd;
         if (sidx < rows) {
           if (!whole) {
             __stcg(ps + N * DH + sidx, m);
@@ -856,7 +855,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         tmem_wait_ld();
         const int c = col0 + 4 * j;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fmaf(o[e], fq[c + e], go[c + e]);
+        for (int e = 0; e < 4; ++e) o[e] *= fq[c + e];
         if (whole) {
           // two rows at a time: the even lane takes both channels of the first, the odd one of the second
 #pragma unroll
