@@ -509,7 +509,8 @@ int space_kvq_read(space_ctx* ctx, const space_kvq_read_args* args, void* stream
  * 0 .. pages_per_seq * SPACE_PAGE_SIZE (SPACE_ST_CAPACITY).  Keys of a page outside the pool are left out
  * (SPACE_ST_BAD_PAGE).  Hidden rows have no influence, whatever they hold; non-finite elements of k_new /
  * v_new count as they do in space_kvq_append (without the status bit).
- * The output is bf16: scores and sums are fp32, the weights of the second product are rounded to 11 bits.
+ * The output is bf16: scores and sums are fp32, the weights of the second product are rounded to 11 bits, and where
+ * a kv head has 49 to 64 or more than 96 query rows the cache's V values, in steps, may be too.
  * The products take query rows as f16, scaled by one power of two for up to 64 rows of a kv head together: elements
  * more than 2^21 times smaller than the largest of those rows are rounded, by at most 2^-29 of it; all others are exact.
  * Asynchronous on `stream`, no allocation; one call at a time per context (scratch of the context).

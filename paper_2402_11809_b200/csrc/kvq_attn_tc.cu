@@ -1,22 +1,26 @@
 // Attention of a step's block rows over the 4-bit cache (space_kvq_attn_step), items of 64 query rows on tcgen05.
 //
-// The mathematics is kvq_attn.cu's: products of bare codes, steps and lowest values in the softmax, weights e step
-// against a reference of their own.  So is the work: (sequence, kv head, query rows) items, one flat list of 128-key
-// pages, an equal share per thread block, cut items joined by the block that stores their last piece.
+// The mathematics is kvq_attn.cu's but for one thing: products of bare K codes, steps and lowest values in the softmax,
+// weights e step against a reference of their own; the V codes become (u + lo / step) 2^-9 on their way (one product and
+// sum of the masked code, rounded to 11 bits once, as the weights are), so that there is no second sum of e (lo + 8 step)
+// to keep per query row and key.  So is the work: (sequence, kv head, query rows) items, one flat list of 128-key pages, an
+// equal share per thread block, cut items joined by the block that stores their last piece.
 //
 // The products are taken transposed, the 128 keys (channels) of a page on the MMA's M extent and the query rows on N:
-//   S^T = U Q^T  (128 x N),      O^T += (U - 8)^T P^T  (d x N).
+//   S^T = U Q^T  (128 x N),      O^T += V^T P^T  (d x N).
 // Both first operands come from tensor memory: the codes are unpacked in registers and stored there (tcgen05.st), because
 // through shared memory the unpacked page would cost 4 d bytes written and as many read per key, more than the tensor
 // core's products take.  The cache's order is that of the 16x256b store: a lane's 16 bytes are its registers.
 //
-// What bounds it is the softmax threads' chain: a page of 64 rows takes 1.54 us, its products 0.2 us, the unpacking
-// 0.5 beside them; left out one at a time, exponentials, products, unpacking or sums change it by 5 % at most.  So: sixteen
-// softmax warps instead of eight (8 x 8 heads, 392 rows of 8192 keys: 451 us on mma.sync, 417 with eight, 396 with
-// sixteen); whether a page's scores pass the limits is asked by an mbarrier under the exponentials, not by a barrier
-// before them (349); block rows read their sums from a list of their own instead of a select per score (335).  Slower were
-// query rows on M (1.9 us a page), scores loaded or barriers asked for ahead of time, a factor common to all rows
-// instead of one each, and wider reads of tensor memory.
+// What bounds it is the softmax threads: a page of 64 rows takes 1.45 us, its products 0.2 us, the unpacking 0.5 beside
+// them; left out one at a time, exponentials, products, unpacking or sums change it by 5 % at most, and what it follows
+// is the number of instructions that the loops of all roles have, and whether the softmax warps run through theirs together.
+// So (8 x 8 heads, 392 rows of 8192 keys; 451 us on mma.sync): sixteen softmax warps instead of eight (417 -> 396); whether
+// a page's scores pass the limits is asked by an mbarrier under the exponentials, not by a barrier before them (349); block
+// rows read their sums from a list of their own instead of a select per score (335); the unpacking in short loops (329); V
+// in steps and one sum per row (323); scores in one read of tensor memory (320).  Slower were query rows on M (1.9 us a
+// page), four groups of softmax warps, sixteen rows each, that do not wait for each other (+11 %), weights published, barriers asked
+// for or parameters looked up a page ahead (+5 to 10 %), a factor common to all rows beside one each (+27 %).
 //
 // Warps (28, one thread block per SM):
 //   0      bulk copies, a page of one kv head (4 (32 d + 256) contiguous bytes) per stage of the ring
@@ -87,6 +91,11 @@ template <int R> __device__ __forceinline__ void regs_inc() { asm volatile("setm
 
 __device__ __forceinline__ void tmem_ld4(uint32_t a, float* r) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t a, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+                 "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]) : "r"(a) : "memory");
 }
 __device__ __forceinline__ void tmem_st4(uint32_t a, const float* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]) : "memory");
@@ -565,6 +574,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
     regs_inc<88>();
     // ================= softmax, output ==========================================
     constexpr int NC = 4 * NP;                       // query rows of a thread
+    static_assert(NC == 16, "one read of tensor memory");
     const int quarter = warp & 3, part = (warp - SOFT_WARP0) >> 2;
     const int kl = quarter * 32 + lane;              // key of the page; channel in the epilogue
     const int sidx = part * 128 + kl, col0 = part * NC;
@@ -657,8 +667,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
 #pragma unroll 1
         for (;;) {
           // ---- scores less the rows' references, for this key and its rows
-#pragma unroll
-          for (int j = 0; j < NP; ++j) tmem_ld4(TM_S + buf * 64 + lanes + col0 + 4 * j, x + 4 * j);
+          tmem_ld16(TM_S + buf * 64 + lanes + col0, x);
           tmem_wait_ld();
           {
             const uint64_t k1p = pack2(k1, k1), k0p = pack2(k0, k0);
