@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
           for (int i = 0; i < 4; ++i) { sc[i >> 1][nt][2 * (i & 1)] += s0; sc[i >> 1][nt][2 * (i & 1) + 1] += s1; }
         }
         acc.set_vtop();
-        mx = fminf(mx, 0.f);                         // (none is above its reference now; one that is not a number stays out of this)
+        mx = 0.f;                                    // (none is above its reference now; a first reference can also have moved the scores up)
       }
       // ---- could a weight pass the limit?  By a bound, the largest e times the largest step and factor of the lane; then
       // by the weights themselves
