@@ -75,6 +75,7 @@ struct Smem {
   static constexpr int N_BARS = 2 * STAGES + 24;
   static constexpr int MISC_OFF = BAR_OFF + (N_BARS * 8 + 15) / 16 * 16;
   static constexpr int OVER_OFF = MISC_OFF + 16;             // [2] the last page (of those that ask) whose scores pass a limit
+  static constexpr int LIMIT_OFF = MISC_OFF + 24;            // {score that the references move at, the largest vinv}
   static constexpr int RATIO_OFF = MISC_OFF + 32;            // [2][TILE] f16: lo / step of a page's V rows, times 2^-9
   static constexpr int MASK_OFF = RATIO_OFF + 2 * TILE * 2;             // [64] Eq. 5
   static constexpr int TABLE_OFF = MASK_OFF + SPACE_MAX_ROWS * 8;            // prefix[max_batch + 1], seq_len[max_batch]
@@ -593,7 +594,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
     float* xz = reinterpret_cast<float*>(sm + S::XZ_OFF);
     float* vspan = reinterpret_cast<float*>(sm + S::VSPAN_OFF);   // [2][4] largest and smallest V step of a quarter's keys
     int* roff = reinterpret_cast<int*>(sm + S::ROFF_OFF);         // [N] where a query row's output begins, in elements
-    volatile float* vtop = reinterpret_cast<volatile float*>(sm + S::MISC_OFF + 12);   // the largest vinv
+    volatile float* limit = reinterpret_cast<volatile float*>(sm + S::LIMIT_OFF);
     const float* qsum = reinterpret_cast<const float*>(sm + S::QSUM_OFF);
     const volatile float* qc = reinterpret_cast<const volatile float*>(sm + S::QTOP_OFF + 32);
     const float* par = reinterpret_cast<const float*>(sm + S::PAR_OFF);
@@ -696,13 +697,15 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
           }
           if (!fresh) {
             if (!settled) {
-              // do scores or weights pass the limits?  (the weights by a bound: the largest score, the largest vinv)
+              // do scores or weights pass the limits?  (the weights by a bound: the largest score, the largest vinv; any score
+              // does while a row has no reference)
               float a = fmaxf(x[0], x[1]), b = fmaxf(x[2], x[3]);
 #pragma unroll
               for (int i = 4; i < NC; i += 4) { a = max3(a, x[i], x[i + 1]); b = max3(b, x[i + 2], x[i + 3]); }
               a = fmaxf(a, b);
               ++asked;
-              if (a > X_LIMIT || fast_exp2(a) * v1 * *vtop > W_LIMIT) over_at[asked & 1] = asked;
+              const uint2 lim = lds64(base + S::LIMIT_OFF);
+              if (a > __uint_as_float(lim.x) || fast_exp2(a) * v1 * __uint_as_float(lim.y) > W_LIMIT) over_at[asked & 1] = asked;
               __syncwarp();
               if (lane == 0) mbar_arrive(BAR(OVER));
             }
@@ -775,11 +778,13 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
             go[sidx] = f; vinv[sidx] = v;
           }
           soft_sync();
-          if (warp == SOFT_WARP0) {                  // (a row without any key so far has the largest bound: the next page settles again)
+          if (warp == SOFT_WARP0) {                  // (a row without any key so far: the next page with one settles again)
             float v = 0.f;
-            for (int i = lane; i < rows; i += 32) v = fmaxf(v, vinv[i]);
+            bool none = false;
+            for (int i = lane; i < rows; i += 32) { v = fmaxf(v, vinv[i]); none |= mref[i] == -CUDART_INF_F; }
             const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v));
-            if (lane == 0) *vtop = __uint_as_float(m);
+            none = __any_sync(0xFFFFFFFFu, none);
+            if (lane == 0) { limit[0] = none ? -CUDART_INF_F : X_LIMIT; limit[1] = __uint_as_float(m); }
           }
           if (!first) {
 #pragma unroll

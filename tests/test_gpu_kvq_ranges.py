@@ -7,12 +7,13 @@ import pytest
 
 from oracle import kvq
 from oracle.bf16 import bf16_bits_to_f64, f32_to_bf16_bits
-from test_gpu_kvq import B, P, check, random_cache, run_attention, span_of  # noqa: F401 (B: a fixture)
+from test_gpu_kvq import B, P, WIDE, check, random_cache, run_attention, span_of  # noqa: F401 (B: a fixture)
 
 pytestmark = pytest.mark.gpu
 
-# G, k, pages per sequence in the table (0: as many as there are): 8, 16, 24-row items full to the last row, 24 and a rest
-FORMS = [(8, 0, 0), (16, 0, 0), (8, 2, 0), (1, 5, 0)]
+# G, k, pages per sequence in the table (0: as many as there are): 8, 16, 24-row items full to the last row, 24 and a rest,
+# and the tensor-memory form's 64 rows (full, and full with a rest)
+FORMS = [(8, 0, 0), (16, 0, 0), (8, 2, 0), (1, 5, 0), (16, 1, WIDE), (2, 6, WIDE)]
 
 
 def params(pool, d, which):
