@@ -94,16 +94,16 @@ __device__ __forceinline__ float col_sum(float v) {
 template <int DH, int NT>
 struct Acc {
   float o[DH / 16][NT][4];                           // channels 16 ct + n (+ 8): {row 2t, 2t + 1} each
-  float m[NT][2], R[NT][2];                          // references (log2 units) of the sums, of the accumulators
+  float m[NT][2], D[NT][2];                          // reference of the sums (log2 units), that of the accumulators less it (m can be too large for the difference to show in a sum)
   uint64_t l[NT], z[NT];                             // sums of e, of e (lo + 8 step); pairs of rows 2t, 2t + 1
-  uint64_t nref[NT], vinv[NT];                       // -m (0 while there is none), 2^(m - R + 6)
+  uint64_t nref[NT], vinv[NT];                       // -m (0 while there is none, or one far below 0), 2^(6 - D)
   float vtop;                                        // the largest of those
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
       for (int ct = 0; ct < DH / 16; ++ct) o[ct][nt][0] = o[ct][nt][1] = o[ct][nt][2] = o[ct][nt][3] = 0.f;
-      m[nt][0] = m[nt][1] = R[nt][0] = R[nt][1] = -CUDART_INF_F;
+      m[nt][0] = m[nt][1] = D[nt][0] = D[nt][1] = -CUDART_INF_F;
       l[nt] = z[nt] = nref[nt] = pack2(0.f, 0.f);
       vinv[nt] = pack2(0x1p126f, 0x1p126f);
     }
@@ -121,19 +121,20 @@ struct Acc {
     for (int s = 0; s < 2; ++s) {
       const float n = fmaxf(m[nt][s], mx[s]);
       f[s] = m[nt][s] == n ? 1.f : fast_exp2(m[nt][s] - n);
+      D[nt][s] -= m[nt][s] == n ? 0.f : n - m[nt][s];
       m[nt][s] = n;
-      r[s] = n == -CUDART_INF_F ? 0.f : -n;
+      r[s] = n < FAR_BELOW ? 0.f : -n;
     }
     nref[nt] = pack2(r[0], r[1]);
     const uint64_t f2 = pack2(f[0], f[1]);
     l[nt] = mul2(l[nt], f2); z[nt] = mul2(z[nt], f2);
     return make_float2(f[0], f[1]);
   }
-  // 2^(m - R + 6), bounded: a weight of at least 2^-100 times the bound is over what set_scale lets through
+  // 2^(6 - D), bounded: a weight of at least 2^-100 times the bound is over what set_scale lets through
   __device__ __forceinline__ void set_vinv(int nt) {
     float v[2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) v[s] = R[nt][s] == -CUDART_INF_F ? 0x1p126f : fast_exp2(fminf(m[nt][s] - R[nt][s] + 6.f, 126.f));
+    for (int s = 0; s < 2; ++s) v[s] = fast_exp2(fminf(6.f - D[nt][s], 126.f));
     vinv[nt] = pack2(v[0], v[1]);
   }
   __device__ __forceinline__ void set_vtop() {
@@ -152,9 +153,9 @@ struct Acc {
     for (int s = 0; s < 2; ++s) {
       f[s] = 1.f;
       if (t[s] * v[s] > W_LIMIT) {
-        const float n = m[nt][s] + (float)((int)(__float_as_uint(t[s]) >> 23) - 127);
-        f[s] = fast_exp2(R[nt][s] - n);
-        R[nt][s] = n;
+        const float n = (float)((int)(__float_as_uint(t[s]) >> 23) - 127);
+        f[s] = fast_exp2(D[nt][s] - n);
+        D[nt][s] = n;
       }
     }
     scale_rows(nt, f[0], f[1]);
@@ -355,7 +356,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) sum[nt] = *reinterpret_cast<const uint64_t*>(qsum + 8 * nt + 2 * t);
     acc.clear();
-    bool unset = true;                               // a row has no reference yet
+    bool unset = true;                               // a row has no reference yet, or one far below 0
     for (int j = 0; j < n_blk; ++j, ++step) {
       request(j + STAGES - 1, step + STAGES - 1);
       const uint32_t s = step % STAGES, parity = (step / STAGES) & 1;
@@ -407,17 +408,41 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
       uint64_t vs[4], vz[4];
       float mx = -CUDART_INF_F, vmax = 0.f;
       const float c24 = qc * 16777216.f;            // undoes the codes' 2^-24
+      uint32_t kp[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int key = 8 * i + (lane >> 2);
-        const uint32_t kp = lds32(blk + F::K_PAR + key * 4), vp = lds32(blk + F::V_PAR + key * 4);
-        const float k1 = bf_lo(kp) * c24, k0 = bf_hi(kp), v1 = bf_lo(vp), v0 = fmaf(v1, 8.f, bf_hi(vp));
-        const uint64_t k1p = pack2(k1, k1), k0p = pack2(k0, k0);
+        kp[i] = lds32(blk + F::K_PAR + key * 4);
+        const uint32_t vp = lds32(blk + F::V_PAR + key * 4);
+        const float v1 = bf_lo(vp), v0 = fmaf(v1, 8.f, bf_hi(vp));
         vs[i] = pack2(v1, v1); vz[i] = pack2(v0, v0);
+      }
+      if (__any_sync(0xFFFFFFFFu, fmaxf(max3(bf_lo(kp[0]), bf_lo(kp[1]), bf_lo(kp[2])), bf_lo(kp[3])) * c24 > K_LARGE)) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float* x = &sc[i >> 1][nt][2 * (i & 1)];
-          unpack2(fma2(pack2(x[0], x[1]), k1p, fma2(k0p, sum[nt], acc.nref[nt])), x[0], x[1]);
+        for (int i = 0; i < 4; ++i) {
+          const float k1 = bf_lo(kp[i]) * 0x1p-64f * c24, k0 = bf_hi(kp[i]) * 0x1p-64f;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float s[2], r[2];
+            unpack2(sum[nt], s[0], s[1]);
+            unpack2(acc.nref[nt], r[0], r[1]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float& x = sc[i >> 1][nt][2 * (i & 1) + e];
+              x = clamp_score(fmaf(x, k1, k0 * s[e]) * 0x1p64f) + r[e];
+            }
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float k1 = bf_lo(kp[i]) * c24, k0 = bf_hi(kp[i]);
+          const uint64_t k1p = pack2(k1, k1), k0p = pack2(k0, k0);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float* x = &sc[i >> 1][nt][2 * (i & 1)];
+            unpack2(fma2(pack2(x[0], x[1]), k1p, fma2(k0p, sum[nt], acc.nref[nt])), x[0], x[1]);
+          }
         }
       }
       if (valid < BLOCK_ROWS) {                      // rows past the end may hold anything
@@ -437,7 +462,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) mx = max3(mx, sc[i >> 1][nt][2 * (i & 1)], sc[i >> 1][nt][2 * (i & 1) + 1]);
       }
-      // the references move when a score exceeds them by 2^8, or while a row has none
+      // the references move when a score exceeds them by 2^8, or while a row has none (or one far below 0)
       if (__any_sync(0xFFFFFFFFu, unset || mx > REF_SLACK)) {
         unset = false;
 #pragma unroll
@@ -450,9 +475,9 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
           unpack2(acc.nref[nt], r0_, r1_);
           acc.raise(nt, col_max(a0) - r0_, col_max(a1) - r1_);
           acc.set_vinv(nt);
-          unset |= acc.m[nt][0] == -CUDART_INF_F || acc.m[nt][1] == -CUDART_INF_F;
-          unpack2(acc.nref[nt], s0, s1);
-          s0 -= r0_; s1 -= r1_;
+          unset |= acc.m[nt][0] < FAR_BELOW || acc.m[nt][1] < FAR_BELOW;
+          s0 = acc.m[nt][0] == -CUDART_INF_F ? 0.f : -acc.m[nt][0] - r0_;
+          s1 = acc.m[nt][1] == -CUDART_INF_F ? 0.f : -acc.m[nt][1] - r1_;
 #pragma unroll
           for (int i = 0; i < 4; ++i) { sc[i >> 1][nt][2 * (i & 1)] += s0; sc[i >> 1][nt][2 * (i & 1) + 1] += s1; }
         }
@@ -517,7 +542,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
       unpack2(acc.z[nt], z[0], z[1]);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        f[s] = acc.R[nt][s] == -CUDART_INF_F ? 1.f : fast_exp2(acc.R[nt][s] - acc.m[nt][s] - 6.f);
+        f[s] = acc.D[nt][s] == -CUDART_INF_F ? 1.f : fast_exp2(acc.D[nt][s] - 6.f);
         ls[nt][s] = col_sum(ls[nt][s]);
         z[s] = col_sum(z[s]);
       }
@@ -602,7 +627,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
             float& x = sc[nt][2 * i + s];
             const bool vis = (see >> (k0 + 8 * i + (lane >> 2))) & 1ull;
             x *= kf[i];                              // (rows next to the largest number: a score stays one, and NaN NaN)
-            x = !vis ? -CUDART_INF_F : x > 1e38f ? 1e38f : x < -1e38f ? -1e38f : x;
+            x = vis ? clamp_score(x) : -CUDART_INF_F;
             mx[s] = fmaxf(mx[s], x);
           }
         }

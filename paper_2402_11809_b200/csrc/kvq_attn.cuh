@@ -12,6 +12,12 @@ namespace kvq {
 using namespace tc;
 
 constexpr float REF_SLACK = 8.f;                     // a row's reference moves when a score exceeds it by 2^8
+constexpr float FAR_BELOW = -4096.f;                 // a reference below this is not taken into the scores of later keys, whose bits it would cost
+// Keys whose step, times a score's factors, is beyond this (rows that hold numbers next to the largest one): their scores are
+// taken 2^-64 times as large and held to the range of numbers.  The lowest value is 4096 steps at most and the sums of query
+// rows are of 128 elements: below the limit no term of a score passes 2^104.
+constexpr float K_LARGE = 0x1p100f;
+constexpr float SCORE_MAX = 1e38f;                   // (log2 units; the difference of two of them is a number)
 constexpr float W_LIMIT = 16384.f;                   // weights of the second product stay below this (f16 ends at 65504)
 constexpr uint64_t WAIT_NS = 1000000000ull;
 
@@ -72,6 +78,9 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   return r;
 }
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }     // -126 <= e <= 127
+__device__ __forceinline__ float clamp_score(float x) {                         // (NaN stays)
+  return x > SCORE_MAX ? SCORE_MAX : x < -SCORE_MAX ? -SCORE_MAX : x;
+}
 __device__ __forceinline__ float quad_sum(float v) {
   v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
   return v + __shfl_xor_sync(0xFFFFFFFFu, v, 2);

@@ -642,11 +642,13 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         // ---- this key's step and lowest value
         hold(FULL + s, g / STAGES, 13);
         float k1, k0, v1;
+        uint32_t kp = 0;
         bool gone;
         if (!own) {
           const uint32_t blk = base + S::RING_OFF + s * S::PAGE + quarter * F::BLOCK + lane * 4;
           gone = bad[s] != 0 || t * TILE + kl >= wk.L;
-          const uint32_t kp = gone ? 0u : lds32(blk + F::K_PAR), vp = gone ? 0u : lds32(blk + F::V_PAR);
+          kp = gone ? 0u : lds32(blk + F::K_PAR);
+          const uint32_t vp = gone ? 0u : lds32(blk + F::V_PAR);
           k1 = bf_lo(kp) * c24; k0 = bf_hi(kp); v1 = bf_lo(vp);
         } else {
           hold(BLK + buf, blocks >> (16 * buf), 14);
@@ -659,8 +661,12 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         if (lane == 0) mbar_arrive(BAR(EMPTY + s));
         hold(SF + buf, g >> 1, 15);
         tc_fence_after();
-        const uint32_t rc_page = rc_at + (own ? S::RC0_OFF - S::RC_OFF : 0);   // (block rows' references come after a clamp)
-        const bool plain = !own && !__any_sync(0xFFFFFFFFu, gone);     // every row sees every key of this warp
+        const bool large = bf_lo(kp) * c24 > K_LARGE;                          // (2^-64 of its scores are taken first)
+        const bool plain = !own && !__any_sync(0xFFFFFFFFu, gone || large);    // every row sees every key of this warp, none is large
+        const bool careful = own || (!plain && __any_sync(0xFFFFFFFFu, large));
+        if (!plain && large) { k1 = bf_lo(kp) * 0x1p-64f * c24; k0 *= 0x1p-64f; }
+        // scores that settle are taken without references; where they are held to the range of numbers, references come after that
+        uint32_t rc_page = rc_at + (careful ? S::RC0_OFF - S::RC_OFF : 0);
         float x[NC];
         uint32_t hw[NC / 2];
         // `fresh`: the references have to come from this page; `settled`: they have
@@ -679,17 +685,17 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
               unpack2(fma2(pack2(x[2 * i], x[2 * i + 1]), k1p, fma2(k0p, sum, ref)), x[2 * i], x[2 * i + 1]);
             }
           }
-          if (own) {                                 // (rows next to the largest number: a score stays one)
-            uint32_t see = 0;                        // (a loop: this code runs once an item, and is fetched for it)
-            if (!gone) {
+          if (careful) {                             // (rows next to the largest number: a score stays one)
+            uint32_t see = own ? 0u : ~0u;           // (a loop: this code runs once an item, and is fetched for it)
+            if (own && !gone) {
 #pragma unroll 1
               for (int i = 0; i < NC; ++i)
                 if (col0 + i < rows) see |= (uint32_t)((masks[(r0 + col0 + i) >> p.gsh] >> kl) & 1ull) << i;
             }
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-              const float y = (x[i] > 1e38f ? 1e38f : x[i] < -1e38f ? -1e38f : x[i]) + rcf[4 * ((col0 + i) >> 1) + 2 + (i & 1)];
-              x[i] = (see >> i) & 1u ? y : -CUDART_INF_F;
+              const float y = clamp_score(large ? x[i] * 0x1p64f : x[i]) + (fresh ? 0.f : rcf[4 * ((col0 + i) >> 1) + 2 + (i & 1)]);
+              x[i] = !gone && ((see >> i) & 1u) ? y : -CUDART_INF_F;
             }
           } else if (!plain && gone) {
 #pragma unroll
@@ -698,7 +704,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
           if (!fresh) {
             if (!settled) {
               // do scores or weights pass the limits?  (the weights by a bound: the largest score, the largest vinv; any score
-              // does while a row has no reference)
+              // does while a row has no reference, or one far below 0, which would cost the scores their bits)
               float a = fmaxf(x[0], x[1]), b = fmaxf(x[2], x[3]);
 #pragma unroll
               for (int i = 4; i < NC; i += 4) { a = max3(a, x[i], x[i + 1]); b = max3(b, x[i + 2], x[i + 3]); }
@@ -731,6 +737,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
             }
             if (over_at[asked & 1] != asked) break;
             fresh = settled = true;                  // (from the scores again: they are still in tensor memory)
+            rc_page = rc_at + S::RC0_OFF - S::RC_OFF;
             continue;
           }
           // ---- new references, from this page's largest scores and weights per query row
@@ -747,11 +754,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
           soft_sync();
           const float vhi = of_quarters_v(vspan, fmax2), vlo = of_quarters_v(vspan + 4, fmin2);
           if (sidx < N) {
-            // (relative to the reference so far, or to 0)
-            const float up = of_quarters(xq, fmax2);
-            const float mo = mref[sidx], mn = fmaxf(mo, mo == -CUDART_INF_F ? up : mo + up);
+            const float mo = mref[sidx], mn = fmaxf(mo, of_quarters(xq, fmax2));
             fq[sidx] = mo == mn ? 1.f : fast_exp2(mo - mn);
-            xz[sidx] = mn == -CUDART_INF_F ? 0.f : mo == -CUDART_INF_F ? -mn : mo - mn;   // what the scores move by
+            xz[sidx] = mn == -CUDART_INF_F ? 0.f : -mn;                        // what the scores move by
             mref[sidx] = mn;
             rref[sidx] -= mo == mn || mo == -CUDART_INF_F ? 0.f : mn - mo;
             rcf[4 * (sidx >> 1) + 2 + (sidx & 1)] = mn == -CUDART_INF_F ? 0.f : -mn;
@@ -778,10 +783,10 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
             go[sidx] = f; vinv[sidx] = v;
           }
           soft_sync();
-          if (warp == SOFT_WARP0) {                  // (a row without any key so far: the next page with one settles again)
+          if (warp == SOFT_WARP0) {                  // (a row without any key so far, or with a reference far below 0: the next page settles again)
             float v = 0.f;
             bool none = false;
-            for (int i = lane; i < rows; i += 32) { v = fmaxf(v, vinv[i]); none |= mref[i] == -CUDART_INF_F; }
+            for (int i = lane; i < rows; i += 32) { v = fmaxf(v, vinv[i]); none |= mref[i] < FAR_BELOW; }
             const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v));
             none = __any_sync(0xFFFFFFFFu, none);
             if (lane == 0) { limit[0] = none ? -CUDART_INF_F : X_LIMIT; limit[1] = __uint_as_float(m); }
@@ -804,6 +809,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
             tmem_wait_st();
           }
           soft_sync();
+          if (!careful) rc_page = rc_at;
         }
         // ---- S^T goes back; P^T out; sums of e
         tc_fence_before();

@@ -4,10 +4,11 @@ import math
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import kvq
 from oracle.bf16 import bf16_bits_to_f64, f32_to_bf16_bits
-from test_gpu_kvq import B, P, WIDE, check, random_cache, run_attention, span_of  # noqa: F401 (B: a fixture)
+from test_gpu_kvq import B, P, WIDE, bits, check, dev, random_cache, run_attention, span_of  # noqa: F401 (B: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +60,102 @@ def test_scores_far_from_zero(B, d, G, k, pps, hole, level):
     spans = [np.nan_to_num(x) * (1 + 2048 * 8 * 2.0 ** -24 * s) for x in span_of(pool, table, lens, d, None)]
     check(out, lse, want, want_lse, spans, scores=s)
     assert status == [B.ST_BAD_PAGE if hole else 0] * len(lens)
+
+
+# ------------------------------------------------------------------------------------------------ next to the largest number
+
+@pytest.mark.parametrize("which", ["k"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,k,pps", FORMS + [(4, 0, 0), (4, 3, WIDE)])
+def test_infinities_in_cached_rows(B, d, G, k, pps, which):
+    """Rows with infinities and the largest numbers, appended (an infinity counts as the largest finite bf16): the outputs
+    stay numbers, and are the softmax over what the cache holds."""
+    rng = np.random.default_rng(32)
+    H, lens, n_q = 2, [400, 300, 40, 333], (k + 1) ** 2
+    n, pps = len(lens), pps or 5
+    raw = bits(rng, n, 2, 400, H, d)                                     # K, V
+    x = raw[:, 0 if which == "k" else 1]
+    if which == "k":
+        rows = [3, 70, 130, 131, 200, 260]                               # (sequence 2 has the first of them only)
+        x[:, 3, :, 5], x[:, 70, :, 9] = 0x7F80, 0xFF80
+        x[:, 130, :, 7], x[:, 131, :, 8] = 0x7F7F, 0xFF7F
+        x[:, 200, :, ::2] = 0x7F80                                       # in many channels, and with both signs
+        x[:, 260, :, ::16], x[:, 260, :, 8::16] = 0xFF80, 0x7F7F
+        x[1, rows[1:]] = raw[1, 1, rows[1:]]                             # sequence 1: one element of one row
+    else:
+        x[:, 10:, :, 3] = 0x7F80                                         # a channel of which nearly every row is an infinity
+        x[:, 5, :, 4] = 0xFF80
+        x[3, 100:130, :, ::2] = 0x7F7F
+    # scores: ordinary queries for V; for K small enough that c |k| |q| stays a number of 32 bits in most rows
+    q = bits(rng, n, n_q, G * H, d, scale=2.0 if which == "v" else 0.05)
+    pool = B.kvq_pool(n * 4 + 1, H, d)
+    pool.fill_(255)
+    table = np.full((n, pps), -1, np.int32)
+    table[:, :4] = rng.permutation(4 * n).reshape(n, 4)
+    ctx = B.Context(max_batch=n, n_q_heads=G * H, n_kv_heads=H, head_dim=d, k_max=7, vocab=8, s_cap=1 << 14)
+    status = torch.zeros(n, dtype=torch.int32, device="cuda")
+    kv, dt, count = dev(raw), dev(table), dev(np.array(lens, np.int32))
+    ctx.space_kvq_append(ctx.kvq_append_args(kv[:, 0], kv[:, 1], pool, dt, torch.zeros_like(count), count=count, status=status))
+    assert (status == B.ST_NONFINITE).all()
+    held = pool.cpu().numpy()
+    kb, vb = (bits(rng, n, n_q, H, d), bits(rng, n, n_q, H, d)) if k else (None, None)
+    out, lse, st = run_attention(B, q, held, table, lens, k, kb, vb, H, d)
+    with np.errstate(over="ignore"):
+        want, want_lse = kvq.attention(bf16_bits_to_f64(q), held, table, lens, k, 1 / math.sqrt(d),
+                                       *((bf16_bits_to_f64(kb), bf16_bits_to_f64(vb)) if k else (None, None)))
+    assert not any(st) and np.isfinite(out).all() and np.isfinite(lse).all()
+    spans = span_of(held, table, lens, d, bf16_bits_to_f64(vb) if k else None)
+    if which == "v":
+        check(out, lse, want, want_lse, spans)
+        # the other rows' channels: every weight is rounded, and multiplies the row's whole span; the channel itself is a number
+        top = np.abs(want[..., 3]).max()
+        assert top > 1e38 and (np.abs(out[..., 3] - want[..., 3]) <= 2.0 ** -8 * np.abs(want[..., 3]) + 2.0 ** -10 * max(spans)).all()
+        return
+    # one key takes the whole softmax of a row, or none of the unusual ones does
+    held_to = 6.9e37                                                     # 1e38 in units of log2: larger scores are held to it
+    clear = np.abs(want_lse) < held_to
+    assert clear.mean() > 0.9 and (np.abs(want_lse) > 1e30).mean() > 0.2 and (np.abs(want_lse) < 100).any()
+    rel = np.abs(lse - want_lse) / np.maximum(np.abs(want_lse), 1.0)
+    assert rel[clear].max() <= 128 * 2.0 ** -23 * 40                     # (sums of up to 128 products with terms of both signs)
+    sel = clear.transpose(0, 2, 1)
+    for b in range(n):
+        err = np.abs(out[b] - want[b])[sel[b]]
+        assert (err <= np.abs(want[b])[sel[b]] * 2.0 ** -8 + spans[b] * 2.0 ** -11 * 1.5).all(), (b, err.max(), spans[b])
+    # scores past the largest number: held to it
+    out, lse, st = run_attention(B, bits(rng, n, n_q, G * H, d, scale=8.0), held, table, lens, k, kb, vb, H, d)
+    assert not any(st) and np.isfinite(out).all() and np.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,k,pps", FORMS)
+def test_ordinary_rows_behind_rows_far_below(B, d, G, k, pps):
+    """The first keys score -1e36, all of them, the ones behind them as usual: those keep their bits."""
+    rng = np.random.default_rng(35)
+    H, lens, n_q = 8, [1, 130, 400, 650, 700, 257, 131, 690], (k + 1) ** 2
+    n, pps = len(lens), pps or 6
+    raw = bits(rng, n, 2, 700, H, d)
+    raw[:, 0, :130, :, 11] = 0xFF80                                      # the first rows of K, and a few more
+    raw[:, 0, 256:256 + 40, :, 11] = 0xFF80
+    q = f32_to_bf16_bits((0.3 + 0.05 * rng.standard_normal((n, n_q, G * H, d))).astype(np.float32))
+    pool = B.kvq_pool(n * 6 + 1, H, d)
+    table = np.full((n, pps), -1, np.int32)
+    table[:, :6] = rng.permutation(6 * n).reshape(n, 6)
+    ctx = B.Context(max_batch=n, n_q_heads=G * H, n_kv_heads=H, head_dim=d, k_max=7, vocab=8, s_cap=1 << 14)
+    kv, dt, count = dev(raw), dev(table), dev(np.array(lens, np.int32))
+    ctx.space_kvq_append(ctx.kvq_append_args(kv[:, 0], kv[:, 1], pool, dt, torch.zeros_like(count), count=count))
+    held = pool.cpu().numpy()
+    kb, vb = bits(rng, n, n_q, H, d), bits(rng, n, n_q, H, d)
+    for block in ((kb, vb), (None, None)):
+        out, lse, st = run_attention(B, q, held, table, lens, k, *block, H, d)
+        want, want_lse = kvq.attention(bf16_bits_to_f64(q), held, table, lens, k, 1 / math.sqrt(d),
+                                       *(None if x is None else bf16_bits_to_f64(x) for x in block))
+        assert not any(st)
+        # keys that all score -1e36 lie apart by far more than a score's bits or are the same key's; the others are ordinary
+        few = np.array(lens) <= 130
+        if block[0] is None:
+            assert np.isfinite(out).all() and (want_lse[few] < -1e30).all()
+            rel = np.abs(lse[few] - want_lse[few]) / np.abs(want_lse[few])
+            assert rel.max() <= 128 * 2.0 ** -23 * 40
+        rest = ~few if block[0] is None else np.ones(n, bool)
+        check(out[rest], lse[rest], want[rest], want_lse[rest],
+              [s for s, r in zip(span_of(held, table, lens, d, None if block[0] is None else bf16_bits_to_f64(vb)), rest) if r])
