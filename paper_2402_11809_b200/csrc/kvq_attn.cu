@@ -8,7 +8,7 @@
 // (second one, whose codes are centred by 8 first: sums of one sign would collect what the tensor core cuts off; without
 // it 65536 keys in one piece with even weights were 1.4 % off, and 64 sequences took 121 us instead of 127).
 // f16 holds a bf16 query row exactly, scaled by a power of two, and the weights e step to 11 bits.  The sums of e and of
-// e (lo + 8 step) refer to the largest score so far, the weights to the largest e step of their row so far: a row of V
+// e (lo + 8 step) refer to a bound on the scores so far, the weights to the largest e step of their row so far: a row of V
 // that is large and hardly seen costs the others no bits.
 //
 // The work.  The cache's bytes, (d + 8) per key and head, bind up to 8 rows, unpacking, exponentials and products beyond:
@@ -35,6 +35,8 @@ namespace {
 using namespace kvq;
 using namespace tc;
 
+// A row's reference moves when a score exceeds it, to 2^8 above that: no e passes 1, so that no e step overflows.
+constexpr float REF_SLACK = 8.f;
 constexpr int WARPS = PAGE_BLOCKS, THREADS = 32 * WARPS;   // a warp per 32-row block of a page
 
 // NT: query rows of an item in eights.
@@ -95,7 +97,7 @@ template <int DH, int NT>
 struct Acc {
   float o[DH / 16][NT][4];                           // channels 16 ct + n (+ 8): {row 2t, 2t + 1} each
   float m[NT][2], D[NT][2];                          // reference of the sums (log2 units), that of the accumulators less it (m can be too large for the difference to show in a sum)
-  uint64_t l[NT], z[NT];                             // sums of e, of e (lo + 8 step); pairs of rows 2t, 2t + 1
+  uint64_t l[NT], z[NT];                             // sums of e, of e (lo + 8 step) V_UNIT; pairs of rows 2t, 2t + 1
   uint64_t nref[NT], vinv[NT];                       // -m (0 while there is none, or one far below 0), 2^(6 - D)
   float vtop;                                        // the largest of those
   __device__ __forceinline__ void clear() {
@@ -113,13 +115,13 @@ struct Acc {
 #pragma unroll
     for (int ct = 0; ct < DH / 16; ++ct) { o[ct][nt][0] *= f0; o[ct][nt][1] *= f1; o[ct][nt][2] *= f0; o[ct][nt][3] *= f1; }
   }
-  // Rows' references raised to mx where that is more; the sums follow.  Returns the factors they took.
+  // Rows' references raised to 2^8 above mx where that is more than they are; the sums follow.  Returns the factors they took.
   __device__ __forceinline__ float2 raise(int nt, float mx0, float mx1) {
     const float mx[2] = {mx0, mx1};
     float f[2], r[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const float n = fmaxf(m[nt][s], mx[s]);
+      const float n = mx[s] > m[nt][s] ? mx[s] + REF_SLACK : m[nt][s];
       f[s] = m[nt][s] == n ? 1.f : fast_exp2(m[nt][s] - n);
       D[nt][s] -= m[nt][s] == n ? 0.f : n - m[nt][s];
       m[nt][s] = n;
@@ -414,7 +416,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
         const int key = 8 * i + (lane >> 2);
         kp[i] = lds32(blk + F::K_PAR + key * 4);
         const uint32_t vp = lds32(blk + F::V_PAR + key * 4);
-        const float v1 = bf_lo(vp), v0 = fmaf(v1, 8.f, bf_hi(vp));
+        const float v1 = bf_lo(vp), v0 = fmaf(v1, 8.f * V_UNIT, bf_hi(vp) * V_UNIT);
         vs[i] = pack2(v1, v1); vz[i] = pack2(v0, v0);
       }
       if (__any_sync(0xFFFFFFFFu, fmaxf(max3(bf_lo(kp[0]), bf_lo(kp[1]), bf_lo(kp[2])), bf_lo(kp[3])) * c24 > K_LARGE)) {
@@ -462,8 +464,8 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) mx = max3(mx, sc[i >> 1][nt][2 * (i & 1)], sc[i >> 1][nt][2 * (i & 1) + 1]);
       }
-      // the references move when a score exceeds them by 2^8, or while a row has none (or one far below 0)
-      if (__any_sync(0xFFFFFFFFu, unset || mx > REF_SLACK)) {
+      // the references move when a score exceeds them, or while a row has none (or one far below 0)
+      if (__any_sync(0xFFFFFFFFu, unset || mx > 0.f)) {
         unset = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -533,7 +535,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
       }
       __syncwarp();                                  // the stage is free for the next request
     }
-    // ---- sums over the lanes, accumulators in real units
+    // ---- sums over the lanes, accumulators in units of V_UNIT
     float ls[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -549,7 +551,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
 #pragma unroll
       for (int ct = 0; ct < DH / 16; ++ct)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc.o[ct][nt][e] = fmaf(acc.o[ct][nt][e] * (e >= 2 ? 1048576.f : 16777216.f), f[e & 1], z[e & 1]);
+        for (int e = 0; e < 4; ++e) acc.o[ct][nt][e] = fmaf(acc.o[ct][nt][e] * ((e >= 2 ? 0x1p20f : 0x1p24f) * V_UNIT), f[e & 1], z[e & 1]);
     }
 
     // ---- the block's own rows: keys 16 warp .. + 15 of it, products in bf16 as they are (no code, no scale), weights as two
@@ -639,10 +641,11 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
           const float e0 = sc[nt][2 * i] == -CUDART_INF_F ? 0.f : fast_exp2(sc[nt][2 * i] - acc.m[nt][0]);
           const float e1 = sc[nt][2 * i + 1] == -CUDART_INF_F ? 0.f : fast_exp2(sc[nt][2 * i + 1] - acc.m[nt][1]);
           lb[0] += e0; lb[1] += e1;
-          const __nv_bfloat162 hi = __floats2bfloat162_rn(e0, e1);
+          const float w0 = e0 * V_UNIT, w1 = e1 * V_UNIT;
+          const __nv_bfloat162 hi = __floats2bfloat162_rn(w0, w1);
           const uint32_t hw = *reinterpret_cast<const uint32_t*>(&hi);
           float l0, l1;
-          low_terms(hw, e0, e1, l0, l1);
+          low_terms(hw, w0, w1, l0, l1);
           const __nv_bfloat162 lo = __floats2bfloat162_rn(l0, l1);
           ph[nt][i] = transpose8(hw);
           pl[nt][i] = transpose8(*reinterpret_cast<const uint32_t*>(&lo));

@@ -11,7 +11,6 @@
 namespace kvq {
 using namespace tc;
 
-constexpr float REF_SLACK = 8.f;                     // a row's reference moves when a score exceeds it by 2^8
 constexpr float FAR_BELOW = -4096.f;                 // a reference below this is not taken into the scores of later keys, whose bits it would cost
 // Keys whose step, times a score's factors, is beyond this (rows that hold numbers next to the largest one): their scores are
 // taken 2^-64 times as large and held to the range of numbers.  The lowest value is 4096 steps at most and the sums of query
@@ -19,6 +18,7 @@ constexpr float FAR_BELOW = -4096.f;                 // a reference below this i
 constexpr float K_LARGE = 0x1p100f;
 constexpr float SCORE_MAX = 1e38f;                   // (log2 units; the difference of two of them is a number)
 constexpr float W_LIMIT = 16384.f;                   // weights of the second product stay below this (f16 ends at 65504)
+constexpr float V_UNIT = 0x1p-32f;                   // of sums of V rows: with rows next to the largest number they stay numbers (2^24 keys of weight 2^8)
 constexpr uint64_t WAIT_NS = 1000000000ull;
 
 struct Params {
@@ -31,7 +31,7 @@ struct Params {
   const char* kn; const char* vn; int64_t n_sb, n_sr, n_sh;
   const int32_t* kv_len;
   __nv_bfloat16* out; float* lse; int32_t* status;
-  float* part;                                       // [2 * n_groups][rows * (DH + 2)]
+  float* part;                                       // [2 * n_groups][rows * (DH + 2)]: sums times V_UNIT, references, sums of e
   int* arrived;                                      // [B * H_kv * n_rt], self-resetting
   int* err;
   uint64_t mask[SPACE_MAX_ROWS];                     // Eq. 5: bit j of word i: block row i sees block row j
@@ -111,11 +111,12 @@ struct Cut {
   }
 };
 
+// o: a row's sums, times V_UNIT
 template <int DH>
 __device__ __forceinline__ void store_row4(const Params& p, int b, int h, int r, int c4, float4 o, float m, float l) {
   int i, hq;
   row_of(p, h, r, i, hq);
-  const float rd = l > 0.f || l != l ? 1.f / l : 0.f;      // a row without keys: zeros
+  const float rd = l > 0.f || l != l ? 0x1p32f / l : 0.f;  // a row without keys: zeros
   const __nv_bfloat162 x = __floats2bfloat162_rn(o.x * rd, o.y * rd), y = __floats2bfloat162_rn(o.z * rd, o.w * rd);
   __nv_bfloat16* dst = p.out + (((int64_t)b * p.n_q + i) * p.H_q + hq) * DH + 4 * c4;
   *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));

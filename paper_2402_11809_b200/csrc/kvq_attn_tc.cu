@@ -850,7 +850,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
       float* ps = p.part + (int64_t)(2 * (int)blockIdx.x + (wk.opens ? 0 : 1)) * SLOT;
       if (sidx < N) {
         const float ls = of_quarters(xq, fsum2);
-        const float m = mref[sidx], f = rref[sidx] == -CUDART_INF_F ? 1.f : fast_exp2(rref[sidx] - W_SHIFT + 9.f);
+        const float m = mref[sidx], up = rref[sidx] - W_SHIFT + 9.f;           // (times V_UNIT before or after: neither 0 nor infinite)
+        const float f = rref[sidx] == -CUDART_INF_F ? 1.f : up > 0.f ? fast_exp2(up - 32.f) : fast_exp2(up) * V_UNIT;
         const float rd = !whole ? 1.f : ls > 0.f || ls != ls ? 1.f / ls : 0.f;   // a row without keys: zeros
         fq[sidx] = f * rd;
         if (sidx < rows) {
@@ -877,6 +878,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] *= fq[c + e];
         if (whole) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] *= 0x1p32f;
           // two rows at a time: the even lane takes both channels of the first, the odd one of the second
 #pragma unroll
           for (int e = 0; e < 4; e += 2) {

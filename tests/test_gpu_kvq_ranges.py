@@ -64,7 +64,7 @@ def test_scores_far_from_zero(B, d, G, k, pps, hole, level):
 
 # ------------------------------------------------------------------------------------------------ next to the largest number
 
-@pytest.mark.parametrize("which", ["k"])
+@pytest.mark.parametrize("which", ["k", "v"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("G,k,pps", FORMS + [(4, 0, 0), (4, 3, WIDE)])
 def test_infinities_in_cached_rows(B, d, G, k, pps, which):
@@ -99,6 +99,8 @@ def test_infinities_in_cached_rows(B, d, G, k, pps, which):
     assert (status == B.ST_NONFINITE).all()
     held = pool.cpu().numpy()
     kb, vb = (bits(rng, n, n_q, H, d), bits(rng, n, n_q, H, d)) if k else (None, None)
+    if which == "v" and k:
+        vb[..., 3] = 0x7F80                                              # and of every row of the block
     out, lse, st = run_attention(B, q, held, table, lens, k, kb, vb, H, d)
     with np.errstate(over="ignore"):
         want, want_lse = kvq.attention(bf16_bits_to_f64(q), held, table, lens, k, 1 / math.sqrt(d),
