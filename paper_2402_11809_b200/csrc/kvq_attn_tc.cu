@@ -761,9 +761,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
             rref[sidx] -= mo == mn || mo == -CUDART_INF_F ? 0.f : mn - mo;
             rcf[4 * (sidx >> 1) + 2 + (sidx & 1)] = mn == -CUDART_INF_F ? 0.f : -mn;
           }
-          // The rows' largest weights: where the page's steps are within 2^6 of each other the largest step serves for every
-          // row; else (a row of V far above the rest, seen by some query rows or hardly) each row's own.
-          const bool wide = vhi > 64.f * vlo;
+          // The rows' largest weights: each row's own, for rows that hardly see a V far above the rest should not follow it.  In a
+          // first page whose steps are within 2^6 of each other the largest step serves for every row: each has a key of e = 1 there.
+          const bool wide = !first || vhi > 64.f * vlo;
           if (wide) {
             soft_sync();
 #pragma unroll

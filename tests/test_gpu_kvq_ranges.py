@@ -161,3 +161,42 @@ def test_ordinary_rows_behind_rows_far_below(B, d, G, k, pps):
         rest = ~few if block[0] is None else np.ones(n, bool)
         check(out[rest], lse[rest], want[rest], want_lse[rest],
               [s for s, r in zip(span_of(held, table, lens, d, None if block[0] is None else bf16_bits_to_f64(vb)), rest) if r])
+
+
+# ------------------------------------------------------------------------------------------------ V far above the others
+
+@pytest.mark.parametrize("factor", [2.0 ** 20, 2.0 ** 30])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,k,pps", [(8, 0, 0), (16, 0, 0), (1, 5, 0), (16, 1, WIDE), (2, 6, WIDE)])
+def test_a_page_of_large_values_costs_rows_that_do_not_see_it_nothing(B, d, G, k, pps, factor):
+    """Whole pages whose V is far above the rest, which one query row sees and the others hardly: those are as near to
+    their values as without such pages."""
+    rng = np.random.default_rng(33)
+    H, lens, n_q = 8, [1500, 1400, 1300, 1500, 1500, 1100, 1500, 1450], (k + 1) ** 2
+    pps = pps or 12
+    pool, table = random_cache(rng, lens, H, d, pps)
+    large = np.unique(table[:, [1, 6]])
+    kp, vp = params(pool, d, 0), params(pool, d, 1)
+    kp[large, ..., 0], kp[large, ..., 1] = 2.0 ** -7, 4.0                # keys of these pages: 4 and a little in every channel
+    other = np.setdiff1d(np.arange(pool.shape[0]), large)
+    there = np.sign(kp[other, ..., 0])                                   # (NaN where nothing lives)
+    kp[other, ..., 0], kp[other, ..., 1] = 0.0625 * there, -0.46875 * there
+    step = 0.25 + 0.05 * rng.random(vp.shape[:-1])                       # (steps within 2^6 of each other in every page)
+    new = np.stack([step, -7.5 * step], -1)
+    new[large] *= factor
+    set_params(pool, d, 0, kp)
+    set_params(pool, d, 1, np.where(np.isfinite(vp), new, np.nan))
+    q = rng.standard_normal((len(lens), n_q, G * H, d)) * 0.3 - 1.0      # away from the large pages' keys
+    row, head = n_q // 2, np.arange(H) * G + G // 2
+    q[:, row, head] *= -0.9                                              # one row of every kv head: towards them
+    q = f32_to_bf16_bits(q.astype(np.float32))
+    out, lse, status = run_attention(B, q, pool, table, lens, k, None, None, H, d)
+    want, want_lse = kvq.attention(bf16_bits_to_f64(q), pool, table, lens, k, 1 / math.sqrt(d))
+    assert not any(status) and np.isfinite(out).all()
+    sees = np.zeros(out.shape[1:3], bool)
+    sees[row, head] = True
+    assert np.abs(want[:, sees]).max() > factor / 100 and np.abs(want[:, ~sees]).max() < 10
+    for rows, span in ((sees, 6.0 * factor), (~sees, 6.0)):
+        err = np.abs(out[:, rows] - want[:, rows])
+        assert (err <= np.abs(want[:, rows]) * 2.0 ** -8 + span * 2.0 ** -11 * 1.5).all(), (err.max(), span)
+    assert np.abs(lse - want_lse).max() <= 128 * 2.0 ** -23 * (np.abs(want_lse).max() + 40) + 1e-6 * np.abs(want_lse).max()
