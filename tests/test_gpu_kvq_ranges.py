@@ -200,3 +200,25 @@ def test_a_page_of_large_values_costs_rows_that_do_not_see_it_nothing(B, d, G, k
         err = np.abs(out[:, rows] - want[:, rows])
         assert (err <= np.abs(want[:, rows]) * 2.0 ** -8 + span * 2.0 ** -11 * 1.5).all(), (err.max(), span)
     assert np.abs(lse - want_lse).max() <= 128 * 2.0 ** -23 * (np.abs(want_lse).max() + 40) + 1e-6 * np.abs(want_lse).max()
+
+
+# ------------------------------------------------------------------------------------------------ V of one sign
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("d,H,G,k", [(64, 4, 8, 0), (128, 4, 8, 0), (64, 4, 16, 0), (128, 4, 4, 2), (128, 1, 16, 1), (64, 1, 1, 7), (128, 1, 16, 3)])
+def test_values_of_one_sign(B, d, H, G, k, sign):
+    """Tens of thousands of keys of nearly even weight in few pieces, with V on one side of zero: sums that only grow."""
+    rng = np.random.default_rng(34)
+    n, L, n_q = 128, 40000, (k + 1) ** 2
+    pages = (L + P - 1) // P
+    pool, one = random_cache(rng, [L], H, d, pages)
+    vp = params(pool, d, 1)
+    vp[..., 1] = vp[..., 0] * (2.0 if sign > 0 else -17.0)
+    set_params(pool, d, 1, vp)
+    table = np.repeat(one, n, 0)                                         # every sequence has the same pages
+    q = bits(rng, n, n_q, G * H, d, scale=0.05)
+    out, lse, status = run_attention(B, q, pool, table, [L] * n, k, None, None, H, d)
+    assert not any(status)
+    some = [0, 77, n - 1]
+    want, want_lse = kvq.attention(bf16_bits_to_f64(q[some]), pool, table[some], [L] * 3, k, 1 / math.sqrt(d))
+    check(out[some], lse[some], want, want_lse, span_of(pool, table[:1], [L], d, None) * 3)
