@@ -313,6 +313,7 @@ def page_pool(t):
     """Descriptor of a page pool for space_pages_copy: a 4-bit pool (uint8 [n_pages, H_kv, bytes]), or one of the two
     pools of a bf16 cache ([n_pages, H_kv, PAGE_SIZE, d]).  Keep the tensor alive as long as the descriptor is used."""
     import torch
+    assert t.is_cuda
     if t.dtype == torch.uint8:
         assert t.dim() == 3 and t.stride(2) == 1 and t.shape[2] % 4 == 0
         return PagePool(base=_ptr(t), page_stride=t.stride(0), part_stride=t.stride(1), parts=t.shape[1], group_rows=32,
@@ -342,10 +343,18 @@ def _keeping(args, *tensors):
     return args
 
 
-def _kvq_cache(pool, page_table):
+def _check_i32(n, *tensors):
+    """One int32 per sequence on the device, or None."""
     import torch
-    assert pool.dtype == torch.uint8 and pool.dim() == 3 and pool.stride(2) == 1
-    assert page_table.dtype == torch.int32 and page_table.is_contiguous()
+    for t in tensors:
+        assert t is None or (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous() and t.numel() >= n)
+
+
+def _kvq_cache(pool, page_table, kv_len, batch):
+    import torch
+    assert pool.dtype == torch.uint8 and pool.is_cuda and pool.dim() == 3 and pool.stride(2) == 1
+    assert page_table.dtype == torch.int32 and page_table.is_cuda and page_table.is_contiguous() and page_table.shape[0] >= batch
+    assert kv_len is not None
     return KvqCache(pool=_ptr(pool), page_stride=pool.stride(0), head_stride=pool.stride(1), page_table=_ptr(page_table),
                     pages_per_seq=page_table.shape[1], n_pages=pool.shape[0])
 
@@ -471,7 +480,8 @@ class Context:
     # -- 4-bit cache ------------------------------------------------------
     def _check_rows(self, k, v):
         import torch
-        assert k.dtype == v.dtype == torch.bfloat16 and k.shape == v.shape and k.stride() == v.stride() and k.stride(3) == 1
+        assert k.dtype == v.dtype == torch.bfloat16 and k.is_cuda and v.is_cuda
+        assert k.shape == v.shape and k.stride() == v.stride() and k.stride(3) == 1
         assert k.shape[2] == self.cfg.n_kv_heads and k.shape[3] == self.cfg.head_dim
 
     def _check_pool(self, pool):
@@ -481,12 +491,14 @@ class Context:
                         kv_len_out=None, status=None):
         """k_new / v_new [B, rows, H_kv, d] bf16 by strides.  A prompt or a token: row_step 1; the accepted rows of a
         step's block: row_step k + 1, count n_accept, count_bias 1."""
+        n = k_new.shape[0]
         self._check_rows(k_new, v_new)
         self._check_pool(pool)
-        return _keeping(KvqAppendArgs(batch=k_new.shape[0], rows=k_new.shape[1], row_step=row_step, count_bias=count_bias,
+        _check_i32(n, kv_len, count, kv_len_out, status)
+        return _keeping(KvqAppendArgs(batch=n, rows=k_new.shape[1], row_step=row_step, count_bias=count_bias,
                                       k_new=_ptr(k_new), v_new=_ptr(v_new), new_stride_b=k_new.stride(0),
                                       new_stride_r=k_new.stride(1), new_stride_h=k_new.stride(2),
-                                      cache=_kvq_cache(pool, page_table), kv_len=_ptr(kv_len), count=_ptr(count),
+                                      cache=_kvq_cache(pool, page_table, kv_len, n), kv_len=_ptr(kv_len), count=_ptr(count),
                                       kv_len_out=_ptr(kv_len_out), status=_ptr(status)),
                         k_new, v_new, pool, page_table, kv_len, count, kv_len_out, status)
 
@@ -495,9 +507,11 @@ class Context:
 
     def kvq_read_args(self, pool, page_table, kv_len, k_out, v_out, first=None, status=None):
         """k_out / v_out [B, rows, H_kv, d] bf16 by strides."""
+        n = k_out.shape[0]
         self._check_rows(k_out, v_out)
         self._check_pool(pool)
-        return _keeping(KvqReadArgs(batch=k_out.shape[0], rows=k_out.shape[1], cache=_kvq_cache(pool, page_table),
+        _check_i32(n, kv_len, first, status)
+        return _keeping(KvqReadArgs(batch=n, rows=k_out.shape[1], cache=_kvq_cache(pool, page_table, kv_len, n),
                                     kv_len=_ptr(kv_len), first=_ptr(first), k_out=_ptr(k_out), v_out=_ptr(v_out),
                                     out_stride_b=k_out.stride(0), out_stride_r=k_out.stride(1), out_stride_h=k_out.stride(2),
                                     status=_ptr(status)),
@@ -510,18 +524,24 @@ class Context:
                       mask_variant=MASK_SAME_GROUP):
         """q [B, (k+1)^2, H_q, d] and k_new / v_new [B, (k+1)^2, H_kv, d] bf16 by strides, out contiguous bf16."""
         import torch
-        assert q.dtype == out.dtype == torch.bfloat16 and q.stride(3) == 1 and out.is_contiguous() and out.shape == q.shape
+        n = q.shape[0]
+        assert q.dtype == out.dtype == torch.bfloat16 and q.is_cuda and out.is_cuda
+        assert q.stride(3) == 1 and out.is_contiguous() and out.shape == q.shape
         assert q.shape[1:] == ((k + 1) ** 2, self.cfg.n_q_heads, self.cfg.head_dim)
         self._check_pool(pool)
+        _check_i32(n, kv_len, status)
+        assert lse is None or (lse.dtype == torch.float32 and lse.is_cuda and lse.is_contiguous() and
+                               lse.numel() == n * q.shape[1] * q.shape[2])
         sb = sr = sh = 0
+        assert (k_new is None) == (v_new is None)
         if k_new is not None:
             self._check_rows(k_new, v_new)
             assert k_new.shape[:2] == q.shape[:2]
             sb, sr, sh = k_new.stride()[:3]
-        return _keeping(KvqAttnArgs(batch=q.shape[0], k=k, mask_variant=mask_variant, scale=scale, q=_ptr(q),
+        return _keeping(KvqAttnArgs(batch=n, k=k, mask_variant=mask_variant, scale=scale, q=_ptr(q),
                                     q_stride_b=q.stride(0), q_stride_r=q.stride(1), q_stride_h=q.stride(2), k_new=_ptr(k_new),
                                     v_new=_ptr(v_new), new_stride_b=sb, new_stride_r=sr, new_stride_h=sh,
-                                    cache=_kvq_cache(pool, page_table), kv_len=_ptr(kv_len), out=_ptr(out), lse=_ptr(lse),
+                                    cache=_kvq_cache(pool, page_table, kv_len, n), kv_len=_ptr(kv_len), out=_ptr(out), lse=_ptr(lse),
                                     status=_ptr(status)),
                         q, k_new, v_new, pool, page_table, kv_len, out, lse, status)
 
