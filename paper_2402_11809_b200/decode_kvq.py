@@ -76,7 +76,7 @@ class Decoder:
         self.pools = [B.kvq_pool(samples * pps, model.h_kv, model.d) for _ in range(model.layers)]
         self.moves_to = B.page_pools(self.pools)
         self.pager = B.Pager(samples * pps, pps, samples)
-        kv = model.prompt(torch.tensor(prompt[:-1], device="cuda"))
+        kv = model.prompt(torch.tensor(prompt[:-1], device="cuda")) if self.prompt_rows else []
         first = self.pager.admit()
         self.pager.reserve(first, self.prompt_rows)
         self._append([first], [x[0] for x in kv], [x[1] for x in kv], [0])
