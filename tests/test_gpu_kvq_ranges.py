@@ -35,7 +35,7 @@ def set_params(pool, d, which, val):
 
 # ------------------------------------------------------------------------------------------------ scores far from zero
 
-@pytest.mark.parametrize("level", [-1000.0, -100.0, -80.0, 1000.0])
+@pytest.mark.parametrize("level", [-20000.0, -1000.0, -100.0, -80.0, 1000.0])
 @pytest.mark.parametrize("hole", [False, True])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("G,k,pps", FORMS)
