@@ -434,8 +434,8 @@ typedef struct {
 int space_sar_sft_transform(const space_sar_args* args, void* stream);
 
 /* ---- KV cache in 4 bits ------------------------------------------------------------------------
- * (No counterpart in the paper: what a step costs at serving lengths is reading the cache, and a cache in
- * 4 bits is about a quarter of the bf16 one.)  Paged like the bf16 cache: a pool of pages of
+ * (No counterpart in the paper: a cache in 4 bits is about a quarter of the bf16 one, so that a server holds
+ * more or longer sequences.)  Paged like the bf16 cache: a pool of pages of
  * SPACE_PAGE_SIZE rows behind a page table, row s of sequence b in row s % SPACE_PAGE_SIZE of page
  * page_table[b * pages_per_seq + s / SPACE_PAGE_SIZE], K and V of a row in the same page.
  *
@@ -509,10 +509,14 @@ int space_kvq_read(space_ctx* ctx, const space_kvq_read_args* args, void* stream
  * 0 .. pages_per_seq * SPACE_PAGE_SIZE (SPACE_ST_CAPACITY).  Keys of a page outside the pool are left out
  * (SPACE_ST_BAD_PAGE).  Hidden rows have no influence, whatever they hold; non-finite elements of k_new /
  * v_new count as they do in space_kvq_append (without the status bit).
- * The output is bf16: scores and sums are fp32, the weights of the second product are rounded to 11 bits, and where
- * a kv head has 49 to 64 or more than 96 query rows the cache's V values, in steps, may be too.
+ * The output is bf16: scores and sums are fp32, the weights of the second product are rounded to 11 bits.  A call whose
+ * kv heads have 49 to 64 or most numbers above 96 of query rows may run in another form, if pages_per_seq gives every SM
+ * work: it rounds the cache's V values, in steps, and the block's K and V rows to 11 bits too.  (So a wider table can
+ * change last bits.)
  * The products take query rows as f16, scaled by one power of two for up to 64 rows of a kv head together: elements
- * more than 2^21 times smaller than the largest of those rows are rounded, by at most 2^-29 of it; all others are exact.
+ * more than 2^21 times smaller than the largest of those rows are rounded, by at most 2^-29 of it; all others are exact
+ * below 2^109.  Scores are held to +-6.9e37 (1e38 in units of log2): of keys beyond that none is preferred.  Outputs below
+ * 2^-110 may be rounded to multiples of 2^-117.
  * Asynchronous on `stream`, no allocation; one call at a time per context (scratch of the context).
  * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE (batch or k beyond the context's), UNSUPPORTED (batch * n_kv_heads *
  * ceil(query rows of a kv head / 8) * (pages_per_seq + 4) above 2e9), CUDA. */

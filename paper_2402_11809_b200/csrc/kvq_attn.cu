@@ -6,7 +6,7 @@
 // its 32-bit word is already an f16 number, the subnormal u 2^-24 (or u 2^-20 for the nibbles at bits 4..7), which
 // the tensor cores take at full rate; the powers of two go into the query row (first product) and into the epilogue
 // (second one, whose codes are centred by 8 first: sums of one sign would collect what the tensor core cuts off; without
-// it 65536 keys in one piece with even weights were 1.4 % off, and 64 sequences took 121 us instead of 127).
+// it 65536 keys in one piece with even weights were 1.4 % off, and 64 sequences, one input set, took 121 us instead of 127).
 // f16 holds a bf16 query row exactly, scaled by a power of two, and the weights e step to 11 bits.  The sums of e and of
 // e (lo + 8 step) refer to a bound on the scores so far, the weights to the largest e step of their row so far: a row of V
 // that is large and hardly seen costs the others no bits.
@@ -23,9 +23,11 @@
 // 32 keys leave registers for 4, 3, 2 blocks per SM.  The block's own rows are bf16 products, their weights two bf16
 // terms each.  The pieces of an item that was cut are joined by the block that stores the last of them, always in the
 // same order.
-// Measured, d = 128: 64 sequences of 1024 to 16384 keys, 8 kv heads of 4 rows, 127 us (72 % of the copy rate: four
-// warps per scheduler issue 0.56 instructions a cycle); one sequence of 131071 keys 43 us, of which the pages are
-// 26 (91 %), the start 5 and the join of 74 pieces a head 12; 16 sequences of 512 to 4096 keys, 32 heads, 36 rows 142 us,
+// Rows next to the largest number: where a block of keys holds one its scores are taken 2^-64 times as large and held to
+// +-1e38, references are put above the scores, so that no weight passes 1, and sums of V rows are 2^-32 as large.
+// Measured, d = 128, three input sets in turn: 64 sequences of 1024 to 16384 keys, 8 kv heads of 4 rows, 136.5 us (0.69 of
+// the copy rate: four warps per scheduler issue 0.54 instructions a cycle); one sequence of 131071 keys 42 us, of which the
+// pages are 26 (0.9), the start 5 and the join of 74 pieces a head 11; 16 sequences of 512 to 4096 keys, 32 heads, 36 rows 143 us,
 // 1.7 us a page of 24 rows and block, two blocks per SM, of which the products are half and 0.37 instructions a cycle is
 // what two warps per scheduler give; an item costs 8 us beside its pages.
 // Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT and the block drains and exits.

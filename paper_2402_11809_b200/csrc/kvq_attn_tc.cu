@@ -18,7 +18,8 @@
 // So (8 x 8 heads, 392 rows of 8192 keys; 451 us on mma.sync): sixteen softmax warps instead of eight (417 -> 396); whether
 // a page's scores pass the limits is asked by an mbarrier under the exponentials, not by a barrier before them (349); block
 // rows read their sums from a list of their own instead of a select per score (335); the unpacking in short loops (329); V
-// in steps and one sum per row (323); scores in one read of tensor memory (320).  Slower were query rows on M (1.9 us a
+// in steps and one sum per row (323); scores in one read of tensor memory (320; 321 with all that keeps rows next to the
+// largest number and references far below 0 right).  Slower were query rows on M (1.9 us a
 // page), four groups of softmax warps, sixteen rows each, that do not wait for each other (+11 %), weights published, barriers asked
 // for or parameters looked up a page ahead (+5 to 10 %), a factor common to all rows beside one each (+27 %).
 //
@@ -41,7 +42,7 @@ constexpr int SOFT_WARPS = 16, SOFT = 32 * SOFT_WARPS;          // four threads 
 constexpr int THREADS = 12 * 32 + SOFT;
 constexpr int TILE = SPACE_PAGE_SIZE;
 constexpr int NP = 4;                                // sixteens of query rows of an item
-constexpr int SHARE_COST = 5;                        // fixed cost of an item, in pages (8 us against 1.6 us a page)
+constexpr int SHARE_COST = 5;                        // fixed cost of an item, in pages (8 us against 1.45 us a page)
 constexpr int K_WARP0 = 4, V_WARP0 = 8, SOFT_WARP0 = 12;
 constexpr float W_SHIFT = 2.f;                       // weights of a new reference lie in [2^2, 2^3) (below 2^-14 f16 has fewer bits)
 constexpr float X_LIMIT = 16.f;                      // a row's reference moves when a score exceeds it by 2^16

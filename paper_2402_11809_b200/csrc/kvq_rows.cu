@@ -14,7 +14,7 @@
 // store their V bytes two at a time where they belong; for the few rows of a step or a token, where a thread block
 // per 32-row block would be nearly empty.  Sixteen channels a lane, in pairs of floats and with one shuffle for both
 // ends of the span, because the first form (eight channels, single floats) was held up by its instructions: 16 sequences
-// of 512 to 4096 rows, 32 heads, d = 128, took it 257 us; now 156, of which the bytes (5 d + 8 a row and head, K and V)
+// of 512 to 4096 rows, 32 heads, d = 128, took it 257 us; now 156 (166 with three input sets in turn), of which the bytes (5 d + 8 a row and head, K and V)
 // are 111.
 //
 // Read back: a thread block per 32-row block, V codes through shared memory; 204 us of 190 for the same rows (a second
