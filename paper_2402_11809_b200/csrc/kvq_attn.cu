@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
         unset = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float a0 = -CUDART_INF_F, a1 = -CUDART_INF_F, r0_, r1_, s0, s1;
+          float a0 = -CUDART_INF_F, a1 = -CUDART_INF_F, r0_, r1_;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             a0 = fmaxf(a0, sc[i >> 1][nt][2 * (i & 1)]); a1 = fmaxf(a1, sc[i >> 1][nt][2 * (i & 1) + 1]);
@@ -480,10 +480,16 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvq_attn_kernel(c
           acc.raise(nt, col_max(a0) - r0_, col_max(a1) - r1_);
           acc.set_vinv(nt);
           unset |= acc.m[nt][0] < FAR_BELOW || acc.m[nt][1] < FAR_BELOW;
-          s0 = acc.m[nt][0] == -CUDART_INF_F ? 0.f : -acc.m[nt][0] - r0_;
-          s1 = acc.m[nt][1] == -CUDART_INF_F ? 0.f : -acc.m[nt][1] - r1_;
+          // (without the old reference, then less the new one, whose scores are these: a difference of two references would
+          // have the rounding of their size, and could leave the largest score above its own reference)
+          float n0 = acc.m[nt][0] == -CUDART_INF_F ? 0.f : -acc.m[nt][0], n1 = acc.m[nt][1] == -CUDART_INF_F ? 0.f : -acc.m[nt][1];
+          if (n0 == r0_) n0 = r0_ = 0.f;
+          if (n1 == r1_) n1 = r1_ = 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) { sc[i >> 1][nt][2 * (i & 1)] += s0; sc[i >> 1][nt][2 * (i & 1) + 1] += s1; }
+          for (int i = 0; i < 4; ++i) {
+            float &x0 = sc[i >> 1][nt][2 * (i & 1)], &x1 = sc[i >> 1][nt][2 * (i & 1) + 1];
+            x0 = (x0 - r0_) + n0; x1 = (x1 - r1_) + n1;
+          }
         }
         acc.set_vtop();
         mx = 0.f;                                    // (none is above its reference now; a first reference can also have moved the scores up)

@@ -45,6 +45,10 @@ constexpr int NP = 4;                                // sixteens of query rows o
 constexpr int SHARE_COST = 5;                        // fixed cost of an item, in pages (8 us against 1.45 us a page)
 constexpr int K_WARP0 = 4, V_WARP0 = 8, SOFT_WARP0 = 12;
 constexpr float W_SHIFT = 2.f;                       // weights of a new reference lie in [2^2, 2^3) (below 2^-14 f16 has fewer bits)
+// Where references are set, the scores that they come from are taken without any and then once more with them, which rounds
+// otherwise: by 2^-22 of a score's largest term, 16 times the key's step times the score's factors at most.  Below this limit
+// that is 4, which leaves the weights below 2^7; for steps beyond it the reference comes off the very same score.
+constexpr float K_CAREFUL = 0x1p20f;
 constexpr float X_LIMIT = 16.f;                      // a row's reference moves when a score exceeds it by 2^16
 
 template <int DH>
@@ -662,7 +666,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvq_attn_tc_kernel(const __grid_co
         if (lane == 0) mbar_arrive(BAR(EMPTY + s));
         hold(SF + buf, g >> 1, 15);
         tc_fence_after();
-        const bool large = bf_lo(kp) * c24 > K_LARGE;                          // (2^-64 of its scores are taken first)
+        const bool large = bf_lo(kp) * c24 > K_CAREFUL;                         // (2^-64 of its scores are taken first)
         const bool plain = !own && !__any_sync(0xFFFFFFFFu, gone || large);    // every row sees every key of this warp, none is large
         const bool careful = own || (!plain && __any_sync(0xFFFFFFFFu, large));
         if (!plain && large) { k1 = bf_lo(kp) * 0x1p-64f * c24; k0 *= 0x1p-64f; }

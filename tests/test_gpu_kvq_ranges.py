@@ -62,6 +62,43 @@ def test_scores_far_from_zero(B, d, G, k, pps, hole, level):
     assert status == [B.ST_BAD_PAGE if hole else 0] * len(lens)
 
 
+@pytest.mark.parametrize("top", [12, 24, 40, 60])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,k,pps", FORMS)
+def test_scores_that_are_large_and_grow(B, d, G, k, pps, top):
+    """Pages of K that are up to 2^top as large as others, in any order: a reference is never below the scores it comes from,
+    whatever the rounding of their size."""
+    rng = np.random.default_rng(36)
+    H, lens, n_q = 8, [1500, 1400, 1300, 700, 1500, 33, 128, 1450], (k + 1) ** 2
+    pps = pps or 12
+    pool, table = random_cache(rng, lens, H, d, pps)
+    kp = params(pool, d, 0)
+    kp *= 2.0 ** rng.integers(0, top + 1, size=(pool.shape[0], 1, 1, 1))
+    set_params(pool, d, 0, kp)
+    q = bits(rng, len(lens), n_q, G * H, d)
+    kb, vb = bits(rng, len(lens), n_q, H, d, scale=2.0 ** (top // 2)), bits(rng, len(lens), n_q, H, d)
+    out, lse, status = run_attention(B, q, pool, table, lens, k, kb, vb, H, d)
+    assert not any(status) and np.isfinite(out).all() and np.isfinite(lse).all()
+    q64, kb64, vb64, scale = bf16_bits_to_f64(q), bf16_bits_to_f64(kb), bf16_bits_to_f64(vb), 1 / math.sqrt(d)
+    want, want_lse = kvq.attention(q64, pool, table, lens, k, scale, kb64, vb64)
+    spans, sure = span_of(pool, table, lens, d, vb64), 0
+    see = kvq.visible(k)
+    for b, L in enumerate(lens):
+        K, V = (np.concatenate([x, y[b].transpose(1, 0, 2)], 1) for x, y in zip(kvq.read_rows(pool, table[b], L, d), (kb64, vb64)))
+        for hq in range(G * H):
+            # a score: sums of 128 products and of a lowest value's, each off by 2^-24 of its terms' sizes
+            a, h = q64[b, :, hq], hq // G
+            s = np.where(np.concatenate([np.ones((n_q, L), bool), see], 1), scale * (a @ K[h].T), -np.inf)
+            off = 128 * 2.0 ** -24 * 4 * scale * np.abs(a).sum(-1) * np.abs(K[h]).max()
+            assert (np.abs(lse[b, hq] - want_lse[b, hq]) <= off + 1e-3).all()
+            two = np.sort(s, -1)[:, -2:]
+            one = two[:, 1] - two[:, 0] > 2 * off + 30                   # one key has all the weight
+            sure += one.sum()
+            err = np.abs(out[b, one, hq] - V[h][s.argmax(-1)[one]])
+            assert (err <= np.abs(want[b, one, hq]) * 2.0 ** -8 + spans[b] * 2.0 ** -11 * 1.5).all(), err.max()
+    assert sure > 0
+
+
 # ------------------------------------------------------------------------------------------------ next to the largest number
 
 @pytest.mark.parametrize("which", ["k", "v"])
