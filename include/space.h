@@ -515,8 +515,8 @@ int space_kvq_read(space_ctx* ctx, const space_kvq_read_args* args, void* stream
  * change last bits.)
  * The products take query rows as f16, scaled by one power of two for up to 64 rows of a kv head together: elements
  * more than 2^21 times smaller than the largest of those rows are rounded, by at most 2^-29 of it; all others are exact
- * below 2^109.  Scores are held to +-6.9e37 (1e38 in units of log2): of keys beyond that none is preferred.  Outputs below
- * 2^-110 may be rounded to multiples of 2^-117.
+ * below 2^109.  Scores are held to +-6.9e37 (1e38 in units of log2): of keys beyond that none is preferred.  A weight below
+ * 2^-118 of a row's largest counts as nothing; outputs below 2^-110 may be rounded to multiples of 2^-117.
  * Asynchronous on `stream`, no allocation; one call at a time per context (scratch of the context).
  * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE (batch or k beyond the context's), UNSUPPORTED (batch * n_kv_heads *
  * ceil(query rows of a kv head / 8) * (pages_per_seq + 4) above 2e9), CUDA. */
