@@ -266,7 +266,7 @@ def prepare(case, seed):
     if case["paged"]:
         st["cache"] = torch.zeros(2, n_pages, H, PAGE, d, dtype=torch.bfloat16, device="cuda")
     else:
-        st["cache"] = torch.zeros(2, B, H, int(total.max()) + 1, d, dtype=torch.bfloat16, device="cuda")
+        st["cache"] = torch.zeros(2, B, H, max(128, int(total.max()) + 1), d, dtype=torch.bfloat16, device="cuda")
     return st
 
 
@@ -287,8 +287,10 @@ def _context(state):
         from paper_2402_11809_b200 import binding as S
         c = state["case"]
         rows = state["table"].shape[1] * PAGE if "table" in state else 128
+        if c["kind"] == "rope" and not c["paged"]:
+            rows = state["cache"].shape[3]                 # (a contiguous cache has as many rows as the handle says)
         ctx = S.Context(max_batch=c["B"], n_q_heads=c.get("H_q", 1), n_kv_heads=c.get("H_kv", 1), head_dim=c.get("d", 64), k_max=7,
-                        vocab=c.get("V", 1), s_cap=max(128, rows, state["cache"].shape[3] if "cache" in state else 0))
+                        vocab=c.get("V", 1), s_cap=max(128, rows))
         if c["kind"] == "attn":
             kn, vn = state["new"]
             args = (ctx.kvb_attn_args(state["q"], state["pool"], state["table"], state["kv_len"], state["out"], c["k"],
