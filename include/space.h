@@ -62,8 +62,11 @@ enum {
   SPACE_ST_BAD_PAGE      = 8,  /* a page-table entry outside [0, n_pages): that page is not
                                   touched (attention reads zeros in its place, the commit skips
                                   the row)                                     */
-  SPACE_ST_NONFINITE     = 16  /* a row handed to the 4-bit cache (space_kvq_*) held a NaN, counted
-                                  as 0, or an infinity, counted as the largest finite bf16       */
+  SPACE_ST_NONFINITE     = 16, /* a row handed to the 4-bit or 8-bit cache (space_kvq_*, space_kvb_*) held a
+                                  NaN, counted as 0, or an infinity, counted as the largest finite bf16 */
+  SPACE_ST_BAD_POSITION  = 32, /* a position outside the rotation table: the nearest one in it was used */
+  SPACE_ST_BAD_MASK      = 64  /* space_logits_adjust: a mask number from n_masks on (the row counts as one
+                                  without a mask), or a mask that leaves a row no token          */
 };
 
 typedef struct space_ctx space_ctx;   /* opaque; owns only its own workspace */
@@ -538,6 +541,195 @@ typedef struct {
 } space_kvq_attn_args;
 int space_kvq_attn_step(space_ctx* ctx, const space_kvq_attn_args* args, void* stream);
 
+/* ---- Positions by rotation ---------------------------------------------------------------------
+ * (No counterpart in the paper, whose models bring it along; its block has positions of its own, Sec. 3.2.)
+ * Channel pairs (x1, x2) of a query or key row at position p turn by the p-th row of a table:
+ *   x1' = x1 cos - x2 sin,   x2' = x2 cos + x1 sin,
+ * in fp32, each product and the sum rounded, then to the output's type.  Channels from rot_dim on stay as they are. */
+typedef struct {
+  const float* table;          /* device [n_pos, rot_dim], 16-byte aligned: cosines of a position's rot_dim/2
+                                  angles, then their sines                                            */
+  int32_t n_pos;
+  int32_t rot_dim;             /* a multiple of 16, at most head_dim                               */
+  int32_t interleaved;         /* 0: channel i turns with i + rot_dim/2; 1: channel 2i with 2i + 1 */
+  int32_t reserved;            /* 0                                                                */
+  const int32_t* pos;          /* device [B, rows] (row r of the call), or NULL: the cache row that r becomes */
+} space_rope;
+
+/* The rows that attention is about to see: queries and keys of row r < count[b] are rotated, the keys and the values
+ * go to cache row kv_len[b] + r (bf16, contiguous or paged as in space_attn_args; without `pos` that is the position
+ * too).  With k_cache == NULL the rotated keys go to k_out instead, for a cache that takes its rows after the step
+ * (space_kvq_*, space_kvb_*).  q_out may be q and k_out may be k, with their strides; q may be NULL.  Rows from count[b] on stay
+ * untouched, and so does all of a sequence whose rows would not fit its capacity (SPACE_ST_CAPACITY); K and V of a page
+ * outside the pool are skipped (SPACE_ST_BAD_PAGE).  Asynchronous on `stream`, no allocation.
+ * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE (batch beyond the context's), UNSUPPORTED (rot_dim), CUDA. */
+typedef struct {
+  int32_t batch;
+  int32_t rows;                /* rows per sequence in q, k and v                                  */
+  space_rope rope;
+  const void* q;               /* device bf16, element (b, r, h, :) at b*stride_b + r*stride_r + h*stride_h */
+  int64_t q_stride_b, q_stride_r, q_stride_h;          /* elements, multiples of 8; bases 16-byte aligned */
+  void* q_out;
+  int64_t q_out_stride_b, q_out_stride_r, q_out_stride_h;
+  const void* k;               /* device bf16 [B, rows, H_kv, d] by strides                        */
+  const void* v;               /* the same strides; NULL without a cache                           */
+  int64_t new_stride_b, new_stride_r, new_stride_h;
+  void* k_out;                 /* device bf16 [B, rows, H_kv, d] by strides, or NULL with a cache  */
+  int64_t k_out_stride_b, k_out_stride_r, k_out_stride_h;
+  void* k_cache;               /* device bf16, addressing as in space_attn_args                    */
+  void* v_cache;
+  int64_t kv_stride_b, kv_stride_h, kv_stride_s;
+  const int32_t* page_table;   /* device [B, pages_per_seq] or NULL (contiguous)                   */
+  int32_t pages_per_seq;
+  int32_t n_pages;
+  const int32_t* kv_len;       /* device [B] lengths before the call                               */
+  const int32_t* count;        /* device [B], or NULL: all of `rows` (less than 0 counts as 0, more than `rows` as `rows`) */
+  int32_t* kv_len_out;         /* device [B] lengths after, or NULL; must not be kv_len            */
+  int32_t* status;             /* device [B], OR-ed, or NULL                                       */
+} space_rope_args;
+int space_rope_append(space_ctx* ctx, const space_rope_args* args, void* stream);
+
+/* ---- KV cache in 8 bits ------------------------------------------------------------------------
+ * (No counterpart in the paper: half the bf16 cache.)  Paged as the 4-bit one: row s of sequence b in row
+ * s % SPACE_PAGE_SIZE of page page_table[b * pages_per_seq + s / SPACE_PAGE_SIZE], K and V of a row in the same page.
+ *
+ * Elements are e4m3 numbers (four bits of significance, up to 448); the 32 rows of a block (rows 0..31, 32..63, ..
+ * of a page) share a power of two 2^e per kv head, one for K and one for V, and an element stands for code * 2^e:
+ *   e = the least whole number with max|x| <= 448 2^e, -100 at least;   code = x / 2^e to the nearest, ties to even.
+ * NaN counts as 0 and an infinity as the largest finite bf16 (SPACE_ST_NONFINITE).  Rows come one after another: e covers
+ * the rows that a block has had since its first row was last written, and where a later row raises it the block's earlier
+ * codes are rounded once more, to multiples of 2^(e - 9) (all others stay exactly what they were).
+ *
+ * Bytes of a page, per kv head (head_stride apart), the order of the attention's tensor-core operands:
+ *   K codes [d/16][128][16]: channel c of row r in byte (c/16) 2048 + 16 r + c%16
+ *   V codes [8][d][16]:      channel c of row r in byte 128 d + (r/16) 16 d + 16 c + r%16
+ *   scales  [4] {f32 K 2^e, f32 V 2^e} */
+typedef space_kvq_cache space_kvb_cache;   /* (head_stride: at least 256 d + 32 bytes) */
+
+/* Bytes of one page of a contiguous pool: n_kv_heads * (256 head_dim + 32); 0 for a head_dim other than 64 and 128. */
+int64_t space_kvb_page_bytes(int32_t n_kv_heads, int32_t head_dim);
+
+/* Puts rows behind the cached ones, as space_kvq_append does: row g * row_step of k_new / v_new becomes cache row
+ * kv_len[b] + g for g < count[b] + count_bias.  With rope.table the keys are rotated on the way (rope.pos [B, rows]) and, where q is
+ * given, the same source rows of q into q_out.  Whether a sequence fits, bad pages, errors and the rest: as space_kvq_append;
+ * UNSUPPORTED (rot_dim).  A sequence that does not fit keeps its q_out too. */
+typedef struct {
+  int32_t batch;
+  int32_t rows;                /* rows per sequence in k_new / v_new                               */
+  int32_t row_step;            /* >= 1                                                             */
+  int32_t count_bias;
+  const void* k_new;           /* device bf16, element (b, r, h, :) at b*stride_b + r*stride_r + h*stride_h */
+  const void* v_new;           /*   (elements, multiples of 8; base 16-byte aligned), d contiguous  */
+  int64_t new_stride_b, new_stride_r, new_stride_h;
+  space_kvb_cache cache;
+  const int32_t* kv_len;       /* device [B] lengths before the call                               */
+  const int32_t* count;        /* device [B], or NULL: all of `rows` (every row_step-th)           */
+  int32_t* kv_len_out;         /* device [B] lengths after, or NULL; must not be kv_len            */
+  int32_t* status;             /* device [B], OR-ed, or NULL                                       */
+  space_rope rope;             /* table == NULL: the rows as they are                              */
+  const void* q;               /* device bf16 [B, rows, H_q, d] by strides, or NULL                */
+  int64_t q_stride_b, q_stride_r, q_stride_h;
+  void* q_out;                 /* may be q, with its strides                                       */
+  int64_t q_out_stride_b, q_out_stride_r, q_out_stride_h;
+} space_kvb_append_args;
+int space_kvb_append(space_ctx* ctx, const space_kvb_append_args* args, void* stream);
+
+/* Reads cache rows first[b] .. first[b] + rows - 1 back: arguments, zeros and errors as space_kvq_read.  The bf16 values
+ * are exactly what the codes stand for. */
+typedef struct {
+  int32_t batch;
+  int32_t rows;
+  space_kvb_cache cache;
+  const int32_t* kv_len;       /* device [B]                                                       */
+  const int32_t* first;        /* device [B], or NULL (0)                                          */
+  void* k_out;                 /* device bf16, element (b, r, h, :) at b*stride_b + r*stride_r + h*stride_h */
+  void* v_out;                 /*   (elements, multiples of 8; base 16-byte aligned), d contiguous  */
+  int64_t out_stride_b, out_stride_r, out_stride_h;
+  int32_t* status;             /* device [B], OR-ed, or NULL                                       */
+} space_kvb_read_args;
+int space_kvb_read(space_ctx* ctx, const space_kvb_read_args* args, void* stream);
+
+/* Attention of a step's block rows over an 8-bit cache: softmax(scale q k^T) v over cache rows 0 .. kv_len[b]-1 and, with
+ * k_new / v_new, over the block's own rows (bf16, not in the cache yet) as Eq. 5 shows them.  k = 0 is one row per
+ * sequence.  Rows that see nothing, sequences that do not fit, bad pages, hidden rows and non-finite elements of
+ * k_new / v_new: as space_kvq_attn_step.  A query row that holds a NaN or an infinity gives NaN.
+ * The output is bf16, the sums are fp32.  Query rows and the block's rows are taken as two e4m3 numbers an element with a power of
+ * two per row: bf16 exactly, but elements more than 2^9 times smaller than the largest of their row are rounded, by at most
+ * 2^-18 of it.  The weights of a page's keys (times their V scales) are rounded likewise, to eight bits and by at most 2^-18 of the largest.
+ * Scores, in units of log2, are held to +-1e30: of keys beyond that none is preferred.
+ * Asynchronous on `stream`, no allocation; one call at a time per context (scratch of the context).
+ * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE (batch or k beyond the context's), UNSUPPORTED (batch * n_kv_heads *
+ * ceil(query rows of a kv head / 32) * (pages_per_seq + 8) above 2e9), CUDA. */
+typedef struct {
+  int32_t batch;
+  int32_t k;                   /* 0 .. k_max; (k+1)^2 query rows                                   */
+  int32_t mask_variant;        /* SPACE_MASK_*                                                     */
+  float   scale;               /* > 0, normally 1/sqrt(d)                                          */
+  const void* q;               /* device bf16, element (b, i, h, :) at b*stride_b + i*stride_r + h*stride_h */
+  int64_t q_stride_b, q_stride_r, q_stride_h;          /* elements, multiples of 8                 */
+  const void* k_new;           /* device bf16 [B, n_q, H_kv, d] by strides, or NULL together with v_new */
+  const void* v_new;
+  int64_t new_stride_b, new_stride_r, new_stride_h;
+  space_kvb_cache cache;
+  const int32_t* kv_len;       /* device [B] rows cached                                           */
+  void*    out;                /* device bf16 [B, n_q, H_q, d]                                     */
+  float*   lse;                /* device [B, H_q, n_q] natural-log sum-exp, or NULL                */
+  int32_t* status;             /* device [B], OR-ed, or NULL                                       */
+} space_kvb_attn_args;
+int space_kvb_attn_step(space_ctx* ctx, const space_kvb_attn_args* args, void* stream);
+
+/* ---- Logits before verification ----------------------------------------------------------------
+ * (No counterpart in the paper, which decodes unpenalised.)  Changes a step's logits [B, (k+1)^2, vocab] (k = 0: one row
+ * per sequence) before space_verify.  Row (g, o) stands behind the generated tokens and candidates 1 .. g: with n the times that
+ * a token occurs among them, and z its logit, in fp32, each operation rounded, then to the logits' type:
+ *   z > 0 ? z / repetition : z * repetition      where n > 0 or the token occurs in the prompt
+ *   z - frequency * n,   then z - presence       where n > 0
+ *   z + bias                                     for a token of the list (named twice: the sum, in order)
+ *   -infinity                                    where the row's mask has a 0 bit
+ * A row that its mask leaves no token is -infinity throughout (SPACE_ST_BAD_MASK): no token can be taken from it.
+ * `out` may be `logits` with its row stride: then only what changes is written.  Asynchronous on `stream`, no
+ * allocation; one call at a time per context.  Errors: INVALID_ARG, ALIGNMENT, WORKSPACE (batch, k or vocab beyond the
+ * context's), CUDA. */
+#define SPACE_COUNT_PROMPT    (1 << 30)   /* bit of a count: the token occurs in the prompt; below it, how often it was generated
+                                             (from 2^24 - 1 on counts as 2^24 - 1)                         */
+#define SPACE_LOGITS_MAX_BIAS 1024
+typedef struct {
+  int32_t batch, k, vocab;
+  int32_t dtype;               /* SPACE_DTYPE_* of logits and out                                  */
+  const void* logits;          /* device [B, (k+1)^2, vocab]; batch stride = (k+1)^2 * row stride  */
+  int64_t logits_row_stride;   /* elements                                                         */
+  void* out;                   /* the same shape                                                   */
+  int64_t out_row_stride;
+  const int32_t* counts;       /* device [B, vocab] (space_token_counts), or NULL: no token so far */
+  const int32_t* cand;         /* device [B, k], or NULL: candidates do not count; ids outside [0, vocab) never do */
+  const float* repetition;     /* device [B], > 0, or NULL (1)                                     */
+  const float* presence;       /* device [B], or NULL (0)                                          */
+  const float* frequency;      /* device [B], or NULL (0)                                          */
+  int32_t n_bias;              /* 0 .. SPACE_LOGITS_MAX_BIAS                                       */
+  int32_t n_masks;
+  const int32_t* bias_tok;     /* device [B, n_bias]; ids outside [0, vocab) are skipped           */
+  const float* bias_val;       /* device [B, n_bias]                                               */
+  const uint32_t* mask_bits;   /* device [n_masks, ceil(vocab / 32)]: bit t % 32 of word t / 32 allows token t; or NULL */
+  const int32_t* mask_row;     /* device [B, (k+1)^2]: mask of every row, below 0: none; with mask_bits */
+  int32_t* status;             /* device [B], OR-ed, or NULL                                       */
+} space_logits_args;
+int space_logits_adjust(space_ctx* ctx, const space_logits_args* args, void* stream);
+
+/* Counts tokens [B, n] for space_logits_adjust: the first n_tokens[b] of a sequence are added to its counts, or, with `prompt`, marked
+ * as occurring in the prompt.  After a step: the emitted ones (out_tokens, n_out of space_verify).  Ids outside
+ * [0, vocab) are skipped.  With `reset` the counts are 0 before.  Asynchronous on `stream`, no allocation.
+ * Errors: INVALID_ARG, WORKSPACE (batch or vocab beyond the context's), CUDA. */
+typedef struct {
+  int32_t batch, vocab, n;
+  int32_t prompt, reset;
+  int32_t reserved;            /* 0                                                                */
+  const int32_t* tokens;       /* device, n of a sequence stride_b elements apart                  */
+  int64_t tokens_stride_b;
+  const int32_t* n_tokens;     /* device [B], or NULL: all n (less than 0 counts as 0, more than n as n) */
+  int32_t* counts;             /* device [B, vocab]                                                */
+} space_counts_args;
+int space_token_counts(space_ctx* ctx, const space_counts_args* args, void* stream);
+
 /* ---- Moving pages ------------------------------------------------------------------------------
  * Rows 0 .. rows-1 of page src become those of page dst, for every move and in every pool (the pools of all
  * layers, K and V, share their page numbers), in one launch per SPACE_PAGES_MAX_MOVES moves: what a fork's
@@ -545,7 +737,7 @@ int space_kvq_attn_step(space_ctx* ctx, const space_kvq_attn_args* args, void* s
  * A page is `parts` pieces, part_stride apart, of rows in groups of group_rows, group_bytes each; of a
  * group that `rows` ends in all is copied.  bf16 pool [n_pages, H_kv, 128, d]: one pool for K, one for V,
  * parts = H_kv, group_rows = 1, group_bytes = 2 d.  4-bit pool: parts = H_kv, group_rows = 32,
- * group_bytes = 32 d + 256.  No page may be written twice in a call, or both read and written.
+ * group_bytes = 32 d + 256.  8-bit pool: parts = H_kv, group_rows = 128, group_bytes = 256 d + 32.  No page may be written twice in a call, or both read and written.
  * Both lists are host memory, read before the call returns; no context, current device, asynchronous on
  * `stream`, no allocation on the device.
  * Errors: INVALID_ARG (sizes, pages, overlap), ALIGNMENT (base, strides and group_bytes not multiples of 16), CUDA. */

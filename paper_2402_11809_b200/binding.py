@@ -23,6 +23,8 @@ RESAMPLE_RESIDUAL_POINTMASS, RESAMPLE_PAPER_LITERAL, RESAMPLE_RESIDUAL_DRAFT = 0
 DTYPE_BF16, DTYPE_F32 = 0, 1
 ATTN_TENSOR, ATTN_SIMT, ATTN_TENSOR_ROWS = 0, 1, 2
 ST_CAPACITY, ST_BAD_CANDIDATE, ST_TIMEOUT, ST_BAD_PAGE, ST_NONFINITE = 1, 2, 4, 8, 16
+ST_BAD_POSITION, ST_BAD_MASK = 32, 64
+COUNT_PROMPT, LOGITS_MAX_BIAS = 1 << 30, 1024
 PAGE_SIZE = 128
 
 EXPORTS = ["space_create", "space_destroy", "space_workspace_bytes", "space_layout",
@@ -36,7 +38,8 @@ EXPORTS = ["space_create", "space_destroy", "space_workspace_bytes", "space_layo
            "space_pager_release", "space_pager_free_pages", "space_pager_rows", "space_pager_batch_table",
            "space_pager_fork", "space_pager_make_writable", "space_pager_truncate", "space_pager_compact",
            "space_pager_page_refs", "space_kvq_page_bytes", "space_kvq_append", "space_kvq_read",
-           "space_kvq_attn_step", "space_pages_copy"]
+           "space_kvq_attn_step", "space_pages_copy", "space_rope_append", "space_kvb_page_bytes", "space_kvb_append",
+           "space_kvb_read", "space_kvb_attn_step", "space_logits_adjust", "space_token_counts"]
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -161,6 +164,50 @@ class KvqAttnArgs(C.Structure):
                 ("kv_len", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("status", C.c_void_p)]
 
 
+class Rope(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("n_pos", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("reserved", C.c_int32), ("pos", C.c_void_p)]
+
+
+class RopeArgs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("rows", C.c_int32), ("rope", Rope), ("q", C.c_void_p), ("q_stride_b", C.c_int64),
+                ("q_stride_r", C.c_int64), ("q_stride_h", C.c_int64), ("q_out", C.c_void_p), ("q_out_stride_b", C.c_int64),
+                ("q_out_stride_r", C.c_int64), ("q_out_stride_h", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("new_stride_b", C.c_int64), ("new_stride_r", C.c_int64), ("new_stride_h", C.c_int64), ("k_out", C.c_void_p),
+                ("k_out_stride_b", C.c_int64), ("k_out_stride_r", C.c_int64), ("k_out_stride_h", C.c_int64),
+                ("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("kv_stride_b", C.c_int64), ("kv_stride_h", C.c_int64),
+                ("kv_stride_s", C.c_int64), ("page_table", C.c_void_p), ("pages_per_seq", C.c_int32), ("n_pages", C.c_int32),
+                ("kv_len", C.c_void_p), ("count", C.c_void_p), ("kv_len_out", C.c_void_p), ("status", C.c_void_p)]
+
+
+class KvbAppendArgs(C.Structure):
+    _fields_ = KvqAppendArgs._fields_ + [("rope", Rope), ("q", C.c_void_p), ("q_stride_b", C.c_int64), ("q_stride_r", C.c_int64),
+                                         ("q_stride_h", C.c_int64), ("q_out", C.c_void_p), ("q_out_stride_b", C.c_int64),
+                                         ("q_out_stride_r", C.c_int64), ("q_out_stride_h", C.c_int64)]
+
+
+class KvbReadArgs(C.Structure):
+    _fields_ = KvqReadArgs._fields_
+
+
+class KvbAttnArgs(C.Structure):
+    _fields_ = KvqAttnArgs._fields_
+
+
+class LogitsArgs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("k", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("logits", C.c_void_p),
+                ("logits_row_stride", C.c_int64), ("out", C.c_void_p), ("out_row_stride", C.c_int64), ("counts", C.c_void_p),
+                ("cand", C.c_void_p), ("repetition", C.c_void_p), ("presence", C.c_void_p), ("frequency", C.c_void_p),
+                ("n_bias", C.c_int32), ("n_masks", C.c_int32), ("bias_tok", C.c_void_p), ("bias_val", C.c_void_p),
+                ("mask_bits", C.c_void_p), ("mask_row", C.c_void_p), ("status", C.c_void_p)]
+
+
+class CountsArgs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("vocab", C.c_int32), ("n", C.c_int32), ("prompt", C.c_int32), ("reset", C.c_int32),
+                ("reserved", C.c_int32), ("tokens", C.c_void_p), ("tokens_stride_b", C.c_int64), ("n_tokens", C.c_void_p),
+                ("counts", C.c_void_p)]
+
+
 class PagePool(C.Structure):
     _fields_ = [("base", C.c_void_p), ("page_stride", C.c_int64), ("part_stride", C.c_int64), ("parts", C.c_int32),
                 ("group_rows", C.c_int32), ("group_bytes", C.c_int32), ("n_pages", C.c_int32)]
@@ -181,7 +228,10 @@ lib.space_layout.restype = C.c_int
 for _name, _arg in (("space_attn_step", AttnArgs), ("space_verify", VerifyArgs),
                     ("space_kv_commit", CommitArgs), ("space_step_host", HostStepArgs),
                     ("space_lmhead_verify", LmHeadArgs), ("space_kvq_append", KvqAppendArgs),
-                    ("space_kvq_read", KvqReadArgs), ("space_kvq_attn_step", KvqAttnArgs)):
+                    ("space_kvq_read", KvqReadArgs), ("space_kvq_attn_step", KvqAttnArgs),
+                    ("space_rope_append", RopeArgs), ("space_kvb_append", KvbAppendArgs), ("space_kvb_read", KvbReadArgs),
+                    ("space_kvb_attn_step", KvbAttnArgs), ("space_logits_adjust", LogitsArgs),
+                    ("space_token_counts", CountsArgs)):
     getattr(lib, _name).argtypes = [C.c_void_p, C.POINTER(_arg), C.c_void_p]
     getattr(lib, _name).restype = C.c_int
 lib.space_sar_sft_transform.argtypes = [C.POINTER(SarArgs), C.c_void_p]
@@ -235,6 +285,8 @@ lib.space_pager_page_refs.argtypes = [C.c_void_p, C.c_int32]
 lib.space_pager_page_refs.restype = C.c_int32
 lib.space_kvq_page_bytes.argtypes = [C.c_int32, C.c_int32]
 lib.space_kvq_page_bytes.restype = C.c_int64
+lib.space_kvb_page_bytes.argtypes = [C.c_int32, C.c_int32]
+lib.space_kvb_page_bytes.restype = C.c_int64
 lib.space_pages_copy.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p]
 lib.space_pages_copy.restype = C.c_int
 
@@ -309,15 +361,50 @@ def kvq_pool(n_pages, n_kv_heads, head_dim, device="cuda"):
     return torch.zeros(n_pages, n_kv_heads, kvq_page_bytes(1, head_dim), dtype=torch.uint8, device=device)
 
 
+def kvb_page_bytes(n_kv_heads, head_dim):
+    """Bytes of a page of the 8-bit cache: a pool is a uint8 tensor [n_pages, n_kv_heads, page_bytes(1, d)]."""
+    return lib.space_kvb_page_bytes(n_kv_heads, head_dim)
+
+
+def kvb_pool(n_pages, n_kv_heads, head_dim, device="cuda"):
+    """An empty 8-bit page pool."""
+    import torch
+    return torch.zeros(n_pages, n_kv_heads, kvb_page_bytes(1, head_dim), dtype=torch.uint8, device=device)
+
+
+def rope_table(n_pos, rot_dim, theta=10000.0, device="cuda"):
+    """Cosines, then sines, of positions 0 .. n_pos - 1 (angles in 64 bits): what `rope` takes."""
+    import torch
+    freq = theta ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
+    angle = torch.arange(n_pos, dtype=torch.float64)[:, None] * freq[None]
+    return torch.cat([angle.cos(), angle.sin()], 1).float().to(device)
+
+
+def rope(table, interleaved=False, pos=None):
+    """Rotation by position: table float32 [n_pos, rot_dim] (rope_table), pos int32 [B, rows] or None (the cache row)."""
+    import torch
+    assert table.dtype == torch.float32 and table.is_cuda and table.dim() == 2 and table.is_contiguous()
+    assert pos is None or (pos.dtype == torch.int32 and pos.is_cuda and pos.dim() == 2 and pos.is_contiguous())
+    return _keeping(Rope(table=_ptr(table), n_pos=table.shape[0], rot_dim=table.shape[1], interleaved=int(interleaved), reserved=0,
+                         pos=_ptr(pos)), table, pos)
+
+
+def _check_pos(rope, n, rows):
+    """One position per row of the call, where there are any."""
+    pos = rope._tensors[1]
+    assert pos is None or (pos.shape[0] >= n and pos.shape[1] == rows)
+
+
 def page_pool(t):
-    """Descriptor of a page pool for space_pages_copy: a 4-bit pool (uint8 [n_pages, H_kv, bytes]), or one of the two
+    """Descriptor of a page pool for space_pages_copy: a 4-bit or 8-bit pool (uint8 [n_pages, H_kv, bytes]), or one of the two
     pools of a bf16 cache ([n_pages, H_kv, PAGE_SIZE, d]).  Keep the tensor alive as long as the descriptor is used."""
     import torch
     assert t.is_cuda
     if t.dtype == torch.uint8:
         assert t.dim() == 3 and t.stride(2) == 1 and t.shape[2] % 4 == 0
-        return PagePool(base=_ptr(t), page_stride=t.stride(0), part_stride=t.stride(1), parts=t.shape[1], group_rows=32,
-                        group_bytes=t.shape[2] // 4, n_pages=t.shape[0])
+        whole = t.shape[2] in (kvb_page_bytes(1, 64), kvb_page_bytes(1, 128))        # 8 bits: a page's rows lie together
+        return PagePool(base=_ptr(t), page_stride=t.stride(0), part_stride=t.stride(1), parts=t.shape[1],
+                        group_rows=PAGE_SIZE if whole else 32, group_bytes=t.shape[2] if whole else t.shape[2] // 4, n_pages=t.shape[0])
     assert t.dim() == 4 and t.shape[2] == PAGE_SIZE and t.stride(3) == 1 and t.stride(2) == t.shape[3]
     e = t.element_size()
     return PagePool(base=_ptr(t), page_stride=t.stride(0) * e, part_stride=t.stride(1) * e, parts=t.shape[1], group_rows=1,
@@ -547,6 +634,170 @@ class Context:
 
     def space_kvq_attn_step(self, args):
         _check(lib.space_kvq_attn_step(self._h, C.byref(args), _stream()))
+
+    # -- rotation by position, bf16 cache ---------------------------------
+    def _check_q(self, q, q_out, n, rows):
+        import torch
+        assert q.dtype == q_out.dtype == torch.bfloat16 and q.is_cuda and q_out.is_cuda and q.stride(3) == q_out.stride(3) == 1
+        assert q.shape == q_out.shape == (n, rows, self.cfg.n_q_heads, self.cfg.head_dim)
+
+    def rope_append_args(self, rope, q, q_out, k, kv_len, v=None, k_cache=None, v_cache=None, k_out=None, count=None,
+                         kv_len_out=None, status=None, page_table=None):
+        """q / q_out [B, rows, H_q, d] (or None), k / v [B, rows, H_kv, d] bf16 by strides; k_cache / v_cache as attn_args takes
+        them (page_table: pools), or k_out [B, rows, H_kv, d] instead."""
+        import torch
+        n, rows = k.shape[:2]
+        self._check_rows(k, k if v is None else v)
+        assert (k_cache is None) == (v_cache is None) and (k_cache is None) != (k_out is None) and (q is None) == (q_out is None)
+        assert k_cache is None or v is not None
+        _check_pos(rope, n, rows)
+        assert kv_len is not None
+        _check_i32(n, kv_len, count, kv_len_out, status)
+        a = RopeArgs(batch=n, rows=rows, rope=rope, k=_ptr(k), v=_ptr(v), new_stride_b=k.stride(0), new_stride_r=k.stride(1),
+                     new_stride_h=k.stride(2), kv_len=_ptr(kv_len), count=_ptr(count), kv_len_out=_ptr(kv_len_out), status=_ptr(status))
+        if q is not None:
+            self._check_q(q, q_out, n, rows)
+            a.q, a.q_stride_b, a.q_stride_r, a.q_stride_h = _ptr(q), *q.stride()[:3]
+            a.q_out, a.q_out_stride_b, a.q_out_stride_r, a.q_out_stride_h = _ptr(q_out), *q_out.stride()[:3]
+        if k_out is not None:
+            self._check_rows(k, k if v is None else v)
+            assert k_out.dtype == torch.bfloat16 and k_out.is_cuda and k_out.shape == k.shape and k_out.stride(3) == 1
+            assert page_table is None
+            a.k_out, a.k_out_stride_b, a.k_out_stride_r, a.k_out_stride_h = _ptr(k_out), *k_out.stride()[:3]
+        else:
+            assert k_cache.dtype == v_cache.dtype == torch.bfloat16 and k_cache.is_cuda and v_cache.is_cuda
+            assert k_cache.shape == v_cache.shape and k_cache.stride() == v_cache.stride() and k_cache.stride(3) == 1
+            assert k_cache.shape[1] == self.cfg.n_kv_heads and k_cache.shape[3] == self.cfg.head_dim
+            a.k_cache, a.v_cache = _ptr(k_cache), _ptr(v_cache)
+            a.kv_stride_b, a.kv_stride_h, a.kv_stride_s = k_cache.stride()[:3]
+            if page_table is None:
+                assert k_cache.shape[0] >= n and k_cache.shape[2] >= self.cfg.s_cap
+            else:
+                assert k_cache.shape[2] == PAGE_SIZE and page_table.dtype == torch.int32 and page_table.is_cuda
+                assert page_table.is_contiguous() and page_table.shape[0] >= n
+                a.page_table, a.pages_per_seq, a.n_pages = _ptr(page_table), page_table.shape[1], k_cache.shape[0]
+        return _keeping(a, rope, q, q_out, k, v, k_cache, v_cache, k_out, kv_len, count, kv_len_out, status, page_table)
+
+    def space_rope_append(self, args):
+        _check(lib.space_rope_append(self._h, C.byref(args), _stream()))
+
+    # -- 8-bit cache ------------------------------------------------------
+    def _check_pool8(self, pool):
+        assert pool.shape[1] == self.cfg.n_kv_heads and pool.shape[2] == kvb_page_bytes(1, self.cfg.head_dim)
+
+    def kvb_append_args(self, k_new, v_new, pool, page_table, kv_len, count=None, count_bias=0, row_step=1, kv_len_out=None,
+                        status=None, rope=None, q=None, q_out=None):
+        """As kvq_append_args; with rope the keys are rotated on the way, and q [B, rows, H_q, d] into q_out."""
+        n, rows = k_new.shape[:2]
+        self._check_rows(k_new, v_new)
+        self._check_pool8(pool)
+        _check_i32(n, kv_len, count, kv_len_out, status)
+        assert (q is None) == (q_out is None) and (q is None or rope is not None)
+        a = KvbAppendArgs(batch=n, rows=rows, row_step=row_step, count_bias=count_bias, k_new=_ptr(k_new), v_new=_ptr(v_new),
+                          new_stride_b=k_new.stride(0), new_stride_r=k_new.stride(1), new_stride_h=k_new.stride(2),
+                          cache=_kvq_cache(pool, page_table, kv_len, n), kv_len=_ptr(kv_len), count=_ptr(count),
+                          kv_len_out=_ptr(kv_len_out), status=_ptr(status))
+        if rope is not None:
+            _check_pos(rope, n, rows)
+            a.rope = rope
+        if q is not None:
+            self._check_q(q, q_out, n, rows)
+            a.q, a.q_stride_b, a.q_stride_r, a.q_stride_h = _ptr(q), *q.stride()[:3]
+            a.q_out, a.q_out_stride_b, a.q_out_stride_r, a.q_out_stride_h = _ptr(q_out), *q_out.stride()[:3]
+        return _keeping(a, k_new, v_new, pool, page_table, kv_len, count, kv_len_out, status, rope, q, q_out)
+
+    def space_kvb_append(self, args):
+        _check(lib.space_kvb_append(self._h, C.byref(args), _stream()))
+
+    def kvb_read_args(self, pool, page_table, kv_len, k_out, v_out, first=None, status=None):
+        """k_out / v_out [B, rows, H_kv, d] bf16 by strides."""
+        n = k_out.shape[0]
+        self._check_rows(k_out, v_out)
+        self._check_pool8(pool)
+        _check_i32(n, kv_len, first, status)
+        return _keeping(KvbReadArgs(batch=n, rows=k_out.shape[1], cache=_kvq_cache(pool, page_table, kv_len, n),
+                                    kv_len=_ptr(kv_len), first=_ptr(first), k_out=_ptr(k_out), v_out=_ptr(v_out),
+                                    out_stride_b=k_out.stride(0), out_stride_r=k_out.stride(1), out_stride_h=k_out.stride(2),
+                                    status=_ptr(status)),
+                        pool, page_table, kv_len, first, k_out, v_out, status)
+
+    def space_kvb_read(self, args):
+        _check(lib.space_kvb_read(self._h, C.byref(args), _stream()))
+
+    def kvb_attn_args(self, q, pool, page_table, kv_len, out, k, scale, k_new=None, v_new=None, lse=None, status=None,
+                      mask_variant=MASK_SAME_GROUP):
+        """As kvq_attn_args."""
+        import torch
+        n = q.shape[0]
+        assert q.dtype == out.dtype == torch.bfloat16 and q.is_cuda and out.is_cuda
+        assert q.stride(3) == 1 and out.is_contiguous() and out.shape == q.shape
+        assert q.shape[1:] == ((k + 1) ** 2, self.cfg.n_q_heads, self.cfg.head_dim)
+        self._check_pool8(pool)
+        _check_i32(n, kv_len, status)
+        assert lse is None or (lse.dtype == torch.float32 and lse.is_cuda and lse.is_contiguous() and
+                               lse.numel() == n * q.shape[1] * q.shape[2])
+        sb = sr = sh = 0
+        assert (k_new is None) == (v_new is None)
+        if k_new is not None:
+            self._check_rows(k_new, v_new)
+            assert k_new.shape[:2] == q.shape[:2]
+            sb, sr, sh = k_new.stride()[:3]
+        return _keeping(KvbAttnArgs(batch=n, k=k, mask_variant=mask_variant, scale=scale, q=_ptr(q),
+                                    q_stride_b=q.stride(0), q_stride_r=q.stride(1), q_stride_h=q.stride(2), k_new=_ptr(k_new),
+                                    v_new=_ptr(v_new), new_stride_b=sb, new_stride_r=sr, new_stride_h=sh,
+                                    cache=_kvq_cache(pool, page_table, kv_len, n), kv_len=_ptr(kv_len), out=_ptr(out), lse=_ptr(lse),
+                                    status=_ptr(status)),
+                        q, k_new, v_new, pool, page_table, kv_len, out, lse, status)
+
+    def space_kvb_attn_step(self, args):
+        _check(lib.space_kvb_attn_step(self._h, C.byref(args), _stream()))
+
+    # -- logits before verification ---------------------------------------
+    def logits_adjust_args(self, logits, out, k, counts=None, cand=None, repetition=None, presence=None, frequency=None,
+                           bias_tok=None, bias_val=None, mask_bits=None, mask_row=None, status=None):
+        """logits / out [B, (k+1)^2, V] (out may be logits), counts int32 [B, V], cand int32 [B, k], penalties float32 [B],
+        bias_tok int32 and bias_val float32 [B, n], mask_bits int32 [n_masks, ceil(V / 32)], mask_row int32 [B, (k+1)^2]."""
+        import torch
+        n, rows, V = logits.shape
+        assert rows == (k + 1) ** 2 and out.shape == logits.shape and out.dtype == logits.dtype
+        assert logits.dtype in (torch.float32, torch.bfloat16) and logits.is_cuda and out.is_cuda
+        for t in (logits, out):
+            assert t.stride(2) == 1 and (n == 1 or t.stride(0) == rows * t.stride(1))
+        i32 = lambda t, *shape: t is None or (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous() and t.shape == shape)
+        assert i32(counts, n, V) and i32(mask_row, n, rows) and (cand is None or k == 0 or i32(cand, n, k))
+        _check_i32(n, status)
+        for t in (repetition, presence, frequency):
+            assert t is None or (t.dtype == torch.float32 and t.is_cuda and t.is_contiguous() and t.numel() >= n)
+        assert (bias_tok is None) == (bias_val is None) and (mask_bits is None) == (mask_row is None)
+        if bias_tok is not None:
+            assert i32(bias_tok, n, bias_tok.shape[1]) and bias_val.dtype == torch.float32 and bias_val.is_cuda
+            assert bias_val.is_contiguous() and bias_val.shape == bias_tok.shape
+        if mask_bits is not None:
+            assert i32(mask_bits, mask_bits.shape[0], (V + 31) // 32)
+        return _keeping(LogitsArgs(batch=n, k=k, vocab=V, dtype=DTYPE_F32 if logits.dtype == torch.float32 else DTYPE_BF16,
+                                   logits=_ptr(logits), logits_row_stride=logits.stride(1), out=_ptr(out), out_row_stride=out.stride(1),
+                                   counts=_ptr(counts), cand=_ptr(cand), repetition=_ptr(repetition), presence=_ptr(presence),
+                                   frequency=_ptr(frequency), n_bias=0 if bias_tok is None else bias_tok.shape[1],
+                                   n_masks=0 if mask_bits is None else mask_bits.shape[0], bias_tok=_ptr(bias_tok),
+                                   bias_val=_ptr(bias_val), mask_bits=_ptr(mask_bits), mask_row=_ptr(mask_row), status=_ptr(status)),
+                        logits, out, counts, cand, repetition, presence, frequency, bias_tok, bias_val, mask_bits, mask_row, status)
+
+    def space_logits_adjust(self, args):
+        _check(lib.space_logits_adjust(self._h, C.byref(args), _stream()))
+
+    def token_counts_args(self, tokens, counts, n_tokens=None, prompt=False, reset=False):
+        """tokens int32 [B, n] (rows by stride), counts int32 [B, V], n_tokens int32 [B]."""
+        import torch
+        n = tokens.shape[0]
+        assert tokens.dtype == torch.int32 and tokens.is_cuda and tokens.dim() == 2 and tokens.stride(1) == 1
+        assert counts.dtype == torch.int32 and counts.is_cuda and counts.is_contiguous() and counts.shape[0] >= n
+        _check_i32(n, n_tokens)
+        return _keeping(CountsArgs(batch=n, vocab=counts.shape[1], n=tokens.shape[1], prompt=int(prompt), reset=int(reset), reserved=0,
+                                   tokens=_ptr(tokens), tokens_stride_b=tokens.stride(0), n_tokens=_ptr(n_tokens), counts=_ptr(counts)),
+                        tokens, counts, n_tokens)
+
+    def space_token_counts(self, args):
+        _check(lib.space_token_counts(self._h, C.byref(args), _stream()))
 
     # -- decoding loop state (Algorithm 1) ---------------------------------
     def decode_state(self, tokens, n_tokens, last_token, cand, cand_prob, kv_len, finished, block_tokens,

@@ -169,6 +169,9 @@ struct space_ctx {
   char* lm_part;           // output-projection statistics [256 block rows][sm_count] x 16 bytes
   char* lm_gather;         // gathered mask rows of the projection's second phase
   int* lm_counter;         // {arrival counter, first timeout site}
+  unsigned long long* logits_alive;  // per sequence: rows that a mask leaves a token (self-resetting, as the next)
+  int* logits_arrived;     // and the thread blocks that have said which
+  int* kvb_arrived;        // attention over the 8-bit cache: pieces of an item that are stored, per (sequence, kv head, 32 query rows)
   // staging for space_step_host
   char* stage;
   char* host_small;        // pinned host mirror of the staging area's small per-sequence arrays (host_staging only)
@@ -346,6 +349,17 @@ inline size_t kvq_items(const space_config* c) {
   const size_t rows = (size_t)(c->k_max + 1) * (c->k_max + 1) * (c->n_q_heads / c->n_kv_heads);
   return (size_t)c->max_batch * c->n_kv_heads * ((rows + 7) / 8);
 }
+int launch_kvb_append(space_ctx* ctx, const space_kvb_append_args* a, cudaStream_t st);
+int launch_kvb_read(space_ctx* ctx, const space_kvb_read_args* a, cudaStream_t st);
+int launch_kvb_attn(space_ctx* ctx, const space_kvb_attn_args* a, const uint64_t* mask_rows, cudaStream_t st);
+// Scratch of the attention over the 8-bit cache: its thread blocks (two per SM) have two slots each for the rows of an item, 32, 64 or
+// 128; arrival counters of its items.
+inline int kvb_item_rows(int rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+inline size_t kvb_rows(const space_config* c) { return (size_t)(c->k_max + 1) * (c->k_max + 1) * (c->n_q_heads / c->n_kv_heads); }
+inline size_t kvb_partial_floats(const space_config* c, int sm_count) {
+  return 4 * (size_t)sm_count * kvb_item_rows((int)kvb_rows(c)) * (c->head_dim + 2);
+}
+inline size_t kvb_items(const space_config* c) { return (size_t)c->max_batch * c->n_kv_heads * ((kvb_rows(c) + 31) / 32); }
 int launch_philox_debug(uint64_t seed, int64_t n, const uint32_t* c0, const uint32_t* c1,
                         const uint32_t* c2, const uint32_t* c3, uint32_t* out, cudaStream_t st);
 

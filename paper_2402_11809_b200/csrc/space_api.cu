@@ -6,6 +6,7 @@
 #include <cstddef>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 
 namespace {
@@ -30,7 +31,7 @@ int config_supported(const space_config* c) {
 }
 
 struct Carve {
-  size_t attn_part, counters, merge_cnt, arrived, kvq_arrived, vtopk, vpart, vfused, vrow, status, lm_part, lm_gather, lm_counter, stage, total;
+  size_t attn_part, counters, merge_cnt, arrived, kvq_arrived, kvb_arrived, logits_alive, logits_arrived, vtopk, vpart, vfused, vrow, status, lm_part, lm_gather, lm_counter, stage, total;
   size_t part_slots;
   // staging sub-offsets (relative to stage)
   size_t st_q, st_k, st_v, st_logits, st_small;
@@ -40,9 +41,11 @@ Carve carve(const space_config* c, int sm_count) {
   Carve v{};
   size_t off = 0;
   v.attn_part = off;
-  // (the attention over the 4-bit cache keeps its partials in the same place)
-  const size_t part_floats = attn_tensor_partial_floats(c, sm_count, &v.part_slots), kvq_floats = kvq_partial_floats(c, sm_count);
-  off += align_up((part_floats > kvq_floats ? part_floats : kvq_floats) * sizeof(float), 256);
+  // (the attention over the 4-bit and over the 8-bit cache keep their partials in the same place)
+  size_t part_floats = attn_tensor_partial_floats(c, sm_count, &v.part_slots);
+  for (const size_t other : {kvq_partial_floats(c, sm_count), kvb_partial_floats(c, sm_count)})
+    if (other > part_floats) part_floats = other;
+  off += align_up(part_floats * sizeof(float), 256);
   v.counters = off; off += align_up((size_t)(3 * c->max_batch + 4) * sizeof(int), 256);
   v.merge_cnt = off;
   // up to 8 row blocks, one {first, count} pair each; then four words per thread block of the attention grid
@@ -50,6 +53,9 @@ Carve carve(const space_config* c, int sm_count) {
   // pieces of a cut that are stored, per (sequence, kv head, row block)
   v.arrived = off; off += align_up((size_t)c->max_batch * c->n_kv_heads * 8 * sizeof(int), 256);
   v.kvq_arrived = off; off += align_up(kvq_items(c) * sizeof(int), 256);
+  v.kvb_arrived = off; off += align_up(kvb_items(c) * sizeof(int), 256);
+  v.logits_alive = off; off += align_up((size_t)c->max_batch * sizeof(unsigned long long), 256);
+  v.logits_arrived = off; off += align_up((size_t)c->max_batch * sizeof(int), 256);
   v.vtopk = off; off += align_up(verify_filter_scratch_bytes(c->max_batch, c->k_max), 256);
   v.vpart = off;
   off += align_up((size_t)c->max_batch * (c->k_max + 2) * SPACE_VERIFY_MAX_CHUNKS * sizeof(VerifyPartial), 256);
@@ -260,6 +266,9 @@ int space_create(space_ctx** out, const space_config* cfg) {
   ctx->merge_cnt = (int*)(ctx->ws + cv.merge_cnt);
   ctx->arrived = (int*)(ctx->ws + cv.arrived);
   ctx->kvq_arrived = (int*)(ctx->ws + cv.kvq_arrived);
+  ctx->kvb_arrived = (int*)(ctx->ws + cv.kvb_arrived);
+  ctx->logits_alive = (unsigned long long*)(ctx->ws + cv.logits_alive);
+  ctx->logits_arrived = (int*)(ctx->ws + cv.logits_arrived);
   ctx->vpart = (VerifyPartial*)(ctx->ws + cv.vpart);
   ctx->vtopk = ctx->ws + cv.vtopk;
   ctx->vrow = (VerifyRow*)(ctx->ws + cv.vrow);
