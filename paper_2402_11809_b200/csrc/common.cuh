@@ -352,14 +352,11 @@ inline size_t kvq_items(const space_config* c) {
 int launch_kvb_append(space_ctx* ctx, const space_kvb_append_args* a, cudaStream_t st);
 int launch_kvb_read(space_ctx* ctx, const space_kvb_read_args* a, cudaStream_t st);
 int launch_kvb_attn(space_ctx* ctx, const space_kvb_attn_args* a, const uint64_t* mask_rows, cudaStream_t st);
-// Scratch of the attention over the 8-bit cache: its thread blocks (two per SM) have two slots each for the rows of an item, 32, 64 or
-// 128; arrival counters of its items.
-inline int kvb_item_rows(int rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
-inline size_t kvb_rows(const space_config* c) { return (size_t)(c->k_max + 1) * (c->k_max + 1) * (c->n_q_heads / c->n_kv_heads); }
-inline size_t kvb_partial_floats(const space_config* c, int sm_count) {
-  return 4 * (size_t)sm_count * kvb_item_rows((int)kvb_rows(c)) * (c->head_dim + 2);
-}
-inline size_t kvb_items(const space_config* c) { return (size_t)c->max_batch * c->n_kv_heads * ((kvb_rows(c) + 31) / 32); }
+// Scratch of the attention over the 8-bit cache: two slots per thread block, of all the query rows that the blocks of an SM
+// hold; arrival counters of its items, eight query rows each at least.
+constexpr int KVB_SM_ROWS = 64;
+inline size_t kvb_partial_floats(const space_config* c, int sm_count) { return 2 * (size_t)sm_count * KVB_SM_ROWS * (c->head_dim + 2); }
+inline size_t kvb_items(const space_config* c) { return kvq_items(c); }
 int launch_philox_debug(uint64_t seed, int64_t n, const uint32_t* c0, const uint32_t* c1,
                         const uint32_t* c2, const uint32_t* c3, uint32_t* out, cudaStream_t st);
 

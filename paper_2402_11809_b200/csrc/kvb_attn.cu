@@ -1,289 +1,209 @@
-// Attention of a step's block rows over the 8-bit cache (space_kvb_attn_step) on tcgen05, e4m3 operands.
+// Attention of a step's block rows over the 8-bit cache (space_kvb_attn_step), 8 to 32 query rows at a time.
 //
-// The mathematics.  The cache's codes are tensor-core operands as they lie; what they are multiplied with is split in two:
-// a query row, scaled by a power of two of its own, is q0 + q1 with e4m3 numbers (four bits each: bf16 has eight), and so is a weight.
-//   S = q0 K^T + q1 K^T,    O_page = w0 V + w1 V.
-// A page's weights are taken relative to the page's largest (weight times V scale) of their row, so that V rows which are large and
-// hardly seen cost the others no bits, and the page's result joins an fp32 sum in registers with its own factor:
-//   chunk b of 32 keys (one K and one V scale 2^k_b, 2^v_b):   m_b = max_j s_j,   e_j = 2^(s_j - m_b),
-//   w_j = e_j 2^((m_b - m) + v_b - E + 8),  m = max m_b,  E = max_b (m_b - m) + v_b,     l += sum_b 2^(m_b - M) sum_j e_j,
-//   o = o 2^(R - R') + O_page 2^(E + (m - M) - R' - 8)   with R' the larger of R and E + (m - M), both relative to the running maximum M.
-// Only differences of scores are ever added to exponents of scales: large scores cost no bits.
+// The mathematics.  The cache's codes are tensor-core operands as they lie (mma.sync m16n8k32, e4m3): nothing is unpacked.
+// What they are multiplied with is split in two: a query row, scaled by a power of two of its own, is q0 + q1 with e4m3 numbers (four
+// bits each: bf16 has eight), and so is a weight.
+//   S = K q0 + K q1,   D = V^T w0 + V^T w1     for the 32 keys of a block, which share a K and a V scale 2^k, 2^v:
+//   e_j = 2^(s_j - r), r the block's largest score less 8,   l += 2^(r - M) sum_j e_j,   o = o 2^(R - R') + D 2^(v + (r - M) - R')
+// with M the running maximum of r and R' the larger of R and v + (r - M): weights are always taken relative to the largest of
+// their own block, whatever other blocks hold, V rows that are large and hardly seen cost the others no bits, and only
+// differences of scores are added to exponents of scales, so that large scores cost none.
 //
-// The work.  Query rows are the MMA's M extent, a row per thread: 128 of them, or 64 or 32 held twice or four times over,
-// each copy with keys of its own (32-key chunks), so that a row's softmax needs no other thread until the item ends and few rows
-// keep four warps busy.  The flat list of 128-key pages over all (sequence, kv head, query rows) items is cut evenly
-// over the thread blocks, two per SM: one's softmax runs under the other's products.  Pieces of a cut item are joined by the
-// block that stores the last of them, always in the same order.
-// The block's own rows are one more page: bf16 rows as two e4m3 terms each, the second ones as keys 64 ..; their scores are summed in
-// pairs, their weights used twice.
-//
-// Warps: 0-3 softmax and sums, 4 copies and products (one thread), 5-7 only give their registers away.
-// Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT, no role leaves its loop early, and the block drains and exits.
-#include "kvq_attn.cuh"
-#include "kvb_common.cuh"
+// The work.  The keys of all (sequence, kv head, query rows) items form one flat list of 128-key pages, every thread block takes an
+// equal share of it, and a page's four blocks of 32 keys go to its four warps.  A warp streams its blocks into a ring of its own with
+// bulk copies and never meets another warp until the item ends.  The products are taken transposed, keys (channels) on
+// the sixteen rows and query rows on the eight columns.  Which key and which channel stand where in a product is free as long as both
+// operands agree: a lane takes 16 bytes of a K row at a time (four products' worth), 8 bytes of a V channel, and the
+// weights' codes change lanes by an 8 x 8 transpose.  The block's own rows are bf16 products, their weights two bf16 terms each.
+// The pieces of an item that was cut are joined by the block that stores the last of them, always in the same order.
+// Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT and the block drains and exits.
+#include "kvb_attn.cuh"
 
 namespace {
-using kvq::Cut;
-using kvq::lds128;
-using kvq::mul2;
-using kvq::wait;
-using kvq::WAIT_NS;
 using namespace kvb;
-using namespace tc;
 
-constexpr int TILE = SPACE_PAGE_SIZE;                // keys of a page, rows of an MMA
-constexpr int SOFT = 128, THREADS = 2 * SOFT;      // (registers move by groups of four warps)
-constexpr int CTAS = 2;                              // per SM
-constexpr int SHARE_COST = 2;                        // fixed cost of an item, in pages
-constexpr int RING = 8;                              // scales and flags of that many pages
-constexpr float F_MIN = 0x1p-120f, F_MAX = 0x1p75f;  // factor of a score: products stay numbers, and differ from 0
-constexpr float REF_EXACT = 0x1p23f;                 // up to this a reference's rounding moves weights by 2^0.5 at most
+constexpr int WARPS = PAGE_BLOCKS, THREADS = 32 * WARPS;   // a warp per 32-row block of a page
+constexpr float REF_FAR = 0x1p22f;                   // up to this a reference's rounding moves weights by 2^0.25 at most
 
-struct Params {
-  Cache cache;
-  int B, n_q, H_q, H_kv, G, gsh, n_rt;               // G = 1 << gsh; n_rt: items per (sequence, kv head)
-  int n_groups;                                      // thread blocks
-  int has_new;
-  float c;                                           // scale * log2(e)
-  const char* q; int64_t q_sb, q_sr, q_sh;           // bytes
-  const char* kn; const char* vn; int64_t n_sb, n_sr, n_sh;
-  const int32_t* kv_len;
-  __nv_bfloat16* out; float* lse; int32_t* status;
-  float* part;                                       // [2 * n_groups][rows * (DH + 2)]: outputs of a piece, then M, l of its rows
-  int* arrived;                                      // [B * H_kv * n_rt], self-resetting
-  int* err;
-  uint64_t mask[SPACE_MAX_ROWS];                     // Eq. 5: bit j of word i: block row i sees block row j
-};
-
-template <int DH>
+// NT: query rows of an item in eights.
+template <int DH, int NT>
 struct Smem {
   using F = Fmt<DH>;
-  static constexpr int STAGES = DH == 128 ? 2 : 4;
-  static constexpr int Q_PIECE = TILE * DH;                  // [DH / 16][128][16] codes; two of them
-  static constexpr int K_OFF = 2 * Q_PIECE;                  // [STAGES]
-  static constexpr int V_OFF = K_OFF + STAGES * F::CODES;    // [STAGES]
-  static constexpr int SCALE_OFF = V_OFF + STAGES * F::CODES;        // [RING][4] {K, V}
-  static constexpr int OWN_OFF = SCALE_OFF + RING * 32;      // [64] {K factor, V exponent} of the block's own rows
-  static constexpr int ML_OFF = OWN_OFF + 64 * 8;            // [128] {M, l}
-  static constexpr int SRC_OFF = ML_OFF + 128 * 8;           // [RING] addresses of pages on their way
-  static constexpr int BAD_OFF = SRC_OFF + RING * 8;         // [RING]
-  static constexpr int BAR_OFF = BAD_OFF + RING * 4;
-  static constexpr int N_BARS = 2 * STAGES + 4;
-  static constexpr int MISC_OFF = BAR_OFF + N_BARS * 8;
-  static constexpr int MASK_OFF = (MISC_OFF + 16 + 7) / 8 * 8;
-  static constexpr int TABLE_OFF = MASK_OFF + SPACE_MAX_ROWS * 8;    // prefix[max_batch + 1], seq_len[max_batch]
-  static_assert(CTAS * (TABLE_OFF + 129 * 4 + 128 * 4 + 1024) <= 228 * 1024, "two blocks per SM");
+  static constexpr int RT = 8 * NT;
+  static constexpr int SHARE_COST = 2;                       // fixed cost of an item, in pages of the list
+  static constexpr int STAGES = NT == 1 ? 2 : 3;
+  static constexpr int CTAS = NT == 1 ? 3 : 2;               // per SM
+  static constexpr int K_PITCH = 16 * BLOCK_ROWS + 16;       // bytes between sixteens of K channels: a lane quad reaches different banks
+  static constexpr int V_PITCH = F::V_ROWS + 64;             // between sixteens of V rows
+  static constexpr int V_AT = DH / 16 * K_PITCH;
+  static constexpr int SCALE_AT = V_AT + 2 * V_PITCH;        // {K, V} scales of this block and its neighbour
+  static constexpr int BLOCK = SCALE_AT + 16;
+  static constexpr int RING = STAGES * BLOCK;                // of a warp
+  static constexpr int O_PITCH = DH + 4;                     // floats
+  static_assert(RT * O_PITCH * 4 <= RING, "a warp's accumulators are parked in its ring once that has run dry");
+  static constexpr int OWN_PITCH = DH * 2 + 16;              // bytes: the block's own V rows
+  static_assert(16 * OWN_PITCH <= RING, "so are the block's V rows");
+  static constexpr int Q_PITCH = DH;                         // bytes: rows of one term (of 128 channels, odd rows with halves exchanged: eight lanes reach different banks)
+  static constexpr int Q_OFF = WARPS * RING;                 // [2][RT]
+  static constexpr int QF_OFF = Q_OFF + 2 * RT * Q_PITCH;    // [RT] factors of the rows' scores, NaN: the row holds a NaN or infinity
+  static constexpr int ML_OFF = QF_OFF + RT * 4;             // [WARPS][RT] {M, l}
+  static constexpr int BAR_OFF = ML_OFF + WARPS * RT * 8;
+  static constexpr int MISC_OFF = BAR_OFF + WARPS * STAGES * 8;
+  static constexpr int TABLE_OFF = MISC_OFF + 16;            // prefix[max_batch + 1], seq_len[max_batch]
+  static_assert(CTAS * (TABLE_OFF + 129 * 4 + 128 * 4 + 1024) <= 228 * 1024, "blocks of the largest batch that an SM holds");
 };
 
-__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-template <int R> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
-template <int R> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
-__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-#define KVB_R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
-#define KVB_W8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
-__device__ __forceinline__ void tmem_ld32(uint32_t a, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-               "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-               : KVB_R8(r, 0), KVB_R8(r, 8), KVB_R8(r, 16), KVB_R8(r, 24) : "r"(a) : "memory");
+__device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3},{%4,%5,%6,%7},{%8,%9},{%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t a, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-               : KVB_R8(r, 0), KVB_R8(r, 8) : "r"(a) : "memory");
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3},{%4,%5,%6,%7},{%8,%9},{%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-               ::"r"(a), KVB_W8(r, 0), KVB_W8(r, 8) : "memory");
+// 8 x 8 halves transposed over the warp
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
 }
-__device__ __forceinline__ void tmem_st4(uint32_t a, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+// Lane (n, t) has word n of the columns 2t and 2t + 1; it gets words 2t and 2t + 1 of column n.
+__device__ __forceinline__ void transpose_words(uint32_t x, uint32_t y, uint32_t& a, uint32_t& b) {
+  const uint32_t lo = transpose8(__byte_perm(x, y, 0x5410)), hi = transpose8(__byte_perm(x, y, 0x7632));
+  a = __byte_perm(lo, hi, 0x5410);
+  b = __byte_perm(lo, hi, 0x7632);
 }
-// e4m3 x e4m3 -> f32, both operands K-major, M = 128
-__device__ __forceinline__ void mma8_ss(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-               ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc) : "memory");
+// Over the eight lanes that hold a query row's keys.
+__device__ __forceinline__ float col_max(float v) {
+  v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 4));
+  v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 8));
+  return fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 16));
 }
-__device__ __forceinline__ void mma8_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}"
-               ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(acc) : "memory");
-}
-__device__ __forceinline__ constexpr uint32_t instr_desc(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24); }
-// Unswizzled K-major operand: 8 rows x 16 bytes lie together, lbo bytes to the next sixteen bytes of K, sbo to the next eight rows.
-__device__ __forceinline__ uint64_t plain_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-  return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)((lbo >> 4) & 0x3FFF) << 16 | (uint64_t)((sbo >> 4) & 0x3FFF) << 32 | (uint64_t)1 << 46;
-}
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const char* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+__device__ __forceinline__ float col_sum(float v) {
+  v += __shfl_xor_sync(0xFFFFFFFFu, v, 4);
+  v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
+  return v + __shfl_xor_sync(0xFFFFFFFFu, v, 16);
 }
 
-// Four numbers as two e4m3 terms each: w0 the codes nearest to them, w1 those of what is left.
-__device__ __forceinline__ void split4(float a, float b, float c, float d, uint32_t& w0, uint32_t& w1) {
-  const uint32_t x = codes2(a, b), y = codes2(c, d);
-  const uint32_t hx = halves2(x), hy = halves2(y);
-  asm("{\n\t.reg .b16 p, q, m;\n\tmov.b32 {p, q}, %4;\n\tmov.b16 m, 0xBC00;\n\t"       // -1
-      "fma.rn.f32.f16 %0, p, m, %2;\n\tfma.rn.f32.f16 %1, q, m, %3;\n\t}" : "=f"(a), "=f"(b) : "f"(a), "f"(b), "r"(hx));
-  asm("{\n\t.reg .b16 p, q, m;\n\tmov.b32 {p, q}, %4;\n\tmov.b16 m, 0xBC00;\n\t"
-      "fma.rn.f32.f16 %0, p, m, %2;\n\tfma.rn.f32.f16 %1, q, m, %3;\n\t}" : "=f"(c), "=f"(d) : "f"(c), "f"(d), "r"(hy));
-  w0 = x | y << 16;
-  w1 = codes4(a, b, c, d);
-}
-
-__device__ __forceinline__ float max32(const uint32_t* s) {
-  float m[4];
+// State of a warp: lane (n = lane / 4, t = lane % 4) holds columns 2t and 2t + 1 of every eight query rows.
+template <int DH, int NT>
+struct Acc {
+  float o[DH / 16][NT][4];                           // channels 16 ct + n (+ 8): {row 2t, 2t + 1} each
+  float M[NT][2], R[NT][2], l[NT][2];                // (l: of this lane's keys)
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) m[i] = __uint_as_float(s[i]);
+    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-  for (int j = 4; j < 28; j += 8) {
+      for (int ct = 0; ct < DH / 16; ++ct) o[ct][nt][0] = o[ct][nt][1] = o[ct][nt][2] = o[ct][nt][3] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m[i] = max3(m[i], __uint_as_float(s[j + 2 * i]), __uint_as_float(s[j + 2 * i + 1]));
-  }
-  m[0] = max3(m[0], __uint_as_float(s[28]), __uint_as_float(s[29]));
-  m[1] = max3(m[1], __uint_as_float(s[30]), __uint_as_float(s[31]));
-  return fmaxf(max3(m[0], m[1], m[2]), m[3]);
-}
-
-// The items of a block's share, in order: every role walks them for itself.
-struct Walk {
-  uint32_t cur, end, at;                             // at: the item's place in the list
-  int b, it;                                         // item h * n_rt + block of query rows
-  int L, t0, t1;                                     // pages [t0, t1) of it; cached rows (-1: the sequence does not fit)
-  bool opens;                                        // the share begins with this item
-  __device__ __forceinline__ int cached() const { return (max(L, 0) + TILE - 1) / TILE; }    // that page: the block's own rows
-  __device__ __forceinline__ int pages(int has_new) const { return max(cached() + has_new, 1); }
-  __device__ __forceinline__ bool next(const uint32_t* prefix, const int* seq_len, int has_new, uint32_t share0) {
-    while (cur < end) {
-      while (prefix[b + 1] <= cur) ++b;
-      L = seq_len[b];
-      const int Tv = pages(has_new) + SHARE_COST;
-      const uint32_t rem = cur - prefix[b];
-      it = (int)(rem / (uint32_t)Tv);
-      const int x0 = (int)rem - it * Tv, n = min(Tv - x0, (int)(end - cur));
-      opens = cur == share0;
-      at = cur - x0;
-      cur += n;
-      t0 = max(x0 - SHARE_COST, 0); t1 = x0 + n - SHARE_COST;
-      if (t1 > t0) return true;                      // (else only the cost of starting)
+      for (int s = 0; s < 2; ++s) { M[nt][s] = -CUDART_INF_F; R[nt][s] = l[nt][s] = 0.f; }
     }
-    return false;
+  }
+  // A block of keys with reference r, this lane's sum of weights and V's exponent v joins: the accumulators move to the new
+  // references; returns the factor of the block's result.  (r = -infinity: the row sees none of it.)
+  __device__ __forceinline__ float2 join(int nt, const float (&r)[2], const float (&sum)[2], float v) {
+    float a[2], b[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const float Mn = fmaxf(M[nt][s], r[s]);
+      const bool none = r[s] == -CUDART_INF_F;
+      const float down = M[nt][s] == Mn ? 0.f : M[nt][s] - Mn, up = none ? 0.f : r[s] - Mn;
+      l[nt][s] = fmaf(l[nt][s], fast_exp2(down), none ? 0.f : sum[s] * fast_exp2(up));
+      const float r_old = R[nt][s] + down, r_new = v + up, Rn = none ? r_old : fmaxf(r_old, r_new);
+      a[s] = r_old - Rn;
+      b[s] = none ? 0.f : fast_exp2(r_new - Rn);
+      M[nt][s] = Mn; R[nt][s] = Rn;
+    }
+    if (__any_sync(0xFFFFFFFFu, a[0] != 0.f || a[1] != 0.f)) {
+      const float f0 = fast_exp2(a[0]), f1 = fast_exp2(a[1]);
+#pragma unroll
+      for (int ct = 0; ct < DH / 16; ++ct) { o[ct][nt][0] *= f0; o[ct][nt][1] *= f1; o[ct][nt][2] *= f0; o[ct][nt][3] *= f1; }
+    }
+    return make_float2(b[0], b[1]);
   }
 };
 
-__device__ __forceinline__ uint4 pack_row8(const float* y) {
-  uint32_t r[4];
+// The item's query rows as two terms in shared memory, by all threads: DH / 8 of them a row.
+template <int DH, int NT>
+struct Query {
+  static constexpr int LANES = DH / 8, PER = THREADS / LANES, PASSES = (8 * NT + PER - 1) / PER;   // rows at a time
+  uint4 v[PASSES];
+  __device__ __forceinline__ void fetch(const Params& p, int b, int h, int r0) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
-    r[i] = *reinterpret_cast<const uint32_t*>(&v);
+    for (int k = 0; k < PASSES; ++k) {
+      const int r = k * PER + threadIdx.x / LANES;
+      int i, hq;
+      row_of(p, h, r0 + r, i, hq);
+      v[k] = make_uint4(0, 0, 0, 0);
+      if (r < 8 * NT && i < p.n_q)
+        v[k] = *(reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh) + threadIdx.x % LANES);
+    }
   }
-  return make_uint4(r[0], r[1], r[2], r[3]);
-}
-
-// The pieces of an item that was cut over several thread blocks: outputs of their own keys, weighed by l 2^M.  A thread has
-// four channels of a row; the DH / 4 threads of a row look up that many pieces' M and l at once.
-template <int DH, int RT>
-__device__ __forceinline__ void join_pieces(const Params& p, const Cut& cut, int b, int h, int r0, int rows, uint32_t piece0, int pieces, uint32_t item_at, int tid) {
-  constexpr int C4 = DH / 4, SLOT = RT * (DH + 2), BATCH = 8;
-  const float* part = p.part + (int64_t)(2 * piece0) * SLOT;
-  const int first = cut.begin(piece0) >= item_at ? 0 : SLOT, n = rows * C4, c4 = tid % C4;
-  auto at = [&](int x) { return part + (x == 0 ? (int64_t)first : (int64_t)x * (2 * SLOT)); };
-#pragma unroll 1
-  for (int idx = tid - tid % 32; idx < n; idx += SOFT) {                       // (warps stay whole)
-    const int r = min((idx + tid % 32) / C4, rows - 1);
-    float M = -CUDART_INF_F, den = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-    for (int x0 = 0; x0 < pieces; x0 += C4) {
-      const bool there = x0 + c4 < pieces;
-      const float m = there ? __ldcg(at(x0 + c4) + RT * DH + r) : -CUDART_INF_F;
-      const float l = there ? __ldcg(at(x0 + c4) + RT * DH + RT + r) : 0.f;
-      float w = 0.f;
-#pragma unroll 1
-      for (int y = 0; y < C4 && x0 + y < pieces; y += BATCH) {
-        float4 v[BATCH];
+  __device__ __forceinline__ void store(const Params& p, unsigned char* sm) const {
+    using S = Smem<DH, NT>;
+    const int x = threadIdx.x % LANES;
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j)
-          v[j] = x0 + y + j < pieces && y + j < C4 ? __ldcg(reinterpret_cast<const float4*>(at(x0 + y + j) + r * DH) + c4) : make_float4(0.f, 0.f, 0.f, 0.f);
-        if (y == 0) {
-          float top = m;
+    for (int k = 0; k < PASSES; ++k) {
+      const int r = k * PER + threadIdx.x / LANES;
+      uint32_t top = kvq::max_bits(v[k]);
 #pragma unroll
-          for (int k = 1; k < C4; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, k));
-          top = fmaxf(top, M);
-          const float down = M == -CUDART_INF_F ? 0.f : fast_exp2(M - top);
-          M = top;
-          w = m == -CUDART_INF_F ? 0.f : l * fast_exp2(m - top);
-          float sum = w;
-#pragma unroll
-          for (int k = 1; k < C4; k <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, k);
-          den = fmaf(den, down, sum);
-          o.x *= down; o.y *= down; o.z *= down; o.w *= down;
-        }
-#pragma unroll
-        for (int j = 0; j < BATCH; ++j) {
-          const float f = __shfl_sync(0xFFFFFFFFu, w, (y + j) % C4, C4);       // (past the last: v is 0)
-          o.x = fmaf(v[j].x, f, o.x); o.y = fmaf(v[j].y, f, o.y); o.z = fmaf(v[j].z, f, o.z); o.w = fmaf(v[j].w, f, o.w);
-        }
+      for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+      const bool nan = top >= 0x7F80u;
+      const int e = nan ? 0 : max((int)(top >> 7) - 127, -100) - 7;            // the largest element to [2^7, 2^8)
+      const float up = nan ? 0.f : pow2(-e);
+      uint32_t w0[2], w1[2];
+      split4(kvq::bf_lo(v[k].x) * up, kvq::bf_hi(v[k].x) * up, kvq::bf_lo(v[k].y) * up, kvq::bf_hi(v[k].y) * up, w0[0], w1[0]);
+      split4(kvq::bf_lo(v[k].z) * up, kvq::bf_hi(v[k].z) * up, kvq::bf_lo(v[k].w) * up, kvq::bf_hi(v[k].w) * up, w0[1], w1[1]);
+      if (r < S::RT) {
+        unsigned char* to = sm + S::Q_OFF + r * S::Q_PITCH + (8 * x ^ (DH == 128 ? (r & 1) * 64 : 0));
+        *reinterpret_cast<uint2*>(to) = nan ? make_uint2(0, 0) : make_uint2(w0[0], w0[1]);
+        *reinterpret_cast<uint2*>(to + S::RT * S::Q_PITCH) = nan ? make_uint2(0, 0) : make_uint2(w1[0], w1[1]);
+        if (x == 0) reinterpret_cast<float*>(sm + S::QF_OFF)[r] = nan ? __int_as_float(0x7FFFFFFF) : p.c * pow2(e);
       }
     }
-    if (idx + tid % 32 < n) {
-      const int i = (r0 + r) >> p.gsh, hq = (h << p.gsh) + ((r0 + r) & (p.G - 1));
-      const float rd = den > 0.f ? 1.f / den : 0.f;  // a row without keys: zeros
-      const __nv_bfloat162 x = __floats2bfloat162_rn(o.x * rd, o.y * rd), y = __floats2bfloat162_rn(o.z * rd, o.w * rd);
-      __nv_bfloat16* dst = p.out + (((int64_t)b * p.n_q + i) * p.H_q + hq) * DH + 4 * c4;
-      *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-      if (c4 == 0 && p.lse) p.lse[((int64_t)b * p.H_q + hq) * p.n_q + i] = (M + log2f(den)) * 0.6931471805599453f;
-    }
   }
-}
+};
 
-template <int DH, int REP>
-__global__ void __launch_bounds__(THREADS, CTAS) kvb_attn_kernel(const __grid_constant__ Params p, int max_batch) {
+template <int DH, int NT>
+__global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(const __grid_constant__ Params p, int max_batch) {
   using F = Fmt<DH>;
-  using S = Smem<DH>;
-  constexpr int STAGES = S::STAGES, RT = TILE / REP, NC = 4 / REP;             // rows of an item, chunks of a copy of them
-  extern __shared__ __align__(1024) unsigned char sm[];
-  const uint32_t base = smem_u32(sm), bar0 = base + S::BAR_OFF;
-  auto BAR = [&](int i) { return bar0 + 8u * i; };
-  // GO: the softmax warps have come to a page, and what they bring for its products is there; SDONE: its scores are (or it has
-  // none).  Both sides pass each page through these two, products or not: neither gets a phase ahead of the other.
-  constexpr int FULLK = 0, FULLV = STAGES, GO = 2 * STAGES, SDONE = GO + 1, PREADY = GO + 2, ODONE = GO + 3;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::MISC_OFF);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF + 4);
-  volatile int* last_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF + 8);
+  using S = Smem<DH, NT>;
+  constexpr int STAGES = S::STAGES, RT = S::RT, SHARE_COST = S::SHARE_COST;
+  extern __shared__ __align__(128) unsigned char sm[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & 3, n8 = lane >> 2;
+  const uint32_t base = smem_u32(sm);
+  const uint32_t ring = base + warp * S::RING, bar = base + S::BAR_OFF + warp * STAGES * 8;
+  float2* ml = reinterpret_cast<float2*>(sm + S::ML_OFF);
+  const float* qf = reinterpret_cast<const float*>(sm + S::QF_OFF);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF);
+  int* last_flag = reinterpret_cast<int*>(sm + S::MISC_OFF + 4);
   uint32_t* prefix = reinterpret_cast<uint32_t*>(sm + S::TABLE_OFF);
   int* seq_len = reinterpret_cast<int*>(prefix + max_batch + 1);
-  volatile int* bad = reinterpret_cast<volatile int*>(sm + S::BAD_OFF);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
 
-  if (tid == 0) {
-    *abort_flag = 0;
-    for (int s = 0; s < 2 * STAGES; ++s) mbar_init(BAR(s), 1);
-    mbar_init(BAR(GO), 4); mbar_init(BAR(SDONE), 1); mbar_init(BAR(PREADY), 4); mbar_init(BAR(ODONE), 1);
+  pdl_launch_dependents();
+  if (threadIdx.x == 0) *abort_flag = 0;
+  if (lane == 0) {
+    for (int s = 0; s < STAGES; ++s) mbar_init(bar + 8 * s, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    fence_async();
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (tid < SPACE_MAX_ROWS) reinterpret_cast<uint64_t*>(sm + S::MASK_OFF)[tid] = p.mask[tid];
-  // Tensor memory is taken when the kernel before has given its own back, and the next kernel's blocks may come when all of these
-  // have theirs: nobody holds some while it waits for somebody who wants some.
   pdl_wait();
-  if (warp == 4) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(256u) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
+  // Lengths, and the list's running sums: a (sequence, kv head, row block) has a page per 128 keys, one more where the
+  // block's own rows are given, at least one (rows without any key still get their zeros), and SHARE_COST ahead.
+  auto pages_of = [&](int L) { return max((L + SPACE_PAGE_SIZE - 1) / SPACE_PAGE_SIZE + p.has_new, 1); };
   if (warp == 0) {
-    uint32_t carry = 0;                              // running sums of the list
+    uint32_t carry = 0;
     for (int b0 = 0; b0 < p.B; b0 += 32) {
       const int b = b0 + lane;
       int L = -1;
       uint32_t n = 0;
       if (b < p.B) {
         L = p.kv_len[b];
-        if (L < 0 || (int64_t)L > (int64_t)p.cache.pages_per_seq * TILE) {
+        if (L < 0 || (int64_t)L > (int64_t)p.cache.pages_per_seq * SPACE_PAGE_SIZE) {
           if (blockIdx.x == 0 && p.status) atomicOr(p.status + b, SPACE_ST_CAPACITY);
           L = -1;
         }
-        n = (uint32_t)((max((max(L, 0) + TILE - 1) / TILE + p.has_new, 1) + SHARE_COST) * p.H_kv * p.n_rt);
+        n = (uint32_t)((pages_of(max(L, 0)) + SHARE_COST) * p.H_kv * p.n_rt);
       }
       uint32_t incl = n;
 #pragma unroll
@@ -296,555 +216,422 @@ __global__ void __launch_bounds__(THREADS, CTAS) kvb_attn_kernel(const __grid_co
     }
     if (lane == 0) prefix[p.B] = carry;
   }
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
-  pdl_launch_dependents();
-  const uint32_t tmem = *tmem_slot;
-  const uint32_t TM_S = tmem, TM_O = tmem + TILE;    // S (its columns are the weights' afterwards), O
   const Cut cut(prefix[p.B], p.n_groups);
-  Walk wk;
-  const bool mine = blockIdx.x < cut.NG;
-  const uint32_t share0 = mine ? cut.begin(blockIdx.x) : 0;
-  wk.b = 0; wk.cur = share0;
-  wk.end = mine ? cut.begin(blockIdx.x + 1) : 0;
-  uint32_t g = 0, m = 0;                             // pages, and pages with products, so far
-  auto hold = [&](int bar, uint32_t use, int site) { return wait(BAR(bar), use & 1, abort_flag, p.err, site); };
+  if (blockIdx.x >= cut.NG) return;
+  uint32_t cur = cut.begin(blockIdx.x);
+  const uint32_t share0 = cur, end = cut.begin(blockIdx.x + 1);
 
-  if (warp >= 4) {
-    regs_dec<48>();
-    if (warp == 4 && elect_one()) {
-      // ---- pages ahead: K, scales and V of page `fetched`, K as soon as a stage's K has been used, V when its V has been
-      Walk pw = wk;
-      uint32_t fetched = 0;
-      volatile uint64_t* src_ring = reinterpret_cast<volatile uint64_t*>(sm + S::SRC_OFF);
-      bool live = pw.next(prefix, seq_len, p.has_new, share0);
-      int t = live ? pw.t0 : 0;
-      auto page_of = [&]() { return live && t < pw.cached() ? __ldg(p.cache.page_table + (int64_t)pw.b * p.cache.pages_per_seq + t) : -1; };
-      int pg = page_of();                            // (one page ahead of its use)
-      auto fetch_k = [&]() {
-        if (!live) return;
-        const uint32_t s = fetched % STAGES, e = fetched % RING;
-        const bool cached = t < pw.cached(), good = cached && pg >= 0 && pg < p.cache.n_pages;
-        bad[e] = !good;
-        uint64_t src = 0;
-        if (good) {
-          const char* head = p.cache.pool + (int64_t)pg * p.cache.page_stride + (int64_t)(pw.it / p.n_rt) * p.cache.head_stride;
-          src = (uint64_t)head;
-          mbar_expect_tx(BAR(FULLK + s), F::CODES + 32);
-          bulk_copy(base + S::K_OFF + s * F::CODES, head, F::CODES, BAR(FULLK + s));
-          bulk_copy(base + S::SCALE_OFF + e * 32, head + F::SCALES, 32, BAR(FULLK + s));
-        } else {
-          if (cached && p.status) atomicOr(p.status + pw.b, SPACE_ST_BAD_PAGE);
-          mbar_arrive(BAR(FULLK + s));
-        }
-        src_ring[e] = src;
-        ++fetched;
-        if (++t == pw.t1) {
-          live = pw.next(prefix, seq_len, p.has_new, share0);
-          t = pw.t0;
-        }
-        pg = page_of();
-      };
-      auto fetch_v = [&](uint32_t j) {
-        if (j >= fetched) return;
-        const uint32_t s = j % STAGES;
-        const char* head = reinterpret_cast<const char*>(src_ring[j % RING]);
-        if (head) {
-          mbar_expect_tx(BAR(FULLV + s), F::CODES);
-          bulk_copy(base + S::V_OFF + s * F::CODES, head + F::CODES, F::CODES, BAR(FULLV + s));
-        } else {
-          mbar_arrive(BAR(FULLV + s));
-        }
-      };
-      for (uint32_t j = 0; j < STAGES; ++j) { fetch_k(); fetch_v(j); }
-      const uint64_t q0 = plain_desc(base, 16 * TILE, 128);
-      bool ok = true;
-      while (wk.next(prefix, seq_len, p.has_new, share0)) {
-        const int Tc = wk.cached();
-        for (int tt = wk.t0; tt < wk.t1; ++tt, ++g) {
-          const uint32_t s = g % STAGES;
-          ok = hold(FULLK + s, g / STAGES, 2) && ok;
-          const bool own = tt >= Tc;
-          const bool products = own ? p.has_new && wk.L >= 0 : !bad[g % RING];
-          ok = hold(GO, g, 1) && ok;
-          if (products && ok) {
-            tc_fence_after();
-            const uint64_t kd = plain_desc(base + S::K_OFF + s * F::CODES, 16 * TILE, 128);
+  uint32_t step = 0;                                 // blocks of the ring used so far, by this warp
+  Acc<DH, NT> acc;
+  int b = 0;
+  while (cur < end) {
+    while (prefix[b + 1] <= cur) ++b;
+    const int L0 = seq_len[b], L = max(L0, 0);
+    const int T = pages_of(L), Tv = T + SHARE_COST;
+    const uint32_t rem = cur - prefix[b];
+    const int it = (int)(rem / (uint32_t)Tv), x0 = (int)rem - it * Tv;        // item h * n_rt + row block
+    const int h = it / p.n_rt, rt = it - h * p.n_rt;
+    const int n_list = min(Tv - x0, (int)(end - cur));
+    const uint32_t item_at = cur - x0;               // the item's place in the list
+    const bool opens = cur == share0;
+    cur += n_list;
+    const int t0 = max(x0 - SHARE_COST, 0), t1 = x0 + n_list - SHARE_COST;
+    if (t1 <= t0) continue;                          // only the cost of starting: no pages here
+    const int r0 = rt * RT;
+    const int rows = min(RT, p.n_q * p.G - r0);
+    const int Tc = (L + SPACE_PAGE_SIZE - 1) / SPACE_PAGE_SIZE;        // pages of the cache; page Tc is the block's rows
+    const int c1 = min(t1, Tc);
+
+    // this warp's blocks: rows [32 warp, +32) of pages t0 .. c1-1; a sequence's last page may leave it none
+    int n_blk = *abort_flag ? 0 : max(c1 - t0, 0);   // (after a wait that ran out: no more requests, but every item is counted)
+    if (*abort_flag && p.status && threadIdx.x == 0) atomicOr(p.status + b, SPACE_ST_TIMEOUT);
+    if (n_blk > 0 && L - (c1 - 1) * SPACE_PAGE_SIZE <= warp * BLOCK_ROWS) --n_blk;
+    const int32_t* table = p.cache.page_table + (int64_t)b * p.cache.pages_per_seq;
+    // A block's pieces, one a lane: sixteens of K channels, sixteens of V rows, the scales of two blocks.
+    const char* piece = p.cache.pool + (int64_t)h * p.cache.head_stride;
+    uint32_t piece_at = 0, piece_bytes = 0;
+    if (lane < DH / 16) {
+      piece += lane * F::K_COLS + warp * (16 * BLOCK_ROWS);
+      piece_at = lane * S::K_PITCH; piece_bytes = 16 * BLOCK_ROWS;
+    } else if (lane < DH / 16 + 2) {
+      piece += F::CODES + (2 * warp + lane - DH / 16) * F::V_ROWS;
+      piece_at = S::V_AT + (lane - DH / 16) * S::V_PITCH; piece_bytes = F::V_ROWS;
+    } else if (lane == DH / 16 + 2) {
+      piece += F::SCALES + (warp >> 1) * 16;
+      piece_at = S::SCALE_AT; piece_bytes = 16;
+    }
+    int pages = 0, pages0 = -32;                     // lane j: page of tile t0 + pages0 + j
+    uint32_t good = 0;                               // bit j: that page is in the pool
+    auto look = [&](int j) {                         // pages of the 32 tiles that tile j is among (converged warp)
+      if (j - pages0 < 32) return;
+      pages0 = j;
+      const int at = t0 + j + lane;
+      pages = (j + lane < n_blk && at < p.cache.pages_per_seq) ? table[at] : -1;
+      const bool ok = pages >= 0 && pages < p.cache.n_pages;
+      good = __ballot_sync(0xFFFFFFFFu, ok);
+      if (!ok && j + lane < n_blk && p.status) atomicOr(p.status + b, SPACE_ST_BAD_PAGE);
+    };
+    // (requests run STAGES - 1 blocks ahead of the products, so they look pages up first; whether the page was good
+    // travels with the request as a bit per stage)
+    uint32_t staged = 0;
+    auto request = [&](int j, uint32_t at) {
+      if (j >= n_blk) return;
+      look(j);
+      const int pg = __shfl_sync(0xFFFFFFFFu, pages, j - pages0);
+      const uint32_t s = at % STAGES;
+      const bool ok = (good >> (j - pages0)) & 1u;
+      staged = (staged & ~(1u << s)) | (uint32_t)ok << s;
+      if (ok) {
+        if (lane == 0) mbar_expect_tx(bar + 8 * s, 2 * BLOCK_ROWS * DH + 16);
+        __syncwarp();
+        if (piece_bytes)
+          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                       ::"r"(ring + s * S::BLOCK + piece_at), "l"(piece + (int64_t)pg * p.cache.page_stride), "r"(piece_bytes), "r"(bar + 8 * s) : "memory");
+      } else if (lane == 0) {
+        mbar_arrive(bar + 8 * s);
+      }
+    };
+    Query<DH, NT> query;
+    query.fetch(p, b, h, r0);                        // (ahead of the requests, which wait for the page table)
+#pragma unroll 1
+    for (int j = 0; j < STAGES - 1; ++j) request(j, step + j);
+    query.store(p, sm);
+    __syncthreads();
+    float f[NT][2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+    for (int nt = 0; nt < NT; ++nt) {
+      const float2 v = *reinterpret_cast<const float2*>(qf + 8 * nt + 2 * t);
+      f[nt][0] = v.x; f[nt][1] = v.y;                // (NaN: fmaxf below takes the other one; the row is made NaN at the end)
+    }
+    acc.clear();
+    const uint32_t qs = base + S::Q_OFF + n8 * S::Q_PITCH + 16 * t, swap = DH == 128 ? (n8 & 1) * 64 : 0;          // row n8 of every eight
+    for (int j = 0; j < n_blk; ++j, ++step) {
+      request(j + STAGES - 1, step + STAGES - 1);
+      const uint32_t s = step % STAGES, parity = (step / STAGES) & 1;
+      if (!wait(bar + 8 * s, parity, abort_flag, p.err, 40 + warp)) {
+        if (p.status && lane == 0) atomicOr(p.status + b, SPACE_ST_TIMEOUT);
+        // what is on its way has to land before the ring is used for anything else
+        const uint32_t issued = step + min(STAGES, n_blk - j);
+        for (; step < issued; ++step) mbar_drain_bounded(bar + 8 * (step % STAGES), (step / STAGES) & 1, WAIT_NS);
+        break;
+      }
+      if (!((staged >> s) & 1u)) continue;           // a page outside the pool: its keys are left out
+      const uint32_t blk = ring + s * S::BLOCK;
+      const int valid = min(L - (t0 + j) * SPACE_PAGE_SIZE - warp * BLOCK_ROWS, BLOCK_ROWS);   // keys of this block, >= 1
+
+      // ---- S^T = K Q^T: rows n8 and n8 + 8 of product u are keys 4 n8 + 2u and + 1; a k-step has of each lane's sixteen channels
+      // 64 cg + 16 t .. eight
+      float sc[2][NT][4];
 #pragma unroll
-              for (int ks = 0; ks < DH / 32; ++ks)
-                mma8_ss(TM_S, q0 + (uint64_t)((i * S::Q_PIECE + ks * 32 * TILE) >> 4), kd + (uint64_t)((ks * 32 * TILE) >> 4), instr_desc(TILE), i + ks > 0);
-          }
-          if (products) tc_commit(BAR(SDONE));
-          else mbar_arrive(BAR(SDONE));
-          ok = hold(SDONE, g, 3) && ok;
-          fetch_k();
-          ok = hold(FULLV + s, g / STAGES, 5) && ok;
-          if (products) {
-            ok = hold(PREADY, m, 6) && ok;
-            if (ok) {
-              tc_fence_after();
-              const uint64_t vd = plain_desc(base + S::V_OFF + s * F::CODES, F::V_ROWS, 128);
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int b = 0; b < 4; ++b)
+        for (int nt = 0; nt < NT; ++nt) sc[u][nt][0] = sc[u][nt][1] = sc[u][nt][2] = sc[u][nt][3] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                  mma8_ts(TM_O, TM_S + 16 * b + 8 * i, vd + (uint64_t)((2 * b * F::V_ROWS) >> 4), instr_desc(DH), b + i > 0);
+      for (int cg = 0; cg < DH / 64; ++cg) {
+        uint4 k[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[i] = lds128(blk + (4 * cg + t) * S::K_PITCH + (4 * n8 + i) * 16);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int term = 0; term < 2; ++term) {
+            const uint4 q = lds128(qs + (term * RT + 8 * nt) * S::Q_PITCH + (64 * cg ^ swap));
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              mma8(sc[u][nt], k[2 * u].x, k[2 * u + 1].x, k[2 * u].y, k[2 * u + 1].y, q.x, q.y);
+              mma8(sc[u][nt], k[2 * u].z, k[2 * u + 1].z, k[2 * u].w, k[2 * u + 1].w, q.z, q.w);
             }
-            tc_commit(BAR(ODONE));
-            ok = hold(ODONE, m, 7) && ok;
-            ++m;
           }
-          fetch_v(g + STAGES);
+      }
+      const uint2 scales = lds64(blk + S::SCALE_AT + (warp & 1) * 8);
+      const float ks = __uint_as_float(scales.x), ev = (float)((int)((scales.y >> 23) & 255u) - 127);
+      // ---- weights: lane has of columns 2t, 2t + 1 the keys 4 n8 .. + 3
+      uint32_t b0[NT][2], b1[NT][2];                 // second operands of both terms
+      float2 beta[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float x[2][4], r[2], sum[2];
+        uint32_t w[2][2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[c][i] = sc[i >> 1][nt][2 * (i & 1) + c];
+          if (valid < BLOCK_ROWS) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (4 * n8 + i >= valid) x[c][i] = -CUDART_INF_F;
+          }
+          const float ms = col_max(fmaxf(fmaxf(x[c][0], x[c][1]), fmaxf(x[c][2], x[c][3])));       // (a number: the block has a key)
+          float fk = fminf(fmaxf(f[nt][c] * ks, F_MIN), F_MAX);
+          float mb = ms * fk;
+          r[c] = mb - 8.f;
+          if (__any_sync(0xFFFFFFFFu, fabsf(mb) > REF_FAR)) {                  // scores off the largest first, then times the factor
+            if (fabsf(mb) > SCORE_MAX) {
+              fk = SCORE_MAX / fabsf(ms);
+              r[c] = copysignf(SCORE_MAX, ms);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[c][i] = fast_exp2(fmaf(x[c][i] - ms, fk, 8.f));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[c][i] = fast_exp2(fmaf(x[c][i], fk, -r[c]));
+          }
+          sum[c] = (x[c][0] + x[c][1]) + (x[c][2] + x[c][3]);
+          split4(x[c][0], x[c][1], x[c][2], x[c][3], w[0][c], w[1][c]);
+        }
+        transpose_words(w[0][0], w[0][1], b0[nt][0], b1[nt][0]);
+        transpose_words(w[1][0], w[1][1], b0[nt][1], b1[nt][1]);
+        beta[nt] = acc.join(nt, r, sum, ev);
+      }
+      // ---- D^T = V^T W^T: the lane's keys of a channel are 8 t .. + 7
+      const uint32_t vat = blk + S::V_AT + (t >> 1) * S::V_PITCH + n8 * 16 + 8 * (t & 1);
+      uint32_t keep0 = 0xFFFFFFFFu, keep1 = 0xFFFFFFFFu;
+      if (valid < BLOCK_ROWS) {                      // what lies behind the last row must not count, whatever it is
+        const int a = min(max(valid - 8 * t, 0), 4), c = min(max(valid - 8 * t - 4, 0), 4);
+        keep0 = a == 4 ? 0xFFFFFFFFu : (1u << (8 * a)) - 1u;
+        keep1 = c == 4 ? 0xFFFFFFFFu : (1u << (8 * c)) - 1u;
+      }
+#pragma unroll
+      for (int ct = 0; ct < DH / 16; ++ct) {
+        uint2 x = lds64(vat + ct * 256), y = lds64(vat + ct * 256 + 128);
+        x.x &= keep0; x.y &= keep1; y.x &= keep0; y.y &= keep1;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float d[4] = {0.f, 0.f, 0.f, 0.f};
+          mma8(d, x.x, y.x, x.y, y.y, b0[nt][0], b1[nt][0]);
+          mma8(d, x.x, y.x, x.y, y.y, b0[nt][1], b1[nt][1]);
+          acc.o[ct][nt][0] = fmaf(d[0], beta[nt].x, acc.o[ct][nt][0]); acc.o[ct][nt][1] = fmaf(d[1], beta[nt].y, acc.o[ct][nt][1]);
+          acc.o[ct][nt][2] = fmaf(d[2], beta[nt].x, acc.o[ct][nt][2]); acc.o[ct][nt][3] = fmaf(d[3], beta[nt].y, acc.o[ct][nt][3]);
         }
       }
-      // (every copy was waited for above; after a wait that ran out, here)
-      if (*abort_flag)
-        for (uint32_t j = fetched > STAGES ? fetched - STAGES : 0; j < fetched; ++j) {
-          mbar_drain_bounded(BAR(FULLK + j % STAGES), (j / STAGES) & 1, WAIT_NS);
-          mbar_drain_bounded(BAR(FULLV + j % STAGES), (j / STAGES) & 1, WAIT_NS);
-        }
+      __syncwarp();                                  // everybody has read the stage: the next request may fill it
     }
-  } else {
-    regs_inc<208>();                                 // (128 threads x 208 + 128 x 48 = the 256 x 128 of the launch)
-    const int rep = warp / (4 / REP), row = tid % RT;
-    const uint32_t lanes = (uint32_t)(32 * warp) << 16;
-    float2* ml = reinterpret_cast<float2*>(sm + S::ML_OFF);
-    float2* own = reinterpret_cast<float2*>(sm + S::OWN_OFF);
-    while (wk.next(prefix, seq_len, p.has_new, share0)) {
-      const int h = wk.it / p.n_rt, r0 = (wk.it - h * p.n_rt) * RT, rows = min(p.n_q * p.G - r0, RT), Tc = wk.cached();
-      const int qi = (r0 + row) >> p.gsh, hq = (h << p.gsh) + ((r0 + row) & (p.G - 1));
-      const bool there = row < rows;
-      // ---- the query row, as two terms
-      float f;                                       // factor of a score
-      bool nan = false;
-      {
-        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)wk.b * p.q_sb + (int64_t)qi * p.q_sr + (int64_t)hq * p.q_sh);
-        uint4 v[DH / 8];
+
+    // ---- the block's own rows: keys 16 warp .. + 15 of it, products in bf16 as they are (no code, no scale), weights as two
+    // bf16 terms, 2^-32 as large: sums of rows next to the largest number stay numbers
+    if (t1 > Tc && p.has_new && 16 * warp < p.n_q && L0 >= 0) {
+      const int k0 = 16 * warp;
+      constexpr int LANES = DH / 8, V_LOADS = 16 * LANES / 32;
+      uint4 kr[2][DH / 32], vr[V_LOADS], qr[NT][DH / 32];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        int i, hq;
+        row_of(p, h, r0 + 8 * nt + n8, i, hq);
+        const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh) + t * (DH / 32);
+#pragma unroll
+        for (int j = 0; j < DH / 32; ++j) qr[nt][j] = i < p.n_q ? src[j] : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int key = k0 + 8 * i + n8;
+        const uint4* src = reinterpret_cast<const uint4*>(p.kn + (int64_t)b * p.n_sb + (int64_t)key * p.n_sr + (int64_t)h * p.n_sh) + t * (DH / 32);
+#pragma unroll
+        for (int j = 0; j < DH / 32; ++j) kr[i][j] = key < p.n_q ? src[j] : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < V_LOADS; ++i) {
+        const int key = k0 + i * (32 / LANES) + lane / LANES;
+        vr[i] = make_uint4(0, 0, 0, 0);
+        if (key < p.n_q) vr[i] = *(reinterpret_cast<const uint4*>(p.vn + (int64_t)b * p.n_sb + (int64_t)key * p.n_sr + (int64_t)h * p.n_sh) + lane % LANES);
+      }
+      float sc[NT][4], kf[2] = {p.c, p.c};
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
         uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < DH / 8; ++j) v[j] = there ? src[j] : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < DH / 32; ++j) top = max(top, kvq::max_bits(kr[i][j]));
+        if (__any_sync(0xFFFFFFFFu, top >= 0x7200u)) { // (from 2^101 on: what is not finite, and sums that fp32 would not hold)
+          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
 #pragma unroll
-        for (int j = 0; j < DH / 8; ++j) top = max(top, kvq::max_bits(v[j]));
-        nan = top >= 0x7F80u;
-        const int e = nan ? 0 : max((int)(top >> 7) - 127, -100) - 7;          // the largest element to [2^7, 2^8)
-        const float up = pow2(-e);
-        f = p.c * pow2(e);
-#pragma unroll
-        for (int j = 0; j < DH / 16; ++j) {
-          uint32_t w0[4], w1[4];
-          const uint32_t x[8] = {v[2 * j].x, v[2 * j].y, v[2 * j].z, v[2 * j].w, v[2 * j + 1].x, v[2 * j + 1].y, v[2 * j + 1].z, v[2 * j + 1].w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            split4(kvq::bf_lo(x[2 * k]) * up, kvq::bf_hi(x[2 * k]) * up, kvq::bf_lo(x[2 * k + 1]) * up, kvq::bf_hi(x[2 * k + 1]) * up, w0[k], w1[k]);
-          const uint32_t to = base + j * (16 * TILE) + 16 * tid;
-          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(w0[0]), "r"(w0[1]), "r"(w0[2]), "r"(w0[3]) : "memory");
-          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to + S::Q_PIECE), "r"(w1[0]), "r"(w1[1]), "r"(w1[2]), "r"(w1[3]) : "memory");
+          for (int j = 0; j < DH / 32; ++j) {
+            kvq::make_finite(kr[i][j]);
+            if (top >= 0x7200u) kr[i][j] = kvq::scale_bf16(kr[i][j], 0x1p-64f);
+          }
+          if (top >= 0x7200u) kf[i] = p.c * 0x1p64f;
         }
-        fence_async();
       }
-      uint64_t o2[DH / 2];
 #pragma unroll
-      for (int j = 0; j < DH / 2; ++j) o2[j] = 0ull;
-      float M = -CUDART_INF_F, l = 0.f, R = 0.f, alpha = 1.f, beta = 0.f;
-      bool pending = false;
-      // the last page's result joins the sum
-      auto take = [&]() {
-        hold(ODONE, m - 1, 8);
-        tc_fence_after();
-        if (__any_sync(0xFFFFFFFFu, alpha != 1.f)) {
-          const uint64_t a2 = pack2(alpha, alpha);
+      for (int k = 0; k < DH / 32; ++k) {
 #pragma unroll
-          for (int j = 0; j < DH / 2; ++j) o2[j] = mul2(o2[j], a2);
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint4 q = qr[nt][k];
+          mma_bf16(sc[nt], kr[0][k].x, kr[1][k].x, kr[0][k].y, kr[1][k].y, q.x, q.y);
+          mma_bf16(sc[nt], kr[0][k].z, kr[1][k].z, kr[0][k].w, kr[1][k].w, q.z, q.w);
         }
-        const uint64_t b2 = pack2(beta, beta);
-#pragma unroll
-        for (int c = 0; c < DH; c += 32) {
-          uint32_t v[32];
-          tmem_ld32(TM_O + lanes + c, v);
-          tmem_wait_ld();
-#pragma unroll
-          for (int j = 0; j < 16; ++j) o2[c / 2 + j] = fma2(pack2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), b2, o2[c / 2 + j]);
-        }
-        tc_fence_before();
-        pending = false;
-      };
-      // a page's maximum pm, and E: the running ones, and the factors of the sums
-      auto advance = [&](float pm, float E, float& lead) {
-        lead = 0.f; alpha = 1.f; beta = 0.f;
-        if (pm == -CUDART_INF_F) return;             // this row sees nothing of the page
-        const float Mn = fmaxf(M, pm), d_old = M - Mn;
-        lead = fast_exp2(pm - Mn);
-        l *= fast_exp2(d_old);
-        const float r_old = R + d_old, r_new = E + (pm - Mn), Rn = fmaxf(r_old, r_new);
-        alpha = fast_exp2(r_old - Rn);
-        beta = fast_exp2(r_new - Rn - 8.f);
-        M = Mn; R = Rn;
-      };
-      for (int t = wk.t0; t < wk.t1; ++t, ++g) {
-        const uint32_t s = g % STAGES;
-        const bool is_own = t >= Tc;
-        hold(FULLK + s, g / STAGES, 9);
-        const bool products = is_own ? p.has_new && wk.L >= 0 : !bad[g % RING];
-        if (!is_own || !products) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(BAR(GO));
-        }
-        if (!products) {
-          hold(SDONE, g, 13);
-          continue;
-        }
-        if (pending) take();
-        if (!is_own) {
-          const float2* sc = reinterpret_cast<const float2*>(sm + S::SCALE_OFF + (g % RING) * 32);
-          const int vis0 = wk.L - t * TILE;          // visible keys of the page
-          if (vis0 < TILE) {                         // what lies behind the last row must not count, whatever it is
-            hold(FULLV + s, g / STAGES, 10);
-            const int g0 = vis0 >> 4;
-            for (int e = tid; e < (8 - g0) * DH; e += SOFT) {
-              const int grp = g0 + e / DH, keep = min(max(vis0 - 16 * grp, 0), 16);
-              unsigned char* at = sm + S::V_OFF + s * F::CODES + grp * F::V_ROWS + (e % DH) * 16;
-              uint4 w = make_uint4(0, 0, 0, 0);
-              if (keep) {
-                w = *reinterpret_cast<const uint4*>(at);
-                uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  const int n = min(max(keep - 4 * j, 0), 4);
-                  x[j] &= n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
-                }
-                w = make_uint4(x[0], x[1], x[2], x[3]);
-              }
-              *reinterpret_cast<uint4*>(at) = w;
-            }
-            fence_async();
-          }
-          hold(SDONE, g, 11);
-          tc_fence_after();
-          // ---- largest scores
-          float fk[NC], mb[NC];
-          uint32_t v[32];
-          float pm = -CUDART_INF_F;
-#pragma unroll
-          for (int k = 0; k < NC; ++k) {
-            const int cb = rep * NC + k, vis = vis0 - BLOCK_ROWS * cb;
-            mb[k] = -CUDART_INF_F;
-            fk[k] = fminf(fmaxf(f * sc[cb].x, F_MIN), F_MAX);
-            if (vis > 0) {
-              tmem_ld32(TM_S + lanes + 32 * cb, v);
-              tmem_wait_ld();
-              if (vis < BLOCK_ROWS) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) if (j >= vis) v[j] = 0xFF800000u;
-              }
-              mb[k] = max32(v) * fk[k];
-            }
-            pm = fmaxf(pm, mb[k]);
-          }
-          float x[NC], E = -CUDART_INF_F;
-#pragma unroll
-          for (int k = 0; k < NC; ++k) {
-            const int ev = (int)((__float_as_uint(sc[rep * NC + k].y) >> 23) & 255u) - 127;
-            x[k] = mb[k] == -CUDART_INF_F ? -CUDART_INF_F : (mb[k] - pm) + (float)ev;
-            E = fmaxf(E, x[k]);
-          }
-          float lead;
-          advance(pm, E, lead);
-          // ---- weights
-#pragma unroll
-          for (int k = 0; k < NC; ++k) {
-            const int cb = rep * NC + k, vis = vis0 - BLOCK_ROWS * cb;
-            uint32_t w[16];
-            if (vis > 0) {
-              if (NC > 1) {
-                tmem_ld32(TM_S + lanes + 32 * cb, v);
-                tmem_wait_ld();
-                if (vis < BLOCK_ROWS) {
-#pragma unroll
-                  for (int j = 0; j < 32; ++j) if (j >= vis) v[j] = 0xFF800000u;
-                }
-              }
-              float nb = mb[k] == -CUDART_INF_F ? 0.f : -mb[k];
-              if (__any_sync(0xFFFFFFFFu, fabsf(nb) > REF_EXACT)) {            // scores off the largest first, then times the factor
-                const float top = max32(v);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) - (nb == 0.f ? 0.f : top));
-                nb = 0.f;
-              }
-              const float wf = mb[k] == -CUDART_INF_F ? 0.f : fast_exp2(x[k] - E + 8.f);
-              const uint64_t f2 = pack2(fk[k], fk[k]), n2 = pack2(nb, nb), w2 = pack2(wf, wf);
-              uint64_t sum0 = 0ull, sum1 = 0ull;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                float a, b, c, d;
-                unpack2(fma2(pack2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), f2, n2), a, b);
-                unpack2(fma2(pack2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), f2, n2), c, d);
-                const uint64_t e0 = pack2(fast_exp2(a), fast_exp2(b)), e1 = pack2(fast_exp2(c), fast_exp2(d));
-                sum0 = add2(sum0, e0); sum1 = add2(sum1, e1);
-                unpack2(mul2(e0, w2), a, b);
-                unpack2(mul2(e1, w2), c, d);
-                split4(a, b, c, d, w[j], w[8 + j]);
-              }
-              float a, b;
-              unpack2(add2(sum0, sum1), a, b);
-              if (mb[k] != -CUDART_INF_F) l = fmaf(a + b, lead * fast_exp2(mb[k] - pm), l);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 16; ++j) w[j] = 0;
-            }
-            tmem_st16(TM_S + lanes + 16 * cb, w);
-          }
-          if (REP > 1) {                             // keys that other copies of the row have
-            const uint32_t zero[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-              if (b / NC != rep) tmem_st16(TM_S + lanes + 16 * b, zero);
-          }
-        } else {
-          // ---- the block's own rows: keys j and 64 + j of the page are the two terms of row j
-          {
-            const int key = tid >> 1, c0 = (tid & 1) * (DH / 2);
-            const bool real = key < p.n_q;
-#pragma unroll 1
-            for (int which = 0; which < 2; ++which) {
-              const uint4* src = reinterpret_cast<const uint4*>((which ? p.vn : p.kn) + (int64_t)wk.b * p.n_sb + (int64_t)key * p.n_sr + (int64_t)h * p.n_sh) + c0 / 8;
-              uint4 v[DH / 16];
-              uint32_t top = 0;
-#pragma unroll
-              for (int j = 0; j < DH / 16; ++j) v[j] = real ? src[j] : make_uint4(0, 0, 0, 0);
-#pragma unroll
-              for (int j = 0; j < DH / 16; ++j) top = max(top, kvq::top_bits(v[j]));       // (and what is not finite made so)
-              top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-              const int e = max((int)(top >> 7) - 127, -100) - 7;
-              const float up = pow2(-e);
-              if ((tid & 1) == 0) {
-                if (which) own[key].y = (float)e;
-                else own[key].x = pow2(e);
-              }
-#pragma unroll
-              for (int j = 0; j < DH / 32; ++j) {
-                uint32_t w0[4], w1[4];
-                const uint32_t x[8] = {v[2 * j].x, v[2 * j].y, v[2 * j].z, v[2 * j].w, v[2 * j + 1].x, v[2 * j + 1].y, v[2 * j + 1].z, v[2 * j + 1].w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  split4(kvq::bf_lo(x[2 * k]) * up, kvq::bf_hi(x[2 * k]) * up, kvq::bf_lo(x[2 * k + 1]) * up, kvq::bf_hi(x[2 * k + 1]) * up, w0[k], w1[k]);
-                if (which == 0) {
-                  unsigned char* to = sm + S::K_OFF + s * F::CODES + (c0 / 16 + j) * F::K_COLS + 16 * key;
-                  *reinterpret_cast<uint4*>(to) = make_uint4(w0[0], w0[1], w0[2], w0[3]);
-                  *reinterpret_cast<uint4*>(to + 16 * 64) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
-                } else {
-                  unsigned char* to = sm + S::V_OFF + s * F::CODES + (key >> 4) * F::V_ROWS + (c0 + 16 * j) * 16 + (key & 15);
-#pragma unroll
-                  for (int k = 0; k < 16; ++k) {
-                    to[16 * k] = (unsigned char)(w0[k >> 2] >> (8 * (k & 3)));
-                    to[16 * k + 4 * F::V_ROWS] = (unsigned char)(w1[k >> 2] >> (8 * (k & 3)));
-                  }
-                }
-              }
-            }
-            fence_async();
-            soft_sync();
-            if (lane == 0) mbar_arrive(BAR(GO));
-          }
-          hold(SDONE, g, 12);
-          tc_fence_after();
-          // (the first copy of the rows has them all)
-          const uint64_t see = rep == 0 && there ? reinterpret_cast<const uint64_t*>(sm + S::MASK_OFF)[qi] : 0ull;
-          float pm = -CUDART_INF_F, E = -CUDART_INF_F;
-          auto scores = [&](int j0, float* sc) {     // sixteen of them
-            uint32_t a[16], b[16];
-            tmem_ld16(TM_S + lanes + j0, a);
-            tmem_ld16(TM_S + lanes + 64 + j0, b);
-            tmem_wait_ld();
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const float fj = fminf(fmaxf(f * own[j0 + j].x, F_MIN), F_MAX);
-              sc[j] = (see >> (j0 + j)) & 1ull ? (__uint_as_float(a[j]) + __uint_as_float(b[j])) * fj : -CUDART_INF_F;
-            }
-          };
-          float sc[16];
-          if (rep == 0) {
-#pragma unroll 1
-            for (int j0 = 0; j0 < 64; j0 += 16) {
-              scores(j0, sc);
-#pragma unroll
-              for (int j = 0; j < 16; ++j) pm = fmaxf(pm, sc[j]);
-            }
-#pragma unroll 1
-            for (int j0 = 0; j0 < 64; j0 += 16) {
-              scores(j0, sc);
-#pragma unroll
-              for (int j = 0; j < 16; ++j) E = fmaxf(E, sc[j] == -CUDART_INF_F ? -CUDART_INF_F : (sc[j] - pm) + own[j0 + j].y);
-            }
-          }
-          float lead, sum = 0.f;
-          advance(pm, E, lead);
-#pragma unroll 1
-          for (int j0 = 0; j0 < 64; j0 += 16) {
-            uint32_t w0[4], w1[4];
-            if (rep == 0) {
-              scores(j0, sc);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                float y[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  const float d = sc[4 * j + k] - pm;
-                  const bool vis = sc[4 * j + k] != -CUDART_INF_F;
-                  sum += vis ? fast_exp2(d) : 0.f;
-                  y[k] = vis ? fast_exp2(d + own[j0 + 4 * j + k].y - E + 8.f) : 0.f;
-                }
-                split4(y[0], y[1], y[2], y[3], w0[j], w1[j]);
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) w0[j] = w1[j] = 0;
-            }
-            // words of keys j0 .. of their chunk of 32, in columns whose scores have been read
-            tmem_st4(TM_S + lanes + (j0 >> 5) * 16 + ((j0 >> 4) & 1) * 4, w0);
-            tmem_st4(TM_S + lanes + (j0 >> 5) * 16 + ((j0 >> 4) & 1) * 4 + 8, w1);
-          }
-          l = fmaf(sum, lead, l);
-          tmem_wait_st();
-          {
-            uint32_t w[32];
-            tmem_ld32(TM_S + lanes, w);
-            tmem_wait_ld();
-            tmem_st16(TM_S + lanes + 32, w);
-            tmem_st16(TM_S + lanes + 48, w + 16);
-          }
-        }
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(BAR(PREADY));
-        pending = true;
-        ++m;
       }
-      if (pending) take();
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < V_LOADS; ++i) {            // V rows into the (dry) ring
+        kvq::make_finite(vr[i]);
+        const uint32_t at = ring + (i * (32 / LANES) + lane / LANES) * S::OWN_PITCH + (lane % LANES) * 16;
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(vr[i].x), "r"(vr[i].y), "r"(vr[i].z), "r"(vr[i].w) : "memory");
+      }
+      __syncwarp();
+      uint32_t ph[NT][2], pl[NT][2];
+      float2 beta[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float r[2], sum[2] = {0.f, 0.f}, y[2][2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int row = r0 + 8 * nt + 2 * t + c;
+          const uint64_t see = row < p.n_q * p.G ? p.mask[row >> p.gsh] : 0ull;                    // Eq. 5
+          r[c] = -CUDART_INF_F;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const bool vis = (see >> (k0 + 8 * i + n8)) & 1ull;
+            const float x = sc[nt][2 * i + c] * kf[i];       // (a row that is not finite: NaN here, and at the end)
+            y[c][i] = vis ? (x > SCORE_MAX ? SCORE_MAX : x < -SCORE_MAX ? -SCORE_MAX : x) : -CUDART_INF_F;
+            r[c] = fmaxf(r[c], y[c][i]);
+          }
+          r[c] = col_max(r[c]);
+          const float from = r[c] == -CUDART_INF_F ? 0.f : r[c];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            y[c][i] = fast_exp2(y[c][i] - from);
+            sum[c] += y[c][i];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float w0 = y[0][i] * 0x1p-32f, w1 = y[1][i] * 0x1p-32f;
+          const __nv_bfloat162 hi = __floats2bfloat162_rn(w0, w1);
+          const uint32_t hw = *reinterpret_cast<const uint32_t*>(&hi);
+          float l0, l1;
+          low_terms(hw, w0, w1, l0, l1);
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(l0, l1);
+          ph[nt][i] = transpose8(hw);
+          pl[nt][i] = transpose8(*reinterpret_cast<const uint32_t*>(&lo));
+        }
+        beta[nt] = acc.join(nt, r, sum, 32.f);
+      }
+#pragma unroll
+      for (int ct = 0; ct < DH / 16; ++ct) {
+        uint32_t a0, a1, a2, a3;
+        const uint32_t at = ring + (8 * (lane >> 4) + (lane & 7)) * S::OWN_PITCH + ct * 32 + ((lane >> 3) & 1) * 16;
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3) : "r"(at) : "memory");
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float d[4] = {0.f, 0.f, 0.f, 0.f};
+          mma_bf16(d, a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
+          mma_bf16(d, a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
+          acc.o[ct][nt][0] = fmaf(d[0], beta[nt].x, acc.o[ct][nt][0]); acc.o[ct][nt][1] = fmaf(d[1], beta[nt].y, acc.o[ct][nt][1]);
+          acc.o[ct][nt][2] = fmaf(d[2], beta[nt].x, acc.o[ct][nt][2]); acc.o[ct][nt][3] = fmaf(d[3], beta[nt].y, acc.o[ct][nt][3]);
+        }
+      }
+      __syncwarp();
+    }
 
-      // ---- the item's rows, or its piece of them
-      const bool whole = wk.t0 == 0 && wk.t1 == wk.pages(p.has_new);
-      const int slot = 2 * (int)blockIdx.x + (wk.opens ? 0 : 1);
-      constexpr int SLOT = RT * (DH + 2);
-      float* ps = p.part + (int64_t)slot * SLOT;
-      __nv_bfloat16* dst = p.out + (((int64_t)wk.b * p.n_q + qi) * p.H_q + hq) * DH;
-      const float NAN_F = __int_as_float(0x7FFFFFFF);
-      float Mx = M, Lx = l;
-      if (REP > 1) {
-        ml[tid] = make_float2(M, l);
-        soft_sync();
+    // ---- the four warps' states meet
 #pragma unroll
-        for (int r = 0; r < REP; ++r) Mx = fmaxf(Mx, ml[r * RT + row].x);
-        Lx = 0.f;
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int r = 0; r < REP; ++r) {
-          const float2 v = ml[r * RT + row];
-          Lx += v.x == -CUDART_INF_F ? 0.f : v.y * fast_exp2(v.x - Mx);
-        }
+      for (int e = 0; e < 2; ++e) {
+        const float sum = col_sum(acc.l[nt][e]);
+        if (lane < 4) ml[warp * RT + 8 * nt + 2 * t + e] = make_float2(acc.M[nt][e], sum);
       }
-      float fac = M == -CUDART_INF_F ? 0.f : fast_exp2(M - Mx) / Lx * fast_exp2(R);
-      if (nan && Mx != -CUDART_INF_F) { fac = NAN_F; Lx = NAN_F; }
-      if (REP == 1) {
-        if (there) {
+    __syncthreads();
+    const bool whole = t0 == 0 && t1 == T;
+    auto total = [&](int r, float& M, float& l) {
+      M = -CUDART_INF_F; l = 0.f;
 #pragma unroll
-          for (int c = 0; c < DH; c += 8) {
-            float y[8];
+      for (int w = 0; w < WARPS; ++w) M = fmaxf(M, ml[w * RT + r].x);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              unpack2(o2[c / 2 + j], y[2 * j], y[2 * j + 1]);
-              y[2 * j] *= fac; y[2 * j + 1] *= fac;
-            }
-            if (whole) *reinterpret_cast<uint4*>(dst + c) = pack_row8(y);
-            else {
-              __stcg(reinterpret_cast<float4*>(ps + row * DH + c), make_float4(y[0], y[1], y[2], y[3]));
-              __stcg(reinterpret_cast<float4*>(ps + row * DH + c + 4), make_float4(y[4], y[5], y[6], y[7]));
-            }
+      for (int w = 0; w < WARPS; ++w) {
+        const float2 v = ml[w * RT + r];
+        l += v.x == -CUDART_INF_F ? 0.f : v.y * fast_exp2(v.x - M);
+      }
+    };
+    {
+      float* mine = reinterpret_cast<float*>(sm + warp * S::RING);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int r = 8 * nt + 2 * t + e;
+          float M, l;
+          total(r, M, l);
+          float fac = acc.M[nt][e] == -CUDART_INF_F ? 0.f : fast_exp2(acc.M[nt][e] - M) / l * fast_exp2(acc.R[nt][e]);
+          if (M != -CUDART_INF_F && f[nt][e] != f[nt][e]) fac = __int_as_float(0x7FFFFFFF);
+#pragma unroll
+          for (int ct = 0; ct < DH / 16; ++ct) {
+            mine[r * S::O_PITCH + 16 * ct + n8] = acc.o[ct][nt][e] * fac;
+            mine[r * S::O_PITCH + 16 * ct + 8 + n8] = acc.o[ct][nt][2 + e] * fac;
           }
         }
-      } else {
-        // copies of a row meet, half of the channels at a time, where the query rows were
-        constexpr int CP = DH / 2, CS = CP / REP;
-        float* buf = reinterpret_cast<float*>(sm);   // [CP][128]
+    }
+    __syncthreads();
+    uint32_t piece0 = 0;
+    int pieces = 1;
+    if (!whole) {
+      piece0 = cut.owner(item_at + SHARE_COST);
+      pieces = (int)(cut.owner(item_at + SHARE_COST + T - 1) - piece0) + 1;
+    }
+    const int slot = 2 * (int)blockIdx.x + (opens ? 0 : 1);
+    constexpr int C4 = DH / 4;
+    constexpr int SLOT = RT * (DH + 2);
+    for (int idx = threadIdx.x; idx < rows * C4; idx += THREADS) {
+      const int r = idx / C4, c4 = idx % C4;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll
-          for (int c = 0; c < CP / 2; ++c) {
-            float a, b;
-            unpack2(o2[pass * (CP / 2) + c], a, b);
-            buf[(2 * c) * TILE + tid] = a * fac;
-            buf[(2 * c + 1) * TILE + tid] = b * fac;
-          }
-          soft_sync();
-          if (there) {
-#pragma unroll
-            for (int c = 0; c < CS; c += 8) {
-              float y[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                y[j] = 0.f;
-#pragma unroll
-                for (int r = 0; r < REP; ++r) y[j] += buf[(rep * CS + c + j) * TILE + r * RT + row];
-              }
-              const int ch = pass * CP + rep * CS + c;
-              if (whole) *reinterpret_cast<uint4*>(dst + ch) = pack_row8(y);
-              else {
-                __stcg(reinterpret_cast<float4*>(ps + row * DH + ch), make_float4(y[0], y[1], y[2], y[3]));
-                __stcg(reinterpret_cast<float4*>(ps + row * DH + ch + 4), make_float4(y[4], y[5], y[6], y[7]));
-              }
-            }
-          }
-          soft_sync();
-        }
+      for (int w = 0; w < WARPS; ++w) {
+        const float4 x = *reinterpret_cast<const float4*>(sm + w * S::RING + (r * S::O_PITCH + 4 * c4) * 4);
+        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
       }
-      if (there && rep == 0) {
-        if (!whole) { __stcg(ps + RT * DH + row, Mx); __stcg(ps + RT * DH + RT + row, Lx); }
-        else if (p.lse) p.lse[((int64_t)wk.b * p.H_q + hq) * p.n_q + qi] = (Mx + log2f(Lx)) * 0.6931471805599453f;
-      }
-      if (*abort_flag && p.status && tid == 0) atomicOr(p.status + wk.b, SPACE_ST_TIMEOUT);
-      if (!whole) {
-        const int T = wk.pages(p.has_new);
-        const uint32_t piece0 = cut.owner(wk.at + SHARE_COST);
-        const int pieces = (int)(cut.owner(wk.at + SHARE_COST + T - 1) - piece0) + 1;
-        soft_sync();
-        if (tid == 0) {
-          __threadfence();                           // (after the barrier: for all the stores)
-          int* arrived = p.arrived + (wk.b * p.H_kv * p.n_rt + wk.it);
-          const int last = atomicAdd(arrived, 1) == pieces - 1;
-          if (last) *arrived = 0;                    // ready for the next call
-          __threadfence();
-          *last_flag = last;
+      if (whole) store_row4<DH>(p, b, h, r0 + r, c4, o);
+      else __stcg(reinterpret_cast<float4*>(p.part + (int64_t)slot * SLOT + r * DH) + c4, o);
+      if (c4 == 0) {
+        float M, l;
+        total(r, M, l);
+        if (M != -CUDART_INF_F && qf[r] != qf[r]) l = qf[r];
+        if (whole) {
+          store_lse(p, b, h, r0 + r, M, l);
+        } else {
+          __stcg(p.part + (int64_t)slot * SLOT + RT * DH + r, M);
+          __stcg(p.part + (int64_t)slot * SLOT + RT * DH + RT + r, l);
         }
-        soft_sync();
-        if (*last_flag) join_pieces<DH, RT>(p, cut, wk.b, h, r0, rows, piece0, pieces, wk.at, tid);
-        soft_sync();                                 // the flag is free for the next item
       }
     }
+    if (!whole) {
+      const int item = (b * p.H_kv + h) * p.n_rt + rt;
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        __threadfence();                             // (after the barrier: for the whole block's stores)
+        const int last = atomicAdd(p.arrived + item, 1) == pieces - 1;
+        if (last) p.arrived[item] = 0;               // ready for the next call
+        __threadfence();
+        *last_flag = last;
+      }
+      __syncthreads();
+      if (*last_flag) join_pieces<DH, RT, NT == 1 ? 1 : NT, NT == 1 ? 16 : 4>(p, cut, b, h, r0, rows, piece0, pieces, item_at, (int)threadIdx.x, THREADS);
+    }
+    __syncthreads();                                 // everybody has read the rings: the next item's requests may fill them
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u));
 }
 
-template <int DH>
-size_t smem_bytes(int max_batch) { return Smem<DH>::TABLE_OFF + (size_t)(max_batch + 1) * 4 + (size_t)max_batch * 4; }
+template <int DH, int NT>
+size_t smem_bytes(int max_batch) { return Smem<DH, NT>::TABLE_OFF + (size_t)(max_batch + 1) * 4 + (size_t)max_batch * 4; }
 
-template <int DH, int REP>
+template <int DH, int NT>
 cudaError_t launch_dim(Params& p, const space_ctx* ctx, cudaStream_t st) {
   static unsigned long long done_mask = 0;           // devices on which the kernel may have its shared memory
+  const int max_batch = ctx->cfg.max_batch;
   int dev = 0;
   cudaGetDevice(&dev);
   if (dev >= 64 || !((done_mask >> dev) & 1ull)) {
-    const cudaError_t e = cudaFuncSetAttribute(kvb_attn_kernel<DH, REP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<DH>(128));
+    const cudaError_t e = cudaFuncSetAttribute(kvb_attn_kernel<DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<DH, NT>(128));
     if (e != cudaSuccess) return e;
     if (dev < 64) done_mask |= 1ull << dev;
   }
-  p.n_rt = (p.n_q * p.G + TILE / REP - 1) / (TILE / REP);
-  p.n_groups = CTAS * ctx->sm_count;
-  return launch_pdl(kvb_attn_kernel<DH, REP>, dim3(p.n_groups), dim3(THREADS), smem_bytes<DH>(ctx->cfg.max_batch), st, p, ctx->cfg.max_batch);
+  static_assert(Smem<DH, NT>::CTAS * 8 * NT <= KVB_SM_ROWS, "a slot per block");
+  p.n_rt = (p.n_q * p.G + 8 * NT - 1) / (8 * NT);
+  p.n_groups = Smem<DH, NT>::CTAS * ctx->sm_count;
+  return launch_pdl(kvb_attn_kernel<DH, NT>, dim3(p.n_groups), dim3(THREADS), smem_bytes<DH, NT>(max_batch), st, p, max_batch);
 }
 
 }  // namespace
@@ -865,13 +652,14 @@ int launch_kvb_attn(space_ctx* ctx, const space_kvb_attn_args* a, const uint64_t
   p.part = ctx->attn_part; p.arrived = ctx->kvb_arrived; p.err = ctx->counters + 3 * ctx->cfg.max_batch;
   for (int i = 0; i < p.n_q; ++i) p.mask[i] = mask_rows[i];
   const int rows = p.n_q * p.G;
-  // the flat list is counted in 32 bits
-  if ((double)p.B * p.H_kv * ((rows + 31) / 32) * ((double)p.cache.pages_per_seq + 8) > 2e9) return SPACE_E_UNSUPPORTED;
+  // the flat list is counted in 32 bits: items of eight rows at least, a page and the cost of starting more than a table names
+  if ((double)p.B * p.H_kv * ((rows + 7) / 8) * ((double)p.cache.pages_per_seq + 4) > 2e9) return SPACE_E_UNSUPPORTED;
   ctx->launches += 1;
   const bool wide = ctx->cfg.head_dim == 128;
-  const int rt = kvb_item_rows(rows);
+  int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 24 ? 3 : 4;
+  if (rows > 32) nt = (rows + 23) / 24 * 3 <= (rows + 31) / 32 * 4 ? 3 : 4;
   cudaError_t e;
-  if (wide) e = rt == 32 ? launch_dim<128, 4>(p, ctx, st) : rt == 64 ? launch_dim<128, 2>(p, ctx, st) : launch_dim<128, 1>(p, ctx, st);
-  else e = rt == 32 ? launch_dim<64, 4>(p, ctx, st) : rt == 64 ? launch_dim<64, 2>(p, ctx, st) : launch_dim<64, 1>(p, ctx, st);
+  if (wide) e = nt == 1 ? launch_dim<128, 1>(p, ctx, st) : nt == 2 ? launch_dim<128, 2>(p, ctx, st) : nt == 3 ? launch_dim<128, 3>(p, ctx, st) : launch_dim<128, 4>(p, ctx, st);
+  else e = nt == 1 ? launch_dim<64, 1>(p, ctx, st) : nt == 2 ? launch_dim<64, 2>(p, ctx, st) : nt == 3 ? launch_dim<64, 3>(p, ctx, st) : launch_dim<64, 4>(p, ctx, st);
   return cuda_ok(e);
 }
