@@ -99,27 +99,33 @@ struct Acc {
       for (int s = 0; s < 2; ++s) { M[nt][s] = -CUDART_INF_F; R[nt][s] = l[nt][s] = 0.f; }
     }
   }
-  // A block of keys with reference r, this lane's sum of weights and V's exponent v joins: the accumulators move to the new
-  // references; returns the factor of the block's result.  (r = -infinity: the row sees none of it.)
-  __device__ __forceinline__ float2 join(int nt, const float (&r)[2], const float (&sum)[2], float v) {
-    float a[2], b[2];
+  // A block of keys with references r, this lane's sums of weights and V's exponent v joins: the accumulators move to the new
+  // references, and beta are the factors of the block's results.  (r = -infinity: the row sees none of it.)
+  __device__ __forceinline__ void join(const float (&r)[NT][2], const float (&sum)[NT][2], float v, float (&beta)[NT][2]) {
+    float a[NT][2];
+    bool move = false;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const float Mn = fmaxf(M[nt][s], r[s]);
-      const bool none = r[s] == -CUDART_INF_F;
-      const float down = M[nt][s] == Mn ? 0.f : M[nt][s] - Mn, up = none ? 0.f : r[s] - Mn;
-      l[nt][s] = fmaf(l[nt][s], fast_exp2(down), none ? 0.f : sum[s] * fast_exp2(up));
-      const float r_old = R[nt][s] + down, r_new = v + up, Rn = none ? r_old : fmaxf(r_old, r_new);
-      a[s] = r_old - Rn;
-      b[s] = none ? 0.f : fast_exp2(r_new - Rn);
-      M[nt][s] = Mn; R[nt][s] = Rn;
-    }
-    if (__any_sync(0xFFFFFFFFu, a[0] != 0.f || a[1] != 0.f)) {
-      const float f0 = fast_exp2(a[0]), f1 = fast_exp2(a[1]);
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int ct = 0; ct < DH / 16; ++ct) { o[ct][nt][0] *= f0; o[ct][nt][1] *= f1; o[ct][nt][2] *= f0; o[ct][nt][3] *= f1; }
+      for (int s = 0; s < 2; ++s) {
+        const float Mn = fmaxf(M[nt][s], r[nt][s]);
+        const bool none = r[nt][s] == -CUDART_INF_F;
+        const float down = M[nt][s] == Mn ? 0.f : M[nt][s] - Mn, up = none ? 0.f : r[nt][s] - Mn;
+        l[nt][s] = fmaf(l[nt][s], fast_exp2(down), none ? 0.f : sum[nt][s] * fast_exp2(up));
+        const float r_old = R[nt][s] + down, r_new = v + up, Rn = none ? r_old : fmaxf(r_old, r_new);
+        a[nt][s] = r_old - Rn;
+        move = move || a[nt][s] != 0.f;
+        beta[nt][s] = none ? 0.f : fast_exp2(r_new - Rn);
+        M[nt][s] = Mn; R[nt][s] = Rn;
+      }
+    if (__any_sync(0xFFFFFFFFu, move)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float f0 = fast_exp2(a[nt][0]), f1 = fast_exp2(a[nt][1]);
+#pragma unroll
+        for (int ct = 0; ct < DH / 16; ++ct) { o[ct][nt][0] *= f0; o[ct][nt][1] *= f1; o[ct][nt][2] *= f0; o[ct][nt][3] *= f1; }
+      }
     }
-    return make_float2(b[0], b[1]);
   }
 };
 
@@ -346,43 +352,75 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
       }
       const uint2 scales = lds64(blk + S::SCALE_AT + (warp & 1) * 8);
       const float ks = __uint_as_float(scales.x), ev = (float)((int)((scales.y >> 23) & 255u) - 127);
-      // ---- weights: lane has of columns 2t, 2t + 1 the keys 4 n8 .. + 3
-      uint32_t b0[NT][2], b1[NT][2];                 // second operands of both terms
-      float2 beta[NT];
+      // ---- weights: lane has of columns 2t, 2t + 1 the keys 4 n8 .. + 3.  (One thing after the other for all columns: they do not
+      // wait for each other's latencies.)
+      if (valid < BLOCK_ROWS) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float x[2][4], r[2], sum[2];
-        uint32_t w[2][2];
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (4 * n8 + i >= valid) sc[i >> 1][nt][2 * (i & 1)] = sc[i >> 1][nt][2 * (i & 1) + 1] = -CUDART_INF_F;
+      }
+      float ms[NT][2], fk[NT][2], r[NT][2], sum[NT][2], beta[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) ms[nt][c] = fmaxf(max3(sc[0][nt][c], sc[0][nt][2 + c], sc[1][nt][c]), sc[1][nt][2 + c]);
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) ms[nt][c] = fmaxf(ms[nt][c], __shfl_xor_sync(0xFFFFFFFFu, ms[nt][c], o));     // (a number: the block has a key)
+      bool far = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[c][i] = sc[i >> 1][nt][2 * (i & 1) + c];
-          if (valid < BLOCK_ROWS) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) if (4 * n8 + i >= valid) x[c][i] = -CUDART_INF_F;
-          }
-          const float ms = col_max(fmaxf(fmaxf(x[c][0], x[c][1]), fmaxf(x[c][2], x[c][3])));       // (a number: the block has a key)
-          float fk = fminf(fmaxf(f[nt][c] * ks, F_MIN), F_MAX);
-          float mb = ms * fk;
-          r[c] = mb - 8.f;
-          if (__any_sync(0xFFFFFFFFu, fabsf(mb) > REF_FAR)) {                  // scores off the largest first, then times the factor
-            if (fabsf(mb) > SCORE_MAX) {
-              fk = SCORE_MAX / fabsf(ms);
-              r[c] = copysignf(SCORE_MAX, ms);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[c][i] = fast_exp2(fmaf(x[c][i] - ms, fk, 8.f));
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[c][i] = fast_exp2(fmaf(x[c][i], fk, -r[c]));
-          }
-          sum[c] = (x[c][0] + x[c][1]) + (x[c][2] + x[c][3]);
-          split4(x[c][0], x[c][1], x[c][2], x[c][3], w[0][c], w[1][c]);
+          fk[nt][c] = fminf(fmaxf(f[nt][c] * ks, F_MIN), F_MAX);
+          const float mb = ms[nt][c] * fk[nt][c];
+          r[nt][c] = mb - 8.f;
+          far = far || fabsf(mb) > REF_FAR;
         }
-        transpose_words(w[0][0], w[0][1], b0[nt][0], b1[nt][0]);
-        transpose_words(w[1][0], w[1][1], b0[nt][1], b1[nt][1]);
-        beta[nt] = acc.join(nt, r, sum, ev);
+      if (__any_sync(0xFFFFFFFFu, far)) {            // scores off the largest first, then times the factor
+#pragma unroll 1
+        for (int x = 0; x < 2 * NT; ++x)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              if (x != 2 * nt + c) continue;
+              if (fabsf(ms[nt][c] * fk[nt][c]) > SCORE_MAX) {
+                fk[nt][c] = SCORE_MAX / fabsf(ms[nt][c]);
+                r[nt][c] = copysignf(SCORE_MAX, ms[nt][c]);
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                float& y = sc[i >> 1][nt][2 * (i & 1) + c];
+                y = fast_exp2(fmaf(y - ms[nt][c], fk[nt][c], 8.f));
+              }
+            }
+      } else {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[u][nt][e] = fast_exp2(fmaf(sc[u][nt][e], fk[nt][e & 1], -r[nt][e & 1]));
       }
+      uint32_t w[NT][2][2], b0[NT][2], b1[NT][2];    // second operands of both terms
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          sum[nt][c] = (sc[0][nt][c] + sc[0][nt][2 + c]) + (sc[1][nt][c] + sc[1][nt][2 + c]);
+          split4(sc[0][nt][c], sc[0][nt][2 + c], sc[1][nt][c], sc[1][nt][2 + c], w[nt][0][c], w[nt][1][c]);
+        }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int term = 0; term < 2; ++term) transpose_words(w[nt][term][0], w[nt][term][1], b0[nt][term], b1[nt][term]);
+      acc.join(r, sum, ev, beta);
       // ---- D^T = V^T W^T: the lane's keys of a channel are 8 t .. + 7
       const uint32_t vat = blk + S::V_AT + (t >> 1) * S::V_PITCH + n8 * 16 + 8 * (t & 1);
       uint32_t keep0 = 0xFFFFFFFFu, keep1 = 0xFFFFFFFFu;
@@ -400,8 +438,8 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
           float d[4] = {0.f, 0.f, 0.f, 0.f};
           mma8(d, x.x, y.x, x.y, y.y, b0[nt][0], b1[nt][0]);
           mma8(d, x.x, y.x, x.y, y.y, b0[nt][1], b1[nt][1]);
-          acc.o[ct][nt][0] = fmaf(d[0], beta[nt].x, acc.o[ct][nt][0]); acc.o[ct][nt][1] = fmaf(d[1], beta[nt].y, acc.o[ct][nt][1]);
-          acc.o[ct][nt][2] = fmaf(d[2], beta[nt].x, acc.o[ct][nt][2]); acc.o[ct][nt][3] = fmaf(d[3], beta[nt].y, acc.o[ct][nt][3]);
+          acc.o[ct][nt][0] = fmaf(d[0], beta[nt][0], acc.o[ct][nt][0]); acc.o[ct][nt][1] = fmaf(d[1], beta[nt][1], acc.o[ct][nt][1]);
+          acc.o[ct][nt][2] = fmaf(d[2], beta[nt][0], acc.o[ct][nt][2]); acc.o[ct][nt][3] = fmaf(d[3], beta[nt][1], acc.o[ct][nt][3]);
         }
       }
       __syncwarp();                                  // everybody has read the stage: the next request may fill it
@@ -471,28 +509,29 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
       }
       __syncwarp();
       uint32_t ph[NT][2], pl[NT][2];
-      float2 beta[NT];
+      float r[NT][2], sum[NT][2], beta[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float r[2], sum[2] = {0.f, 0.f}, y[2][2];
+        float y[2][2];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const int row = r0 + 8 * nt + 2 * t + c;
           const uint64_t see = row < p.n_q * p.G ? p.mask[row >> p.gsh] : 0ull;                    // Eq. 5
-          r[c] = -CUDART_INF_F;
+          float top = -CUDART_INF_F;
+          sum[nt][c] = 0.f;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const bool vis = (see >> (k0 + 8 * i + n8)) & 1ull;
             const float x = sc[nt][2 * i + c] * kf[i];       // (a row that is not finite: NaN here, and at the end)
             y[c][i] = vis ? (x > SCORE_MAX ? SCORE_MAX : x < -SCORE_MAX ? -SCORE_MAX : x) : -CUDART_INF_F;
-            r[c] = fmaxf(r[c], y[c][i]);
+            top = fmaxf(top, y[c][i]);
           }
-          r[c] = col_max(r[c]);
-          const float from = r[c] == -CUDART_INF_F ? 0.f : r[c];
+          r[nt][c] = top = col_max(top);
+          const float from = top == -CUDART_INF_F ? 0.f : top;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             y[c][i] = fast_exp2(y[c][i] - from);
-            sum[c] += y[c][i];
+            sum[nt][c] += y[c][i];
           }
         }
 #pragma unroll
@@ -506,8 +545,8 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
           ph[nt][i] = transpose8(hw);
           pl[nt][i] = transpose8(*reinterpret_cast<const uint32_t*>(&lo));
         }
-        beta[nt] = acc.join(nt, r, sum, 32.f);
       }
+      acc.join(r, sum, 32.f, beta);
 #pragma unroll
       for (int ct = 0; ct < DH / 16; ++ct) {
         uint32_t a0, a1, a2, a3;
@@ -519,8 +558,8 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
           float d[4] = {0.f, 0.f, 0.f, 0.f};
           mma_bf16(d, a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
           mma_bf16(d, a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
-          acc.o[ct][nt][0] = fmaf(d[0], beta[nt].x, acc.o[ct][nt][0]); acc.o[ct][nt][1] = fmaf(d[1], beta[nt].y, acc.o[ct][nt][1]);
-          acc.o[ct][nt][2] = fmaf(d[2], beta[nt].x, acc.o[ct][nt][2]); acc.o[ct][nt][3] = fmaf(d[3], beta[nt].y, acc.o[ct][nt][3]);
+          acc.o[ct][nt][0] = fmaf(d[0], beta[nt][0], acc.o[ct][nt][0]); acc.o[ct][nt][1] = fmaf(d[1], beta[nt][1], acc.o[ct][nt][1]);
+          acc.o[ct][nt][2] = fmaf(d[2], beta[nt][0], acc.o[ct][nt][2]); acc.o[ct][nt][3] = fmaf(d[3], beta[nt][1], acc.o[ct][nt][3]);
         }
       }
       __syncwarp();
@@ -655,6 +694,7 @@ int launch_kvb_attn(space_ctx* ctx, const space_kvb_attn_args* a, const uint64_t
   // the flat list is counted in 32 bits: items of eight rows at least, a page and the cost of starting more than a table names
   if ((double)p.B * p.H_kv * ((rows + 7) / 8) * ((double)p.cache.pages_per_seq + 4) > 2e9) return SPACE_E_UNSUPPORTED;
   ctx->launches += 1;
+  if (rows > 16) return launch_kvb_attn_tc(ctx, p, st);
   const bool wide = ctx->cfg.head_dim == 128;
   int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 24 ? 3 : 4;
   if (rows > 32) nt = (rows + 23) / 24 * 3 <= (rows + 31) / 32 * 4 ? 3 : 4;

@@ -144,3 +144,5 @@ __device__ __forceinline__ void join_pieces(const Params& p, const Cut& cut, int
 }
 
 }  // namespace kvb
+
+int launch_kvb_attn_tc(space_ctx* ctx, kvb::Params& p, cudaStream_t st);

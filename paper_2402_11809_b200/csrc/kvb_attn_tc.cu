@@ -1,0 +1,861 @@
+// Attention of a step's block rows over the 8-bit cache (space_kvb_attn_step), items of up to 32, 64 or 128 query rows on tcgen05.
+//
+// The mathematics is kvb_attn.cu's (codes as operands as they lie, query rows and weights as two e4m3 terms each), with a page
+// of 128 keys in the place of a block of 32:
+//   S = q0 K^T + q1 K^T,    D = w0 V + w1 V,    chunk b of 32 keys (one K and one V scale 2^k_b, 2^v_b):   m_b = max_j s_j,
+//   e_j = 2^(s_j - m_b),    w_j = e_j 2^((m_b - m) + v_b - E + 8),    m = max m_b,  E = max_b (m_b - m) + v_b,
+//   l += sum_b 2^(m_b - M) sum_j e_j,    o = o 2^(R - R') + D 2^(E + (m - M) - R' - 8)     with R' the larger of R and E + (m - M).
+//
+// The work.  Query rows are the MMA's M extent: 128 of them, or 64 or 32 held twice or four times over, each copy with keys of its own
+// (chunks of 32).  Both first operands, query rows and weights, are in tensor memory: an M = 128, K = 32 product takes 10 + N/2 cycles
+// then, 43 + N/2 with the first operand in shared memory.  Two threads have a row (of a copy), half of its keys and half of the
+// result's channels each; they tell each other their largest scores.  The flat list of 128-key pages over all (sequence, kv head,
+// query rows) items is cut evenly over the thread blocks, one per SM.  A page's scores are there when the softmax of the page before ends,
+// and its result is added up in the next page's time: the softmax never waits for products, nor they for each other.  Pieces of
+// a cut item are joined by the block that stores the last of them, always in the same order.
+// The block's own rows are bf16 products on mma.sync (eight query rows a warp) when an item ends; their results meet the others there.
+//
+// Warps: 0-7 softmax and sums, 8 products (one thread), 9 copies (one thread), 10 asks L2 for the rows that items will want, 11 only gives
+// its registers away.  The copying thread walks the list and leaves out what has no keys (pages outside the pool); what it
+// brings it announces in order, and everybody else goes by that.
+// Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT, no role leaves its loop early, and the block drains and exits.
+#include "kvb_attn.cuh"
+
+namespace {
+using namespace kvb;
+
+constexpr int TILE = SPACE_PAGE_SIZE;                // keys of a page, rows of an MMA
+constexpr int GROUP = 128, SOFT = 2 * GROUP, THREADS = SOFT + GROUP;           // (registers move by groups of four warps)
+constexpr int SHARE_COST = 3;                        // fixed cost of an item, in pages
+constexpr int RING = 16;                             // scales and announcements of that many pages
+enum { NO_MORE = 0x7FFFFFFF };
+constexpr float REF_FAR = 0x1p22f;                   // up to this a reference's rounding moves weights by 2^0.25 at most
+
+template <int DH>
+struct Smem {
+  using F = Fmt<DH>;
+  static constexpr int STAGES = DH == 128 ? 5 : 8;
+  static constexpr int MEET = DH / 4;                        // channels of a thread that copies of a row meet in at a time
+  static constexpr int PITCH = SOFT + 1;                     // floats (four channels apart: another bank)
+  static constexpr int MEET_OFF = 0;                         // [MEET][PITCH]; the block's own V rows before
+  static constexpr int OWN_PITCH = 2 * DH + 16;              // bytes of those
+  static constexpr int MEET_BYTES = MEET * PITCH * 4 / 128 * 128 + 128;
+  static_assert(SPACE_MAX_ROWS * OWN_PITCH <= MEET_BYTES, "the block's V rows fit where sums meet");
+  static constexpr int K_OFF = MEET_BYTES;                   // [STAGES]
+  static constexpr int V_OFF = K_OFF + STAGES * F::CODES;    // [STAGES]
+  static constexpr int SCALE_OFF = V_OFF + STAGES * F::CODES;        // [RING][4] {K, V}
+  static constexpr int ML_OFF = SCALE_OFF + RING * 32;       // [2][SOFT] {M, l} of rows' halves and copies, by item
+  static constexpr int OWN_OFF = ML_OFF + 2 * SOFT * 8;      // [2][128] {M, l} of rows over the block's own rows
+  static constexpr int XCH_OFF = OWN_OFF + 2 * GROUP * 8;    // [2][SOFT] a page's {largest score, E} of a row's halves
+  static constexpr int DESC_OFF = XCH_OFF + 2 * SOFT * 8;    // [RING] {item of the share, page of it}
+  static constexpr int BAR_OFF = DESC_OFF + RING * 8;
+  static constexpr int N_BARS = 4 * STAGES + RING + 13;
+  static constexpr int MISC_OFF = BAR_OFF + N_BARS * 8;
+  static constexpr int MASK_OFF = (MISC_OFF + 16 + 7) / 8 * 8;
+  static constexpr int TABLE_OFF = MASK_OFF + SPACE_MAX_ROWS * 8;    // prefix[max_batch + 1], seq_len[max_batch]
+  static_assert(TABLE_OFF + 129 * 4 + 128 * 4 <= 227 * 1024, "shared-memory plan too large");
+  static_assert(RING >= STAGES + 6, "an announcement outlives everybody who reads it");
+};
+
+__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"n"(SOFT) : "memory"); }
+template <int R> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
+template <int R> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+#define KVB_R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
+#define KVB_W8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
+__device__ __forceinline__ void tmem_ld32(uint32_t a, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+               "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : KVB_R8(r, 0), KVB_R8(r, 8), KVB_R8(r, 16), KVB_R8(r, 24) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t a, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : KVB_R8(r, 0), KVB_R8(r, 8) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+               ::"r"(a), KVB_W8(r, 0), KVB_W8(r, 8) : "memory");
+}
+__device__ __forceinline__ void tmem_st4(uint32_t a, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+// e4m3 x e4m3 -> f32, M = 128, first operand in tensor memory (a row per lane, four bytes of it per column), second one K-major
+__device__ __forceinline__ void mma8_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ constexpr uint32_t instr_desc(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24); }
+// Unswizzled K-major operand: 8 rows x 16 bytes lie together, lbo bytes to the next sixteen bytes of K, sbo to the next eight rows.
+__device__ __forceinline__ uint64_t plain_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+  return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)((lbo >> 4) & 0x3FFF) << 16 | (uint64_t)((sbo >> 4) & 0x3FFF) << 32 | (uint64_t)1 << 46;
+}
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const char* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+__device__ __forceinline__ float max16(const uint32_t* s) {
+  const float* x = reinterpret_cast<const float*>(s);
+  const float a = max3(max3(x[0], x[1], x[2]), x[3], x[4]), b = max3(max3(x[5], x[6], x[7]), x[8], x[9]);
+  const float c = max3(max3(x[10], x[11], x[12]), x[13], x[14]);
+  return fmaxf(max3(a, b, c), x[15]);
+}
+
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3},{%4,%5,%6,%7},{%8,%9},{%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {                   // 8 x 8 halves over the warp
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ void prefetch_line(const char* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
+// The items of a block's share, in order: every role walks them for itself.
+struct Walk {
+  uint32_t cur, end, at;                             // at: the item's place in the list
+  int b, it;                                         // item h * n_rt + block of query rows
+  int L, t0, t1;                                     // pages [t0, t1) of it; cached rows (-1: the sequence does not fit)
+  bool opens;                                        // the share begins with this item
+  __device__ __forceinline__ int cached() const { return (max(L, 0) + TILE - 1) / TILE; }    // that page: the block's own rows
+  __device__ __forceinline__ int pages(int has_new) const { return max(cached() + has_new, 1); }
+  __device__ __forceinline__ bool next(const uint32_t* prefix, const int* seq_len, int has_new, uint32_t share0) {
+    while (cur < end) {
+      while (prefix[b + 1] <= cur) ++b;
+      L = seq_len[b];
+      const int Tv = pages(has_new) + SHARE_COST;
+      const uint32_t rem = cur - prefix[b];
+      it = (int)(rem / (uint32_t)Tv);
+      const int x0 = (int)rem - it * Tv, n = min(Tv - x0, (int)(end - cur));
+      opens = cur == share0;
+      at = cur - x0;
+      cur += n;
+      t0 = max(x0 - SHARE_COST, 0); t1 = x0 + n - SHARE_COST;
+      if (t1 > t0) return true;                      // (else only the cost of starting)
+    }
+    return false;
+  }
+};
+
+template <int DH, int REP>
+__global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_constant__ Params p, int max_batch) {
+  using F = Fmt<DH>;
+  using S = Smem<DH>;
+  constexpr int STAGES = S::STAGES, RT = TILE / REP;                           // rows of an item
+  constexpr int KEYS = TILE / REP / 2;               // of a page, that a thread has
+  extern __shared__ __align__(1024) unsigned char sm[];
+  const uint32_t base = smem_u32(sm), bar0 = base + S::BAR_OFF;
+  auto BAR = [&](int i) { return bar0 + 8u * i; };
+  // Of a stage: K, V are there / have been used.  SAID: page m is announced and its scales are there.  QREADY: an item's query rows are
+  // there.  SDONE (two, by page): scores.  PREADY: weights (and the result before has been added up).  ODONE: a page's result.
+  // XCH, QTOP (by pair of warps): largest scores, elements of both halves.
+  constexpr int FULLK = 0, FULLV = STAGES, FREEK = 2 * STAGES, FREEV = 3 * STAGES, SAID = 4 * STAGES, QREADY = SAID + RING,
+                SDONE = QREADY + 1, PREADY = QREADY + 3, ODONE = QREADY + 4, XCH = QREADY + 5, QTOP = QREADY + 9;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::MISC_OFF);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF + 4);
+  volatile int* last_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF + 8);
+  uint32_t* prefix = reinterpret_cast<uint32_t*>(sm + S::TABLE_OFF);
+  int* seq_len = reinterpret_cast<int*>(prefix + max_batch + 1);
+  volatile int2* desc = reinterpret_cast<volatile int2*>(sm + S::DESC_OFF);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    *abort_flag = 0;
+    for (int s = 0; s < 4 * STAGES + RING; ++s) mbar_init(BAR(s), 1);
+    mbar_init(BAR(QREADY), 8); mbar_init(BAR(SDONE), 1); mbar_init(BAR(SDONE + 1), 1); mbar_init(BAR(PREADY), 8); mbar_init(BAR(ODONE), 1);
+    for (int i = 0; i < 4; ++i) { mbar_init(BAR(XCH + i), 2); mbar_init(BAR(QTOP + i), 2); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async();
+  }
+  if (threadIdx.x < SPACE_MAX_ROWS) reinterpret_cast<uint64_t*>(sm + S::MASK_OFF)[threadIdx.x] = p.mask[threadIdx.x];
+  // Tensor memory is taken when the kernel before has given its own back, and the next kernel's blocks may come when all of these
+  // have theirs: nobody holds some while it waits for somebody who wants some.
+  pdl_wait();
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (warp == 0) {
+    uint32_t carry = 0;                              // running sums of the list
+    for (int b0 = 0; b0 < p.B; b0 += 32) {
+      const int b = b0 + lane;
+      int L = -1;
+      uint32_t n = 0;
+      if (b < p.B) {
+        L = p.kv_len[b];
+        if (L < 0 || (int64_t)L > (int64_t)p.cache.pages_per_seq * TILE) {
+          if (blockIdx.x == 0 && p.status) atomicOr(p.status + b, SPACE_ST_CAPACITY);
+          L = -1;
+        }
+        n = (uint32_t)((max((max(L, 0) + TILE - 1) / TILE + p.has_new, 1) + SHARE_COST) * p.H_kv * p.n_rt);
+      }
+      uint32_t incl = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      if (b < p.B) { seq_len[b] = L; prefix[b] = carry + incl - n; }
+      carry += __shfl_sync(0xFFFFFFFFu, incl, 31);
+    }
+    if (lane == 0) prefix[p.B] = carry;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_launch_dependents();
+  const uint32_t tmem = *tmem_slot;
+  // columns: scores (two buffers; those of 32 keys make way for their weights, 16 columns), a page's result, query rows (two buffers of
+  // two terms)
+  const uint32_t TM_S = tmem, TM_O = tmem + 2 * TILE, TM_Q = TM_O + TILE;
+  const Cut cut(prefix[p.B], p.n_groups);
+  Walk wk;
+  const bool mine = blockIdx.x < cut.NG;
+  const uint32_t share0 = mine ? cut.begin(blockIdx.x) : 0;
+  wk.b = 0; wk.cur = share0;
+  wk.end = mine ? cut.begin(blockIdx.x + 1) : 0;
+  uint32_t m = 0;                                    // pages so far
+  auto hold = [&](int bar, uint32_t use, int site) { return wait(BAR(bar), use & 1, abort_flag, p.err, site); };
+
+  if (warp >= 8) {
+    regs_dec<40>();
+    if (warp == 9 && elect_one()) {
+      // ---- copies: K of a page when the K of the page that had its stage has been used, V likewise
+      bool ok = true;
+      int item = 0;
+      for (; ok && wk.next(prefix, seq_len, p.has_new, share0); ++item) {
+        const int32_t* table = p.cache.page_table + (int64_t)wk.b * p.cache.pages_per_seq;
+        const char* pool = p.cache.pool + (int64_t)(wk.it / p.n_rt) * p.cache.head_stride;
+        const int end = min(wk.t1, wk.cached());
+        int pg = wk.t0 < end ? __ldg(table + wk.t0) : -1;
+        for (int t = wk.t0; t < end && ok; ++t) {
+          const int page = pg;
+          if (t + 1 < end) pg = __ldg(table + t + 1);        // (one page ahead of its use)
+          if (page < 0 || page >= p.cache.n_pages) {
+            if (p.status) atomicOr(p.status + wk.b, SPACE_ST_BAD_PAGE);
+            continue;
+          }
+          const uint32_t s = m % STAGES, e = m % RING;
+          const char* head = pool + (int64_t)page * p.cache.page_stride;
+          desc[e].x = item; desc[e].y = t;
+          mbar_expect_tx(BAR(SAID + e), 32);
+          bulk_copy(base + S::SCALE_OFF + e * 32, head + F::SCALES, 32, BAR(SAID + e));
+          if (m >= STAGES) ok = hold(FREEK + s, m / STAGES - 1, 1);
+          if (ok) {
+            mbar_expect_tx(BAR(FULLK + s), F::CODES);
+            bulk_copy(base + S::K_OFF + s * F::CODES, head, F::CODES, BAR(FULLK + s));
+            if (m >= STAGES) ok = hold(FREEV + s, m / STAGES - 1, 2);
+          }
+          if (ok) {
+            mbar_expect_tx(BAR(FULLV + s), F::CODES);
+            bulk_copy(base + S::V_OFF + s * F::CODES, head + F::CODES, F::CODES, BAR(FULLV + s));
+          }
+          ++m;
+        }
+      }
+      if (ok) {
+        desc[m % RING].x = NO_MORE;
+        mbar_arrive(BAR(SAID + m % RING));
+      }
+      // every copy has landed before the block may exit (a page whose copies a wait that ran out cut short is the last)
+      for (uint32_t j = m > STAGES ? m - STAGES : 0; j < m; ++j) {
+        mbar_drain_bounded(BAR(SAID + j % RING), (j / RING) & 1, WAIT_NS / 10);
+        mbar_drain_bounded(BAR(FULLK + j % STAGES), (j / STAGES) & 1, WAIT_NS / 10);
+        mbar_drain_bounded(BAR(FULLV + j % STAGES), (j / STAGES) & 1, WAIT_NS / 10);
+      }
+    } else if (warp == 8 && elect_one()) {
+      // ---- products: scores of page q, a page ahead of the result of page m
+      uint32_t q = 0;
+      int item = -1;
+      bool ok = true, more = true;
+      while (true) {
+        while (more && q < m + 2) {
+          ok = hold(SAID + q % RING, q / RING, 3) && ok;
+          const int it = ok ? desc[q % RING].x : NO_MORE;
+          if (it == NO_MORE) { more = false; break; }
+          if (it != item) {
+            if (q > m) break;                        // (its query rows come when the weights of page m have)
+            ok = hold(QREADY, it, 4) && ok;
+            item = it;
+          }
+          const uint32_t s = q % STAGES;
+          ok = hold(FULLK + s, q / STAGES, 5) && ok;
+          if (m && q > m) ok = hold(ODONE, m - 1, 6) && ok;                    // (the weights of page q - 2 lie where these scores go)
+          tc_fence_after();
+          const uint64_t kd = plain_desc(base + S::K_OFF + s * F::CODES, F::K_COLS, 128);
+          if (ok) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int ks = 0; ks < DH / 32; ++ks)
+                mma8_ts(TM_S + (q & 1) * TILE, TM_Q + (item & 1) * 64 + i * (DH / 4) + 8 * ks, kd + (uint64_t)((ks * 2 * F::K_COLS) >> 4), instr_desc(TILE), i + ks > 0);
+          }
+          tc_commit(BAR(SDONE + (q & 1)));
+          tc_commit(BAR(FREEK + s));
+          ++q;
+        }
+        if (m == q) {
+          if (more) continue;
+          break;
+        }
+        const uint32_t s = m % STAGES;
+        ok = hold(FULLV + s, m / STAGES, 7) && ok;
+        if (m) ok = hold(ODONE, m - 1, 8) && ok;     // (long since: whoever brings the weights has waited for it)
+        ok = hold(PREADY, m, 9) && ok;
+        tc_fence_after();
+        const uint64_t vd = plain_desc(base + S::V_OFF + s * F::CODES, F::V_ROWS, 128);
+        if (ok) {
+#pragma unroll
+          for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              mma8_ts(TM_O, TM_S + (m & 1) * TILE + 32 * b + 8 * i, vd + (uint64_t)((2 * b * F::V_ROWS) >> 4), instr_desc(DH), b + i > 0);
+        }
+        tc_commit(BAR(ODONE));
+        tc_commit(BAR(FREEV + s));
+        ++m;
+      }
+      if (m) hold(ODONE, m - 1, 10);                 // all products done before tensor memory is released
+    } else if (warp == 10) {
+      // ---- query rows, and the block's own, of all the share's items: out of HBM before somebody waits for them
+      while (wk.next(prefix, seq_len, p.has_new, share0)) {
+        const int h = wk.it / p.n_rt, r0 = (wk.it - h * p.n_rt) * RT, rows = min(p.n_q * p.G - r0, RT);
+        for (int r = lane; r < rows; r += 32) {
+          int i, hq;
+          row_of(p, h, r0 + r, i, hq);
+          const char* at = p.q + (int64_t)wk.b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh;
+          prefetch_line(at);
+          if (DH == 128) prefetch_line(at + 128);
+        }
+        if (!p.has_new || wk.t1 <= wk.cached()) continue;
+        for (int r = lane; r < p.n_q; r += 32) {
+          const int64_t at = (int64_t)wk.b * p.n_sb + (int64_t)r * p.n_sr + (int64_t)h * p.n_sh;
+          prefetch_line(p.kn + at); prefetch_line(p.vn + at);
+          if (DH == 128) { prefetch_line(p.kn + at + 128); prefetch_line(p.vn + at + 128); }
+        }
+      }
+    }
+  } else {
+    regs_inc<232>();                                 // (256 threads x 232 + 128 x 40 = the 384 x 168 of the launch)
+    const int half = warp >> 2, tid = threadIdx.x & (GROUP - 1), w4 = warp & 3;
+    const int rep = w4 / (4 / REP), row = tid % RT;
+    const uint32_t lanes = (uint32_t)(32 * w4) << 16;
+    const int key0 = rep * (TILE / REP) + half * KEYS;       // first of this thread's keys of a page
+    const uint32_t TM_C = TM_O + lanes + half * (DH / 2);
+    // The query row of the item that wk stands at, this thread's half of it, as two terms into a buffer.
+    float f_next = 0.f;                              // factor of its scores
+    bool nan_next = false;                           // it holds a NaN or an infinity
+    auto bring_query = [&](int item) {
+      const int h = wk.it / p.n_rt;
+      int i, hq;
+      row_of(p, h, (wk.it - h * p.n_rt) * RT + row, i, hq);
+      const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)wk.b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh) + half * (DH / 16);
+      uint4 v[DH / 16];
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < DH / 16; ++j) v[j] = i < p.n_q ? src[j] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < DH / 16; ++j) top = max(top, kvq::max_bits(v[j]));
+      uint32_t* tops = reinterpret_cast<uint32_t*>(sm + S::ML_OFF) + 2 * SOFT * (item & 1);        // (sums of the item before last were there)
+      tops[threadIdx.x] = top;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(QTOP + w4));
+      hold(QTOP + w4, item, 11);
+      top = max(top, tops[threadIdx.x ^ GROUP]);
+      nan_next = top >= 0x7F80u;
+      const int e = nan_next ? 0 : max((int)(top >> 7) - 127, -100) - 7;       // the largest element to [2^7, 2^8)
+      const float up = pow2(-e);
+      f_next = p.c * pow2(e);
+#pragma unroll
+      for (int j = 0; j < DH / 16; j += 2) {
+        uint32_t w0[4], w1[4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint4 x = v[j + k];
+          split4(kvq::bf_lo(x.x) * up, kvq::bf_hi(x.x) * up, kvq::bf_lo(x.y) * up, kvq::bf_hi(x.y) * up, w0[2 * k], w1[2 * k]);
+          split4(kvq::bf_lo(x.z) * up, kvq::bf_hi(x.z) * up, kvq::bf_lo(x.w) * up, kvq::bf_hi(x.w) * up, w0[2 * k + 1], w1[2 * k + 1]);
+        }
+        const uint32_t to = TM_Q + lanes + (item & 1) * 64 + half * (DH / 8) + 2 * j;
+        tmem_st4(to, w0);
+        tmem_st4(to + DH / 4, w1);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(QREADY));
+    };
+    // What is announced of page m.
+    int next_item, next_page;
+    auto look = [&]() {
+      hold(SAID + m % RING, m / RING, 12);
+      next_item = *abort_flag ? NO_MORE : desc[m % RING].x;
+      next_page = desc[m % RING].y;
+    };
+    bool live = wk.next(prefix, seq_len, p.has_new, share0);
+    if (live) bring_query(0);
+    look();
+    for (int item = 0; live; ++item) {
+      const int b = wk.b, it = wk.it, L = wk.L, T = wk.pages(p.has_new);
+      const bool whole = wk.t0 == 0 && wk.t1 == T, opens = wk.opens, owned = p.has_new && L >= 0 && wk.t1 > wk.cached();
+      const uint32_t item_at = wk.at;
+      const int h = it / p.n_rt, r0 = (it - h * p.n_rt) * RT, rows = min(p.n_q * p.G - r0, RT);
+      const float f = f_next;
+      const bool nan = nan_next;
+      uint64_t o2[DH / 4];
+#pragma unroll
+      for (int j = 0; j < DH / 4; ++j) o2[j] = 0ull;
+      float M = -CUDART_INF_F, l = 0.f, R = 0.f, alpha = 1.f, beta = 0.f;
+      // A page's result joins the sum: asked for, and, when it has come, added.
+      bool pending = false;
+      uint32_t res[DH / 2];
+      auto ask = [&]() {
+        hold(ODONE, m - 1, 13);
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < DH / 2; c += 32) tmem_ld32(TM_C + c, res + c);
+      };
+      auto add = [&]() {
+        if (__any_sync(0xFFFFFFFFu, alpha != 1.f)) {
+          const uint64_t a2 = pack2(alpha, alpha);
+#pragma unroll
+          for (int j = 0; j < DH / 4; ++j) o2[j] = mul2(o2[j], a2);
+        }
+        const uint64_t b2 = pack2(beta, beta);
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < DH / 4; ++j) o2[j] = fma2(pack2(__uint_as_float(res[2 * j]), __uint_as_float(res[2 * j + 1])), b2, o2[j]);
+        tc_fence_before();
+      };
+      while (next_item == item) {
+        const int t = next_page;
+        const uint32_t s = m % STAGES;
+        const uint32_t TM_SM = TM_S + lanes + (m & 1) * TILE;                  // the page's scores
+        const float2* sc = reinterpret_cast<const float2*>(sm + S::SCALE_OFF + (m % RING) * 32) + (key0 >> 5);
+        const int vis0 = L - t * TILE, vis = vis0 - key0;            // visible keys of the page, and of this thread
+        if (vis0 < TILE) {                           // what lies behind the last row must not count, whatever it is
+          hold(FULLV + s, m / STAGES, 14);
+          const int g0 = vis0 >> 4;
+#pragma unroll 1
+          for (int e = threadIdx.x; e < (8 - g0) * DH; e += SOFT) {
+            const int sixteen = g0 + e / DH, keep = min(max(vis0 - 16 * sixteen, 0), 16);
+            unsigned char* at = sm + S::V_OFF + s * F::CODES + sixteen * F::V_ROWS + (e % DH) * 16;
+            const uint4 w = *reinterpret_cast<const uint4*>(at);
+            uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int n = min(max(keep - 4 * j, 0), 4);
+              x[j] &= n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
+            }
+            *reinterpret_cast<uint4*>(at) = make_uint4(x[0], x[1], x[2], x[3]);
+          }
+          fence_async();
+        }
+        hold(SDONE + (m & 1), m >> 1, 15);
+        tc_fence_after();
+        constexpr int NC = (KEYS + 31) / 32, N1 = KEYS < 32 ? KEYS : 32;       // 32 keys share their scales
+        uint32_t v[KEYS];
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+          if (KEYS < 32) tmem_ld16(TM_SM + key0, v);
+          else tmem_ld32(TM_SM + key0 + 32 * k, v + 32 * k);
+        }
+        // ---- largest scores
+        float fk[NC], ms[NC], mb[NC], x[NC], pm = -CUDART_INF_F, E = -CUDART_INF_F;
+        tmem_wait_ld();
+        if (vis < KEYS) {
+#pragma unroll
+          for (int j = 0; j < KEYS; ++j) if (j >= vis) v[j] = 0xFF800000u;
+        }
+        bool far = false;
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+          ms[k] = max16(v + 32 * k);
+          if (N1 > 16) ms[k] = fmaxf(ms[k], max16(v + 32 * k + 16));
+          fk[k] = fminf(fmaxf(f * sc[k].x, F_MIN), F_MAX);
+          x[k] = ms[k] * fk[k];
+          mb[k] = ms[k] == -CUDART_INF_F ? 0.f : x[k];
+          far = far || fabsf(mb[k]) > REF_FAR;
+        }
+        if (__any_sync(0xFFFFFFFFu, far)) {          // scores off the largest first, then times the factor
+#pragma unroll
+          for (int k = 0; k < NC; ++k) {
+            const float top = ms[k] == -CUDART_INF_F ? 0.f : ms[k];
+            if (fabsf(mb[k]) > SCORE_MAX) {
+              fk[k] = SCORE_MAX / fabsf(top);
+              x[k] = copysignf(SCORE_MAX, top);
+            }
+            mb[k] = 0.f;
+#pragma unroll
+            for (int j = 0; j < N1; ++j) v[32 * k + j] = __float_as_uint(__uint_as_float(v[32 * k + j]) - top);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < NC; ++k) pm = fmaxf(pm, x[k]);
+        float ev[NC];
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+          ev[k] = (float)((int)((__float_as_uint(sc[k].y) >> 23) & 255u) - 127);
+          x[k] = x[k] == -CUDART_INF_F ? -CUDART_INF_F : x[k] - pm;
+          E = fmaxf(E, x[k] + ev[k]);
+        }
+        // ---- both halves of the row: the page's largest score, and E relative to it
+        float2* xch = reinterpret_cast<float2*>(sm + S::XCH_OFF) + (m & 1) * SOFT;
+        xch[threadIdx.x] = make_float2(pm, E);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(XCH + w4));
+        if (pending) ask();
+        hold(XCH + w4, m, 16);
+        const float2 other = xch[threadIdx.x ^ GROUP];
+        const float top = fmaxf(pm, other.x), lower = pm - top;
+        const bool none = top == -CUDART_INF_F;      // this row sees nothing of the page
+        E = none ? 0.f : fmaxf(E + lower, other.y + (other.x - top));
+        // ---- weights
+        float wf[NC], part[NC];
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+          const float d = none || x[k] == -CUDART_INF_F ? -CUDART_INF_F : x[k] + lower;
+          wf[k] = fast_exp2(d + (ev[k] + 8.f - E));
+          part[k] = fast_exp2(d);
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+          const uint64_t f2 = pack2(fk[k], fk[k]), n2 = pack2(-mb[k], -mb[k]), w2 = pack2(wf[k], wf[k]);
+          uint64_t sum0 = 0ull, sum1 = 0ull;
+#pragma unroll
+          for (int u = 0; u < N1; u += 16) {
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t* y = v + 32 * k + u + 4 * j;
+              float a, b, c, d;
+              unpack2(fma2(pack2(__uint_as_float(y[0]), __uint_as_float(y[1])), f2, n2), a, b);
+              unpack2(fma2(pack2(__uint_as_float(y[2]), __uint_as_float(y[3])), f2, n2), c, d);
+              const uint64_t e0 = pack2(fast_exp2(a), fast_exp2(b)), e1 = pack2(fast_exp2(c), fast_exp2(d));
+              sum0 = add2(sum0, e0); sum1 = add2(sum1, e1);
+              unpack2(mul2(e0, w2), a, b);
+              unpack2(mul2(e1, w2), c, d);
+              split4(a, b, c, d, w[j], w[4 + j]);
+            }
+            // (sixteen weights, first terms, then second ones: where scores of the same 32 keys were)
+            const int key = key0 + 32 * k + u;
+            const uint32_t at = TM_SM + (key & ~31) + ((key >> 4) & 1) * 4;
+            tmem_st4(at, w);
+            tmem_st4(at + 8, w + 4);
+          }
+          float a, b;
+          unpack2(add2(sum0, sum1), a, b);
+          sum = fmaf(a + b, part[k], sum);
+        }
+        if (REP > 1) {                               // keys that other copies of the row have: each half two of the four chunks
+          const uint32_t zero[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (c * REP / 4 != rep && (c & 1) == half) tmem_st16(TM_SM + 32 * c, zero);
+        }
+        if (pending) add();
+        // the weights are where the products want them
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(PREADY));
+        // ---- the running maxima, and the factors of the results
+        alpha = 1.f; beta = 0.f;
+        if (!none) {
+          const float Mn = fmaxf(M, top), down = M - Mn, up = top - Mn;
+          l = fmaf(sum, fast_exp2(up), l * fast_exp2(down));
+          const float r_old = R + down, r_new = E + up, Rn = fmaxf(r_old, r_new);
+          alpha = fast_exp2(r_old - Rn);
+          beta = fast_exp2(r_new - Rn - 8.f);
+          M = Mn; R = Rn;
+        }
+        pending = true;
+        ++m;
+        look();
+      }
+      // the next item's query rows, while the last products run
+      live = wk.next(prefix, seq_len, p.has_new, share0);
+      if (live) bring_query(item + 1);
+
+      // ---- the block's own rows: eight query rows a warp (sixteen of 128), as columns; products in bf16 as they are, weights as two bf16
+      // terms, 2^-32 as large: sums of rows next to the largest number stay numbers
+      constexpr int ON = RT > 64 ? 2 : 1;            // eights of a warp
+      const int n8 = lane >> 2, t4 = lane & 3;
+      float od[ON][DH / 16][4], om[ON][2], ol[ON][2];
+      float2* own = reinterpret_cast<float2*>(sm + S::OWN_OFF) + (item & 1) * GROUP;
+      if (owned) {
+        unsigned char* vrows = sm + S::MEET_OFF;
+        const int keys = (p.n_q + 15) & ~15;
+        const char* kbase = p.kn + (int64_t)b * p.n_sb + (int64_t)h * p.n_sh;
+        const char* vbase = p.vn + (int64_t)b * p.n_sb + (int64_t)h * p.n_sh;
+#pragma unroll 1
+        for (int e = threadIdx.x; e < keys * (DH / 8); e += SOFT) {
+          const int key = e / (DH / 8), c = e % (DH / 8);
+          uint4 x = make_uint4(0, 0, 0, 0);
+          if (key < p.n_q) x = *(reinterpret_cast<const uint4*>(vbase + (int64_t)key * p.n_sr) + c);
+          kvq::make_finite(x);
+          *reinterpret_cast<uint4*>(vrows + key * S::OWN_PITCH + 16 * c) = x;
+        }
+        uint4 qr[ON][DH / 32];
+#pragma unroll
+        for (int o = 0; o < ON; ++o) {
+          int i, hq;
+          row_of(p, h, r0 + 8 * (ON * warp + o) + n8, i, hq);
+          const bool there = 8 * (ON * warp + o) + n8 < rows;
+          const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh) + t4 * (DH / 32);
+#pragma unroll
+          for (int j = 0; j < DH / 32; ++j) qr[o][j] = there ? src[j] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int ct = 0; ct < DH / 16; ++ct) od[o][ct][0] = od[o][ct][1] = od[o][ct][2] = od[o][ct][3] = 0.f;
+          om[o][0] = om[o][1] = -CUDART_INF_F;
+          ol[o][0] = ol[o][1] = 0.f;
+        }
+        soft_sync();
+#pragma unroll 1
+        for (int k0 = 0; k0 < keys && 8 * ON * warp < rows; k0 += 16) {
+          uint4 kr[2][DH / 32];
+          float sc[ON][4], kf[2] = {p.c, p.c};
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int key = k0 + 8 * i + n8;
+            const uint4* src = reinterpret_cast<const uint4*>(kbase + (int64_t)key * p.n_sr) + t4 * (DH / 32);
+#pragma unroll
+            for (int j = 0; j < DH / 32; ++j) kr[i][j] = key < p.n_q ? src[j] : make_uint4(0, 0, 0, 0);
+          }
+          uint32_t big[2] = {0, 0};
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < DH / 32; ++j) big[i] = max(big[i], kvq::max_bits(kr[i][j]));
+          if (__any_sync(0xFFFFFFFFu, max(big[0], big[1]) >= 0x7200u)) {       // (from 2^101 on: what is not finite, and sums that fp32 would not hold)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              big[i] = max(big[i], __shfl_xor_sync(0xFFFFFFFFu, big[i], 1));
+              big[i] = max(big[i], __shfl_xor_sync(0xFFFFFFFFu, big[i], 2));
+#pragma unroll
+              for (int j = 0; j < DH / 32; ++j) {
+                kvq::make_finite(kr[i][j]);
+                if (big[i] >= 0x7200u) kr[i][j] = kvq::scale_bf16(kr[i][j], 0x1p-64f);
+              }
+              if (big[i] >= 0x7200u) kf[i] = p.c * 0x1p64f;
+            }
+          }
+          uint32_t ph[ON][2], pl[ON][2];
+#pragma unroll
+          for (int o = 0; o < ON; ++o) {
+            sc[o][0] = sc[o][1] = sc[o][2] = sc[o][3] = 0.f;
+#pragma unroll
+            for (int j = 0; j < DH / 32; ++j) {
+              mma_bf16(sc[o], kr[0][j].x, kr[1][j].x, kr[0][j].y, kr[1][j].y, qr[o][j].x, qr[o][j].y);
+              mma_bf16(sc[o], kr[0][j].z, kr[1][j].z, kr[0][j].w, kr[1][j].w, qr[o][j].z, qr[o][j].w);
+            }
+            float down[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const int r = 8 * (ON * warp + o) + 2 * t4 + c;
+              const uint64_t see = r < rows ? reinterpret_cast<const uint64_t*>(sm + S::MASK_OFF)[(r0 + r) >> p.gsh] : 0ull;     // Eq. 5
+              float top = om[o][c];
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                float& y = sc[o][2 * i + c];
+                y *= kf[i];                          // (a row that is not finite: NaN here, and at the end)
+                y = (see >> (k0 + 8 * i + n8)) & 1ull ? (y > SCORE_MAX ? SCORE_MAX : y < -SCORE_MAX ? -SCORE_MAX : y) : -CUDART_INF_F;
+                top = fmaxf(top, y);
+              }
+#pragma unroll
+              for (int k = 4; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, k));
+              down[c] = om[o][c] == top ? 1.f : fast_exp2(om[o][c] - top);
+              om[o][c] = top;
+              const float from = top == -CUDART_INF_F ? 0.f : top;
+              ol[o][c] *= down[c];
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                float& y = sc[o][2 * i + c];
+                y = fast_exp2(y - from);
+                ol[o][c] += y;
+              }
+            }
+            if (__any_sync(0xFFFFFFFFu, down[0] != 1.f || down[1] != 1.f)) {
+#pragma unroll
+              for (int ct = 0; ct < DH / 16; ++ct) { od[o][ct][0] *= down[0]; od[o][ct][1] *= down[1]; od[o][ct][2] *= down[0]; od[o][ct][3] *= down[1]; }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float w0 = sc[o][2 * i] * 0x1p-32f, w1 = sc[o][2 * i + 1] * 0x1p-32f;
+              const __nv_bfloat162 hi = __floats2bfloat162_rn(w0, w1);
+              const uint32_t hw = *reinterpret_cast<const uint32_t*>(&hi);
+              float l0, l1;
+              low_terms(hw, w0, w1, l0, l1);
+              const __nv_bfloat162 lo = __floats2bfloat162_rn(l0, l1);
+              ph[o][i] = transpose8(hw);
+              pl[o][i] = transpose8(*reinterpret_cast<const uint32_t*>(&lo));
+            }
+          }
+#pragma unroll
+          for (int ct = 0; ct < DH / 16; ++ct) {
+            uint32_t a0, a1, a2, a3;
+            const uint32_t at = base + S::MEET_OFF + (k0 + 8 * (lane >> 4) + (lane & 7)) * S::OWN_PITCH + ct * 32 + ((lane >> 3) & 1) * 16;
+            asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                         : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3) : "r"(at) : "memory");
+#pragma unroll
+            for (int o = 0; o < ON; ++o) {
+              mma_bf16(od[o][ct], a0, a1, a2, a3, ph[o][0], ph[o][1]);
+              mma_bf16(od[o][ct], a0, a1, a2, a3, pl[o][0], pl[o][1]);
+            }
+          }
+        }
+#pragma unroll
+        for (int o = 0; o < ON; ++o)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+#pragma unroll
+            for (int k = 4; k < 32; k <<= 1) ol[o][c] += __shfl_xor_sync(0xFFFFFFFFu, ol[o][c], k);
+            const int r = 8 * (ON * warp + o) + 2 * t4 + c;
+            if (n8 == 0 && r < RT) own[r] = make_float2(om[o][c], ol[o][c]);
+          }
+      }
+      if (pending) { ask(); add(); }
+
+      // ---- the item's rows, or its piece of them
+      const int slot = 2 * (int)blockIdx.x + (opens ? 0 : 1);
+      constexpr int SLOT = RT * (DH + 2);
+      float* ps = p.part + (int64_t)slot * SLOT;
+      const float NAN_F = __int_as_float(0x7FFFFFFF);
+      float2* ml = reinterpret_cast<float2*>(sm + S::ML_OFF) + (item & 1) * SOFT;
+      ml[threadIdx.x] = make_float2(M, l);
+      soft_sync();
+      auto total = [&](int r, float& Mx, float& Lx) {        // a row's largest score and sum over all that it has seen
+        const float2 mine = owned ? own[r] : make_float2(-CUDART_INF_F, 0.f);
+        Mx = mine.x;
+#pragma unroll
+        for (int k = 0; k < REP; ++k) Mx = fmaxf(Mx, ml[k * RT + r].x);
+        Lx = mine.x == -CUDART_INF_F ? 0.f : mine.y * fast_exp2(mine.x - Mx);
+#pragma unroll
+        for (int k = 0; k < REP; ++k) {
+          const float2 v = ml[k * RT + r];
+          Lx += v.x == -CUDART_INF_F ? 0.f : (v.y + ml[GROUP + k * RT + r].y) * fast_exp2(v.x - Mx);
+        }
+      };
+      float Mx, Lx;
+      total(row, Mx, Lx);
+      float fac = M == -CUDART_INF_F ? 0.f : fast_exp2(M - Mx) / Lx * fast_exp2(R);
+      if (nan && Mx != -CUDART_INF_F) fac = Lx = NAN_F;
+      if (row < rows && rep == 0 && half == 0) {
+        if (whole) {
+          store_lse(p, b, h, r0 + row, Mx, Lx);
+        } else {
+          __stcg(ps + RT * DH + row, Mx); __stcg(ps + RT * DH + RT + row, Lx);
+        }
+      }
+      float ofac[ON][2];                             // of the block's own rows' results
+#pragma unroll
+      for (int o = 0; o < ON; ++o)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int r = min(8 * (ON * warp + o) + 2 * t4 + c, RT - 1);
+          float Mo, Lo;
+          total(r, Mo, Lo);
+          ofac[o][c] = !owned || om[o][c] == -CUDART_INF_F ? 0.f : fast_exp2(om[o][c] - Mo) / Lo * 0x1p32f;
+        }
+      // a row's copies meet, and what its block's own rows gave, MEET channels of each half at a time
+      float* buf = reinterpret_cast<float*>(sm + S::MEET_OFF);               // [MEET][PITCH]
+#pragma unroll
+      for (int c0 = 0; c0 < DH / 2; c0 += S::MEET) {
+#pragma unroll
+        for (int c = 0; c < S::MEET / 2; ++c) {
+          float a, b;
+          unpack2(o2[c0 / 2 + c], a, b);
+          buf[(2 * c) * S::PITCH + threadIdx.x] = a * fac;
+          buf[(2 * c + 1) * S::PITCH + threadIdx.x] = b * fac;
+        }
+        soft_sync();
+        if (owned) {                                 // (onto the first copy; a row that is not a number has been made one already)
+#pragma unroll
+          for (int o = 0; o < ON; ++o) {
+            const int r = 8 * (ON * warp + o) + 2 * t4;
+            if (r >= rows) continue;
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+              for (int ct = 0; ct < S::MEET / 16; ++ct)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  float& at = buf[(16 * ct + 8 * (e >> 1) + n8) * S::PITCH + hf * GROUP + r + (e & 1)];
+                  at = fmaf(od[o][(hf * (DH / 2) + c0) / 16 + ct][e], ofac[o][e & 1], at);
+                }
+          }
+          soft_sync();
+        }
+        constexpr int QUADS = 2 * S::MEET / 4;       // of a row, both halves
+#pragma unroll 1
+        for (int e = threadIdx.x; e < rows * QUADS; e += SOFT) {
+          const int r = e / QUADS, q = e % QUADS, hf = q / (QUADS / 2), c = 4 * (q % (QUADS / 2));
+          float y[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            y[j] = 0.f;
+#pragma unroll
+            for (int k = 0; k < REP; ++k) y[j] += buf[(c + j) * S::PITCH + hf * GROUP + k * RT + r];
+          }
+          const int c4 = (hf * (DH / 2) + c0 + c) / 4;
+          const float4 o = make_float4(y[0], y[1], y[2], y[3]);
+          if (whole) store_row4<DH>(p, b, h, r0 + r, c4, o);
+          else __stcg(reinterpret_cast<float4*>(ps + r * DH) + c4, o);
+        }
+        soft_sync();
+      }
+      if (*abort_flag && p.status && threadIdx.x == 0) atomicOr(p.status + b, SPACE_ST_TIMEOUT);
+      if (!whole) {
+        const uint32_t piece0 = cut.owner(item_at + SHARE_COST);
+        const int pieces = (int)(cut.owner(item_at + SHARE_COST + T - 1) - piece0) + 1;
+        if (threadIdx.x == 0) {
+          __threadfence();                           // (after the barrier: for all the stores)
+          int* arrived = p.arrived + (b * p.H_kv * p.n_rt + it);
+          const int last = atomicAdd(arrived, 1) == pieces - 1;
+          if (last) *arrived = 0;                    // ready for the next call
+          __threadfence();
+          *last_flag = last;
+        }
+        soft_sync();
+        if (*last_flag) join_pieces<DH, RT, 4, 4>(p, cut, b, h, r0, rows, piece0, pieces, item_at, (int)threadIdx.x, SOFT);
+        soft_sync();                                 // the flag is free for the next item
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+}
+
+template <int DH>
+size_t smem_bytes(int max_batch) { return Smem<DH>::TABLE_OFF + (size_t)(max_batch + 1) * 4 + (size_t)max_batch * 4; }
+
+template <int DH, int REP>
+cudaError_t launch_dim(Params& p, const space_ctx* ctx, cudaStream_t st) {
+  static unsigned long long done_mask = 0;           // devices on which the kernel may have its shared memory
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev >= 64 || !((done_mask >> dev) & 1ull)) {
+    const cudaError_t e = cudaFuncSetAttribute(kvb_attn_tc_kernel<DH, REP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<DH>(128));
+    if (e != cudaSuccess) return e;
+    if (dev < 64) done_mask |= 1ull << dev;
+  }
+  static_assert(TILE / REP <= KVB_SM_ROWS, "a slot per block");
+  p.n_rt = (p.n_q * p.G + TILE / REP - 1) / (TILE / REP);
+  p.n_groups = ctx->sm_count;
+  return launch_pdl(kvb_attn_tc_kernel<DH, REP>, dim3(p.n_groups), dim3(THREADS), smem_bytes<DH>(ctx->cfg.max_batch), st, p, ctx->cfg.max_batch);
+}
+
+}  // namespace
+
+int launch_kvb_attn_tc(space_ctx* ctx, kvb::Params& p, cudaStream_t st) {
+  const bool wide = ctx->cfg.head_dim == 128;
+  const int rows = p.n_q * p.G, rep = rows <= 32 ? 4 : 2;
+  cudaError_t e;
+  if (wide) e = rep == 4 ? launch_dim<128, 4>(p, ctx, st) : launch_dim<128, 2>(p, ctx, st);
+  else e = rep == 4 ? launch_dim<64, 4>(p, ctx, st) : launch_dim<64, 2>(p, ctx, st);
+  return cuda_ok(e);
+}
