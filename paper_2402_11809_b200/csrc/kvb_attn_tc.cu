@@ -47,7 +47,8 @@ struct Smem {
   static constexpr int ML_OFF = SCALE_OFF + RING * 32;       // [2][SOFT] {M, l} of rows' halves and copies, by item
   static constexpr int OWN_OFF = ML_OFF + 2 * SOFT * 8;      // [2][128] {M, l} of rows over the block's own rows
   static constexpr int XCH_OFF = OWN_OFF + 2 * GROUP * 8;    // [2][SOFT] a page's {largest score, E} of a row's halves
-  static constexpr int DESC_OFF = XCH_OFF + 2 * SOFT * 8;    // [RING] {item of the share, page of it}
+  static constexpr int TOPS_OFF = XCH_OFF + 2 * SOFT * 8;    // [2][SOFT] largest elements of query rows' halves, by item
+  static constexpr int DESC_OFF = TOPS_OFF + 2 * SOFT * 4;   // [RING] {item of the share, page of it}
   static constexpr int BAR_OFF = DESC_OFF + RING * 8;
   static constexpr int N_BARS = 4 * STAGES + RING + 13;
   static constexpr int MISC_OFF = BAR_OFF + N_BARS * 8;
@@ -217,6 +218,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
   wk.b = 0; wk.cur = share0;
   wk.end = mine ? cut.begin(blockIdx.x + 1) : 0;
   uint32_t m = 0;                                    // pages so far
+  uint32_t queries = 0;                              // items with pages so far: others' query rows nobody announces or waits for
   auto hold = [&](int bar, uint32_t use, int site) { return wait(BAR(bar), use & 1, abort_flag, p.err, site); };
 
   if (warp >= 8) {
@@ -277,7 +279,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           if (it == NO_MORE) { more = false; break; }
           if (it != item) {
             if (q > m) break;                        // (its query rows come when the weights of page m have)
-            ok = hold(QREADY, it, 4) && ok;
+            ok = hold(QREADY, queries++, 4) && ok;
             item = it;
           }
           const uint32_t s = q % STAGES;
@@ -290,7 +292,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
             for (int i = 0; i < 2; ++i)
 #pragma unroll
               for (int ks = 0; ks < DH / 32; ++ks)
-                mma8_ts(TM_S + (q & 1) * TILE, TM_Q + (item & 1) * 64 + i * (DH / 4) + 8 * ks, kd + (uint64_t)((ks * 2 * F::K_COLS) >> 4), instr_desc(TILE), i + ks > 0);
+                mma8_ts(TM_S + (q & 1) * TILE, TM_Q + ((queries - 1) & 1) * 64 + i * (DH / 4) + 8 * ks, kd + (uint64_t)((ks * 2 * F::K_COLS) >> 4), instr_desc(TILE), i + ks > 0);
           }
           tc_commit(BAR(SDONE + (q & 1)));
           tc_commit(BAR(FREEK + s));
@@ -344,7 +346,14 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
     const uint32_t lanes = (uint32_t)(32 * w4) << 16;
     const int key0 = rep * (TILE / REP) + half * KEYS;       // first of this thread's keys of a page
     const uint32_t TM_C = TM_O + lanes + half * (DH / 2);
-    // The query row of the item that wk stands at, this thread's half of it, as two terms into a buffer.
+    // What is announced of page m.
+    int next_item, next_page;
+    auto look = [&]() {
+      hold(SAID + m % RING, m / RING, 12);
+      next_item = *abort_flag ? NO_MORE : desc[m % RING].x;
+      next_page = desc[m % RING].y;
+    };
+    // The query row of the item that wk stands at, this thread's half of it: as two terms into a buffer, if the item has pages.
     float f_next = 0.f;                              // factor of its scores
     bool nan_next = false;                           // it holds a NaN or an infinity
     auto bring_query = [&](int item) {
@@ -358,7 +367,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
       for (int j = 0; j < DH / 16; ++j) v[j] = i < p.n_q ? src[j] : make_uint4(0, 0, 0, 0);
 #pragma unroll
       for (int j = 0; j < DH / 16; ++j) top = max(top, kvq::max_bits(v[j]));
-      uint32_t* tops = reinterpret_cast<uint32_t*>(sm + S::ML_OFF) + 2 * SOFT * (item & 1);        // (sums of the item before last were there)
+      uint32_t* tops = reinterpret_cast<uint32_t*>(sm + S::TOPS_OFF) + SOFT * (item & 1);
       tops[threadIdx.x] = top;
       __syncwarp();
       if (lane == 0) mbar_arrive(BAR(QTOP + w4));
@@ -368,6 +377,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
       const int e = nan_next ? 0 : max((int)(top >> 7) - 127, -100) - 7;       // the largest element to [2^7, 2^8)
       const float up = pow2(-e);
       f_next = p.c * pow2(e);
+      if (item == 0) look();
+      if (next_item != item) return;
+      const uint32_t to0 = TM_Q + lanes + (queries++ & 1) * 64 + half * (DH / 8);
 #pragma unroll
       for (int j = 0; j < DH / 16; j += 2) {
         uint32_t w0[4], w1[4];
@@ -377,25 +389,16 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           split4(kvq::bf_lo(x.x) * up, kvq::bf_hi(x.x) * up, kvq::bf_lo(x.y) * up, kvq::bf_hi(x.y) * up, w0[2 * k], w1[2 * k]);
           split4(kvq::bf_lo(x.z) * up, kvq::bf_hi(x.z) * up, kvq::bf_lo(x.w) * up, kvq::bf_hi(x.w) * up, w0[2 * k + 1], w1[2 * k + 1]);
         }
-        const uint32_t to = TM_Q + lanes + (item & 1) * 64 + half * (DH / 8) + 2 * j;
-        tmem_st4(to, w0);
-        tmem_st4(to + DH / 4, w1);
+        tmem_st4(to0 + 2 * j, w0);
+        tmem_st4(to0 + 2 * j + DH / 4, w1);
       }
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(BAR(QREADY));
     };
-    // What is announced of page m.
-    int next_item, next_page;
-    auto look = [&]() {
-      hold(SAID + m % RING, m / RING, 12);
-      next_item = *abort_flag ? NO_MORE : desc[m % RING].x;
-      next_page = desc[m % RING].y;
-    };
     bool live = wk.next(prefix, seq_len, p.has_new, share0);
     if (live) bring_query(0);
-    look();
     for (int item = 0; live; ++item) {
       const int b = wk.b, it = wk.it, L = wk.L, T = wk.pages(p.has_new);
       const bool whole = wk.t0 == 0 && wk.t1 == T, opens = wk.opens, owned = p.has_new && L >= 0 && wk.t1 > wk.cached();
@@ -407,25 +410,26 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
 #pragma unroll
       for (int j = 0; j < DH / 4; ++j) o2[j] = 0ull;
       float M = -CUDART_INF_F, l = 0.f, R = 0.f, alpha = 1.f, beta = 0.f;
-      // A page's result joins the sum: asked for, and, when it has come, added.
+      // A page's result joins the sum.  (A load from tensor memory and the wait for it stand side by side: its registers may not be
+      // touched in between, which the compiler does not know.)
       bool pending = false;
-      uint32_t res[DH / 2];
-      auto ask = [&]() {
+      auto add = [&]() {
         hold(ODONE, m - 1, 13);
         tc_fence_after();
-#pragma unroll
-        for (int c = 0; c < DH / 2; c += 32) tmem_ld32(TM_C + c, res + c);
-      };
-      auto add = [&]() {
         if (__any_sync(0xFFFFFFFFu, alpha != 1.f)) {
           const uint64_t a2 = pack2(alpha, alpha);
 #pragma unroll
           for (int j = 0; j < DH / 4; ++j) o2[j] = mul2(o2[j], a2);
         }
         const uint64_t b2 = pack2(beta, beta);
-        tmem_wait_ld();
 #pragma unroll
-        for (int j = 0; j < DH / 4; ++j) o2[j] = fma2(pack2(__uint_as_float(res[2 * j]), __uint_as_float(res[2 * j + 1])), b2, o2[j]);
+        for (int c = 0; c < DH / 2; c += 32) {
+          uint32_t r[32];
+          tmem_ld32(TM_C + c, r);
+          tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o2[c / 2 + j] = fma2(pack2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), b2, o2[c / 2 + j]);
+        }
         tc_fence_before();
       };
       while (next_item == item) {
@@ -461,9 +465,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           if (KEYS < 32) tmem_ld16(TM_SM + key0, v);
           else tmem_ld32(TM_SM + key0 + 32 * k, v + 32 * k);
         }
+        tmem_wait_ld();
         // ---- largest scores
         float fk[NC], ms[NC], mb[NC], x[NC], pm = -CUDART_INF_F, E = -CUDART_INF_F;
-        tmem_wait_ld();
         if (vis < KEYS) {
 #pragma unroll
           for (int j = 0; j < KEYS; ++j) if (j >= vis) v[j] = 0xFF800000u;
@@ -505,7 +509,6 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
         xch[threadIdx.x] = make_float2(pm, E);
         __syncwarp();
         if (lane == 0) mbar_arrive(BAR(XCH + w4));
-        if (pending) ask();
         hold(XCH + w4, m, 16);
         const float2 other = xch[threadIdx.x ^ GROUP];
         const float top = fmaxf(pm, other.x), lower = pm - top;
@@ -716,7 +719,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
             if (n8 == 0 && r < RT) own[r] = make_float2(om[o][c], ol[o][c]);
           }
       }
-      if (pending) { ask(); add(); }
+      if (pending) add();
 
       // ---- the item's rows, or its piece of them
       const int slot = 2 * (int)blockIdx.x + (opens ? 0 : 1);
