@@ -12,7 +12,7 @@
 namespace {
 using namespace kvb;
 
-constexpr int THREADS = 256, Q_PAIRS = 4;
+constexpr int THREADS = 256, Q_ROWS = 2;
 constexpr float BF16_MAX = 3.3895313892515355e38f;
 
 struct AppendParams {
@@ -49,41 +49,23 @@ __device__ __forceinline__ uint32_t coarser(uint32_t w, float ratio) {
   return codes4(a.x * ratio, a.y * ratio, b.x * ratio, b.y * ratio);
 }
 
-// Queries of sequence b, beside the append: pairs of (row, head) as in rope.cu.
+// Queries of two rows of sequence b, beside the append.
 template <int DH>
-__device__ __forceinline__ void turn_queries(const AppendParams& p, int b, uint32_t block) {
-  constexpr int LANES = DH / 8, SLOTS = THREADS / LANES;
-  const int x = threadIdx.x % LANES;
+__device__ __forceinline__ void turn_queries(const AppendParams& p, int b, int block) {
   const int L = p.kv_len[b], n = append_count(p, b, L);
-  if (n <= 0 || (int64_t)block * (SLOTS * Q_PAIRS) >= (int64_t)n * p.H_q) return;
-  const uint32_t pair0 = block * (uint32_t)(SLOTS * Q_PAIRS) + threadIdx.x / LANES;
-  uint4 v[Q_PAIRS];
-  rope::Turn u[Q_PAIRS];
-  char* to[Q_PAIRS];
-#pragma unroll
-  for (int j = 0; j < Q_PAIRS; ++j) {
-    const uint32_t pair = pair0 + j * SLOTS;
-    const int g = (int)(pair / (uint32_t)p.H_q), h = (int)(pair - (uint32_t)g * p.H_q);
-    v[j] = make_uint4(0, 0, 0, 0);
-    to[j] = nullptr;
-    if (g < n) {
-      const int64_t r = (int64_t)g * p.step;
-      bool bad;
-      v[j] = *(reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_sb + r * p.q_sr + (int64_t)h * p.q_sh) + x);
-      rope::load_turn(p.t, rope::table_row(p.t, b, p.rows, (int)r, (int64_t)L + g, bad), x, u[j]);
-      to[j] = p.q_out + (int64_t)b * p.o_sb + r * p.o_sr + (int64_t)h * p.o_sh;
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < Q_PAIRS; ++j) {
-    float y[8];
-    rope::turn_row<LANES>(p.t, v[j], x, u[j], y);
-    if (to[j]) *(reinterpret_cast<uint4*>(to[j]) + x) = rope::pack8(y);
+#pragma unroll 1
+  for (int g = block * Q_ROWS; g < min((block + 1) * Q_ROWS, n); ++g) {
+    const int64_t r = (int64_t)g * p.step;
+    bool bad;
+    const float* row = rope::table_row(p.t, b, p.rows, (int)r, (int64_t)L + g, bad);
+    const char* from = p.q + (int64_t)b * p.q_sb + r * p.q_sr;
+    char* to = p.q_out + (int64_t)b * p.o_sb + r * p.o_sr;
+    rope::turn_heads<DH, THREADS>(p.t, row, p.H_q, p.H_q, [&](int h) { return from + (int64_t)h * p.q_sh; }, [&](int h) { return to + (int64_t)h * p.o_sh; });
   }
 }
 
 template <int DH>
-__global__ void __launch_bounds__(THREADS) kvb_append_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(THREADS, 4) kvb_append_kernel(const __grid_constant__ AppendParams p) {
   using F = Fmt<DH>;
   using VT = VTile<DH>;
   constexpr int LANES = DH / 8, ROWS = THREADS / LANES, PASSES = BLOCK_ROWS / ROWS;
@@ -93,7 +75,7 @@ __global__ void __launch_bounds__(THREADS) kvb_append_kernel(const __grid_consta
   pdl_wait();
   if ((int64_t)blockIdx.x >= p.n_append) {
     const uint32_t rest = blockIdx.x - (uint32_t)p.n_append;
-    turn_queries<DH>(p, (int)(rest / (uint32_t)p.q_blocks), rest % (uint32_t)p.q_blocks);
+    turn_queries<DH>(p, (int)(rest / (uint32_t)p.q_blocks), (int)(rest % (uint32_t)p.q_blocks));
     return;
   }
   const uint32_t bh = blockIdx.x / (uint32_t)p.blocks;
@@ -320,10 +302,7 @@ int launch_kvb_append(space_ctx* ctx, const space_kvb_append_args* a, cudaStream
   if (a->q) {
     p.q = (const char*)a->q; p.q_sb = 2 * a->q_stride_b; p.q_sr = 2 * a->q_stride_r; p.q_sh = 2 * a->q_stride_h;
     p.q_out = (char*)a->q_out; p.o_sb = 2 * a->q_out_stride_b; p.o_sr = 2 * a->q_out_stride_r; p.o_sh = 2 * a->q_out_stride_h;
-    const int per_block = THREADS / (d / 8) * Q_PAIRS;
-    const int64_t pairs = (int64_t)p.max_count * p.H_q;
-    if (pairs > 0x7FFF0000ll) return SPACE_E_UNSUPPORTED;
-    p.q_blocks = (int)((pairs + per_block - 1) / per_block);
+    p.q_blocks = (p.max_count + Q_ROWS - 1) / Q_ROWS;
     grid += (int64_t)p.B * p.q_blocks;
   }
   if (grid > 0x7FFFFFFFll) return SPACE_E_UNSUPPORTED;

@@ -9,7 +9,8 @@
 
 namespace {
 
-constexpr int THREADS = 256, ROWS_AHEAD = 4;
+constexpr int THREADS = 256, AHEAD = 2;              // rows on their way at a time
+constexpr int ROW_TOKENS = 8;                        // of a thread, where a sequence has one row (twice as many on the 16-byte grid)
 constexpr int COUNT_MAX = (1 << 24) - 1;             // (an fp32 number exactly)
 
 struct Params {
@@ -26,28 +27,6 @@ struct Params {
   unsigned long long* alive; int* arrived;           // per sequence: rows with a token left, thread blocks that have said so
 };
 
-template <typename T> __device__ __forceinline__ void unpack(const uint4& v, float* z);
-template <> __device__ __forceinline__ void unpack<float>(const uint4& v, float* z) {
-  z[0] = __uint_as_float(v.x); z[1] = __uint_as_float(v.y); z[2] = __uint_as_float(v.z); z[3] = __uint_as_float(v.w);
-}
-template <> __device__ __forceinline__ void unpack<__nv_bfloat16>(const uint4& v, float* z) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { z[2 * i] = __uint_as_float(w[i] << 16); z[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-}
-template <typename T> __device__ __forceinline__ uint4 pack(const float* z);
-template <> __device__ __forceinline__ uint4 pack<float>(const float* z) {
-  return make_uint4(__float_as_uint(z[0]), __float_as_uint(z[1]), __float_as_uint(z[2]), __float_as_uint(z[3]));
-}
-template <> __device__ __forceinline__ uint4 pack<__nv_bfloat16>(const float* z) {
-  uint32_t r[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(z[2 * i], z[2 * i + 1]);
-    r[i] = *reinterpret_cast<const uint32_t*>(&v);
-  }
-  return make_uint4(r[0], r[1], r[2], r[3]);
-}
 // The elements [lo, hi) of a vector that holds those of `row` from x on.
 template <typename T>
 __device__ __forceinline__ void store_some(T* row, int64_t x, const uint4& v, int lo, int hi) {
@@ -61,174 +40,349 @@ __device__ __forceinline__ void store_some(T* row, int64_t x, const uint4& v, in
   }
 }
 
+// An element of a vector, wherever it lies, and the vector with another one there.
+template <typename T> __device__ __forceinline__ float element(const uint4& v, int t);
+template <> __device__ __forceinline__ float element<float>(const uint4& v, int t) {
+  return __uint_as_float(t & 2 ? (t & 1 ? v.w : v.z) : (t & 1 ? v.y : v.x));
+}
+template <> __device__ __forceinline__ float element<__nv_bfloat16>(const uint4& v, int t) {
+  const uint32_t w = t & 4 ? (t & 2 ? v.w : v.z) : (t & 2 ? v.y : v.x);
+  return __uint_as_float(t & 1 ? w & 0xFFFF0000u : w << 16);
+}
 template <typename T>
-__global__ void __launch_bounds__(THREADS) logits_adjust_kernel(const __grid_constant__ Params p) {
-  constexpr int N = 16 / (int)sizeof(T), CHUNK = THREADS * N;
-  constexpr uint32_t ALL = (1u << N) - 1u;
-  __shared__ float bias_s[CHUNK];
-  __shared__ int32_t tok_s[SPACE_LOGITS_MAX_BIAS];
-  __shared__ float val_s[SPACE_LOGITS_MAX_BIAS];
+__device__ __forceinline__ void set_element(uint4& v, int t, float z) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  const uint32_t bits = sizeof(T) == 4 ? __float_as_uint(z) : (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(z)) << (16 * (t & 1));
+  const uint32_t mask = sizeof(T) == 4 ? 0xFFFFFFFFu : 0xFFFFu << (16 * (t & 1));
+  const int at = sizeof(T) == 4 ? t : t >> 1;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i == at) w[i] = (w[i] & ~mask) | bits;
+  v = make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Elements whose bit is 0 become -infinity.
+template <typename T>
+__device__ __forceinline__ void mask_out(uint4& v, uint32_t keep) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  if (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (!((keep >> i) & 1u)) w[i] = 0xFF800000u;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {                 // four bits to the tops of four bytes, each byte's top all over two bytes
+      const uint32_t tops = ((keep >> (2 * i)) & 0xFu) * 0x10204080u & 0x80808080u;
+      const uint32_t m0 = __byte_perm(tops, 0, 0x9988), m1 = __byte_perm(tops, 0, 0xBBAA);
+      w[i] = (w[i] & m0) | (0xFF80FF80u & ~m0);
+      w[i + 1] = (w[i + 1] & m1) | (0xFF80FF80u & ~m1);
+    }
+  }
+  v = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// GRID: every row begins on the 16-byte grid.
+// Sixteen bytes of a row, the first `there` elements from x on; nothing behind them is read.
+template <bool GRID, typename T>
+__device__ __forceinline__ Piece2 fetch(const T* row, int x, int there) {
+  constexpr int N = 16 / (int)sizeof(T);
+  if (there == N && !GRID) return load_pieces(row, x);
+  if (there == N) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>(row + x));
+    return Piece2{v, v};
+  }
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (e < there) {
+      if (sizeof(T) == 4) w[e % 4] = reinterpret_cast<const uint32_t*>(row)[x + e];
+      else w[(e >> 1) % 4] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[x + e] << (16 * (e & 1));
+    }
+  Piece2 r;
+  r.a = r.b = make_uint4(w[0], w[1], w[2], w[3]);
+  return r;
+}
+template <bool GRID, typename T>
+__device__ __forceinline__ uint4 shifted(const Piece2& got, const T* row, int there) {
+  return !GRID && there == 16 / (int)sizeof(T) ? shift_pieces(got, row) : got.a;
+}
+// Sixteen bytes: the first n of them to lo, the others to hi + n (lo and hi on the 16-byte grid).
+template <typename T>
+__device__ __forceinline__ void store_edges(char* lo, char* hi, const uint4& s, int n) {
+  const uint32_t w[4] = {s.x, s.y, s.z, s.w};
+  if (n & 8) *reinterpret_cast<uint2*>(lo) = make_uint2(w[0], w[1]);
+  if (n & 4) *reinterpret_cast<uint32_t*>(lo + (n & 8)) = n & 8 ? w[2] : w[0];
+  if (sizeof(T) == 2 && (n & 2)) {
+    const uint32_t both = n & 8 ? (n & 4 ? w[3] : w[2]) : (n & 4 ? w[1] : w[0]);
+    *reinterpret_cast<uint16_t*>(lo + (n & 12)) = (uint16_t)both;
+    *reinterpret_cast<uint16_t*>(hi + n) = (uint16_t)(both >> 16);
+  }
+  const int at = (n + 3) & ~3;
+  if (at & 4) *reinterpret_cast<uint32_t*>(hi + at) = at & 8 ? w[3] : w[1];
+  if (at <= 8) *reinterpret_cast<uint2*>(hi + 8) = make_uint2(w[2], w[3]);
+}
+// The vectors of a warp (neighbouring lanes', the first `there` elements of each) to a row, by all of its lanes.
+template <bool GRID, typename T>
+__device__ __forceinline__ void store_vectors(T* dst, int x, const uint4& v, int there, int vocab) {
+  constexpr int N = 16 / (int)sizeof(T);
+  const int lane = threadIdx.x & 31;
+  const uint32_t off = (uint32_t)((uintptr_t)dst & 15);
+  if (x - lane * N + 32 * N > vocab) {               // the row's end
+    store_some<T>(dst, x, v, 0, there);
+  } else if (GRID || off == 0) {
+    *reinterpret_cast<uint4*>(dst + x) = v;
+  } else {
+    // pieces of the grid: a vector's elements from 16 - off bytes on with the first ones of the next lane's; the last lane has the
+    // warp's last elements and its first ones
+    Piece2 two;
+    const int next = (lane + 1) & 31;
+    two.a = v;
+    two.b.x = __shfl_sync(0xFFFFFFFFu, v.x, next); two.b.y = __shfl_sync(0xFFFFFFFFu, v.y, next);
+    two.b.z = __shfl_sync(0xFFFFFFFFu, v.z, next); two.b.w = __shfl_sync(0xFFFFFFFFu, v.w, next);
+    const uint4 piece = shift_pieces(two, reinterpret_cast<const T*>((uintptr_t)(16 - off)));
+    char* at = reinterpret_cast<char*>(dst + x) + (16 - off);
+    if (lane < 31) *reinterpret_cast<uint4*>(at) = piece;
+    else store_edges<T>(at, at - 32 * 16, piece, (int)off);
+  }
+}
+
+struct Penalty { float rep, pres, freq; };
+__device__ __forceinline__ float penalized(float z, int count, int behind, const Penalty& f) {
+  const int times = min(min(count & (SPACE_COUNT_PROMPT - 1), COUNT_MAX) + behind, COUNT_MAX);
+  if (times > 0 || (count & SPACE_COUNT_PROMPT)) z = z > 0.f ? z / f.rep : z * f.rep;
+  if (times > 0) z = __fsub_rn(__fsub_rn(z, __fmul_rn(f.freq, (float)times)), f.pres);
+  return z;
+}
+
+// The biases of the tokens [t0, t0 + CHUNK): a bit per token that has some, and their sum (in the list's order, whoever adds it up).
+// Starts with a barrier of the block (what the caller has written to shared memory is there), ends with one if a bit is set.
+template <int CHUNK>
+struct Biases {
+  uint32_t some[CHUNK / 32], twice[CHUNK / 32];
+  int again[SPACE_LOGITS_MAX_BIAS], n_again;         // entries of tokens that have several
+  float sum[CHUNK];
+  __device__ __forceinline__ bool collect(const Params& p, int b, int t0) {
+    const int32_t* tok = p.bias_tok + (int64_t)b * p.n_bias;
+    const float* val = p.bias_val + (int64_t)b * p.n_bias;
+    auto mine = [&](int i) {
+      const int t = __ldg(tok + i);
+      return t >= t0 && t - t0 < CHUNK && t < p.V ? t - t0 : -1;
+    };
+    bool any = false;
+    for (int i = threadIdx.x; i < p.n_bias; i += THREADS) any = any || mine(i) >= 0;
+    for (int i = threadIdx.x; i < CHUNK / 32; i += THREADS) some[i] = twice[i] = 0;
+    if (threadIdx.x == 0) n_again = 0;
+    if (!__syncthreads_or(any)) return false;
+    for (int i = threadIdx.x; i < p.n_bias; i += THREADS) {
+      const int t = mine(i);
+      if (t < 0) continue;
+      const uint32_t bit = 1u << (t & 31);
+      if (atomicOr(&some[t >> 5], bit) & bit) atomicOr(&twice[t >> 5], bit);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.n_bias; i += THREADS) {
+      const int t = mine(i);
+      if (t < 0) continue;
+      if ((twice[t >> 5] >> (t & 31)) & 1u) again[atomicAdd(&n_again, 1)] = i;
+      else sum[t] = __ldg(val + i);
+    }
+    __syncthreads();
+    if (n_again == 0) return true;
+    const int lane = threadIdx.x & 31;               // a warp for such an entry: the token's first one adds up all of them
+    for (int e = threadIdx.x >> 5; e < n_again; e += THREADS / 32) {
+      const int i = again[e], t = __ldg(tok + i);
+      float total = 0.f;
+      bool first = true;
+      for (int j0 = 0; j0 < p.n_bias && first; j0 += 32) {
+        const int j = j0 + lane;
+        const bool same = j < p.n_bias && __ldg(tok + j) == t;
+        const float v = same ? __ldg(val + j) : 0.f;
+        uint32_t some_of = __ballot_sync(0xFFFFFFFFu, same);
+        if (some_of && j0 + __ffs(some_of) - 1 < i) first = false;
+        for (; some_of && first; some_of &= some_of - 1) {
+          const int from = __ffs(some_of) - 1;
+          const float add = __shfl_sync(0xFFFFFFFFu, v, from);
+          total = j0 + from == i ? add : total + add;
+        }
+      }
+      if (first && lane == 0) sum[t - t0] = total;
+    }
+    __syncthreads();
+    return true;
+  }
+};
+
+// What the masks leave of a sequence's rows, when all of its thread blocks have said so.
+__device__ __forceinline__ void report(const Params& p, int b, int bad, unsigned long long alive, unsigned long long& all_of_block) {
+  if (bad && p.status) atomicOr(p.status + b, bad);
+  if (!p.status) return;
+  if ((threadIdx.x & 31) == 0 && alive) atomicOr(&all_of_block, alive);
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  if (all_of_block) atomicOr(p.alive + b, all_of_block);
+  __threadfence();
+  if (atomicAdd(p.arrived + b, 1) == p.chunks * p.groups - 1) {
+    __threadfence();
+    const unsigned long long all = p.n == 64 ? ~0ull : (1ull << p.n) - 1ull;
+    if (atomicExch(p.alive + b, 0ull) != all) atomicOr(p.status + b, SPACE_ST_BAD_MASK);
+    p.arrived[b] = 0;
+  }
+}
+
+// Sequences of one row: a thread has UNITS vectors of it, all on their way at once with their counts.
+template <typename T, bool GRID>
+__global__ void __launch_bounds__(THREADS, 4) logits_row_kernel(const __grid_constant__ Params p) {
+  constexpr int N = 16 / (int)sizeof(T), UNITS = (GRID ? 2 * ROW_TOKENS : ROW_TOKENS) / N, UNIT = THREADS * N, CHUNK = UNITS * UNIT;
+  __shared__ Biases<CHUNK> biases;
   __shared__ unsigned long long alive_s;
   pdl_launch_dependents();
   pdl_wait();
-  const int b = blockIdx.z, chunk0 = blockIdx.x * CHUNK, lane = threadIdx.x & 31;
+  const int b = blockIdx.z, chunk0 = blockIdx.x * CHUNK;
   const int x0 = chunk0 + (int)threadIdx.x * N;
-  const int there = min(max(p.V - x0, 0), N);        // tokens of this thread
-  float bias[N];
+  const T* row = reinterpret_cast<const T*>(p.logits) + (int64_t)b * p.in_rs;
+  T* dst = reinterpret_cast<T*>(p.out) + (int64_t)b * p.out_rs;
+  const float* counts = reinterpret_cast<const float*>(p.counts + (int64_t)b * p.V);
+  auto there = [&](int u) { return min(max(p.V - (x0 + u * UNIT), 0), N); };
+  int m = -1, bad = 0;
+  if (p.bits) {
+    m = p.mask_row[b];
+    if (m >= p.n_masks) { bad = SPACE_ST_BAD_MASK; m = -1; }
+  }
+  Piece2 got[UNITS], cnt[UNITS][N / 4];
+  uint32_t keep[UNITS];
 #pragma unroll
-  for (int i = 0; i < N; ++i) bias[i] = 0.f;
+  for (int u = 0; u < UNITS; ++u) {
+    const int x = x0 + u * UNIT, n = there(u);
+    keep[u] = n == 0 ? 0u : m < 0 ? (1u << n) - 1u : (__ldg(p.bits + (int64_t)m * p.words + (x >> 5)) >> (x & 31)) & ((1u << n) - 1u);
+    got[u].a = got[u].b = make_uint4(0, 0, 0, 0);
+    if (keep[u]) got[u] = fetch<GRID>(row, x, n);          // (what the mask leaves nothing of is not read)
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      cnt[u][i].a = cnt[u][i].b = make_uint4(0, 0, 0, 0);
+      if (p.counts && keep[u] && n > 4 * i) cnt[u][i] = fetch<GRID>(counts, x + 4 * i, min(n - 4 * i, 4));
+    }
+  }
+  const Penalty f{p.rep ? p.rep[b] : 1.f, p.pres ? p.pres[b] : 0.f, p.freq ? p.freq[b] : 0.f};
   if (threadIdx.x == 0) alive_s = 0;
-  if (p.n_bias) {
-    for (int i = threadIdx.x; i < CHUNK; i += THREADS) bias_s[i] = 0.f;
-    for (int i = threadIdx.x; i < p.n_bias; i += THREADS) {
-      tok_s[i] = p.bias_tok[(int64_t)b * p.n_bias + i];
-      val_s[i] = p.bias_val[(int64_t)b * p.n_bias + i];
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < p.n_bias; i += THREADS) {
-      const int t = tok_s[i];
-      if (t < chunk0 || t >= chunk0 + CHUNK || t >= p.V) continue;
-      bool first = true;                             // the first entry of a token adds up all of them
-      for (int j = 0; j < i && first; ++j) first = tok_s[j] != t;
-      if (!first) continue;
-      float sum = val_s[i];
-      for (int j = i + 1; j < p.n_bias; ++j)
-        if (tok_s[j] == t) sum += val_s[j];
-      bias_s[t - chunk0] = sum;
-    }
-    __syncthreads();
+  const bool biased = p.n_bias && biases.collect(p, b, chunk0);
+  if (!p.n_bias && p.bits) __syncthreads();
+  unsigned long long alive = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) bias[i] = bias_s[threadIdx.x * N + i];
-  } else {
-    __syncthreads();
+  for (int u = 0; u < UNITS; ++u) {
+    const int x = x0 + u * UNIT, n = there(u);
+    if (chunk0 + u * UNIT >= p.V) break;             // (the same for the whole block)
+    uint4 v = shifted<GRID>(got[u], row, n), c[N / 4];
+    uint32_t hit = 0;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      c[i] = shifted<GRID>(cnt[u][i], counts, min(max(n - 4 * i, 0), 4));
+      hit |= ((c[i].x ? 1u : 0u) | (c[i].y ? 2u : 0u) | (c[i].z ? 4u : 0u) | (c[i].w ? 8u : 0u)) << (4 * i);
+    }
+    const uint32_t bias = biased ? biases.some[(x - chunk0) >> 5] >> (x & 31) : 0u;
+    if (p.bits && __any_sync(0xFFFFFFFFu, keep[u] != 0)) alive = 1;
+    uint32_t act = (hit | bias) & keep[u];
+    const bool touch = !p.in_place || __any_sync(0xFFFFFFFFu, act || (n && keep[u] != (1u << n) - 1u));
+    for (; act; act &= act - 1) {
+      const int t = __ffs(act) - 1;
+      const int count = __float_as_int(element<float>(N == 4 || t < 4 ? c[0] : c[N / 4 - 1], t & 3));
+      float z = penalized(element<T>(v, t), count, 0, f);
+      if ((bias >> t) & 1u) z += biases.sum[x - chunk0 + t];
+      set_element<T>(v, t, z);
+    }
+    if (!touch) continue;
+    if (p.bits) mask_out<T>(v, keep[u]);
+    store_vectors<GRID>(dst, x, v, n, p.V);
   }
-  // counts, and which candidates a token is: bit j of nibble pair i: token x0 + i is candidate j + 1
-  int count[N];
-  unsigned long long is_cand = 0;
+  if (p.bits) report(p, b, bad, alive, alive_s);
+}
+
+// Sequences of n rows: a thread has one vector of tokens, whose counts, biases and candidates stay with it from row to row.
+template <typename T, bool GRID>
+__global__ void __launch_bounds__(THREADS, 4) logits_rows_kernel(const __grid_constant__ Params p) {
+  constexpr int N = 16 / (int)sizeof(T), CHUNK = THREADS * N;
+  __shared__ Biases<CHUNK> biases;
+  __shared__ int32_t mask_s[SPACE_MAX_ROWS];
+  __shared__ unsigned long long alive_s;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int b = blockIdx.z, chunk0 = blockIdx.x * CHUNK;
+  const int x = chunk0 + (int)threadIdx.x * N;
+  const int there = min(max(p.V - x, 0), N);         // tokens of this thread
+  const uint32_t valid = (1u << there) - 1u;
+  const int per = (p.n + p.groups - 1) / p.groups, i0 = blockIdx.y * per, i1 = min(i0 + per, p.n);
+  const T* in0 = reinterpret_cast<const T*>(p.logits) + ((int64_t)b * p.n + i0) * p.in_rs;
+  T* out0 = reinterpret_cast<T*>(p.out) + ((int64_t)b * p.n + i0) * p.out_rs;
+  const float* counts = reinterpret_cast<const float*>(p.counts + (int64_t)b * p.V);
+  Piece2 cnt[N / 4];
 #pragma unroll
-  for (int i = 0; i < N; ++i) count[i] = 0;
-  if (p.counts) {
-    const int32_t* row = p.counts + (int64_t)b * p.V + x0;
-    if (there == N && ((uintptr_t)row & 15) == 0) {
-#pragma unroll
-      for (int i = 0; i < N / 4; ++i) {
-        const int4 c = __ldg(reinterpret_cast<const int4*>(row) + i);
-        count[4 * i] = c.x; count[4 * i + 1] = c.y; count[4 * i + 2] = c.z; count[4 * i + 3] = c.w;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) if (i < there) count[i] = __ldg(row + i);
-    }
+  for (int i = 0; i < N / 4; ++i) {
+    cnt[i].a = cnt[i].b = make_uint4(0, 0, 0, 0);
+    if (p.counts && there > 4 * i) cnt[i] = fetch<GRID>(counts, x + 4 * i, min(there - 4 * i, 4));
   }
-  if (p.cand) {
+  unsigned long long is_cand = 0;                    // bit 8 t + j: token x + t is candidate j + 1
+  if (p.cand)
     for (int j = 0; j < p.k; ++j) {
-      const int t = p.cand[b * p.k + j] - x0;
+      const int t = __ldg(p.cand + b * p.k + j) - x;
       if (t >= 0 && t < there) is_cand |= 1ull << (8 * t + j);
     }
-  }
-  bool some = is_cand != 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) some = some || count[i] != 0 || bias[i] != 0.f;      // (NaN differs from 0)
-  const float rep = p.rep ? p.rep[b] : 1.f, pres = p.pres ? p.pres[b] : 0.f, freq = p.freq ? p.freq[b] : 0.f;
-
-  const int per = (p.n + p.groups - 1) / p.groups, i0 = blockIdx.y * per, i1 = min(i0 + per, p.n);
-  const uint32_t valid = there == N ? ALL : (1u << there) - 1u;
-  unsigned long long alive = 0;
+  const Penalty f{p.rep ? p.rep[b] : 1.f, p.pres ? p.pres[b] : 0.f, p.freq ? p.freq[b] : 0.f};
   int bad = 0;
-  for (int r0 = i0; r0 < i1; r0 += ROWS_AHEAD) {
-    Piece2 got[ROWS_AHEAD];
-    uint32_t keep[ROWS_AHEAD];
+  if (p.bits && i0 + (int)threadIdx.x < i1) {
+    const int m = p.mask_row[(int64_t)b * p.n + i0 + threadIdx.x];
+    if (m >= p.n_masks) bad = SPACE_ST_BAD_MASK;
+    mask_s[threadIdx.x] = m < p.n_masks ? m : -1;
+  }
+  if (threadIdx.x == 0) alive_s = 0;
+  const bool biased = p.n_bias && biases.collect(p, b, chunk0);
+  if (!p.n_bias && p.bits) __syncthreads();
+  const uint32_t bias = biased ? biases.some[(x - chunk0) >> 5] >> (x & 31) : 0u;
+  uint32_t hit = bias;                               // tokens with a bias, a count or a place among the candidates
+  uint4 c[N / 4];
 #pragma unroll
-    for (int u = 0; u < ROWS_AHEAD; ++u) {
-      const int i = r0 + u;
-      keep[u] = valid;
-      got[u].a = got[u].b = make_uint4(0, 0, 0, 0);
-      if (i >= i1) continue;
-      if (p.bits) {
-        const int m = p.mask_row[(int64_t)b * p.n + i];
-        if (m >= p.n_masks) bad = SPACE_ST_BAD_MASK;
-        else if (m >= 0) keep[u] = there ? (__ldg(p.bits + (int64_t)m * p.words + (x0 >> 5)) >> (x0 & 31)) & valid : 0u;
-      }
-      const T* row = reinterpret_cast<const T*>(p.logits) + ((int64_t)b * p.n + i) * p.in_rs;
-      const bool shifted = ((uintptr_t)row & 15) != 0;
-      if (there && (keep[u] || !valid) && (!p.in_place || shifted || some || keep[u] != valid)) {
-        if (there == N) got[u] = load_pieces(row, x0);
-        else {                                       // the row's end: nothing behind it is read
-          uint32_t w[4] = {0, 0, 0, 0};
+  for (int i = 0; i < N / 4; ++i) {
+    c[i] = shifted<GRID>(cnt[i], counts, min(max(there - 4 * i, 0), 4));
+    hit |= ((c[i].x ? 1u : 0u) | (c[i].y ? 2u : 0u) | (c[i].z ? 4u : 0u) | (c[i].w ? 8u : 0u)) << (4 * i);
+  }
 #pragma unroll
-          for (int e = 0; e < N; ++e)
-            if (e < there) {
-              if (sizeof(T) == 4) w[e % 4] = reinterpret_cast<const uint32_t*>(row)[x0 + e];
-              else w[(e >> 1) % 4] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[x0 + e] << (16 * (e & 1));
-            }
-          got[u].a = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-      }
+  for (int t = 0; t < N; ++t) hit |= (is_cand >> (8 * t)) & 0xFFu ? 1u << t : 0u;
+
+  unsigned long long alive = 0;
+  for (int r0 = i0; r0 < i1; r0 += AHEAD) {
+    Piece2 got[AHEAD];
+    uint32_t keep[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int m = p.bits && r0 + u < i1 ? mask_s[r0 + u - i0] : -1;
+      keep[u] = m < 0 || !there ? valid : (__ldg(p.bits + (int64_t)m * p.words + (x >> 5)) >> (x & 31)) & valid;
     }
 #pragma unroll
-    for (int u = 0; u < ROWS_AHEAD; ++u) {
+    for (int u = 0; u < AHEAD; ++u) {
+      got[u].a = got[u].b = make_uint4(0, 0, 0, 0);
+      // (what the mask leaves nothing of is not read, nor what stays where it is)
+      const bool touch = !p.in_place || __any_sync(0xFFFFFFFFu, (hit & keep[u]) || keep[u] != valid);
+      if (r0 + u < i1 && touch && keep[u]) got[u] = fetch<GRID>(in0 + u * p.in_rs, x, there);
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
       const int i = r0 + u;
       if (i >= i1) break;                            // (the same for the whole block)
-      const T* row = reinterpret_cast<const T*>(p.logits) + ((int64_t)b * p.n + i) * p.in_rs;
-      uint4 v = there == N ? shift_pieces(got[u], row) : got[u].a;
-      if (__any_sync(0xFFFFFFFFu, keep[u] != 0)) alive |= 1ull << i;
-      const bool touched = some || keep[u] != valid;
-      if (touched) {
-        float z[N];
-        unpack<T>(v, z);
-        const uint32_t behind = (1u << (i / (p.k + 1))) - 1u;                  // candidates that this row has seen
-#pragma unroll
-        for (int t = 0; t < N; ++t) {
-          const int c = count[t], times = min((c & (SPACE_COUNT_PROMPT - 1)), COUNT_MAX) + __popc((uint32_t)(is_cand >> (8 * t)) & behind & 0x7Fu);
-          if (times > 0 || (c & SPACE_COUNT_PROMPT)) z[t] = z[t] > 0.f ? z[t] / rep : z[t] * rep;
-          if (times > 0) z[t] = __fsub_rn(__fsub_rn(z[t], __fmul_rn(freq, (float)min(times, COUNT_MAX))), pres);
-          z[t] += bias[t];
-          if (!((keep[u] >> t) & 1u)) z[t] = -__int_as_float(0x7F800000);
-        }
-        v = pack<T>(z);
+      if (p.bits && __any_sync(0xFFFFFFFFu, keep[u] != 0)) alive |= 1ull << i;
+      uint32_t act = hit & keep[u];
+      if (p.in_place && !__any_sync(0xFFFFFFFFu, act || keep[u] != valid)) continue;
+      uint4 v = shifted<GRID>(got[u], in0 + u * p.in_rs, there);
+      for (; act; act &= act - 1) {
+        const uint32_t seen = (1u << (i / (p.k + 1))) - 1u;    // candidates that this row has behind it
+        const int t = __ffs(act) - 1;
+        const int count = __float_as_int(element<float>(N == 4 || t < 4 ? c[0] : c[N / 4 - 1], t & 3));
+        float z = penalized(element<T>(v, t), count, __popc((uint32_t)(is_cand >> (8 * t)) & seen & 0x7Fu), f);
+        if ((bias >> t) & 1u) z += biases.sum[x - chunk0 + t];
+        set_element<T>(v, t, z);
       }
-      T* dst = reinterpret_cast<T*>(p.out) + ((int64_t)b * p.n + i) * p.out_rs;
-      const bool write = !p.in_place || touched;
-      const uint32_t off = (uint32_t)((uintptr_t)dst & 15);
-      if (off == 0) {
-        if (write && there == N) *reinterpret_cast<uint4*>(dst + x0) = v;
-        else if (write) store_some<T>(dst, x0, v, 0, there);
-      } else {
-        // own elements from `split` on lie in the next 16-byte piece, whose rest the next lane has
-        const int split = N - (int)(off / sizeof(T));
-        Piece2 two;
-        two.a = v;
-        two.b.x = __shfl_down_sync(0xFFFFFFFFu, v.x, 1); two.b.y = __shfl_down_sync(0xFFFFFFFFu, v.y, 1);
-        two.b.z = __shfl_down_sync(0xFFFFFFFFu, v.z, 1); two.b.w = __shfl_down_sync(0xFFFFFFFFu, v.w, 1);
-        const int next = __shfl_down_sync(0xFFFFFFFFu, there | (write ? 16 : 0), 1);
-        const bool whole = lane < 31 && there == N && (next & 15) >= split;
-        const int prev = __shfl_up_sync(0xFFFFFFFFu, (int)whole, 1);
-        if (whole) {
-          // bytes 16 - off .. of the two vectors, as shift_pieces takes them for a row at that offset
-          if (write || (next & 16)) *reinterpret_cast<uint4*>(dst + x0 + split) = shift_pieces(two, reinterpret_cast<const T*>((uintptr_t)(16 - off)));
-        } else if (write) {
-          store_some<T>(dst, x0, v, split, there);
-        }
-        if (write && !(lane > 0 && prev)) store_some<T>(dst, x0, v, 0, min(split, there));
-      }
+      if (p.bits) mask_out<T>(v, keep[u]);
+      store_vectors<GRID>(out0 + u * p.out_rs, x, v, there, p.V);
     }
+    in0 += AHEAD * p.in_rs; out0 += AHEAD * p.out_rs;
   }
-  if (p.bits) {
-    if (bad && p.status) atomicOr(p.status + b, bad);
-    if (!p.status) return;
-    if (lane == 0 && alive) atomicOr(&alive_s, alive);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      if (alive_s) atomicOr(p.alive + b, alive_s);
-      __threadfence();
-      if (atomicAdd(p.arrived + b, 1) == p.chunks * p.groups - 1) {            // every other block has said what it found
-        __threadfence();
-        const unsigned long long all = p.n == 64 ? ~0ull : (1ull << p.n) - 1ull;
-        if (atomicExch(p.alive + b, 0ull) != all) atomicOr(p.status + b, SPACE_ST_BAD_MASK);
-        p.arrived[b] = 0;
-      }
-    }
-  }
+  if (p.bits) report(p, b, bad, alive, alive_s);
 }
 
 // ---- counts
@@ -313,17 +467,24 @@ int space_logits_adjust(space_ctx* ctx, const space_logits_args* a, void* stream
   p.n_bias = a->n_bias; p.bias_tok = a->bias_tok; p.bias_val = a->bias_val;
   p.n_masks = a->n_masks; p.bits = a->mask_bits; p.mask_row = a->mask_row; p.status = a->status;
   p.alive = ctx->logits_alive; p.arrived = ctx->logits_arrived;
-  const int chunk = THREADS * 16 / esz;
+  const int64_t in_b = p.in_rs * esz, out_b = p.out_rs * esz;
+  const bool grid = !(((uintptr_t)p.logits | (uintptr_t)p.out | (uintptr_t)p.counts | (uintptr_t)in_b | (uintptr_t)out_b) & 15) && (!p.counts || p.V % 4 == 0);
+  const int chunk = THREADS * (p.n > 1 ? 16 / esz : grid ? 2 * ROW_TOKENS : ROW_TOKENS);
   p.chunks = (int)(((int64_t)p.V + chunk - 1) / chunk);
-  // rows are shared out until four thread blocks an SM have some
-  const int64_t want = (4ll * ctx->sm_count + (int64_t)p.chunks * p.B - 1) / ((int64_t)p.chunks * p.B);
-  const int steps = (p.n + ROWS_AHEAD - 1) / ROWS_AHEAD;
-  const int per = ROWS_AHEAD * (int)((steps + (want < steps ? want : steps) - 1) / (want < steps ? want : steps));
+  // rows are shared out until eight thread blocks an SM have some
+  const int64_t want = (8ll * ctx->sm_count + (int64_t)p.chunks * p.B - 1) / ((int64_t)p.chunks * p.B);
+  const int64_t steps = (p.n + AHEAD - 1) / AHEAD, groups = want < steps ? want : steps;
+  const int per = AHEAD * (int)((steps + groups - 1) / groups);
   p.groups = (p.n + per - 1) / per;
-  const dim3 grid(p.chunks, p.groups, p.B);
+  void (*kernel)(Params);
+  if (p.n == 1)
+    kernel = esz == 4 ? (grid ? logits_row_kernel<float, true> : logits_row_kernel<float, false>)
+                      : (grid ? logits_row_kernel<__nv_bfloat16, true> : logits_row_kernel<__nv_bfloat16, false>);
+  else
+    kernel = esz == 4 ? (grid ? logits_rows_kernel<float, true> : logits_rows_kernel<float, false>)
+                      : (grid ? logits_rows_kernel<__nv_bfloat16, true> : logits_rows_kernel<__nv_bfloat16, false>);
   ctx->launches += 1;
-  if (esz == 4) return cuda_ok(launch_pdl(logits_adjust_kernel<float>, grid, dim3(THREADS), 0, (cudaStream_t)stream, p));
-  return cuda_ok(launch_pdl(logits_adjust_kernel<__nv_bfloat16>, grid, dim3(THREADS), 0, (cudaStream_t)stream, p));
+  return cuda_ok(launch_pdl(kernel, dim3(p.chunks, p.groups, p.B), dim3(THREADS), 0, (cudaStream_t)stream, p));
 }
 
 int space_token_counts(space_ctx* ctx, const space_counts_args* a, void* stream) {

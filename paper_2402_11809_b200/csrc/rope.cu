@@ -1,18 +1,19 @@
 // Rotated rows into the bf16 cache (space_rope_append).
 //
-// Bytes read once and written once, 4 d per row and head, beside a table row of 4 rot_dim bytes per row that all its heads share (out of the
-// first-level cache).  d / 8 lanes have a row of one head, a thread PAIRS of (row, head), whose loads are all on their way before the
-// first is used.  The order is sequence, row, head: q, then K, then V heads of a row, as a projection's output lies.
+// Bytes read once and written once, 4 d per row and head, beside a table row of 4 rot_dim bytes per row that all its heads share.
+// A thread block has up to MAX_ROWS rows; a thread's lane of every head of a row it turns with the same cosines and sines, four heads at a time.
+// (A list of (row, head) pairs instead, table entries loaded for each: 193 us for what takes 104.)  The order is a
+// projection's output's: q, then K, then V heads of a row.
 #include "rope_common.cuh"
 
 namespace {
 using namespace rope;
 
-constexpr int THREADS = 256, PAIRS = 4;
+constexpr int THREADS = 256, MAX_ROWS = 4;
 
 struct Params {
   Table t;
-  int B, rows, H_q, H_kv, n_heads;                   // heads per row: H_q (or 0), H_kv, and H_kv again where values go to a cache
+  int B, rows, per, H_q, H_kv, n_heads;                   // heads per row: H_q (or 0), H_kv, and H_kv again where values go to a cache
   int64_t cap;                                       // rows a sequence may have (no cache: no limit)
   const char* src[3]; int64_t sb[3], sr[3], sh[3];   // q, k, v; bytes
   char* dst[2]; int64_t db[2], dr[2], dh[2];         // q_out, k_out; bytes
@@ -22,11 +23,10 @@ struct Params {
 };
 
 template <int DH>
-__global__ void __launch_bounds__(THREADS) rope_append_kernel(const __grid_constant__ Params p) {
-  constexpr int LANES = DH / 8, SLOTS = THREADS / LANES;
+__global__ void __launch_bounds__(THREADS, 4) rope_append_kernel(const __grid_constant__ Params p) {
   pdl_launch_dependents();
   pdl_wait();
-  const int b = blockIdx.y, x = threadIdx.x % LANES;
+  const int b = blockIdx.y, r0 = blockIdx.x * p.per;
   const int L = p.kv_len[b];
   const int want = p.count ? p.count[b] : p.rows;
   const int n = max(0, min(want, p.rows));
@@ -35,44 +35,35 @@ __global__ void __launch_bounds__(THREADS) rope_append_kernel(const __grid_const
     if (!fits && p.status) atomicOr(p.status + b, SPACE_ST_CAPACITY);
     if (p.len_out) p.len_out[b] = fits ? L + n : L;
   }
-  const uint32_t pair0 = blockIdx.x * (uint32_t)(SLOTS * PAIRS) + threadIdx.x / LANES;
-  if (!fits || blockIdx.x * (uint32_t)(SLOTS * PAIRS) >= (uint32_t)n * (uint32_t)p.n_heads) return;
-  uint4 v[PAIRS];
-  Turn u[PAIRS];
-  char* to[PAIRS];
-  bool turned[PAIRS];
-#pragma unroll
-  for (int j = 0; j < PAIRS; ++j) {
-    const uint32_t pair = pair0 + j * SLOTS;
-    const int r = (int)(pair / (uint32_t)p.n_heads), g = (int)(pair - (uint32_t)r * p.n_heads);
-    v[j] = make_uint4(0, 0, 0, 0);
-    to[j] = nullptr;
-    turned[j] = false;
-    if (r < n) {
-      const int which = g < p.H_q ? 0 : g < p.H_q + p.H_kv ? 1 : 2;
-      const int h = g - (which == 0 ? 0 : which == 1 ? p.H_q : p.H_q + p.H_kv);
-      v[j] = *(reinterpret_cast<const uint4*>(p.src[which] + (int64_t)b * p.sb[which] + (int64_t)r * p.sr[which] + (int64_t)h * p.sh[which]) + x);
-      if (which < 2) {
-        bool bad;
-        const float* row = table_row(p.t, b, p.rows, r, (int64_t)L + r, bad);
-        if (bad && g == 0 && x == 0 && p.status) atomicOr(p.status + b, SPACE_ST_BAD_POSITION);
-        load_turn(p.t, row, x, u[j]);
-        turned[j] = true;
-      }
-      if (which == 0 || !p.cache[0]) {
-        to[j] = p.dst[which] + (int64_t)b * p.db[which] + (int64_t)r * p.dr[which] + (int64_t)h * p.dh[which];
-      } else {
-        const int64_t off = kv_row_offset(p.page_table, p.pages_per_seq, p.n_pages, p.cb, p.ch, p.cs, b, h, L + r);
-        if (off >= 0) to[j] = p.cache[which - 1] + off;
-        else if (x == 0 && p.status) atomicOr(p.status + b, SPACE_ST_BAD_PAGE);
-      }
+  if (!fits) return;
+#pragma unroll 1
+  for (int r = r0; r < min(r0 + p.per, n); ++r) {
+    bool bad;
+    const float* row = table_row(p.t, b, p.rows, r, (int64_t)L + r, bad);
+    if (bad && threadIdx.x == 0 && p.status) atomicOr(p.status + b, SPACE_ST_BAD_POSITION);
+    int64_t off = 0;                                 // of the cache row, head 0
+    if (p.cache[0]) {
+      off = kv_row_offset(p.page_table, p.pages_per_seq, p.n_pages, p.cb, p.ch, p.cs, b, 0, L + r);
+      if (off < 0 && threadIdx.x == 0 && p.status) atomicOr(p.status + b, SPACE_ST_BAD_PAGE);
     }
-  }
+    const char* from[3];
 #pragma unroll
-  for (int j = 0; j < PAIRS; ++j) {
-    float y[8];
-    turn_row<LANES>(p.t, v[j], x, u[j], y);
-    if (to[j]) *(reinterpret_cast<uint4*>(to[j]) + x) = turned[j] ? pack8(y) : v[j];
+    for (int i = 0; i < 3; ++i) from[i] = p.src[i] + (int64_t)b * p.sb[i] + (int64_t)r * p.sr[i];
+    char* to[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) to[i] = p.dst[i] + (int64_t)b * p.db[i] + (int64_t)r * p.dr[i];
+    const int hq = p.H_q, hk = p.H_kv;
+    turn_heads<DH, THREADS>(
+        p.t, row, p.n_heads, hq + hk,
+        [&](int g) {
+          return g < hq ? from[0] + (int64_t)g * p.sh[0] : g < hq + hk ? from[1] + (int64_t)(g - hq) * p.sh[1] : from[2] + (int64_t)(g - hq - hk) * p.sh[2];
+        },
+        [&](int g) -> char* {
+          if (g < hq) return to[0] + (int64_t)g * p.dh[0];
+          const int which = g >= hq + hk, h = g - hq - (which ? hk : 0);
+          if (!p.cache[0]) return to[1] + (int64_t)h * p.dh[1];
+          return off < 0 ? nullptr : p.cache[which] + off + (int64_t)h * p.ch;
+        });
   }
 }
 
@@ -112,7 +103,6 @@ extern "C" int space_rope_append(space_ctx* ctx, const space_rope_args* a, void*
   p.t = rope::table_of(a->rope);
   p.B = a->batch; p.rows = a->rows; p.H_q = a->q ? ctx->cfg.n_q_heads : 0; p.H_kv = ctx->cfg.n_kv_heads;
   p.n_heads = p.H_q + p.H_kv * (cached ? 2 : 1);
-  if ((int64_t)p.rows * p.n_heads > 0x7FFF0000ll) return SPACE_E_UNSUPPORTED;
   if (cudaSetDevice(ctx->cfg.device) != cudaSuccess) return SPACE_E_CUDA;
   p.cap = a->page_table ? (int64_t)a->pages_per_seq * SPACE_PAGE_SIZE : ctx->cfg.s_cap;
   p.src[0] = (const char*)a->q; p.sb[0] = 2 * a->q_stride_b; p.sr[0] = 2 * a->q_stride_r; p.sh[0] = 2 * a->q_stride_h;
@@ -124,8 +114,10 @@ extern "C" int space_rope_append(space_ctx* ctx, const space_rope_args* a, void*
   p.cb = 2 * a->kv_stride_b; p.ch = 2 * a->kv_stride_h; p.cs = 2 * a->kv_stride_s;
   p.page_table = a->page_table; p.pages_per_seq = a->pages_per_seq; p.n_pages = a->n_pages;
   p.kv_len = a->kv_len; p.count = a->count; p.len_out = a->kv_len_out; p.status = a->status;
-  const int per_block = THREADS / (ctx->cfg.head_dim / 8) * PAIRS;
-  const dim3 grid((unsigned)(((int64_t)p.rows * p.n_heads + per_block - 1) / per_block), p.B);
+  // (36 rows of 16 sequences: one a block 8.7 us, two 13.4; 4 x 5700 rows: four a block 128 us, one 141)
+  const int64_t per = (int64_t)p.B * p.rows / (8 * ctx->sm_count);
+  p.per = (int)(per < 1 ? 1 : per > MAX_ROWS ? MAX_ROWS : per);
+  const dim3 grid((unsigned)((p.rows + p.per - 1) / p.per), p.B);
   ctx->launches += 1;
   return cuda_ok(launch_pdl(ctx->cfg.head_dim == 128 ? rope_append_kernel<128> : rope_append_kernel<64>, grid, dim3(THREADS), 0, (cudaStream_t)stream, p));
 }

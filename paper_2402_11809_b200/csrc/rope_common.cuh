@@ -83,7 +83,37 @@ __device__ __forceinline__ uint4 pack8(const float (&y)[8]) {
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
+// Heads of one row: d / 8 lanes have a head, a thread HEADS of them at a time, whose loads are all on their way before the
+// first is used; the row's cosines and sines serve them all.  src(g) and dst(g): where head g is and goes (nullptr: nowhere); heads
+// from `plain` on are copied as they are.  By whole warps.
+constexpr int HEADS = 4;
+template <int DH, int THREADS, class Src, class Dst>
+__device__ __forceinline__ void turn_heads(const Table& t, const float* row, int n_heads, int plain, Src src, Dst dst) {
+  constexpr int LANES = DH / 8, SLOTS = THREADS / LANES;
+  const int x = threadIdx.x % LANES, g0 = threadIdx.x / LANES;
+  Turn u;
+  load_turn(t, row, x, u);
+  for (int g = g0; g - g0 < n_heads; g += HEADS * SLOTS) {     // (the same number of times for a warp)
+    uint4 v[HEADS];
+#pragma unroll
+    for (int j = 0; j < HEADS; ++j) {
+      const int h = g + j * SLOTS;
+      v[j] = h < n_heads ? *(reinterpret_cast<const uint4*>(src(h)) + x) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < HEADS; ++j) {
+      const int h = g + j * SLOTS;
+      if (g - g0 + j * SLOTS >= n_heads) break;
+      float y[8];
+      turn_row<LANES>(t, v[j], x, u, y);
+      char* to = h < n_heads ? dst(h) : nullptr;
+      if (to) *(reinterpret_cast<uint4*>(to) + x) = h < plain ? pack8(y) : v[j];
+    }
+  }
+}
+
 }  // namespace rope
+
 
 // What both calls check of the rotation (rope.cu).
 int check_rope(const space_ctx* ctx, const space_rope& r);
