@@ -12,14 +12,14 @@
 namespace {
 using namespace kvb;
 
-constexpr int THREADS = 256, Q_ROWS = 2;
+constexpr int THREADS = 256;
 constexpr float BF16_MAX = 3.3895313892515355e38f;
 
 struct AppendParams {
   Cache cache;
   int B, H, H_q, rows, max_count, step, bias, blocks;        // blocks: 32-row blocks a sequence's new rows may touch
   int64_t n_append;                                  // thread blocks that append
-  int q_blocks;                                      // thread blocks per sequence that turn queries
+  int q_blocks, share;                               // thread blocks per sequence that turn queries; warps that share a row
   const char* src[2]; int64_t sb, sr, sh;            // K, V; bytes
   const char* q; int64_t q_sb, q_sr, q_sh;
   char* q_out; int64_t o_sb, o_sr, o_sh;
@@ -49,19 +49,17 @@ __device__ __forceinline__ uint32_t coarser(uint32_t w, float ratio) {
   return codes4(a.x * ratio, a.y * ratio, b.x * ratio, b.y * ratio);
 }
 
-// Queries of two rows of sequence b, beside the append.
+// Queries of sequence b, beside the append.
 template <int DH>
 __device__ __forceinline__ void turn_queries(const AppendParams& p, int b, int block) {
-  const int L = p.kv_len[b], n = append_count(p, b, L);
-#pragma unroll 1
-  for (int g = block * Q_ROWS; g < min((block + 1) * Q_ROWS, n); ++g) {
-    const int64_t r = (int64_t)g * p.step;
-    bool bad;
-    const float* row = rope::table_row(p.t, b, p.rows, (int)r, (int64_t)L + g, bad);
-    const char* from = p.q + (int64_t)b * p.q_sb + r * p.q_sr;
-    char* to = p.q_out + (int64_t)b * p.o_sb + r * p.o_sr;
-    rope::turn_heads<DH, THREADS>(p.t, row, p.H_q, p.H_q, [&](int h) { return from + (int64_t)h * p.q_sh; }, [&](int h) { return to + (int64_t)h * p.o_sh; });
-  }
+  const int task = block * (THREADS / 32) + (int)(threadIdx.x >> 5), g = task / p.share, part = task - g * p.share;
+  const int L = p.kv_len[b];
+  if (g >= append_count(p, b, L)) return;
+  const int64_t r = (int64_t)g * p.step;
+  bool bad;
+  rope::Turn u;
+  rope::load_turn(p.t, rope::table_row(p.t, b, p.rows, (int)r, (int64_t)L + g, bad), (threadIdx.x & 31) % (DH / 8), u);
+  rope::row_heads<DH, true>(p.t, u, p.H_q, part, p.share, p.q + (int64_t)b * p.q_sb + r * p.q_sr, p.q_sh, p.q_out + (int64_t)b * p.o_sb + r * p.o_sr, p.o_sh);
 }
 
 template <int DH>
@@ -96,7 +94,9 @@ __global__ void __launch_bounds__(THREADS, 4) kvb_append_kernel(const __grid_con
 #pragma unroll
   for (int k = 0; k < PASSES; ++k) {
     const int i = k * ROWS + r;
-    v[0][k] = v[1][k] = make_uint4(0, 0, 0, 0);
+    v[0][k] = v[1][k] = make_uint4(0, 0, 0, 0);      // (rows that are not written: zeros, turned by zeros)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[k].c[j] = u[k].s[j] = 0ull;
     if (i >= i_lo && i < i_hi) {
       const int64_t from = (int64_t)(s0 + i - L) * p.step;
 #pragma unroll
@@ -113,30 +113,39 @@ __global__ void __launch_bounds__(THREADS, 4) kvb_append_kernel(const __grid_con
   const int row0 = s0 % SPACE_PAGE_SIZE;
   float2* scales = reinterpret_cast<float2*>(head + F::SCALES) + row0 / BLOCK_ROWS;
   const float2 was = head && i_lo > 0 ? *scales : make_float2(0.f, 0.f);
-  float y[2][PASSES][8];
+  uint64_t y[PASSES][4];                             // the K rows, turned
   float top[2] = {0.f, 0.f};
 #pragma unroll
   for (int k = 0; k < PASSES; ++k) {
+    uint32_t most[2];
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-      if (kvq::any_nonfinite(v[which][k])) { kvq::make_finite(v[which][k]); bits |= SPACE_ST_NONFINITE; }
-      if (which == 0 && p.t.table) {
-        rope::turn_row<LANES>(p.t, v[0][k], x, u[k], y[0][k]);
-      } else {
-        const uint32_t w[4] = {v[which][k].x, v[which][k].y, v[which][k].z, v[which][k].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { y[which][k][2 * j] = rope::lo_f(w[j]); y[which][k][2 * j + 1] = rope::hi_f(w[j]); }
+      most[which] = kvq::max_bits(v[which][k]);
+      if (most[which] >= 0x7F80u) {
+        bits |= SPACE_ST_NONFINITE;
+        kvq::make_finite(v[which][k]);
+        most[which] = kvq::max_bits(v[which][k]);
       }
     }
-    const int i = k * ROWS + r;
-    const bool mine = i >= i_lo && i < i_hi;         // (a lane without a row has read no table)
+    top[1] = fmaxf(top[1], __uint_as_float(most[1] << 16));
+    if (p.t.table) {
+      rope::turn_row<LANES>(p.t, v[0][k], x, u[k], y[k]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      // (two of the largest numbers turned into one can pass the largest)
-      y[0][k][j] = mine ? fminf(fmaxf(y[0][k][j], -BF16_MAX), BF16_MAX) : 0.f;
-      top[0] = fmaxf(top[0], fabsf(y[0][k][j]));
-      top[1] = fmaxf(top[1], fabsf(y[1][k][j]));
+      for (int j = 0; j < 4; ++j) top[0] = fmaxf(top[0], fmaxf(fabsf(rope::first_of(y[k][j])), fabsf(rope::second_of(y[k][j]))));
+    } else {
+      const uint32_t w[4] = {v[0][k].x, v[0][k].y, v[0][k].z, v[0][k].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[k][j] = rope::pair_of(w[j]);
+      top[0] = fmaxf(top[0], __uint_as_float(most[0] << 16));
     }
+  }
+  if (top[0] > BF16_MAX) {                           // (two of the largest numbers turned into one can pass the largest)
+    top[0] = BF16_MAX;
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        y[k][j] = rope::pair(fminf(fmaxf(rope::first_of(y[k][j]), -BF16_MAX), BF16_MAX), fminf(fmaxf(rope::second_of(y[k][j]), -BF16_MAX), BF16_MAX));
   }
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
@@ -171,16 +180,20 @@ __global__ void __launch_bounds__(THREADS, 4) kvb_append_kernel(const __grid_con
     const int i = k * ROWS + r;
     uint2* kc = reinterpret_cast<uint2*>(head + (x >> 1) * F::K_COLS + 16 * (row0 + i) + 8 * (x & 1));
     if (i >= i_lo && i < i_hi) {
-      float z[2][8];
+      const uint32_t w[4] = {v[1][k].x, v[1][k].y, v[1][k].z, v[1][k].w};
+      uint32_t kk[4], vv[4];                         // pairs of codes
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { z[0][j] = y[0][k][j] * down[0]; z[1][j] = y[1][k][j] * down[1]; }
-      *kc = make_uint2(codes4(z[0][0], z[0][1], z[0][2], z[0][3]), codes4(z[0][4], z[0][5], z[0][6], z[0][7]));
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t a = rope::mul_pair(y[k][j], rope::pair(down[0], down[0])), c = rope::mul_pair(rope::pair_of(w[j]), rope::pair(down[1], down[1]));
+        kk[j] = codes2(rope::first_of(a), rope::second_of(a));
+        vv[j] = codes2(rope::first_of(c), rope::second_of(c));
+      }
+      *kc = make_uint2(kk[0] | kk[1] << 16, kk[2] | kk[3] << 16);
       unsigned char* at = vsm + VT::at(i >> 4, 8 * x) + (i & 15);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t two = codes2(z[1][2 * j], z[1][2 * j + 1]);
-        at[32 * j] = (unsigned char)two;
-        at[32 * j + 16] = (unsigned char)(two >> 8);
+        at[32 * j] = (unsigned char)vv[j];
+        at[32 * j + 16] = (unsigned char)(vv[j] >> 8);
       }
     } else if (raised[0] && i < i_lo) {
       const uint2 w = *kc;
@@ -302,7 +315,8 @@ int launch_kvb_append(space_ctx* ctx, const space_kvb_append_args* a, cudaStream
   if (a->q) {
     p.q = (const char*)a->q; p.q_sb = 2 * a->q_stride_b; p.q_sr = 2 * a->q_stride_r; p.q_sh = 2 * a->q_stride_h;
     p.q_out = (char*)a->q_out; p.o_sb = 2 * a->q_out_stride_b; p.o_sr = 2 * a->q_out_stride_r; p.o_sh = 2 * a->q_out_stride_h;
-    p.q_blocks = (p.max_count + Q_ROWS - 1) / Q_ROWS;
+    p.share = rope::warps_per_row((int64_t)p.B * p.max_count, ctx->sm_count, THREADS / 32);
+    p.q_blocks = (int)(((int64_t)p.max_count * p.share + THREADS / 32 - 1) / (THREADS / 32));
     grid += (int64_t)p.B * p.q_blocks;
   }
   if (grid > 0x7FFFFFFFll) return SPACE_E_UNSUPPORTED;

@@ -9,11 +9,12 @@
 namespace {
 using namespace rope;
 
-constexpr int THREADS = 256, MAX_ROWS = 4;
+constexpr int THREADS = 256, WARPS = THREADS / 32;
 
 struct Params {
   Table t;
-  int B, rows, per, H_q, H_kv, n_heads;                   // heads per row: H_q (or 0), H_kv, and H_kv again where values go to a cache
+  int B, rows, H_q, H_kv;                            // (H_q 0: no queries)
+  int share;                                         // warps that share a row
   int64_t cap;                                       // rows a sequence may have (no cache: no limit)
   const char* src[3]; int64_t sb[3], sr[3], sh[3];   // q, k, v; bytes
   char* dst[2]; int64_t db[2], dr[2], dh[2];         // q_out, k_out; bytes
@@ -26,7 +27,7 @@ template <int DH>
 __global__ void __launch_bounds__(THREADS, 4) rope_append_kernel(const __grid_constant__ Params p) {
   pdl_launch_dependents();
   pdl_wait();
-  const int b = blockIdx.y, r0 = blockIdx.x * p.per;
+  const int b = blockIdx.y, task = blockIdx.x * WARPS + (threadIdx.x >> 5), r = task / p.share, part = task - r * p.share;
   const int L = p.kv_len[b];
   const int want = p.count ? p.count[b] : p.rows;
   const int n = max(0, min(want, p.rows));
@@ -35,35 +36,25 @@ __global__ void __launch_bounds__(THREADS, 4) rope_append_kernel(const __grid_co
     if (!fits && p.status) atomicOr(p.status + b, SPACE_ST_CAPACITY);
     if (p.len_out) p.len_out[b] = fits ? L + n : L;
   }
-  if (!fits) return;
-#pragma unroll 1
-  for (int r = r0; r < min(r0 + p.per, n); ++r) {
-    bool bad;
-    const float* row = table_row(p.t, b, p.rows, r, (int64_t)L + r, bad);
-    if (bad && threadIdx.x == 0 && p.status) atomicOr(p.status + b, SPACE_ST_BAD_POSITION);
-    int64_t off = 0;                                 // of the cache row, head 0
-    if (p.cache[0]) {
-      off = kv_row_offset(p.page_table, p.pages_per_seq, p.n_pages, p.cb, p.ch, p.cs, b, 0, L + r);
-      if (off < 0 && threadIdx.x == 0 && p.status) atomicOr(p.status + b, SPACE_ST_BAD_PAGE);
-    }
-    const char* from[3];
-#pragma unroll
-    for (int i = 0; i < 3; ++i) from[i] = p.src[i] + (int64_t)b * p.sb[i] + (int64_t)r * p.sr[i];
-    char* to[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) to[i] = p.dst[i] + (int64_t)b * p.db[i] + (int64_t)r * p.dr[i];
-    const int hq = p.H_q, hk = p.H_kv;
-    turn_heads<DH, THREADS>(
-        p.t, row, p.n_heads, hq + hk,
-        [&](int g) {
-          return g < hq ? from[0] + (int64_t)g * p.sh[0] : g < hq + hk ? from[1] + (int64_t)(g - hq) * p.sh[1] : from[2] + (int64_t)(g - hq - hk) * p.sh[2];
-        },
-        [&](int g) -> char* {
-          if (g < hq) return to[0] + (int64_t)g * p.dh[0];
-          const int which = g >= hq + hk, h = g - hq - (which ? hk : 0);
-          if (!p.cache[0]) return to[1] + (int64_t)h * p.dh[1];
-          return off < 0 ? nullptr : p.cache[which] + off + (int64_t)h * p.ch;
-        });
+  if (!fits || r >= n) return;
+  bool bad;
+  const float* row = table_row(p.t, b, p.rows, r, (int64_t)L + r, bad);
+  Turn u;
+  load_turn(p.t, row, (threadIdx.x & 31) % (DH / 8), u);
+  int64_t off = 0;                                   // of the cache row, head 0
+  if (p.cache[0]) off = kv_row_offset(p.page_table, p.pages_per_seq, p.n_pages, p.cb, p.ch, p.cs, b, 0, L + r);
+  if ((threadIdx.x & 31) == 0 && part == 0 && p.status && (bad || off < 0))
+    atomicOr(p.status + b, (bad ? SPACE_ST_BAD_POSITION : 0) | (off < 0 ? SPACE_ST_BAD_PAGE : 0));
+  if (p.H_q)
+    row_heads<DH, true>(p.t, u, p.H_q, part, p.share, p.src[0] + (int64_t)b * p.sb[0] + (int64_t)r * p.sr[0], p.sh[0],
+                        p.dst[0] + (int64_t)b * p.db[0] + (int64_t)r * p.dr[0], p.dh[0]);
+  const int64_t from = (int64_t)b * p.sb[1] + (int64_t)r * p.sr[1];
+  if (!p.cache[0]) {
+    row_heads<DH, true>(p.t, u, p.H_kv, part, p.share, p.src[1] + from, p.sh[1], p.dst[1] + (int64_t)b * p.db[1] + (int64_t)r * p.dr[1], p.dh[1]);
+  } else if (off >= 0) {
+    row_heads<DH, true>(p.t, u, p.H_kv, part, p.share, p.src[1] + from, p.sh[1], p.cache[0] + off, p.ch);
+    // (V heads from the other end of the warps: few heads leave some of them without K heads)
+    row_heads<DH, false>(p.t, u, p.H_kv, p.share - 1 - part, p.share, p.src[2] + from, p.sh[1], p.cache[1] + off, p.ch);
   }
 }
 
@@ -102,7 +93,6 @@ extern "C" int space_rope_append(space_ctx* ctx, const space_rope_args* a, void*
   memset(&p, 0, sizeof(p));
   p.t = rope::table_of(a->rope);
   p.B = a->batch; p.rows = a->rows; p.H_q = a->q ? ctx->cfg.n_q_heads : 0; p.H_kv = ctx->cfg.n_kv_heads;
-  p.n_heads = p.H_q + p.H_kv * (cached ? 2 : 1);
   if (cudaSetDevice(ctx->cfg.device) != cudaSuccess) return SPACE_E_CUDA;
   p.cap = a->page_table ? (int64_t)a->pages_per_seq * SPACE_PAGE_SIZE : ctx->cfg.s_cap;
   p.src[0] = (const char*)a->q; p.sb[0] = 2 * a->q_stride_b; p.sr[0] = 2 * a->q_stride_r; p.sh[0] = 2 * a->q_stride_h;
@@ -114,10 +104,8 @@ extern "C" int space_rope_append(space_ctx* ctx, const space_rope_args* a, void*
   p.cb = 2 * a->kv_stride_b; p.ch = 2 * a->kv_stride_h; p.cs = 2 * a->kv_stride_s;
   p.page_table = a->page_table; p.pages_per_seq = a->pages_per_seq; p.n_pages = a->n_pages;
   p.kv_len = a->kv_len; p.count = a->count; p.len_out = a->kv_len_out; p.status = a->status;
-  // (36 rows of 16 sequences: one a block 8.7 us, two 13.4; 4 x 5700 rows: four a block 128 us, one 141)
-  const int64_t per = (int64_t)p.B * p.rows / (8 * ctx->sm_count);
-  p.per = (int)(per < 1 ? 1 : per > MAX_ROWS ? MAX_ROWS : per);
-  const dim3 grid((unsigned)((p.rows + p.per - 1) / p.per), p.B);
+  p.share = rope::warps_per_row((int64_t)p.B * p.rows, ctx->sm_count, WARPS);
+  const dim3 grid((unsigned)(((int64_t)p.rows * p.share + WARPS - 1) / WARPS), p.B);
   ctx->launches += 1;
   return cuda_ok(launch_pdl(ctx->cfg.head_dim == 128 ? rope_append_kernel<128> : rope_append_kernel<64>, grid, dim3(THREADS), 0, (cudaStream_t)stream, p));
 }

@@ -23,22 +23,45 @@ __device__ __forceinline__ const float* table_row(const Table& t, int b, int row
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// Cosines and sines of a lane's eight channels 8x .. 8x + 7 (pairs of neighbours: of its four pairs).
-struct Turn { float c[8], s[8]; };
-__device__ __forceinline__ void load4(float* d, const float* src) {
-  const float4 v = __ldg(reinterpret_cast<const float4*>(src));
-  d[0] = v.x; d[1] = v.y; d[2] = v.z; d[3] = v.w;
+// Products and sums of pairs, each rounded by itself.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  return (uint64_t)__float_as_uint(a) | (uint64_t)__float_as_uint(b) << 32;
 }
+__device__ __forceinline__ uint64_t pair_of(uint32_t w) { return pair(lo_f(w), hi_f(w)); }
+__device__ __forceinline__ float first_of(uint64_t p) { return __uint_as_float((uint32_t)p); }
+__device__ __forceinline__ float second_of(uint64_t p) { return __uint_as_float((uint32_t)(p >> 32)); }
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// What a lane's eight channels 8x .. 8x + 7 are multiplied by, as pairs of neighbours: themselves by c, their partners by s, the
+// sine with the sign of its place (a c - b s is a c + b (-s), rounding for rounding).
+struct Turn { uint64_t c[4], s[4]; };
 __device__ __forceinline__ void load_turn(const Table& t, const float* row, int x, Turn& u) {
   const int half = t.rot >> 1, c0 = 8 * x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u.c[i] = u.s[i] = 0ull;
   if (c0 >= t.rot) return;
   if (t.interleaved) {
-    load4(u.c, row + 4 * x);
-    load4(u.s, row + half + 4 * x);
+    const float4 c = __ldg(reinterpret_cast<const float4*>(row) + x), s = __ldg(reinterpret_cast<const float4*>(row + half) + x);
+    u.c[0] = pair(c.x, c.x); u.c[1] = pair(c.y, c.y); u.c[2] = pair(c.z, c.z); u.c[3] = pair(c.w, c.w);
+    u.s[0] = pair(-s.x, s.x); u.s[1] = pair(-s.y, s.y); u.s[2] = pair(-s.z, s.z); u.s[3] = pair(-s.w, s.w);
   } else {
     const int j = c0 < half ? c0 : c0 - half;
-    load4(u.c, row + j); load4(u.c + 4, row + j + 4);
-    load4(u.s, row + half + j); load4(u.s + 4, row + half + j + 4);
+    const float sign = c0 < half ? -1.f : 1.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float4 c = __ldg(reinterpret_cast<const float4*>(row + j) + i), s = __ldg(reinterpret_cast<const float4*>(row + half + j) + i);
+      u.c[2 * i] = pair(c.x, c.y); u.c[2 * i + 1] = pair(c.z, c.w);
+      u.s[2 * i] = pair(sign * s.x, sign * s.y); u.s[2 * i + 1] = pair(sign * s.z, sign * s.w);
+    }
   }
 }
 
@@ -46,70 +69,72 @@ __device__ __forceinline__ void load_turn(const Table& t, const float* row, int 
 // one is x) are neighbours.  Pairs that are rot/2 apart come from the lane that holds the other half: nothing is read
 // a second time, so that a row may be written where it was read.
 template <int LANES>
-__device__ __forceinline__ void turn_row(const Table& t, const uint4& v, int x, const Turn& u, float (&y)[8]) {
+__device__ __forceinline__ void turn_row(const Table& t, const uint4& v, int x, const Turn& u, uint64_t (&y)[4]) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   const int c0 = 8 * x, half = t.rot >> 1;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { y[2 * i] = lo_f(w[i]); y[2 * i + 1] = hi_f(w[i]); }
-  if (t.interleaved) {
-    if (c0 >= t.rot) return;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float a = y[2 * i], b = y[2 * i + 1];
-      y[2 * i] = __fsub_rn(__fmul_rn(a, u.c[i]), __fmul_rn(b, u.s[i]));
-      y[2 * i + 1] = __fadd_rn(__fmul_rn(b, u.c[i]), __fmul_rn(a, u.s[i]));
-    }
-    return;
-  }
-  const bool first = c0 < half;
-  const int from = c0 >= t.rot ? x : first ? x + (half >> 3) : x - (half >> 3);
   uint32_t o[4];
+  if (t.interleaved) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = __shfl_sync(0xFFFFFFFFu, w[i], from, LANES);
-  if (c0 >= t.rot) return;
+    for (int i = 0; i < 4; ++i) o[i] = __funnelshift_l(w[i], w[i], 16);
+  } else {
+    const int from = c0 >= t.rot ? x : c0 < half ? x + (half >> 3) : x - (half >> 3);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float other = __fmul_rn((i & 1) ? hi_f(o[i >> 1]) : lo_f(o[i >> 1]), u.s[i]), mine = __fmul_rn(y[i], u.c[i]);
-    y[i] = first ? __fsub_rn(mine, other) : __fadd_rn(mine, other);
+    for (int i = 0; i < 4; ++i) o[i] = __shfl_sync(0xFFFFFFFFu, w[i], from, LANES);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = pair_of(w[i]);
+  if (c0 < t.rot) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = add_pair(mul_pair(y[i], u.c[i]), mul_pair(pair_of(o[i]), u.s[i]));
   }
 }
-__device__ __forceinline__ uint4 pack8(const float (&y)[8]) {
+__device__ __forceinline__ uint4 pack8(const uint64_t (&y)[4]) {
   uint32_t r[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+    const __nv_bfloat162 v = __floats2bfloat162_rn(first_of(y[i]), second_of(y[i]));
     r[i] = *reinterpret_cast<const uint32_t*>(&v);
   }
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-// Heads of one row: d / 8 lanes have a head, a thread HEADS of them at a time, whose loads are all on their way before the
-// first is used; the row's cosines and sines serve them all.  src(g) and dst(g): where head g is and goes (nullptr: nowhere); heads
-// from `plain` on are copied as they are.  By whole warps.
-constexpr int HEADS = 4;
-template <int DH, int THREADS, class Src, class Dst>
-__device__ __forceinline__ void turn_heads(const Table& t, const float* row, int n_heads, int plain, Src src, Dst dst) {
-  constexpr int LANES = DH / 8, SLOTS = THREADS / LANES;
-  const int x = threadIdx.x % LANES, g0 = threadIdx.x / LANES;
-  Turn u;
-  load_turn(t, row, x, u);
-  for (int g = g0; g - g0 < n_heads; g += HEADS * SLOTS) {     // (the same number of times for a warp)
-    uint4 v[HEADS];
+// Heads of one row by a warp: d / 8 lanes have one, the warp 256 / d of them side by side (a group), AHEAD groups on their way at a
+// time; the row's cosines and sines stay with the lanes.  Where few rows are to be turned, several warps share a row's groups: this one
+// has groups `first`, first + step, ...  turned: else copied as they are.
+constexpr int AHEAD = 4;
+template <int DH, bool TURNED>
+__device__ __forceinline__ void row_heads(const Table& t, const Turn& u, int heads, int first, int step, const char* src, int64_t ss, char* dst, int64_t ds) {
+  constexpr int LANES = DH / 8, GROUP = 32 / LANES;
+  const int lane = threadIdx.x & 31, x = lane % LANES, sub = lane / LANES;
+  src += (int64_t)(first * GROUP + sub) * ss + 16 * x;
+  dst += (int64_t)(first * GROUP + sub) * ds + 16 * x;
+  ss *= step * GROUP; ds *= step * GROUP;
+  for (int h0 = first * GROUP; h0 < heads; h0 += AHEAD * step * GROUP) {
+    uint4 v[AHEAD];
 #pragma unroll
-    for (int j = 0; j < HEADS; ++j) {
-      const int h = g + j * SLOTS;
-      v[j] = h < n_heads ? *(reinterpret_cast<const uint4*>(src(h)) + x) : make_uint4(0, 0, 0, 0);
+    for (int j = 0; j < AHEAD; ++j) {
+      v[j] = make_uint4(0, 0, 0, 0);
+      if (h0 + j * step * GROUP + sub < heads) v[j] = *reinterpret_cast<const uint4*>(src);
+      src += ss;
     }
 #pragma unroll
-    for (int j = 0; j < HEADS; ++j) {
-      const int h = g + j * SLOTS;
-      if (g - g0 + j * SLOTS >= n_heads) break;
-      float y[8];
-      turn_row<LANES>(t, v[j], x, u, y);
-      char* to = h < n_heads ? dst(h) : nullptr;
-      if (to) *(reinterpret_cast<uint4*>(to) + x) = h < plain ? pack8(y) : v[j];
+    for (int j = 0; j < AHEAD; ++j) {
+      if (h0 + j * step * GROUP >= heads) break;     // (the same for the warp)
+      if (TURNED) {
+        uint64_t y[4];
+        turn_row<LANES>(t, v[j], x, u, y);
+        v[j] = pack8(y);
+      }
+      if (h0 + j * step * GROUP + sub < heads) *reinterpret_cast<uint4*>(dst) = v[j];
+      dst += ds;
     }
   }
+}
+// Warps that share a row, a power of two up to `most`: until there are 32 for each SM.
+static inline int warps_per_row(int64_t rows, int sm_count, int most) {
+  int w = 1;
+  while (w < most && rows * w < 32ll * sm_count) w *= 2;
+  return w;
 }
 
 }  // namespace rope
