@@ -28,7 +28,8 @@ constexpr int TILE = SPACE_PAGE_SIZE;                // keys of a page, rows of 
 constexpr int GROUP = 128, SOFT = 2 * GROUP, THREADS = SOFT + GROUP;           // (registers move by groups of four warps)
 constexpr int SHARE_COST = 3;                        // fixed cost of an item, in pages
 constexpr int RING = 16;                             // scales and announcements of that many pages
-enum { NO_MORE = 0x7FFFFFFF };
+enum { NO_MORE = 0x7FFFFFFF };                        // announced behind the last page
+enum { OWN = 0x7FFFFFFE };                            // announced as an item's last page: the block's own rows
 constexpr float REF_FAR = 0x1p22f;                   // up to this a reference's rounding moves weights by 2^0.25 at most
 
 template <int DH>
@@ -37,16 +38,14 @@ struct Smem {
   static constexpr int STAGES = DH == 128 ? 5 : 8;
   static constexpr int MEET = DH / 4;                        // channels of a thread that copies of a row meet in at a time
   static constexpr int PITCH = SOFT + 1;                     // floats (four channels apart: another bank)
-  static constexpr int MEET_OFF = 0;                         // [MEET][PITCH]; the block's own V rows before
-  static constexpr int OWN_PITCH = 2 * DH + 16;              // bytes of those
+  static constexpr int MEET_OFF = 0;                         // [MEET][PITCH]
   static constexpr int MEET_BYTES = MEET * PITCH * 4 / 128 * 128 + 128;
-  static_assert(SPACE_MAX_ROWS * OWN_PITCH <= MEET_BYTES, "the block's V rows fit where sums meet");
   static constexpr int K_OFF = MEET_BYTES;                   // [STAGES]
   static constexpr int V_OFF = K_OFF + STAGES * F::CODES;    // [STAGES]
   static constexpr int SCALE_OFF = V_OFF + STAGES * F::CODES;        // [RING][4] {K, V}
   static constexpr int ML_OFF = SCALE_OFF + RING * 32;       // [2][SOFT] {M, l} of rows' halves and copies, by item
-  static constexpr int OWN_OFF = ML_OFF + 2 * SOFT * 8;      // [2][128] {M, l} of rows over the block's own rows
-  static constexpr int XCH_OFF = OWN_OFF + 2 * GROUP * 8;    // [2][SOFT] a page's {largest score, E} of a row's halves
+  static constexpr int OWN_OFF = ML_OFF + 2 * SOFT * 8;      // [STAGES][64] of the block's own rows {K's power of two, V's exponent}
+  static constexpr int XCH_OFF = OWN_OFF + STAGES * SPACE_MAX_ROWS * 8;    // [2][SOFT] a page's {largest score, E} of a row's halves
   static constexpr int TOPS_OFF = XCH_OFF + 2 * SOFT * 8;    // [2][SOFT] largest elements of query rows' halves, by item
   static constexpr int DESC_OFF = TOPS_OFF + 2 * SOFT * 4;   // [RING] {item of the share, page of it}
   static constexpr int BAR_OFF = DESC_OFF + RING * 8;
@@ -103,16 +102,79 @@ __device__ __forceinline__ float max16(const uint32_t* s) {
   return fmaxf(max3(a, b, c), x[15]);
 }
 
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3},{%4,%5,%6,%7},{%8,%9},{%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t transpose8(uint32_t v) {                   // 8 x 8 halves over the warp
-  uint32_t r;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
-  return r;
-}
+__device__ __forceinline__ void pair_sync() { asm volatile("bar.sync 2, 64;" ::: "memory"); }      // the warps that bring own rows
 __device__ __forceinline__ void prefetch_line(const char* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
+// The block's own rows as a page, by two warps: row j's K as two e4m3 terms in rows j and 64 + j of the stage, V likewise in sixteens
+// j / 16 and 4 + j / 16; each row has powers of two of its own.  Row n_q and those behind it: zeros.
+template <int DH>
+__device__ __forceinline__ void bring_own(const Params& p, int b, int h, unsigned char* ks, unsigned char* vs, float2* sc, uint32_t full_k) {
+  using F = Fmt<DH>;
+  constexpr int LANES = DH / 4, PER = 64 / LANES, BATCH = 4;          // lanes of a row in the first pass, rows of both warps
+  const int t = threadIdx.x & 63;
+  const char* kn = p.kn + (int64_t)b * p.n_sb + (int64_t)h * p.n_sh;
+  const char* vn = p.vn + (int64_t)b * p.n_sb + (int64_t)h * p.n_sh;
+  const int x = t % LANES;
+  const uint32_t lanes = LANES == 32 ? 0xFFFFFFFFu : 0xFFFFu << (t & 16);
+#pragma unroll 1
+  for (int r0 = t / LANES; r0 < SPACE_MAX_ROWS; r0 += BATCH * PER) {
+    uint2 k[BATCH], v[BATCH];
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      const int r = r0 + j * PER;
+      k[j] = v[j] = make_uint2(0, 0);
+      if (r < p.n_q) {
+        k[j] = *(reinterpret_cast<const uint2*>(kn + (int64_t)r * p.n_sr) + x);
+        v[j] = *(reinterpret_cast<const uint2*>(vn + (int64_t)r * p.n_sr) + x);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      const int r = r0 + j * PER;
+      k[j] = make_uint2(kvq::finite_pair(k[j].x), kvq::finite_pair(k[j].y));
+      v[j] = make_uint2(kvq::finite_pair(v[j].x), kvq::finite_pair(v[j].y));
+      const uint32_t kt = __reduce_max_sync(lanes, kvq::max_bits(make_uint4(k[j].x, k[j].y, 0, 0)));
+      const uint32_t vt = __reduce_max_sync(lanes, kvq::max_bits(make_uint4(v[j].x, v[j].y, 0, 0)));
+      const int ke = max((int)(kt >> 7) - 127, -100) - 7, ve = max((int)(vt >> 7) - 127, -100) - 7;      // the largest to [2^7, 2^8)
+      const float up = pow2(-ke);
+      uint32_t w0, w1;
+      split4(kvq::bf_lo(k[j].x) * up, kvq::bf_hi(k[j].x) * up, kvq::bf_lo(k[j].y) * up, kvq::bf_hi(k[j].y) * up, w0, w1);
+      unsigned char* at = ks + (x >> 2) * F::K_COLS + 16 * r + 4 * (x & 3);
+      *reinterpret_cast<uint32_t*>(at) = w0;
+      *reinterpret_cast<uint32_t*>(at + 16 * SPACE_MAX_ROWS) = w1;
+      if (x == 0) sc[r] = make_float2(pow2(ke), (float)ve);
+    }
+  }
+  fence_async();
+  pair_sync();
+  if (t == 0) mbar_arrive(full_k);
+  // a thread has two channels (of 64: with half of the keys), four keys at a time
+  constexpr int PARTS = 128 / DH;
+  const int c = 2 * (t % (DH / 2)), q0 = t / (DH / 2);
+#pragma unroll 2
+  for (int q = q0; q < SPACE_MAX_ROWS / 4; q += PARTS) {
+    uint32_t w[4];
+    float up[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = 4 * q + j;
+      w[j] = r < p.n_q ? *reinterpret_cast<const uint32_t*>(vn + (int64_t)r * p.n_sr + 2 * c) : 0u;
+      up[j] = pow2(-(int)sc[r].y);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = kvq::finite_pair(w[j]);
+    unsigned char* at = vs + (q >> 2) * F::V_ROWS + 16 * c + 4 * (q & 3);
+    uint32_t w0, w1;
+    split4(kvq::bf_lo(w[0]) * up[0], kvq::bf_lo(w[1]) * up[1], kvq::bf_lo(w[2]) * up[2], kvq::bf_lo(w[3]) * up[3], w0, w1);
+    *reinterpret_cast<uint32_t*>(at) = w0;
+    *reinterpret_cast<uint32_t*>(at + 4 * F::V_ROWS) = w1;
+    split4(kvq::bf_hi(w[0]) * up[0], kvq::bf_hi(w[1]) * up[1], kvq::bf_hi(w[2]) * up[2], kvq::bf_hi(w[3]) * up[3], w0, w1);
+    *reinterpret_cast<uint32_t*>(at + 16) = w0;
+    *reinterpret_cast<uint32_t*>(at + 16 + 4 * F::V_ROWS) = w1;
+  }
+  fence_async();
+  pair_sync();
+}
 
 // The items of a block's share, in order: every role walks them for itself.
 struct Walk {
@@ -222,7 +284,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
   auto hold = [&](int bar, uint32_t use, int site) { return wait(BAR(bar), use & 1, abort_flag, p.err, site); };
 
   if (warp >= 8) {
-    regs_dec<40>();
+    regs_dec<56>();
     if (warp == 9 && elect_one()) {
       // ---- copies: K of a page when the K of the page that had its stage has been used, V likewise
       bool ok = true;
@@ -256,6 +318,12 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           }
           ++m;
         }
+        if (ok && p.has_new && wk.L >= 0 && wk.t1 > wk.cached()) {             // (two other warps bring them)
+          desc[m % RING].x = item; desc[m % RING].y = OWN;
+          mbar_arrive(BAR(SAID + m % RING));
+          if (m >= STAGES) ok = hold(FREEK + m % STAGES, m / STAGES - 1, 20) && hold(FREEV + m % STAGES, m / STAGES - 1, 21);
+          ++m;
+        }
       }
       if (ok) {
         desc[m % RING].x = NO_MORE;
@@ -287,12 +355,20 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           if (m && q > m) ok = hold(ODONE, m - 1, 6) && ok;                    // (the weights of page q - 2 lie where these scores go)
           tc_fence_after();
           const uint64_t kd = plain_desc(base + S::K_OFF + s * F::CODES, F::K_COLS, 128);
-          if (ok) {
+          const uint32_t qd = TM_Q + ((queries - 1) & 1) * 64;
+          if (ok && desc[q % RING].y != OWN) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
               for (int ks = 0; ks < DH / 32; ++ks)
-                mma8_ts(TM_S + (q & 1) * TILE, TM_Q + ((queries - 1) & 1) * 64 + i * (DH / 4) + 8 * ks, kd + (uint64_t)((ks * 2 * F::K_COLS) >> 4), instr_desc(TILE), i + ks > 0);
+                mma8_ts(TM_S + (q & 1) * TILE, qd + i * (DH / 4) + 8 * ks, kd + (uint64_t)((ks * 2 * F::K_COLS) >> 4), instr_desc(TILE), i + ks > 0);
+          } else if (ok) {                           // both terms of 64 rows onto the same scores
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int ks = 0; ks < DH / 32; ++ks)
+                mma8_ts(TM_S + (q & 1) * TILE, qd + (i & 1) * (DH / 4) + 8 * ks, kd + (uint64_t)((ks * 2 * F::K_COLS + (i >> 1) * 16 * SPACE_MAX_ROWS) >> 4),
+                        instr_desc(SPACE_MAX_ROWS), i + ks > 0);
           }
           tc_commit(BAR(SDONE + (q & 1)));
           tc_commit(BAR(FREEK + s));
@@ -307,40 +383,61 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
         if (m) ok = hold(ODONE, m - 1, 8) && ok;     // (long since: whoever brings the weights has waited for it)
         ok = hold(PREADY, m, 9) && ok;
         tc_fence_after();
+        const int chunks = desc[m % RING].y == OWN ? 1 : 3;          // (own rows: their second terms with the same weights)
         const uint64_t vd = plain_desc(base + S::V_OFF + s * F::CODES, F::V_ROWS, 128);
         if (ok) {
 #pragma unroll
           for (int b = 0; b < 4; ++b)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-              mma8_ts(TM_O, TM_S + (m & 1) * TILE + 32 * b + 8 * i, vd + (uint64_t)((2 * b * F::V_ROWS) >> 4), instr_desc(DH), b + i > 0);
+              mma8_ts(TM_O, TM_S + (m & 1) * TILE + 32 * (b & chunks) + 8 * i, vd + (uint64_t)((2 * b * F::V_ROWS) >> 4), instr_desc(DH), b + i > 0);
         }
         tc_commit(BAR(ODONE));
         tc_commit(BAR(FREEV + s));
         ++m;
       }
       if (m) hold(ODONE, m - 1, 10);                 // all products done before tensor memory is released
-    } else if (warp == 10) {
+    } else if (warp >= 10) {
       // ---- query rows, and the block's own, of all the share's items: out of HBM before somebody waits for them
-      while (wk.next(prefix, seq_len, p.has_new, share0)) {
-        const int h = wk.it / p.n_rt, r0 = (wk.it - h * p.n_rt) * RT, rows = min(p.n_q * p.G - r0, RT);
-        for (int r = lane; r < rows; r += 32) {
+      Walk ahead = wk;
+      while (ahead.next(prefix, seq_len, p.has_new, share0)) {
+        const int h = ahead.it / p.n_rt, r0 = (ahead.it - h * p.n_rt) * RT, rows = min(p.n_q * p.G - r0, RT), t = threadIdx.x & 63;
+        for (int r = t; r < rows; r += 64) {
           int i, hq;
           row_of(p, h, r0 + r, i, hq);
-          const char* at = p.q + (int64_t)wk.b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh;
+          const char* at = p.q + (int64_t)ahead.b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh;
           prefetch_line(at);
           if (DH == 128) prefetch_line(at + 128);
         }
-        if (!p.has_new || wk.t1 <= wk.cached()) continue;
-        for (int r = lane; r < p.n_q; r += 32) {
-          const int64_t at = (int64_t)wk.b * p.n_sb + (int64_t)r * p.n_sr + (int64_t)h * p.n_sh;
+        if (!p.has_new || ahead.t1 <= ahead.cached()) continue;
+        if (t < p.n_q) {
+          const int64_t at = (int64_t)ahead.b * p.n_sb + (int64_t)t * p.n_sr + (int64_t)h * p.n_sh;
           prefetch_line(p.kn + at); prefetch_line(p.vn + at);
           if (DH == 128) { prefetch_line(p.kn + at + 128); prefetch_line(p.vn + at + 128); }
         }
       }
+      // ---- the block's own rows, wherever they are announced
+      int item = -1;
+      for (;; ++m) {
+        if (!hold(SAID + m % RING, m / RING, 17)) break;
+        const int it = desc[m % RING].x;
+        if (it == NO_MORE) break;
+        if (desc[m % RING].y != OWN) continue;
+        for (; item < it; ++item) wk.next(prefix, seq_len, p.has_new, share0);
+        const uint32_t s = m % STAGES;
+        bool ok = true;
+        if (m >= STAGES) {
+          ok = hold(FREEK + s, m / STAGES - 1, 18);
+          ok = hold(FREEV + s, m / STAGES - 1, 19) && ok;
+        }
+        if (__any_sync(0xFFFFFFFFu, !ok)) break;
+        bring_own<DH>(p, wk.b, wk.it / p.n_rt, sm + S::K_OFF + s * F::CODES, sm + S::V_OFF + s * F::CODES,
+                      reinterpret_cast<float2*>(sm + S::OWN_OFF) + s * SPACE_MAX_ROWS, BAR(FULLK + s));
+        if ((threadIdx.x & 63) == 0) mbar_arrive(BAR(FULLV + s));
+      }
     }
   } else {
-    regs_inc<232>();                                 // (256 threads x 232 + 128 x 40 = the 384 x 168 of the launch)
+    regs_inc<224>();                                 // (256 threads x 224 + 128 x 56 = the 384 x 168 of the launch)
     const int half = warp >> 2, tid = threadIdx.x & (GROUP - 1), w4 = warp & 3;
     const int rep = w4 / (4 / REP), row = tid % RT;
     const uint32_t lanes = (uint32_t)(32 * w4) << 16;
@@ -401,7 +498,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
     if (live) bring_query(0);
     for (int item = 0; live; ++item) {
       const int b = wk.b, it = wk.it, L = wk.L, T = wk.pages(p.has_new);
-      const bool whole = wk.t0 == 0 && wk.t1 == T, opens = wk.opens, owned = p.has_new && L >= 0 && wk.t1 > wk.cached();
+      const bool whole = wk.t0 == 0 && wk.t1 == T, opens = wk.opens;
       const uint32_t item_at = wk.at;
       const int h = it / p.n_rt, r0 = (it - h * p.n_rt) * RT, rows = min(p.n_q * p.G - r0, RT);
       const float f = f_next;
@@ -437,8 +534,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
         const uint32_t s = m % STAGES;
         const uint32_t TM_SM = TM_S + lanes + (m & 1) * TILE;                  // the page's scores
         const float2* sc = reinterpret_cast<const float2*>(sm + S::SCALE_OFF + (m % RING) * 32) + (key0 >> 5);
-        const int vis0 = L - t * TILE, vis = vis0 - key0;            // visible keys of the page, and of this thread
-        if (vis0 < TILE) {                           // what lies behind the last row must not count, whatever it is
+        const int vis0 = L - (t == OWN ? 0 : t) * TILE, vis = vis0 - key0;            // visible keys of the page, and of this thread
+        if (vis0 < TILE && t != OWN) {               // what lies behind the last row must not count, whatever it is
           hold(FULLV + s, m / STAGES, 14);
           const int g0 = vis0 >> 4;
 #pragma unroll 1
@@ -466,91 +563,131 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           else tmem_ld32(TM_SM + key0 + 32 * k, v + 32 * k);
         }
         tmem_wait_ld();
-        // ---- largest scores
-        float fk[NC], ms[NC], mb[NC], x[NC], pm = -CUDART_INF_F, E = -CUDART_INF_F;
-        if (vis < KEYS) {
+        float pm = -CUDART_INF_F, E = -CUDART_INF_F, top = 0.f, lower = 0.f, sum = 0.f;
+        bool none = false;                           // this row sees nothing of the page
+        // both halves of the row: the page's largest score, and E relative to it
+        auto meet = [&]() {
+          float2* xch = reinterpret_cast<float2*>(sm + S::XCH_OFF) + (m & 1) * SOFT;
+          xch[threadIdx.x] = make_float2(pm, E);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(BAR(XCH + w4));
+          hold(XCH + w4, m, 16);
+          const float2 other = xch[threadIdx.x ^ GROUP];
+          top = fmaxf(pm, other.x); lower = pm - top;
+          none = top == -CUDART_INF_F;
+          E = none ? 0.f : fmaxf(E + lower, other.y + (other.x - top));
+        };
+        // (sixteen weights, first terms, then second ones: where scores of the same 32 keys were)
+        auto put = [&](int u, uint32_t* w) {
+          const int key = key0 + u;
+          const uint32_t at = TM_SM + (key & ~31) + ((key >> 4) & 1) * 4;
+          tmem_st4(at, w);
+          tmem_st4(at + 8, w + 4);
+        };
+        if (t != OWN) {
+          float fk[NC], ms[NC], mb[NC], x[NC], ev[NC];
+          if (vis < KEYS) {
 #pragma unroll
-          for (int j = 0; j < KEYS; ++j) if (j >= vis) v[j] = 0xFF800000u;
-        }
-        bool far = false;
-#pragma unroll
-        for (int k = 0; k < NC; ++k) {
-          ms[k] = max16(v + 32 * k);
-          if (N1 > 16) ms[k] = fmaxf(ms[k], max16(v + 32 * k + 16));
-          fk[k] = fminf(fmaxf(f * sc[k].x, F_MIN), F_MAX);
-          x[k] = ms[k] * fk[k];
-          mb[k] = ms[k] == -CUDART_INF_F ? 0.f : x[k];
-          far = far || fabsf(mb[k]) > REF_FAR;
-        }
-        if (__any_sync(0xFFFFFFFFu, far)) {          // scores off the largest first, then times the factor
+            for (int j = 0; j < KEYS; ++j) if (j >= vis) v[j] = 0xFF800000u;
+          }
+          bool far = false;
 #pragma unroll
           for (int k = 0; k < NC; ++k) {
-            const float top = ms[k] == -CUDART_INF_F ? 0.f : ms[k];
-            if (fabsf(mb[k]) > SCORE_MAX) {
-              fk[k] = SCORE_MAX / fabsf(top);
-              x[k] = copysignf(SCORE_MAX, top);
-            }
-            mb[k] = 0.f;
-#pragma unroll
-            for (int j = 0; j < N1; ++j) v[32 * k + j] = __float_as_uint(__uint_as_float(v[32 * k + j]) - top);
+            ms[k] = max16(v + 32 * k);
+            if (N1 > 16) ms[k] = fmaxf(ms[k], max16(v + 32 * k + 16));
+            fk[k] = fminf(fmaxf(f * sc[k].x, F_MIN), F_MAX);
+            x[k] = ms[k] * fk[k];
+            mb[k] = ms[k] == -CUDART_INF_F ? 0.f : x[k];
+            far = far || fabsf(mb[k]) > REF_FAR;
           }
-        }
+          if (__any_sync(0xFFFFFFFFu, far)) {          // scores off the largest first, then times the factor
 #pragma unroll
-        for (int k = 0; k < NC; ++k) pm = fmaxf(pm, x[k]);
-        float ev[NC];
+            for (int k = 0; k < NC; ++k) {
+              const float top = ms[k] == -CUDART_INF_F ? 0.f : ms[k];
+              if (fabsf(mb[k]) > SCORE_MAX) {
+                fk[k] = SCORE_MAX / fabsf(top);
+                x[k] = copysignf(SCORE_MAX, top);
+              }
+              mb[k] = 0.f;
 #pragma unroll
-        for (int k = 0; k < NC; ++k) {
-          ev[k] = (float)((int)((__float_as_uint(sc[k].y) >> 23) & 255u) - 127);
-          x[k] = x[k] == -CUDART_INF_F ? -CUDART_INF_F : x[k] - pm;
-          E = fmaxf(E, x[k] + ev[k]);
-        }
-        // ---- both halves of the row: the page's largest score, and E relative to it
-        float2* xch = reinterpret_cast<float2*>(sm + S::XCH_OFF) + (m & 1) * SOFT;
-        xch[threadIdx.x] = make_float2(pm, E);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(BAR(XCH + w4));
-        hold(XCH + w4, m, 16);
-        const float2 other = xch[threadIdx.x ^ GROUP];
-        const float top = fmaxf(pm, other.x), lower = pm - top;
-        const bool none = top == -CUDART_INF_F;      // this row sees nothing of the page
-        E = none ? 0.f : fmaxf(E + lower, other.y + (other.x - top));
-        // ---- weights
-        float wf[NC], part[NC];
+              for (int j = 0; j < N1; ++j) v[32 * k + j] = __float_as_uint(__uint_as_float(v[32 * k + j]) - top);
+            }
+          }
 #pragma unroll
-        for (int k = 0; k < NC; ++k) {
-          const float d = none || x[k] == -CUDART_INF_F ? -CUDART_INF_F : x[k] + lower;
-          wf[k] = fast_exp2(d + (ev[k] + 8.f - E));
-          part[k] = fast_exp2(d);
-        }
-        float sum = 0.f;
+          for (int k = 0; k < NC; ++k) pm = fmaxf(pm, x[k]);
 #pragma unroll
-        for (int k = 0; k < NC; ++k) {
-          const uint64_t f2 = pack2(fk[k], fk[k]), n2 = pack2(-mb[k], -mb[k]), w2 = pack2(wf[k], wf[k]);
-          uint64_t sum0 = 0ull, sum1 = 0ull;
+          for (int k = 0; k < NC; ++k) {
+            ev[k] = (float)((int)((__float_as_uint(sc[k].y) >> 23) & 255u) - 127);
+            x[k] = x[k] == -CUDART_INF_F ? -CUDART_INF_F : x[k] - pm;
+            E = fmaxf(E, x[k] + ev[k]);
+          }
+          meet();
+          float wf[NC], part[NC];
 #pragma unroll
-          for (int u = 0; u < N1; u += 16) {
+          for (int k = 0; k < NC; ++k) {
+            const float d = none || x[k] == -CUDART_INF_F ? -CUDART_INF_F : x[k] + lower;
+            wf[k] = fast_exp2(d + (ev[k] + 8.f - E));
+            part[k] = fast_exp2(d);
+          }
+#pragma unroll
+          for (int k = 0; k < NC; ++k) {
+            const uint64_t f2 = pack2(fk[k], fk[k]), n2 = pack2(-mb[k], -mb[k]), w2 = pack2(wf[k], wf[k]);
+            uint64_t sum0 = 0ull, sum1 = 0ull;
+#pragma unroll
+            for (int u = 0; u < N1; u += 16) {
+              uint32_t w[8];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint32_t* y = v + 32 * k + u + 4 * j;
+                float a, b, c, d;
+                unpack2(fma2(pack2(__uint_as_float(y[0]), __uint_as_float(y[1])), f2, n2), a, b);
+                unpack2(fma2(pack2(__uint_as_float(y[2]), __uint_as_float(y[3])), f2, n2), c, d);
+                const uint64_t e0 = pack2(fast_exp2(a), fast_exp2(b)), e1 = pack2(fast_exp2(c), fast_exp2(d));
+                sum0 = add2(sum0, e0); sum1 = add2(sum1, e1);
+                unpack2(mul2(e0, w2), a, b);
+                unpack2(mul2(e1, w2), c, d);
+                split4(a, b, c, d, w[j], w[4 + j]);
+              }
+              put(32 * k + u, w);
+            }
+            float a, b;
+            unpack2(add2(sum0, sum1), a, b);
+            sum = fmaf(a + b, part[k], sum);
+          }
+        } else {
+          // the block's own rows: a mask and powers of two for each key
+          hold(FULLK + s, m / STAGES, 22);           // (long since; for those powers of two)
+          const bool sees = rep * (TILE / REP) < SPACE_MAX_ROWS && row < rows;
+          const uint64_t mask = sees ? reinterpret_cast<const uint64_t*>(sm + S::MASK_OFF)[(r0 + row) >> p.gsh] >> (key0 & 63) : 0ull;     // Eq. 5
+          const float2* own = reinterpret_cast<const float2*>(sm + S::OWN_OFF) + s * SPACE_MAX_ROWS + (key0 & 63);
+#pragma unroll
+          for (int j = 0; j < KEYS; ++j) {
+            float y = __uint_as_float(v[j]) * fminf(fmaxf(f * own[j].x, F_MIN), F_MAX);
+            y = (mask >> j) & 1ull ? (y > SCORE_MAX ? SCORE_MAX : y < -SCORE_MAX ? -SCORE_MAX : y) : -CUDART_INF_F;
+            pm = fmaxf(pm, y);
+            v[j] = __float_as_uint(y);
+          }
+          const float from = pm == -CUDART_INF_F ? 0.f : pm;
+#pragma unroll
+          for (int j = 0; j < KEYS; ++j) E = fmaxf(E, __uint_as_float(v[j]) - from + own[j].y);
+          meet();
+          const float ref = none ? 0.f : top, up = 8.f - E;
+#pragma unroll
+          for (int u = 0; u < KEYS; u += 16) {
             uint32_t w[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const uint32_t* y = v + 32 * k + u + 4 * j;
-              float a, b, c, d;
-              unpack2(fma2(pack2(__uint_as_float(y[0]), __uint_as_float(y[1])), f2, n2), a, b);
-              unpack2(fma2(pack2(__uint_as_float(y[2]), __uint_as_float(y[3])), f2, n2), c, d);
-              const uint64_t e0 = pack2(fast_exp2(a), fast_exp2(b)), e1 = pack2(fast_exp2(c), fast_exp2(d));
-              sum0 = add2(sum0, e0); sum1 = add2(sum1, e1);
-              unpack2(mul2(e0, w2), a, b);
-              unpack2(mul2(e1, w2), c, d);
-              split4(a, b, c, d, w[j], w[4 + j]);
+              float y[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float off = __uint_as_float(v[u + 4 * j + i]) - ref;
+                sum += fast_exp2(off);
+                y[i] = fast_exp2(off + (own[u + 4 * j + i].y + up));
+              }
+              split4(y[0], y[1], y[2], y[3], w[j], w[4 + j]);
             }
-            // (sixteen weights, first terms, then second ones: where scores of the same 32 keys were)
-            const int key = key0 + 32 * k + u;
-            const uint32_t at = TM_SM + (key & ~31) + ((key >> 4) & 1) * 4;
-            tmem_st4(at, w);
-            tmem_st4(at + 8, w + 4);
+            put(u, w);
           }
-          float a, b;
-          unpack2(add2(sum0, sum1), a, b);
-          sum = fmaf(a + b, part[k], sum);
         }
         if (REP > 1) {                               // keys that other copies of the row have: each half two of the four chunks
           const uint32_t zero[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
@@ -582,143 +719,6 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
       live = wk.next(prefix, seq_len, p.has_new, share0);
       if (live) bring_query(item + 1);
 
-      // ---- the block's own rows: eight query rows a warp (sixteen of 128), as columns; products in bf16 as they are, weights as two bf16
-      // terms, 2^-32 as large: sums of rows next to the largest number stay numbers
-      constexpr int ON = RT > 64 ? 2 : 1;            // eights of a warp
-      const int n8 = lane >> 2, t4 = lane & 3;
-      float od[ON][DH / 16][4], om[ON][2], ol[ON][2];
-      float2* own = reinterpret_cast<float2*>(sm + S::OWN_OFF) + (item & 1) * GROUP;
-      if (owned) {
-        unsigned char* vrows = sm + S::MEET_OFF;
-        const int keys = (p.n_q + 15) & ~15;
-        const char* kbase = p.kn + (int64_t)b * p.n_sb + (int64_t)h * p.n_sh;
-        const char* vbase = p.vn + (int64_t)b * p.n_sb + (int64_t)h * p.n_sh;
-#pragma unroll 1
-        for (int e = threadIdx.x; e < keys * (DH / 8); e += SOFT) {
-          const int key = e / (DH / 8), c = e % (DH / 8);
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (key < p.n_q) x = *(reinterpret_cast<const uint4*>(vbase + (int64_t)key * p.n_sr) + c);
-          kvq::make_finite(x);
-          *reinterpret_cast<uint4*>(vrows + key * S::OWN_PITCH + 16 * c) = x;
-        }
-        uint4 qr[ON][DH / 32];
-#pragma unroll
-        for (int o = 0; o < ON; ++o) {
-          int i, hq;
-          row_of(p, h, r0 + 8 * (ON * warp + o) + n8, i, hq);
-          const bool there = 8 * (ON * warp + o) + n8 < rows;
-          const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh) + t4 * (DH / 32);
-#pragma unroll
-          for (int j = 0; j < DH / 32; ++j) qr[o][j] = there ? src[j] : make_uint4(0, 0, 0, 0);
-#pragma unroll
-          for (int ct = 0; ct < DH / 16; ++ct) od[o][ct][0] = od[o][ct][1] = od[o][ct][2] = od[o][ct][3] = 0.f;
-          om[o][0] = om[o][1] = -CUDART_INF_F;
-          ol[o][0] = ol[o][1] = 0.f;
-        }
-        soft_sync();
-#pragma unroll 1
-        for (int k0 = 0; k0 < keys && 8 * ON * warp < rows; k0 += 16) {
-          uint4 kr[2][DH / 32];
-          float sc[ON][4], kf[2] = {p.c, p.c};
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int key = k0 + 8 * i + n8;
-            const uint4* src = reinterpret_cast<const uint4*>(kbase + (int64_t)key * p.n_sr) + t4 * (DH / 32);
-#pragma unroll
-            for (int j = 0; j < DH / 32; ++j) kr[i][j] = key < p.n_q ? src[j] : make_uint4(0, 0, 0, 0);
-          }
-          uint32_t big[2] = {0, 0};
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < DH / 32; ++j) big[i] = max(big[i], kvq::max_bits(kr[i][j]));
-          if (__any_sync(0xFFFFFFFFu, max(big[0], big[1]) >= 0x7200u)) {       // (from 2^101 on: what is not finite, and sums that fp32 would not hold)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              big[i] = max(big[i], __shfl_xor_sync(0xFFFFFFFFu, big[i], 1));
-              big[i] = max(big[i], __shfl_xor_sync(0xFFFFFFFFu, big[i], 2));
-#pragma unroll
-              for (int j = 0; j < DH / 32; ++j) {
-                kvq::make_finite(kr[i][j]);
-                if (big[i] >= 0x7200u) kr[i][j] = kvq::scale_bf16(kr[i][j], 0x1p-64f);
-              }
-              if (big[i] >= 0x7200u) kf[i] = p.c * 0x1p64f;
-            }
-          }
-          uint32_t ph[ON][2], pl[ON][2];
-#pragma unroll
-          for (int o = 0; o < ON; ++o) {
-            sc[o][0] = sc[o][1] = sc[o][2] = sc[o][3] = 0.f;
-#pragma unroll
-            for (int j = 0; j < DH / 32; ++j) {
-              mma_bf16(sc[o], kr[0][j].x, kr[1][j].x, kr[0][j].y, kr[1][j].y, qr[o][j].x, qr[o][j].y);
-              mma_bf16(sc[o], kr[0][j].z, kr[1][j].z, kr[0][j].w, kr[1][j].w, qr[o][j].z, qr[o][j].w);
-            }
-            float down[2];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const int r = 8 * (ON * warp + o) + 2 * t4 + c;
-              const uint64_t see = r < rows ? reinterpret_cast<const uint64_t*>(sm + S::MASK_OFF)[(r0 + r) >> p.gsh] : 0ull;     // Eq. 5
-              float top = om[o][c];
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                float& y = sc[o][2 * i + c];
-                y *= kf[i];                          // (a row that is not finite: NaN here, and at the end)
-                y = (see >> (k0 + 8 * i + n8)) & 1ull ? (y > SCORE_MAX ? SCORE_MAX : y < -SCORE_MAX ? -SCORE_MAX : y) : -CUDART_INF_F;
-                top = fmaxf(top, y);
-              }
-#pragma unroll
-              for (int k = 4; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, k));
-              down[c] = om[o][c] == top ? 1.f : fast_exp2(om[o][c] - top);
-              om[o][c] = top;
-              const float from = top == -CUDART_INF_F ? 0.f : top;
-              ol[o][c] *= down[c];
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                float& y = sc[o][2 * i + c];
-                y = fast_exp2(y - from);
-                ol[o][c] += y;
-              }
-            }
-            if (__any_sync(0xFFFFFFFFu, down[0] != 1.f || down[1] != 1.f)) {
-#pragma unroll
-              for (int ct = 0; ct < DH / 16; ++ct) { od[o][ct][0] *= down[0]; od[o][ct][1] *= down[1]; od[o][ct][2] *= down[0]; od[o][ct][3] *= down[1]; }
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float w0 = sc[o][2 * i] * 0x1p-32f, w1 = sc[o][2 * i + 1] * 0x1p-32f;
-              const __nv_bfloat162 hi = __floats2bfloat162_rn(w0, w1);
-              const uint32_t hw = *reinterpret_cast<const uint32_t*>(&hi);
-              float l0, l1;
-              low_terms(hw, w0, w1, l0, l1);
-              const __nv_bfloat162 lo = __floats2bfloat162_rn(l0, l1);
-              ph[o][i] = transpose8(hw);
-              pl[o][i] = transpose8(*reinterpret_cast<const uint32_t*>(&lo));
-            }
-          }
-#pragma unroll
-          for (int ct = 0; ct < DH / 16; ++ct) {
-            uint32_t a0, a1, a2, a3;
-            const uint32_t at = base + S::MEET_OFF + (k0 + 8 * (lane >> 4) + (lane & 7)) * S::OWN_PITCH + ct * 32 + ((lane >> 3) & 1) * 16;
-            asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-                         : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3) : "r"(at) : "memory");
-#pragma unroll
-            for (int o = 0; o < ON; ++o) {
-              mma_bf16(od[o][ct], a0, a1, a2, a3, ph[o][0], ph[o][1]);
-              mma_bf16(od[o][ct], a0, a1, a2, a3, pl[o][0], pl[o][1]);
-            }
-          }
-        }
-#pragma unroll
-        for (int o = 0; o < ON; ++o)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-#pragma unroll
-            for (int k = 4; k < 32; k <<= 1) ol[o][c] += __shfl_xor_sync(0xFFFFFFFFu, ol[o][c], k);
-            const int r = 8 * (ON * warp + o) + 2 * t4 + c;
-            if (n8 == 0 && r < RT) own[r] = make_float2(om[o][c], ol[o][c]);
-          }
-      }
       if (pending) add();
 
       // ---- the item's rows, or its piece of them
@@ -730,11 +730,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
       ml[threadIdx.x] = make_float2(M, l);
       soft_sync();
       auto total = [&](int r, float& Mx, float& Lx) {        // a row's largest score and sum over all that it has seen
-        const float2 mine = owned ? own[r] : make_float2(-CUDART_INF_F, 0.f);
-        Mx = mine.x;
+        Mx = -CUDART_INF_F; Lx = 0.f;
 #pragma unroll
         for (int k = 0; k < REP; ++k) Mx = fmaxf(Mx, ml[k * RT + r].x);
-        Lx = mine.x == -CUDART_INF_F ? 0.f : mine.y * fast_exp2(mine.x - Mx);
 #pragma unroll
         for (int k = 0; k < REP; ++k) {
           const float2 v = ml[k * RT + r];
@@ -752,17 +750,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           __stcg(ps + RT * DH + row, Mx); __stcg(ps + RT * DH + RT + row, Lx);
         }
       }
-      float ofac[ON][2];                             // of the block's own rows' results
-#pragma unroll
-      for (int o = 0; o < ON; ++o)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int r = min(8 * (ON * warp + o) + 2 * t4 + c, RT - 1);
-          float Mo, Lo;
-          total(r, Mo, Lo);
-          ofac[o][c] = !owned || om[o][c] == -CUDART_INF_F ? 0.f : fast_exp2(om[o][c] - Mo) / Lo * 0x1p32f;
-        }
-      // a row's copies meet, and what its block's own rows gave, MEET channels of each half at a time
+      // a row's copies meet, MEET channels of each half at a time
       float* buf = reinterpret_cast<float*>(sm + S::MEET_OFF);               // [MEET][PITCH]
 #pragma unroll
       for (int c0 = 0; c0 < DH / 2; c0 += S::MEET) {
@@ -774,23 +762,6 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           buf[(2 * c + 1) * S::PITCH + threadIdx.x] = b * fac;
         }
         soft_sync();
-        if (owned) {                                 // (onto the first copy; a row that is not a number has been made one already)
-#pragma unroll
-          for (int o = 0; o < ON; ++o) {
-            const int r = 8 * (ON * warp + o) + 2 * t4;
-            if (r >= rows) continue;
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-              for (int ct = 0; ct < S::MEET / 16; ++ct)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  float& at = buf[(16 * ct + 8 * (e >> 1) + n8) * S::PITCH + hf * GROUP + r + (e & 1)];
-                  at = fmaf(od[o][(hf * (DH / 2) + c0) / 16 + ct][e], ofac[o][e & 1], at);
-                }
-          }
-          soft_sync();
-        }
         constexpr int QUADS = 2 * S::MEET / 4;       // of a row, both halves
 #pragma unroll 1
         for (int e = threadIdx.x; e < rows * QUADS; e += SOFT) {
