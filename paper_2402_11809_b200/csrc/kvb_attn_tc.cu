@@ -35,21 +35,21 @@ constexpr float REF_FAR = 0x1p22f;                   // up to this a reference's
 template <int DH>
 struct Smem {
   using F = Fmt<DH>;
-  static constexpr int STAGES = DH == 128 ? 5 : 8;
+  static constexpr int STAGES = DH == 128 ? 4 : 8;           // pages on their way; behind them a place for a block's own rows
   static constexpr int MEET = DH / 4;                        // channels of a thread that copies of a row meet in at a time
   static constexpr int PITCH = SOFT + 1;                     // floats (four channels apart: another bank)
   static constexpr int MEET_OFF = 0;                         // [MEET][PITCH]
   static constexpr int MEET_BYTES = MEET * PITCH * 4 / 128 * 128 + 128;
-  static constexpr int K_OFF = MEET_BYTES;                   // [STAGES]
-  static constexpr int V_OFF = K_OFF + STAGES * F::CODES;    // [STAGES]
-  static constexpr int SCALE_OFF = V_OFF + STAGES * F::CODES;        // [RING][4] {K, V}
+  static constexpr int K_OFF = MEET_BYTES;                   // [STAGES + 1]
+  static constexpr int V_OFF = K_OFF + (STAGES + 1) * F::CODES;      // [STAGES + 1]
+  static constexpr int SCALE_OFF = V_OFF + (STAGES + 1) * F::CODES;        // [RING][4] {K, V}
   static constexpr int ML_OFF = SCALE_OFF + RING * 32;       // [2][SOFT] {M, l} of rows' halves and copies, by item
-  static constexpr int OWN_OFF = ML_OFF + 2 * SOFT * 8;      // [STAGES][64] of the block's own rows {K's power of two, V's exponent}
-  static constexpr int XCH_OFF = OWN_OFF + STAGES * SPACE_MAX_ROWS * 8;    // [2][SOFT] a page's {largest score, E} of a row's halves
+  static constexpr int OWN_OFF = ML_OFF + 2 * SOFT * 8;      // [64] of the block's own rows {K's power of two, V's exponent}
+  static constexpr int XCH_OFF = OWN_OFF + SPACE_MAX_ROWS * 8;    // [2][SOFT] a page's {largest score, E} of a row's halves
   static constexpr int TOPS_OFF = XCH_OFF + 2 * SOFT * 8;    // [2][SOFT] largest elements of query rows' halves, by item
   static constexpr int DESC_OFF = TOPS_OFF + 2 * SOFT * 4;   // [RING] {item of the share, page of it}
   static constexpr int BAR_OFF = DESC_OFF + RING * 8;
-  static constexpr int N_BARS = 4 * STAGES + RING + 13;
+  static constexpr int N_BARS = 4 * (STAGES + 1) + RING + 13;
   static constexpr int MISC_OFF = BAR_OFF + N_BARS * 8;
   static constexpr int MASK_OFF = (MISC_OFF + 16 + 7) / 8 * 8;
   static constexpr int TABLE_OFF = MASK_OFF + SPACE_MAX_ROWS * 8;    // prefix[max_batch + 1], seq_len[max_batch]
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
   // Of a stage: K, V are there / have been used.  SAID: page m is announced and its scales are there.  QREADY: an item's query rows are
   // there.  SDONE (two, by page): scores.  PREADY: weights (and the result before has been added up).  ODONE: a page's result.
   // XCH, QTOP (by pair of warps): largest scores, elements of both halves.
-  constexpr int FULLK = 0, FULLV = STAGES, FREEK = 2 * STAGES, FREEV = 3 * STAGES, SAID = 4 * STAGES, QREADY = SAID + RING,
+  constexpr int FULLK = 0, FULLV = STAGES + 1, FREEK = 2 * (STAGES + 1), FREEV = 3 * (STAGES + 1), SAID = 4 * (STAGES + 1), QREADY = SAID + RING,
                 SDONE = QREADY + 1, PREADY = QREADY + 3, ODONE = QREADY + 4, XCH = QREADY + 5, QTOP = QREADY + 9;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::MISC_OFF);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF + 4);
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
 
   if (threadIdx.x == 0) {
     *abort_flag = 0;
-    for (int s = 0; s < 4 * STAGES + RING; ++s) mbar_init(BAR(s), 1);
+    for (int s = 0; s < 4 * (STAGES + 1) + RING; ++s) mbar_init(BAR(s), 1);
     mbar_init(BAR(QREADY), 8); mbar_init(BAR(SDONE), 1); mbar_init(BAR(SDONE + 1), 1); mbar_init(BAR(PREADY), 8); mbar_init(BAR(ODONE), 1);
     for (int i = 0; i < 4; ++i) { mbar_init(BAR(XCH + i), 2); mbar_init(BAR(QTOP + i), 2); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -280,6 +280,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
   wk.b = 0; wk.cur = share0;
   wk.end = mine ? cut.begin(blockIdx.x + 1) : 0;
   uint32_t m = 0;                                    // pages so far
+  uint32_t cached = 0, own = 0;                      // of the cache, and blocks' own rows, among them
   uint32_t queries = 0;                              // items with pages so far: others' query rows nobody announces or waits for
   auto hold = [&](int bar, uint32_t use, int site) { return wait(BAR(bar), use & 1, abort_flag, p.err, site); };
 
@@ -301,28 +302,28 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
             if (p.status) atomicOr(p.status + wk.b, SPACE_ST_BAD_PAGE);
             continue;
           }
-          const uint32_t s = m % STAGES, e = m % RING;
+          const uint32_t s = cached % STAGES, use = cached / STAGES, e = m % RING;
           const char* head = pool + (int64_t)page * p.cache.page_stride;
           desc[e].x = item; desc[e].y = t;
           mbar_expect_tx(BAR(SAID + e), 32);
           bulk_copy(base + S::SCALE_OFF + e * 32, head + F::SCALES, 32, BAR(SAID + e));
-          if (m >= STAGES) ok = hold(FREEK + s, m / STAGES - 1, 1);
+          if (use) ok = hold(FREEK + s, use - 1, 1);
           if (ok) {
             mbar_expect_tx(BAR(FULLK + s), F::CODES);
             bulk_copy(base + S::K_OFF + s * F::CODES, head, F::CODES, BAR(FULLK + s));
-            if (m >= STAGES) ok = hold(FREEV + s, m / STAGES - 1, 2);
+            if (use) ok = hold(FREEV + s, use - 1, 2);
           }
           if (ok) {
             mbar_expect_tx(BAR(FULLV + s), F::CODES);
             bulk_copy(base + S::V_OFF + s * F::CODES, head + F::CODES, F::CODES, BAR(FULLV + s));
           }
-          ++m;
+          ++m; ++cached;
         }
         if (ok && p.has_new && wk.L >= 0 && wk.t1 > wk.cached()) {             // (two other warps bring them)
           desc[m % RING].x = item; desc[m % RING].y = OWN;
           mbar_arrive(BAR(SAID + m % RING));
-          if (m >= STAGES) ok = hold(FREEK + m % STAGES, m / STAGES - 1, 20) && hold(FREEV + m % STAGES, m / STAGES - 1, 21);
-          ++m;
+          if (own) ok = hold(FREEV + STAGES, own - 1, 18);     // (so that announcements are not far ahead either)
+          ++m; ++own;
         }
       }
       if (ok) {
@@ -330,14 +331,14 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
         mbar_arrive(BAR(SAID + m % RING));
       }
       // every copy has landed before the block may exit (a page whose copies a wait that ran out cut short is the last)
-      for (uint32_t j = m > STAGES ? m - STAGES : 0; j < m; ++j) {
-        mbar_drain_bounded(BAR(SAID + j % RING), (j / RING) & 1, WAIT_NS / 10);
+      for (uint32_t j = m >= RING ? m - RING + 1 : 0; j < m; ++j) mbar_drain_bounded(BAR(SAID + j % RING), (j / RING) & 1, WAIT_NS / 10);
+      for (uint32_t j = cached > STAGES ? cached - STAGES : 0; j < cached; ++j) {
         mbar_drain_bounded(BAR(FULLK + j % STAGES), (j / STAGES) & 1, WAIT_NS / 10);
         mbar_drain_bounded(BAR(FULLV + j % STAGES), (j / STAGES) & 1, WAIT_NS / 10);
       }
     } else if (warp == 8 && elect_one()) {
       // ---- products: scores of page q, a page ahead of the result of page m
-      uint32_t q = 0;
+      uint32_t q = 0, q_cached = 0, q_own = 0;
       int item = -1;
       bool ok = true, more = true;
       while (true) {
@@ -350,13 +351,15 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
             ok = hold(QREADY, queries++, 4) && ok;
             item = it;
           }
-          const uint32_t s = q % STAGES;
-          ok = hold(FULLK + s, q / STAGES, 5) && ok;
+          const bool is_own = ok && desc[q % RING].y == OWN;
+          const uint32_t s = is_own ? STAGES : q_cached % STAGES;
+          ok = hold(FULLK + s, is_own ? q_own : q_cached / STAGES, 5) && ok;
+          is_own ? ++q_own : ++q_cached;
           if (m && q > m) ok = hold(ODONE, m - 1, 6) && ok;                    // (the weights of page q - 2 lie where these scores go)
           tc_fence_after();
           const uint64_t kd = plain_desc(base + S::K_OFF + s * F::CODES, F::K_COLS, 128);
           const uint32_t qd = TM_Q + ((queries - 1) & 1) * 64;
-          if (ok && desc[q % RING].y != OWN) {
+          if (ok && !is_own) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -378,12 +381,14 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           if (more) continue;
           break;
         }
-        const uint32_t s = m % STAGES;
-        ok = hold(FULLV + s, m / STAGES, 7) && ok;
+        const bool is_own = ok && desc[m % RING].y == OWN;
+        const uint32_t s = is_own ? STAGES : cached % STAGES;
+        ok = hold(FULLV + s, is_own ? own : cached / STAGES, 7) && ok;
+        is_own ? ++own : ++cached;
         if (m) ok = hold(ODONE, m - 1, 8) && ok;     // (long since: whoever brings the weights has waited for it)
         ok = hold(PREADY, m, 9) && ok;
         tc_fence_after();
-        const int chunks = desc[m % RING].y == OWN ? 1 : 3;          // (own rows: their second terms with the same weights)
+        const int chunks = is_own ? 1 : 3;          // (own rows: their second terms with the same weights)
         const uint64_t vd = plain_desc(base + S::V_OFF + s * F::CODES, F::V_ROWS, 128);
         if (ok) {
 #pragma unroll
@@ -416,24 +421,16 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           if (DH == 128) { prefetch_line(p.kn + at + 128); prefetch_line(p.vn + at + 128); }
         }
       }
-      // ---- the block's own rows, wherever they are announced
-      int item = -1;
-      for (;; ++m) {
-        if (!hold(SAID + m % RING, m / RING, 17)) break;
-        const int it = desc[m % RING].x;
-        if (it == NO_MORE) break;
-        if (desc[m % RING].y != OWN) continue;
-        for (; item < it; ++item) wk.next(prefix, seq_len, p.has_new, share0);
-        const uint32_t s = m % STAGES;
+      // ---- the block's own rows, an item ahead
+      while (wk.next(prefix, seq_len, p.has_new, share0)) {
+        if (!p.has_new || wk.L < 0 || wk.t1 <= wk.cached()) continue;
         bool ok = true;
-        if (m >= STAGES) {
-          ok = hold(FREEK + s, m / STAGES - 1, 18);
-          ok = hold(FREEV + s, m / STAGES - 1, 19) && ok;
-        }
+        if (own) ok = hold(FREEK + STAGES, own - 1, 19) && hold(FREEV + STAGES, own - 1, 20);
         if (__any_sync(0xFFFFFFFFu, !ok)) break;
-        bring_own<DH>(p, wk.b, wk.it / p.n_rt, sm + S::K_OFF + s * F::CODES, sm + S::V_OFF + s * F::CODES,
-                      reinterpret_cast<float2*>(sm + S::OWN_OFF) + s * SPACE_MAX_ROWS, BAR(FULLK + s));
-        if ((threadIdx.x & 63) == 0) mbar_arrive(BAR(FULLV + s));
+        bring_own<DH>(p, wk.b, wk.it / p.n_rt, sm + S::K_OFF + STAGES * F::CODES, sm + S::V_OFF + STAGES * F::CODES,
+                      reinterpret_cast<float2*>(sm + S::OWN_OFF), BAR(FULLK + STAGES));
+        if ((threadIdx.x & 63) == 0) mbar_arrive(BAR(FULLV + STAGES));
+        ++own;
       }
     }
   } else {
@@ -445,7 +442,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
     const uint32_t TM_C = TM_O + lanes + half * (DH / 2);
     // What is announced of page m.
     int next_item, next_page;
-    auto look = [&]() {
+    auto look = [&](uint32_t m) {
       hold(SAID + m % RING, m / RING, 12);
       next_item = *abort_flag ? NO_MORE : desc[m % RING].x;
       next_page = desc[m % RING].y;
@@ -474,7 +471,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
       const int e = nan_next ? 0 : max((int)(top >> 7) - 127, -100) - 7;       // the largest element to [2^7, 2^8)
       const float up = pow2(-e);
       f_next = p.c * pow2(e);
-      if (item == 0) look();
+      if (item == 0) look(0);
       if (next_item != item) return;
       const uint32_t to0 = TM_Q + lanes + (queries++ & 1) * 64 + half * (DH / 8);
 #pragma unroll
@@ -519,24 +516,22 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           for (int j = 0; j < DH / 4; ++j) o2[j] = mul2(o2[j], a2);
         }
         const uint64_t b2 = pack2(beta, beta);
+        uint32_t r[DH / 2];
 #pragma unroll
-        for (int c = 0; c < DH / 2; c += 32) {
-          uint32_t r[32];
-          tmem_ld32(TM_C + c, r);
-          tmem_wait_ld();
+        for (int c = 0; c < DH / 2; c += 32) tmem_ld32(TM_C + c, r + c);
+        tmem_wait_ld();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) o2[c / 2 + j] = fma2(pack2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), b2, o2[c / 2 + j]);
-        }
+        for (int j = 0; j < DH / 4; ++j) o2[j] = fma2(pack2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), b2, o2[j]);
         tc_fence_before();
       };
       while (next_item == item) {
         const int t = next_page;
-        const uint32_t s = m % STAGES;
+        const uint32_t s = cached % STAGES;          // (of a page of the cache)
         const uint32_t TM_SM = TM_S + lanes + (m & 1) * TILE;                  // the page's scores
         const float2* sc = reinterpret_cast<const float2*>(sm + S::SCALE_OFF + (m % RING) * 32) + (key0 >> 5);
         const int vis0 = L - (t == OWN ? 0 : t) * TILE, vis = vis0 - key0;            // visible keys of the page, and of this thread
         if (vis0 < TILE && t != OWN) {               // what lies behind the last row must not count, whatever it is
-          hold(FULLV + s, m / STAGES, 14);
+          hold(FULLV + s, cached / STAGES, 14);
           const int g0 = vis0 >> 4;
 #pragma unroll 1
           for (int e = threadIdx.x; e < (8 - g0) * DH; e += SOFT) {
@@ -571,6 +566,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           xch[threadIdx.x] = make_float2(pm, E);
           __syncwarp();
           if (lane == 0) mbar_arrive(BAR(XCH + w4));
+          look(m + 1);                               // (meanwhile)
+          if (pending) add();
           hold(XCH + w4, m, 16);
           const float2 other = xch[threadIdx.x ^ GROUP];
           top = fmaxf(pm, other.x); lower = pm - top;
@@ -656,20 +653,20 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           }
         } else {
           // the block's own rows: a mask and powers of two for each key
-          hold(FULLK + s, m / STAGES, 22);           // (long since; for those powers of two)
+          hold(FULLK + STAGES, own, 21);             // (long since; for those powers of two)
           const bool sees = rep * (TILE / REP) < SPACE_MAX_ROWS && row < rows;
           const uint64_t mask = sees ? reinterpret_cast<const uint64_t*>(sm + S::MASK_OFF)[(r0 + row) >> p.gsh] >> (key0 & 63) : 0ull;     // Eq. 5
-          const float2* own = reinterpret_cast<const float2*>(sm + S::OWN_OFF) + s * SPACE_MAX_ROWS + (key0 & 63);
+          const float2* sc = reinterpret_cast<const float2*>(sm + S::OWN_OFF) + (key0 & 63);
 #pragma unroll
           for (int j = 0; j < KEYS; ++j) {
-            float y = __uint_as_float(v[j]) * fminf(fmaxf(f * own[j].x, F_MIN), F_MAX);
+            float y = __uint_as_float(v[j]) * fminf(fmaxf(f * sc[j].x, F_MIN), F_MAX);
             y = (mask >> j) & 1ull ? (y > SCORE_MAX ? SCORE_MAX : y < -SCORE_MAX ? -SCORE_MAX : y) : -CUDART_INF_F;
             pm = fmaxf(pm, y);
             v[j] = __float_as_uint(y);
           }
           const float from = pm == -CUDART_INF_F ? 0.f : pm;
 #pragma unroll
-          for (int j = 0; j < KEYS; ++j) E = fmaxf(E, __uint_as_float(v[j]) - from + own[j].y);
+          for (int j = 0; j < KEYS; ++j) E = fmaxf(E, __uint_as_float(v[j]) - from + sc[j].y);
           meet();
           const float ref = none ? 0.f : top, up = 8.f - E;
 #pragma unroll
@@ -682,7 +679,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
               for (int i = 0; i < 4; ++i) {
                 const float off = __uint_as_float(v[u + 4 * j + i]) - ref;
                 sum += fast_exp2(off);
-                y[i] = fast_exp2(off + (own[u + 4 * j + i].y + up));
+                y[i] = fast_exp2(off + (sc[u + 4 * j + i].y + up));
               }
               split4(y[0], y[1], y[2], y[3], w[j], w[4 + j]);
             }
@@ -695,7 +692,6 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           for (int c = 0; c < 4; ++c)
             if (c * REP / 4 != rep && (c & 1) == half) tmem_st16(TM_SM + 32 * c, zero);
         }
-        if (pending) add();
         // the weights are where the products want them
         tmem_wait_st();
         tc_fence_before();
@@ -713,7 +709,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
         }
         pending = true;
         ++m;
-        look();
+        t == OWN ? ++own : ++cached;
       }
       // the next item's query rows, while the last products run
       live = wk.next(prefix, seq_len, p.has_new, share0);
