@@ -1,4 +1,4 @@
-// Attention of a step's block rows over the 8-bit cache (space_kvb_attn_step), 8 to 32 query rows at a time.
+// Attention of a step's block rows over the 8-bit cache (space_kvb_attn_step), up to sixteen query rows of a kv head.
 //
 // The mathematics.  The cache's codes are tensor-core operands as they lie (mma.sync m16n8k32, e4m3): nothing is unpacked.
 // What they are multiplied with is split in two: a query row, scaled by a power of two of its own, is q0 + q1 with e4m3 numbers (four
@@ -646,7 +646,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
         *last_flag = last;
       }
       __syncthreads();
-      if (*last_flag) join_pieces<DH, RT, NT == 1 ? 1 : NT, NT == 1 ? 16 : 4>(p, cut, b, h, r0, rows, piece0, pieces, item_at, (int)threadIdx.x, THREADS);
+      if (*last_flag) join_pieces<DH, RT, NT, NT == 1 ? 16 : 4>(p, cut, b, h, r0, rows, piece0, pieces, item_at, (int)threadIdx.x, THREADS);
     }
     __syncthreads();                                 // everybody has read the rings: the next item's requests may fill them
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -694,12 +694,12 @@ int launch_kvb_attn(space_ctx* ctx, const space_kvb_attn_args* a, const uint64_t
   // the flat list is counted in 32 bits: items of eight rows at least, a page and the cost of starting more than a table names
   if ((double)p.B * p.H_kv * ((rows + 7) / 8) * ((double)p.cache.pages_per_seq + 4) > 2e9) return SPACE_E_UNSUPPORTED;
   ctx->launches += 1;
+  // More query rows than sixteen go to tcgen05 (us, here / there: 32 rows of 64 sequences up to 8192 keys 395 / 217, 18 rows of 16 sequences
+  // up to 4096 keys 143 / 121, 16 rows of those 107 / 123, 16 rows of 5 short sequences 16 / 22).
   if (rows > 16) return launch_kvb_attn_tc(ctx, p, st);
   const bool wide = ctx->cfg.head_dim == 128;
-  int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 24 ? 3 : 4;
-  if (rows > 32) nt = (rows + 23) / 24 * 3 <= (rows + 31) / 32 * 4 ? 3 : 4;
   cudaError_t e;
-  if (wide) e = nt == 1 ? launch_dim<128, 1>(p, ctx, st) : nt == 2 ? launch_dim<128, 2>(p, ctx, st) : nt == 3 ? launch_dim<128, 3>(p, ctx, st) : launch_dim<128, 4>(p, ctx, st);
-  else e = nt == 1 ? launch_dim<64, 1>(p, ctx, st) : nt == 2 ? launch_dim<64, 2>(p, ctx, st) : nt == 3 ? launch_dim<64, 3>(p, ctx, st) : launch_dim<64, 4>(p, ctx, st);
+  if (rows <= 8) e = wide ? launch_dim<128, 1>(p, ctx, st) : launch_dim<64, 1>(p, ctx, st);
+  else e = wide ? launch_dim<128, 2>(p, ctx, st) : launch_dim<64, 2>(p, ctx, st);
   return cuda_ok(e);
 }

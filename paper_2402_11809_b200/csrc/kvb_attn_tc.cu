@@ -1,23 +1,32 @@
-// Attention of a step's block rows over the 8-bit cache (space_kvb_attn_step), items of up to 32, 64 or 128 query rows on tcgen05.
+// Attention of a step's block rows over the 8-bit cache (space_kvb_attn_step), items of up to 32 or 64 query rows on tcgen05.
 //
 // The mathematics is kvb_attn.cu's (codes as operands as they lie, query rows and weights as two e4m3 terms each), with a page
 // of 128 keys in the place of a block of 32:
 //   S = q0 K^T + q1 K^T,    D = w0 V + w1 V,    chunk b of 32 keys (one K and one V scale 2^k_b, 2^v_b):   m_b = max_j s_j,
 //   e_j = 2^(s_j - m_b),    w_j = e_j 2^((m_b - m) + v_b - E + 8),    m = max m_b,  E = max_b (m_b - m) + v_b,
 //   l += sum_b 2^(m_b - M) sum_j e_j,    o = o 2^(R - R') + D 2^(E + (m - M) - R' - 8)     with R' the larger of R and E + (m - M).
+// The block's own rows go through as one more page: a row, scaled by a power of two of its own, is two e4m3 terms as well (to 2^-18 of
+// its largest element), which stand in for two rows of 64 with the same scores and the same weights:
+//   S = (q0 + q1) (k0 + k1)^T,    D = (w0 + w1) (v0 + v1),    a mask bit and {2^k_j, v_j} for each key.
+// (As bf16 products when an item ended they took 13,000 cycles there, of 25,000 between items: code that runs once an item comes
+// from far away.  Two warps that have nothing else to do bring them an item ahead.)
 //
-// The work.  Query rows are the MMA's M extent: 128 of them, or 64 or 32 held twice or four times over, each copy with keys of its own
+// The work.  Query rows are the MMA's M extent: 64 or 32 of them held twice or four times over, each copy with keys of its own
 // (chunks of 32).  Both first operands, query rows and weights, are in tensor memory: an M = 128, K = 32 product takes 10 + N/2 cycles
 // then, 43 + N/2 with the first operand in shared memory.  Two threads have a row (of a copy), half of its keys and half of the
 // result's channels each; they tell each other their largest scores.  The flat list of 128-key pages over all (sequence, kv head,
 // query rows) items is cut evenly over the thread blocks, one per SM.  A page's scores are there when the softmax of the page before ends,
 // and its result is added up in the next page's time: the softmax never waits for products, nor they for each other.  Pieces of
 // a cut item are joined by the block that stores the last of them, always in the same order.
-// The block's own rows are bf16 products on mma.sync (eight query rows a warp) when an item ends; their results meet the others there.
 //
-// Warps: 0-7 softmax and sums, 8 products (one thread), 9 copies (one thread), 10 asks L2 for the rows that items will want, 11 only gives
-// its registers away.  The copying thread walks the list and leaves out what has no keys (pages outside the pool); what it
-// brings it announces in order, and everybody else goes by that.
+// What bounds it: the softmax's chain of a page, about 2400 cycles with two warps to a scheduler (scores from tensor memory
+// 370, weights 870 of which 512 are exponentials, the result 500, waits and meetings 500) against 1200 of products and 1300 of the page's bytes;
+// between items 11,000 cycles.  16 sequences of up to 4096 keys, 32 heads, 36 rows: 134 us; 8 of 8192, 8 heads, 392 rows: 321 us
+// (330 TFLOP/s of the products that the formulas ask for, twice that of e4m3 ones).
+//
+// Warps: 0-7 softmax and sums, 8 products (one thread), 9 copies (one thread), 10 and 11 ask L2 for the rows that items will want and
+// bring blocks' own rows.  The copying thread walks the list and leaves out what has no keys (pages outside the pool); what
+// there is it announces in order, and everybody else goes by that.
 // Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT, no role leaves its loop early, and the block drains and exits.
 #include "kvb_attn.cuh"
 
