@@ -653,13 +653,14 @@ int space_kvb_read(space_ctx* ctx, const space_kvb_read_args* args, void* stream
  * k_new / v_new, over the block's own rows (bf16, not in the cache yet) as Eq. 5 shows them.  k = 0 is one row per
  * sequence.  Rows that see nothing, sequences that do not fit, bad pages, hidden rows and non-finite elements of
  * k_new / v_new: as space_kvq_attn_step.  A query row that holds a NaN or an infinity gives NaN.
- * The output is bf16, the sums are fp32.  Query rows and the block's rows are taken as two e4m3 numbers an element with a power of
- * two per row: bf16 exactly, but elements more than 2^9 times smaller than the largest of their row are rounded, by at most
- * 2^-18 of it.  The weights of a page's keys (times their V scales) are rounded likewise, to eight bits and by at most 2^-18 of the largest.
- * Scores, in units of log2, are held to +-1e30: of keys beyond that none is preferred.
+ * The output is bf16, the sums are fp32.  Query rows are taken as two e4m3 numbers an element with a power of two per row: bf16
+ * exactly, but elements more than 2^8 times smaller than the largest of their row are rounded, by at most 2^-17 of it; so are
+ * the block's own rows where a kv head has more than sixteen query rows (else they are bf16 as they are).  Weights are rounded likewise:
+ * each to eight bits, and by at most 2^-18 of the largest among the keys that it goes with (32 or 128 of them; there times
+ * their V scales).  Scores, in units of log2, are held to +-2^29: of keys beyond that none is preferred.
  * Asynchronous on `stream`, no allocation; one call at a time per context (scratch of the context).
  * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE (batch or k beyond the context's), UNSUPPORTED (batch * n_kv_heads *
- * ceil(query rows of a kv head / 32) * (pages_per_seq + 8) above 2e9), CUDA. */
+ * ceil(query rows of a kv head / 8) * (pages_per_seq + 4) above 2e9), CUDA. */
 typedef struct {
   int32_t batch;
   int32_t k;                   /* 0 .. k_max; (k+1)^2 query rows                                   */
