@@ -56,7 +56,10 @@ template <int DH>
 __device__ __forceinline__ void store_row4(const Params& p, int b, int h, int r, int c4, float4 o) {
   int i, hq;
   row_of(p, h, r, i, hq);
-  const __nv_bfloat162 x = __floats2bfloat162_rn(o.x, o.y), y = __floats2bfloat162_rn(o.z, o.w);
+  // weights are rounded, their sum is not: a mean of the largest numbers would pass them (NaN stays)
+  const float most = 3.3895313892515355e38f;
+  auto held = [&](float v) { return v > most ? most : v < -most ? -most : v; };
+  const __nv_bfloat162 x = __floats2bfloat162_rn(held(o.x), held(o.y)), y = __floats2bfloat162_rn(held(o.z), held(o.w));
   __nv_bfloat16* dst = p.out + (((int64_t)b * p.n_q + i) * p.H_q + hq) * DH + 4 * c4;
   *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
 }

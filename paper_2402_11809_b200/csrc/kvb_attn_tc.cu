@@ -482,6 +482,10 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
       f_next = p.c * pow2(e);
       if (item == 0) look(0);
       if (next_item != item) return;
+      if (nan_next) {                                // (zeros for the products, so that it is known whether the row sees a key)
+#pragma unroll
+        for (int j = 0; j < DH / 16; ++j) v[j] = make_uint4(0, 0, 0, 0);
+      }
       const uint32_t to0 = TM_Q + lanes + (queries++ & 1) * 64 + half * (DH / 8);
 #pragma unroll
       for (int j = 0; j < DH / 16; j += 2) {

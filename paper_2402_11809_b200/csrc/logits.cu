@@ -72,7 +72,9 @@ __device__ __forceinline__ void mask_out(uint4& v, uint32_t keep) {
 #pragma unroll
     for (int i = 0; i < 4; i += 2) {                 // four bits to the tops of four bytes, each byte's top all over two bytes
       const uint32_t tops = ((keep >> (2 * i)) & 0xFu) * 0x10204080u & 0x80808080u;
-      const uint32_t m0 = __byte_perm(tops, 0, 0x9988), m1 = __byte_perm(tops, 0, 0xBBAA);
+      uint32_t m0, m1;
+      asm("prmt.b32 %0, %1, 0, 0x9988;" : "=r"(m0) : "r"(tops));
+      asm("prmt.b32 %0, %1, 0, 0xBBAA;" : "=r"(m1) : "r"(tops));
       w[i] = (w[i] & m0) | (0xFF80FF80u & ~m0);
       w[i + 1] = (w[i + 1] & m1) | (0xFF80FF80u & ~m1);
     }

@@ -23,7 +23,8 @@ __device__ __forceinline__ const float* table_row(const Table& t, int b, int row
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// Products and sums of pairs, each rounded by itself.
+// Products and sums of pairs, each rounded by itself.  (A sum as add.rn.f32x2 is fused with the product before it, which then
+// is not rounded.)
 __device__ __forceinline__ uint64_t pair(float a, float b) {
   return (uint64_t)__float_as_uint(a) | (uint64_t)__float_as_uint(b) << 32;
 }
@@ -36,9 +37,7 @@ __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
   return r;
 }
 __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
+  return pair(__fadd_rn(first_of(a), first_of(b)), __fadd_rn(second_of(a), second_of(b)));
 }
 
 // What a lane's eight channels 8x .. 8x + 7 are multiplied by, as pairs of neighbours: themselves by c, their partners by s, the
