@@ -354,7 +354,7 @@ int launch_kvb_read(space_ctx* ctx, const space_kvb_read_args* a, cudaStream_t s
 int launch_kvb_attn(space_ctx* ctx, const space_kvb_attn_args* a, const uint64_t* mask_rows, cudaStream_t st);
 // Scratch of the attention over the 8-bit cache: two slots per thread block, of all the query rows that the blocks of an SM
 // hold; arrival counters of its items, eight query rows each at least.
-constexpr int KVB_SM_ROWS = 64;
+constexpr int KVB_SM_ROWS = 128;
 inline size_t kvb_partial_floats(const space_config* c, int sm_count) { return 2 * (size_t)sm_count * KVB_SM_ROWS * (c->head_dim + 2); }
 inline size_t kvb_items(const space_config* c) { return kvq_items(c); }
 int launch_philox_debug(uint64_t seed, int64_t n, const uint32_t* c0, const uint32_t* c1,

@@ -1,5 +1,5 @@
 // What the two attention kernels over the 8-bit cache share (kvb_attn.cu: items of 8 or 16 query rows on mma.sync;
-// kvb_attn_tc.cu: of 32 or 64 on tcgen05): parameters, the split into two e4m3 terms, the join of an item's pieces.
+// kvb_attn_tc.cu: of 32, 64 or 128 on tcgen05): parameters, the split into two e4m3 terms, the join of an item's pieces.
 #pragma once
 #include "kvq_attn.cuh"
 #include "kvb_common.cuh"

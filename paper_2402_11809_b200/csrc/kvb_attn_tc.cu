@@ -1,4 +1,4 @@
-// Attention of a step's block rows over the 8-bit cache (space_kvb_attn_step), items of up to 32 or 64 query rows on tcgen05.
+// Attention of a step's block rows over the 8-bit cache (space_kvb_attn_step), items of up to 32, 64 or 128 query rows on tcgen05.
 //
 // The mathematics is kvb_attn.cu's (codes as operands as they lie, query rows and weights as two e4m3 terms each), with a page
 // of 128 keys in the place of a block of 32:
@@ -11,7 +11,7 @@
 // (As bf16 products when an item ended they took 13,000 cycles there, of 25,000 between items: code that runs once an item comes
 // from far away.  Two warps that have nothing else to do bring them an item ahead.)
 //
-// The work.  Query rows are the MMA's M extent: 64 or 32 of them held twice or four times over, each copy with keys of its own
+// The work.  Query rows are the MMA's M extent: 128 of them, or 64 or 32 held twice or four times over, each copy with keys of its own
 // (chunks of 32).  Both first operands, query rows and weights, are in tensor memory: an M = 128, K = 32 product takes 10 + N/2 cycles
 // then, 43 + N/2 with the first operand in shared memory.  Two threads have a row (of a copy), half of its keys and half of the
 // result's channels each; they tell each other their largest scores.  The flat list of 128-key pages over all (sequence, kv head,
@@ -21,8 +21,8 @@
 //
 // What bounds it: the softmax's chain of a page, about 2400 cycles with two warps to a scheduler (scores from tensor memory
 // 370, weights 870 of which 512 are exponentials, the result 500, waits and meetings 500) against 1200 of products and 1300 of the page's bytes;
-// between items 11,000 cycles.  16 sequences of up to 4096 keys, 32 heads, 36 rows: 134 us; 8 of 8192, 8 heads, 392 rows: 321 us
-// (330 TFLOP/s of the products that the formulas ask for, twice that of e4m3 ones).
+// between items 11,000 cycles.  16 sequences of up to 4096 keys, 32 heads, 36 rows: 133 us; 8 of 8192, 8 heads, 392 rows, 128 at a
+// time: 285 us (370 TFLOP/s of the products that the formulas ask for, twice that of e4m3 ones).
 //
 // Warps: 0-7 softmax and sums, 8 products (one thread), 9 copies (one thread), 10 and 11 ask L2 for the rows that items will want and
 // bring blocks' own rows.  The copying thread walks the list and leaves out what has no keys (pages outside the pool); what
@@ -667,7 +667,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
         } else {
           // the block's own rows: a mask and powers of two for each key
           hold(FULLK + STAGES, own, 21);             // (long since; for those powers of two)
-          const bool sees = rep * (TILE / REP) < SPACE_MAX_ROWS && row < rows;
+          const bool sees = key0 < SPACE_MAX_ROWS && row < rows;
           const uint64_t mask = sees ? reinterpret_cast<const uint64_t*>(sm + S::MASK_OFF)[(r0 + row) >> p.gsh] >> (key0 & 63) : 0ull;     // Eq. 5
           const float2* sc = reinterpret_cast<const float2*>(sm + S::OWN_OFF) + (key0 & 63);
 #pragma unroll
@@ -836,9 +836,15 @@ cudaError_t launch_dim(Params& p, const space_ctx* ctx, cudaStream_t st) {
 
 int launch_kvb_attn_tc(space_ctx* ctx, kvb::Params& p, cudaStream_t st) {
   const bool wide = ctx->cfg.head_dim == 128;
-  const int rows = p.n_q * p.G, rep = rows <= 32 ? 4 : 2;
+  // 128 rows of an item take 3600 cycles a page, 64 of them 2400: where they leave few enough of an item empty, and an SM gets enough pages (as many
+  // as the table names) that coarser items do not cost more than that (us, 64 / 128 rows: 392 rows of 8 sequences of 8192 keys, 8 heads
+  // 303 / 270, with head size 64 256 / 213, 1024 rows of 2 of 16384, 4 heads 178 / 150, 100 rows of 32 of up to 2048, 8 heads 113 / 102: 29 pages an
+  // SM and more; 128 rows of 16 of up to 4096, 4 heads 53 / 70, 200 rows of 4 of up to 3000, 8 heads 55 / 62: 14 and 10).
+  const int rows = p.n_q * p.G, n64 = (rows + 63) / 64, n128 = (rows + 127) / 128;
+  const int64_t pages = (int64_t)p.B * p.H_kv * n128 * p.cache.pages_per_seq;
+  const int rep = rows <= 32 ? 4 : 3 * n128 < 2 * n64 && pages >= 20 * (int64_t)ctx->sm_count ? 1 : 2;
   cudaError_t e;
-  if (wide) e = rep == 4 ? launch_dim<128, 4>(p, ctx, st) : launch_dim<128, 2>(p, ctx, st);
-  else e = rep == 4 ? launch_dim<64, 4>(p, ctx, st) : launch_dim<64, 2>(p, ctx, st);
+  if (wide) e = rep == 4 ? launch_dim<128, 4>(p, ctx, st) : rep == 2 ? launch_dim<128, 2>(p, ctx, st) : launch_dim<128, 1>(p, ctx, st);
+  else e = rep == 4 ? launch_dim<64, 4>(p, ctx, st) : rep == 2 ? launch_dim<64, 2>(p, ctx, st) : launch_dim<64, 1>(p, ctx, st);
   return cuda_ok(e);
 }

@@ -300,11 +300,27 @@ ATTN = [
 ]
 
 
+# 128 query rows at a time: tables that name many pages
+ATTN_WIDE = [
+    (64, 2, 16, 2, [1030, 0, 128], True), (128, 1, 8, 5, [777], False), (128, 4, 4, 6, [300, 1, 0, 2000], True), (64, 3, 16, 7, [129, 500], True),
+    (128, 8, 2, 7, [1999, 37, 1200, 2048, 640], True), (64, 1, 16, 3, [4000, 31], True),
+]
+
+
 @pytest.mark.parametrize("d,H,G,k,lens,block", ATTN)
 def test_attention(B, d, H, G, k, lens, block):
+    attention_case(B, d, H, G, k, lens, block)
+
+
+@pytest.mark.parametrize("d,H,G,k,lens,block", ATTN_WIDE)
+def test_attention_in_wide_tables(B, d, H, G, k, lens, block):
+    attention_case(B, d, H, G, k, lens, block, 6000)
+
+
+def attention_case(B, d, H, G, k, lens, block, pps=0):
     rng = np.random.default_rng(d + 100 * H + 10 * G + k)
     n, n_q, Hq = len(lens), (k + 1) ** 2, H * G
-    pps = max(1, max((L + P - 1) // P for L in lens) + 1)
+    pps = pps or max(1, max((L + P - 1) // P for L in lens) + 1)
     pool, table = random_cache(rng, lens, H, d, pps, spread=1.0)
     qb = bits(rng, n, n_q, Hq + 1, d)                                    # a head more than is used: strided rows
     kb, vb = (bits(rng, n, n_q, H, d), bits(rng, n, n_q, H, d)) if block else (None, None)
@@ -343,13 +359,14 @@ def run(B, q, pool, table, lens, k, kn=None, vn=None, H=1, d=64, scale=None):
     return f64(out), f64(lse), status.tolist()
 
 
-FORMS = [(64, 1), (128, 1), (64, 3), (128, 3), (64, 4), (128, 5), (128, 7)]          # head size and k, two query heads to a kv head
+FORMS = [(64, 1), (128, 1), (64, 3), (128, 3), (64, 4), (128, 5), (128, 7), (64, 6), (128, 6)]       # head size and k, two query heads to a kv head
+WIDE = 6000                                          # pages that a table names: from 65 rows on, 128 at a time
 
 
 @pytest.mark.parametrize("d,k", FORMS)
 def test_sequences_that_do_not_fit_and_pages_outside_the_pool(B, d, k):
     rng = np.random.default_rng(4)
-    lens, n_q, pps = [300, 40, 300, 50, 700], (k + 1) ** 2, 6
+    lens, n_q, pps = [300, 40, 300, 50, 700], (k + 1) ** 2, WIDE if k == 6 else 6
     pool, table = random_cache(rng, lens, 2, d, pps)
     q, kn, vn = bits(rng, 5, n_q, 4, d), bits(rng, 5, n_q, 2, d), bits(rng, 5, n_q, 2, d)
     given = [300, -3, pps * P + 1, 50, 700]
@@ -371,7 +388,7 @@ def test_hidden_rows_have_no_influence(B, d, k):
     """What one block row holds reaches only the rows that see it, whatever it is."""
     rng = np.random.default_rng(5)
     n_q, lens = (k + 1) ** 2, [130, 0]
-    pool, table = random_cache(rng, lens, 1, d, 2)
+    pool, table = random_cache(rng, lens, 1, d, WIDE if k == 6 else 2)
     q, kn, vn = bits(rng, 2, n_q, 2, d), bits(rng, 2, n_q, 1, d), bits(rng, 2, n_q, 1, d)
     see = kvb.visible(k)
     base = run(B, q, pool, table, lens, k, kn, vn, 1, d)
@@ -389,7 +406,7 @@ def test_hidden_rows_have_no_influence(B, d, k):
 def test_a_query_row_that_is_not_finite(B, d, k):
     rng = np.random.default_rng(6)
     n_q, lens = (k + 1) ** 2, [300]
-    pool, table = random_cache(rng, lens, 1, d, 3)
+    pool, table = random_cache(rng, lens, 1, d, WIDE if k == 6 else 3)
     q, kn, vn = bits(rng, 1, n_q, 2, d), bits(rng, 1, n_q, 1, d), bits(rng, 1, n_q, 1, d)
     base = run(B, q, pool, table, lens, k, kn, vn, 1, d)
     for fill in (0x7FC0, 0x7F80, 0xFF80):
@@ -409,7 +426,7 @@ def test_large_scores(B, d, k, size):
     as these are known to d 2^-24 of themselves, which the bound counts."""
     rng = np.random.default_rng(7)
     n_q, lens = (k + 1) ** 2, [400, 31]
-    pool, table = random_cache(rng, lens, 1, d, 4)
+    pool, table = random_cache(rng, lens, 1, d, WIDE if k == 6 else 4)
     q, kn, vn = bits(rng, 2, n_q, 2, d, scale=size), bits(rng, 2, n_q, 1, d, scale=0.01), bits(rng, 2, n_q, 1, d)
     out, lse, status = run(B, q, pool, table, lens, k, kn, vn, 1, d)
     assert status == [0, 0] and np.isfinite(out).all() and np.isfinite(lse).all()
@@ -423,7 +440,7 @@ def test_blocks_of_very_different_sizes(B, d, k):
     """V blocks 2^40 apart, K blocks 2^-60: what is large and hardly seen, and what is small and seen, in one row."""
     rng = np.random.default_rng(8)
     n_q, lens = (k + 1) ** 2, [500]
-    pool, table = random_cache(rng, lens, 1, d, 5)
+    pool, table = random_cache(rng, lens, 1, d, WIDE if k == 6 else 5)
     for j in range(4):
         sc = kvb._views(pool[table[0, j], 0], d)[2]
         sc[:, 1] *= np.float32(2.0 ** 20) if j == 1 else np.float32(2.0 ** -20) if j == 2 else 1
