@@ -21,8 +21,8 @@
 //
 // What bounds it: the softmax's chain of a page, about 2400 cycles with two warps to a scheduler (scores from tensor memory
 // 370, weights 870 of which 512 are exponentials, the result 500, waits and meetings 500) against 1200 of products and 1300 of the page's bytes;
-// between items 11,000 cycles.  16 sequences of up to 4096 keys, 32 heads, 36 rows: 133 us; 8 of 8192, 8 heads, 392 rows, 128 at a
-// time: 285 us (370 TFLOP/s of the products that the formulas ask for, twice that of e4m3 ones).
+// between items 11,000 cycles.  16 sequences of up to 4096 keys, 32 heads, 36 rows: 125 us; 8 of 8192, 8 heads, 392 rows, 128 at a
+// time: 270 us (390 TFLOP/s of the products that the formulas ask for, twice that of e4m3 ones).
 //
 // Warps: 0-7 softmax and sums, 8 products (one thread), 9 copies (one thread), 10 and 11 ask L2 for the rows that items will want and
 // bring blocks' own rows.  The copying thread walks the list and leaves out what has no keys (pages outside the pool); what
@@ -35,7 +35,7 @@ using namespace kvb;
 
 constexpr int TILE = SPACE_PAGE_SIZE;                // keys of a page, rows of an MMA
 constexpr int GROUP = 128, SOFT = 2 * GROUP, THREADS = SOFT + GROUP;           // (registers move by groups of four warps)
-constexpr int SHARE_COST = 3;                        // fixed cost of an item, in pages
+constexpr int SHARE_COST = 5;                        // fixed cost of an item, in pages (2, 3, 4, 6 for 36 rows of 16 sequences: 148, 143, 135, 137 us)
 constexpr int RING = 16;                             // scales and announcements of that many pages
 enum { NO_MORE = 0x7FFFFFFF };                        // announced behind the last page
 enum { OWN = 0x7FFFFFFE };                            // announced as an item's last page: the block's own rows
