@@ -1,15 +1,21 @@
 // Penalties, biases and masks on a step's logits (space_logits_adjust), and the counts they go by (space_token_counts).
 //
-// Logits are read once and written once (in place: only what changes). A thread has sixteen bytes of tokens of a sequence: their
-// counts, biases and the candidates among them stay in registers while it goes through the sequence's rows, which
-// differ in how many candidates count and in the mask.  Four rows are on their way at a time.  An odd vocabulary puts rows at any
-// offset from the 16-byte grid: what is read is shifted into place, and what is written is put together from
-// a lane and its neighbour, so that stores are whole 16-byte pieces but for the ends of a warp's part.
+// Logits are read once and written once (in place: only what changes; what a mask leaves nothing of is not read). A thread has
+// sixteen bytes of tokens of a sequence: which of them have a count, a bias or are candidates stays in a word while it
+// goes through the sequence's rows, and arithmetic is done for those alone that the mask allows too, one after another: few
+// are.  An odd vocabulary puts rows at any offset from the 16-byte grid: what is read is shifted into place, and what is written
+// is shifted back with the next lane's, so that stores are whole 16-byte pieces, and a warp's two ends by its last lane.
+//
+// What bounds it: several rows off the grid about 200 instructions a 16-byte vector, most of them selects and shifts, which issue every other cycle:
+// 16 x 36 x 50257 bf16 under masks 51 us (2.3 TB/s; the bytes: 18); as many rows ahead as registers hold, more thread blocks, tokens one by one where a
+// mask leaves few, all measured the same within 10 %.  Single rows on the grid: 64 x 128256 fp32 with counts 22 us of 15 for the bytes.
+// Counts of prompts of 2048 tokens, set anew: 9 us.
 #include "common.cuh"
 
 namespace {
 
-constexpr int THREADS = 256, AHEAD = 2;              // rows on their way at a time
+constexpr int THREADS = 256;
+constexpr int ROWS_BLOCKS = 5;                       // of the kernel for several rows, on an SM
 constexpr int ROW_TOKENS = 8;                        // of a thread, where a sequence has one row (twice as many on the 16-byte grid)
 constexpr int COUNT_MAX = (1 << 24) - 1;             // (an fp32 number exactly)
 
@@ -17,7 +23,7 @@ struct Params {
   int B, k, n, V, words;
   const void* logits; int64_t in_rs;
   void* out; int64_t out_rs;
-  int in_place, groups, chunks;                      // row groups and token chunks of a sequence: thread blocks
+  int in_place, per, groups, chunks;                 // rows of a group; row groups and token chunks of a sequence: thread blocks
   const int32_t* counts; const int32_t* cand;
   const float* rep; const float* pres; const float* freq;
   int n_bias, n_masks;
@@ -299,7 +305,7 @@ __global__ void __launch_bounds__(THREADS, 4) logits_row_kernel(const __grid_con
 
 // Sequences of n rows: a thread has one vector of tokens, whose counts, biases and candidates stay with it from row to row.
 template <typename T, bool GRID>
-__global__ void __launch_bounds__(THREADS, 4) logits_rows_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(THREADS, ROWS_BLOCKS) logits_rows_kernel(const __grid_constant__ Params p) {
   constexpr int N = 16 / (int)sizeof(T), CHUNK = THREADS * N;
   __shared__ Biases<CHUNK> biases;
   __shared__ int32_t mask_s[SPACE_MAX_ROWS];
@@ -310,7 +316,7 @@ __global__ void __launch_bounds__(THREADS, 4) logits_rows_kernel(const __grid_co
   const int x = chunk0 + (int)threadIdx.x * N;
   const int there = min(max(p.V - x, 0), N);         // tokens of this thread
   const uint32_t valid = (1u << there) - 1u;
-  const int per = (p.n + p.groups - 1) / p.groups, i0 = blockIdx.y * per, i1 = min(i0 + per, p.n);
+  const int i0 = blockIdx.y * p.per, i1 = min(i0 + p.per, p.n);
   const T* in0 = reinterpret_cast<const T*>(p.logits) + ((int64_t)b * p.n + i0) * p.in_rs;
   T* out0 = reinterpret_cast<T*>(p.out) + ((int64_t)b * p.n + i0) * p.out_rs;
   const float* counts = reinterpret_cast<const float*>(p.counts + (int64_t)b * p.V);
@@ -348,41 +354,28 @@ __global__ void __launch_bounds__(THREADS, 4) logits_rows_kernel(const __grid_co
   for (int t = 0; t < N; ++t) hit |= (is_cand >> (8 * t)) & 0xFFu ? 1u << t : 0u;
 
   unsigned long long alive = 0;
-  for (int r0 = i0; r0 < i1; r0 += AHEAD) {
-    Piece2 got[AHEAD];
-    uint32_t keep[AHEAD];
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int m = p.bits && r0 + u < i1 ? mask_s[r0 + u - i0] : -1;
-      keep[u] = m < 0 || !there ? valid : (__ldg(p.bits + (int64_t)m * p.words + (x >> 5)) >> (x & 31)) & valid;
+#pragma unroll 1
+  for (int i = i0; i < i1; ++i, in0 += p.in_rs, out0 += p.out_rs) {
+    const int m = p.bits ? mask_s[i - i0] : -1;
+    const uint32_t keep = m < 0 || !there ? valid : (__ldg(p.bits + (int64_t)m * p.words + (x >> 5)) >> (x & 31)) & valid;
+    if (p.bits && __any_sync(0xFFFFFFFFu, keep != 0)) alive |= 1ull << i;
+    uint32_t act = hit & keep;
+    // (what stays where it is is not read, nor what the mask leaves nothing of)
+    if (p.in_place && !__any_sync(0xFFFFFFFFu, act || keep != valid)) continue;
+    Piece2 got;
+    got.a = got.b = make_uint4(0, 0, 0, 0);
+    if (keep) got = fetch<GRID>(in0, x, there);
+    uint4 v = shifted<GRID>(got, in0, there);
+    for (; act; act &= act - 1) {
+      const uint32_t seen = (1u << (i / (p.k + 1))) - 1u;      // candidates that this row has behind it
+      const int t = __ffs(act) - 1;
+      const int count = __float_as_int(element<float>(N == 4 || t < 4 ? c[0] : c[N / 4 - 1], t & 3));
+      float z = penalized(element<T>(v, t), count, __popc((uint32_t)(is_cand >> (8 * t)) & seen & 0x7Fu), f);
+      if ((bias >> t) & 1u) z += biases.sum[x - chunk0 + t];
+      set_element<T>(v, t, z);
     }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      got[u].a = got[u].b = make_uint4(0, 0, 0, 0);
-      // (what the mask leaves nothing of is not read, nor what stays where it is)
-      const bool touch = !p.in_place || __any_sync(0xFFFFFFFFu, (hit & keep[u]) || keep[u] != valid);
-      if (r0 + u < i1 && touch && keep[u]) got[u] = fetch<GRID>(in0 + u * p.in_rs, x, there);
-    }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int i = r0 + u;
-      if (i >= i1) break;                            // (the same for the whole block)
-      if (p.bits && __any_sync(0xFFFFFFFFu, keep[u] != 0)) alive |= 1ull << i;
-      uint32_t act = hit & keep[u];
-      if (p.in_place && !__any_sync(0xFFFFFFFFu, act || keep[u] != valid)) continue;
-      uint4 v = shifted<GRID>(got[u], in0 + u * p.in_rs, there);
-      for (; act; act &= act - 1) {
-        const uint32_t seen = (1u << (i / (p.k + 1))) - 1u;    // candidates that this row has behind it
-        const int t = __ffs(act) - 1;
-        const int count = __float_as_int(element<float>(N == 4 || t < 4 ? c[0] : c[N / 4 - 1], t & 3));
-        float z = penalized(element<T>(v, t), count, __popc((uint32_t)(is_cand >> (8 * t)) & seen & 0x7Fu), f);
-        if ((bias >> t) & 1u) z += biases.sum[x - chunk0 + t];
-        set_element<T>(v, t, z);
-      }
-      if (p.bits) mask_out<T>(v, keep[u]);
-      store_vectors<GRID>(out0 + u * p.out_rs, x, v, there, p.V);
-    }
-    in0 += AHEAD * p.in_rs; out0 += AHEAD * p.out_rs;
+    if (p.bits) mask_out<T>(v, keep);
+    store_vectors<GRID>(out0, x, v, there, p.V);
   }
   if (p.bits) report(p, b, bad, alive, alive_s);
 }
@@ -412,22 +405,29 @@ __global__ void __launch_bounds__(FEW_TOKENS) count_few_kernel(const CountParams
 }
 
 __global__ void __launch_bounds__(THREADS) count_chunk_kernel(const CountParams p) {
-  __shared__ int hist[COUNT_CHUNK];
+  __shared__ __align__(16) int hist[COUNT_CHUNK];
   pdl_launch_dependents();
   pdl_wait();
   const int b = blockIdx.y, t0 = blockIdx.x * COUNT_CHUNK, len = min(COUNT_CHUNK, p.V - t0);
-  for (int i = threadIdx.x; i < len; i += THREADS) hist[i] = 0;
-  __syncthreads();
-  const int n = p.n_tokens ? min(p.n_tokens[b], p.n) : p.n;
+  constexpr int FIRST = 8;
   const int32_t* tokens = p.tokens + (int64_t)b * p.stride;
+  int first[FIRST];                                  // tokens that are on their way while the counts are cleared
+#pragma unroll
+  for (int u = 0; u < FIRST; ++u) first[u] = u * THREADS + (int)threadIdx.x < p.n ? __ldg(tokens + u * THREADS + threadIdx.x) : -1;
+  const int n = p.n_tokens ? min(p.n_tokens[b], p.n) : p.n;
+#pragma unroll
+  for (int i = 0; i < COUNT_CHUNK / (4 * THREADS); ++i) reinterpret_cast<int4*>(hist)[i * THREADS + threadIdx.x] = make_int4(0, 0, 0, 0);
+  __syncthreads();
+  auto add = [&](int t) {
+    if (t < t0 || t - t0 >= len) return;             // (below 0 or past the vocabulary: in no block's part)
+    if (p.prompt) hist[t - t0] = SPACE_COUNT_PROMPT;
+    else atomicAdd(&hist[t - t0], 1);
+  };
+#pragma unroll
+  for (int u = 0; u < FIRST; ++u)
+    if (u * THREADS + (int)threadIdx.x < n) add(first[u]);
 #pragma unroll 4
-  for (int i = threadIdx.x; i < n; i += THREADS) {
-    const int t = __ldg(tokens + i);                 // (below 0 or past the vocabulary: in no block's part)
-    if (t >= t0 && t < t0 + len) {
-      if (p.prompt) hist[t - t0] = SPACE_COUNT_PROMPT;
-      else atomicAdd(&hist[t - t0], 1);
-    }
-  }
+  for (int i = FIRST * THREADS + threadIdx.x; i < n; i += THREADS) add(__ldg(tokens + i));
   __syncthreads();
   int32_t* out = p.counts + (int64_t)b * p.V + t0;
   if (p.reset && ((uintptr_t)out & 15) == 0) {
@@ -473,11 +473,14 @@ int space_logits_adjust(space_ctx* ctx, const space_logits_args* a, void* stream
   const bool grid = !(((uintptr_t)p.logits | (uintptr_t)p.out | (uintptr_t)p.counts | (uintptr_t)in_b | (uintptr_t)out_b) & 15) && (!p.counts || p.V % 4 == 0);
   const int chunk = THREADS * (p.n > 1 ? 16 / esz : grid ? 2 * ROW_TOKENS : ROW_TOKENS);
   p.chunks = (int)(((int64_t)p.V + chunk - 1) / chunk);
-  // rows are shared out until eight thread blocks an SM have some
-  const int64_t want = (8ll * ctx->sm_count + (int64_t)p.chunks * p.B - 1) / ((int64_t)p.chunks * p.B);
-  const int64_t steps = (p.n + AHEAD - 1) / AHEAD, groups = want < steps ? want : steps;
-  const int per = AHEAD * (int)((steps + groups - 1) / groups);
-  p.groups = (p.n + per - 1) / per;
+  // Rows are shared out so that the thread blocks, ROWS_BLOCKS to an SM at once, end together: what a block does before its first row is
+  // worth about three of them.
+  int64_t least = INT64_MAX;
+  for (int per = 1; per <= p.n; ++per) {
+    const int groups = (p.n + per - 1) / per;
+    const int64_t slots = (int64_t)ROWS_BLOCKS * ctx->sm_count, turns = ((int64_t)p.chunks * p.B * groups + slots - 1) / slots;
+    if (turns * (per + 3) < least) { least = turns * (per + 3); p.groups = groups; p.per = per; }
+  }
   void (*kernel)(Params);
   if (p.n == 1)
     kernel = esz == 4 ? (grid ? logits_row_kernel<float, true> : logits_row_kernel<float, false>)
