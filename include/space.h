@@ -612,7 +612,7 @@ int64_t space_kvb_page_bytes(int32_t n_kv_heads, int32_t head_dim);
 /* Puts rows behind the cached ones, as space_kvq_append does: row g * row_step of k_new / v_new becomes cache row
  * kv_len[b] + g for g < count[b] + count_bias.  With rope.table the keys are rotated on the way (rope.pos [B, rows]) and, where q is
  * given, the same source rows of q into q_out.  Whether a sequence fits, bad pages, errors and the rest: as space_kvq_append;
- * UNSUPPORTED (rot_dim).  A sequence that does not fit keeps its q_out too. */
+ * UNSUPPORTED (rot_dim; more than 2^31 - 1 blocks of 32 rows and heads).  A sequence that does not fit keeps its q_out too. */
 typedef struct {
   int32_t batch;
   int32_t rows;                /* rows per sequence in k_new / v_new                               */

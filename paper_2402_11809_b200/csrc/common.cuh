@@ -171,7 +171,7 @@ struct space_ctx {
   int* lm_counter;         // {arrival counter, first timeout site}
   unsigned long long* logits_alive;  // per sequence: rows that a mask leaves a token (self-resetting, as the next)
   int* logits_arrived;     // and the thread blocks that have said which
-  int* kvb_arrived;        // attention over the 8-bit cache: pieces of an item that are stored, per (sequence, kv head, 32 query rows)
+  int* kvb_arrived;        // attention over the 8-bit cache: pieces of an item that are stored, per (sequence, kv head, query rows of an item)
   // staging for space_step_host
   char* stage;
   char* host_small;        // pinned host mirror of the staging area's small per-sequence arrays (host_staging only)

