@@ -140,6 +140,13 @@ __device__ __forceinline__ void bring_own(const Params& p, int b, int h, unsigne
 #pragma unroll
     for (int j = 0; j < BATCH; ++j) {
       const int r = r0 + j * PER;
+      unsigned char* at = ks + (x >> 2) * F::K_COLS + 16 * r + 4 * (x & 3);
+      if (r >= p.n_q) {                              // (the same for a row's lanes)
+        *reinterpret_cast<uint32_t*>(at) = 0;
+        *reinterpret_cast<uint32_t*>(at + 16 * SPACE_MAX_ROWS) = 0;
+        if (x == 0) sc[r] = make_float2(1.f, 0.f);
+        continue;
+      }
       k[j] = make_uint2(kvq::finite_pair(k[j].x), kvq::finite_pair(k[j].y));
       v[j] = make_uint2(kvq::finite_pair(v[j].x), kvq::finite_pair(v[j].y));
       const uint32_t kt = __reduce_max_sync(lanes, kvq::max_bits(make_uint4(k[j].x, k[j].y, 0, 0)));
@@ -148,7 +155,6 @@ __device__ __forceinline__ void bring_own(const Params& p, int b, int h, unsigne
       const float up = pow2(-ke);
       uint32_t w0, w1;
       split4(kvq::bf_lo(k[j].x) * up, kvq::bf_hi(k[j].x) * up, kvq::bf_lo(k[j].y) * up, kvq::bf_hi(k[j].y) * up, w0, w1);
-      unsigned char* at = ks + (x >> 2) * F::K_COLS + 16 * r + 4 * (x & 3);
       *reinterpret_cast<uint32_t*>(at) = w0;
       *reinterpret_cast<uint32_t*>(at + 16 * SPACE_MAX_ROWS) = w1;
       if (x == 0) sc[r] = make_float2(pow2(ke), (float)ve);
@@ -162,6 +168,15 @@ __device__ __forceinline__ void bring_own(const Params& p, int b, int h, unsigne
   const int c = 2 * (t % (DH / 2)), q0 = t / (DH / 2);
 #pragma unroll 2
   for (int q = q0; q < SPACE_MAX_ROWS / 4; q += PARTS) {
+    unsigned char* at = vs + (q >> 2) * F::V_ROWS + 16 * c + 4 * (q & 3);
+    if (4 * q >= p.n_q) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        *reinterpret_cast<uint32_t*>(at + 16 * i) = 0;
+        *reinterpret_cast<uint32_t*>(at + 16 * i + 4 * F::V_ROWS) = 0;
+      }
+      continue;
+    }
     uint32_t w[4];
     float up[4];
 #pragma unroll
@@ -172,7 +187,6 @@ __device__ __forceinline__ void bring_own(const Params& p, int b, int h, unsigne
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) w[j] = kvq::finite_pair(w[j]);
-    unsigned char* at = vs + (q >> 2) * F::V_ROWS + 16 * c + 4 * (q & 3);
     uint32_t w0, w1;
     split4(kvq::bf_lo(w[0]) * up[0], kvq::bf_lo(w[1]) * up[1], kvq::bf_lo(w[2]) * up[2], kvq::bf_lo(w[3]) * up[3], w0, w1);
     *reinterpret_cast<uint32_t*>(at) = w0;

@@ -56,9 +56,9 @@ __device__ __forceinline__ uint32_t coarser(uint32_t w, float ratio) {
 // Queries of sequence b, beside the append.
 template <int DH>
 __device__ __forceinline__ void turn_queries(const AppendParams& p, int b, int block) {
-  const int task = block * (THREADS / 32) + (int)(threadIdx.x >> 5), g = task / p.share, part = task - g * p.share;
-  const int L = p.kv_len[b];
-  if (g >= append_count(p, b, L)) return;
+  const uint32_t task = (uint32_t)block * (THREADS / 32) + (threadIdx.x >> 5), row = task / (uint32_t)p.share;
+  const int L = p.kv_len[b], n = append_count(p, b, L), g = (int)row, part = (int)(task - row * (uint32_t)p.share);
+  if (n <= 0 || row >= (uint32_t)n) return;
   const int64_t r = (int64_t)g * p.step;
   bool bad;
   rope::Turn u;

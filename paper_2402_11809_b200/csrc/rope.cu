@@ -29,7 +29,8 @@ template <int DH>
 __global__ void __launch_bounds__(THREADS, 4) rope_append_kernel(const __grid_constant__ Params p) {
   pdl_launch_dependents();
   pdl_wait();
-  const int b = blockIdx.y, task = blockIdx.x * WARPS + (threadIdx.x >> 5), r = task / p.share, part = task - r * p.share;
+  const uint32_t task = blockIdx.x * WARPS + (threadIdx.x >> 5), row_of_task = task / (uint32_t)p.share;
+  const int b = blockIdx.y, part = (int)(task - row_of_task * (uint32_t)p.share);
   const int L = p.kv_len[b];
   const int want = p.count ? p.count[b] : p.rows;
   const int n = max(0, min(want, p.rows));
@@ -38,7 +39,8 @@ __global__ void __launch_bounds__(THREADS, 4) rope_append_kernel(const __grid_co
     if (!fits && p.status) atomicOr(p.status + b, SPACE_ST_CAPACITY);
     if (p.len_out) p.len_out[b] = fits ? L + n : L;
   }
-  if (!fits || r >= n) return;
+  if (!fits || row_of_task >= (uint32_t)n) return;
+  const int r = (int)row_of_task;
   bool bad;
   const float* row = table_row(p.t, b, p.rows, r, (int64_t)L + r, bad);
   Turn u;
