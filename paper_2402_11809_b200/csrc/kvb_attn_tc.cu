@@ -466,8 +466,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
     // What is announced of page m.
     int next_item, next_page;
     auto look = [&](uint32_t m) {
-      hold(SAID + m % RING, m / RING, 12);
-      next_item = *abort_flag ? NO_MORE : desc[m % RING].x;
+      const bool said = hold(SAID + m % RING, m / RING, 12);
+      next_item = said ? desc[m % RING].x : NO_MORE;
       next_page = desc[m % RING].y;
     };
     // The query row of the item that wk stands at, this thread's half of it: as two terms into a buffer, if the item has pages.
@@ -555,7 +555,10 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
         const int t = next_page;
         const uint32_t s = cached % STAGES;          // (of a page of the cache)
         const uint32_t TM_SM = TM_S + lanes + (m & 1) * TILE;                  // the page's scores
-        const float2* sc = reinterpret_cast<const float2*>(sm + S::SCALE_OFF + (m % RING) * 32) + (key0 >> 5);
+        constexpr int NC = (KEYS + 31) / 32, N1 = KEYS < 32 ? KEYS : 32;       // 32 keys share their scales
+        float2 sc[NC];
+#pragma unroll
+        for (int k = 0; k < NC; ++k) sc[k] = *(reinterpret_cast<const float2*>(sm + S::SCALE_OFF + (m % RING) * 32) + (key0 >> 5) + k);
         const int vis0 = L - (t == OWN ? 0 : t) * TILE, vis = vis0 - key0;            // visible keys of the page, and of this thread
         if (vis0 < TILE && t != OWN) {               // what lies behind the last row must not count, whatever it is
           hold(FULLV + s, cached / STAGES, 14);
@@ -577,7 +580,6 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
         }
         hold(SDONE + (m & 1), m >> 1, 15);
         tc_fence_after();
-        constexpr int NC = (KEYS + 31) / 32, N1 = KEYS < 32 ? KEYS : 32;       // 32 keys share their scales
         uint32_t v[KEYS];
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
