@@ -515,6 +515,46 @@ def test_captured_and_on_another_stream(B, k):
             check(f64(out), want[1], *want)
 
 
+def test_two_contexts_on_two_streams_at_once(B):
+    """Calls of both forms in turn on each stream, the streams not waiting for each other, behind appends that move the lengths on."""
+    d, H, n, steps = 128, 4, 3, 12
+    rng = np.random.default_rng(13)
+    runs = []
+    for i in range(2):
+        pool, table = random_cache(rng, [900] * n, H, d, 8)
+        runs.append(dict(ctx=context(B, n, 2 * H, H, d), stream=torch.cuda.Stream(), table=dev(table), first=pool))
+    new = [dev(bits(rng, n, 16, h, d)) for h in (2 * H, H, H)]
+
+    def go(r, pool, lens, outs):
+        for j in range(steps):
+            k = (1, 3, 2)[j % 3]
+            n_q, out = (k + 1) ** 2, outs[j]
+            q, kn, vn = (x[:, :n_q] for x in new)
+            r["keep"].append(a := r["ctx"].kvb_attn_args(q, pool, r["table"], lens[j], out, k, 0.09, k_new=kn, v_new=vn))
+            r["ctx"].space_kvb_attn_step(a)
+            r["keep"].append(a := r["ctx"].kvb_append_args(kn, vn, pool, r["table"], lens[j], row_step=k + 1, kv_len_out=lens[j + 1]))
+            r["ctx"].space_kvb_append(a)
+    got = []
+    for at_once in (False, True):
+        work = []
+        for r in runs:
+            r["keep"] = []
+            lens = [i32([700, 13, 0]) for _ in range(steps + 1)]
+            outs = [torch.zeros(n, ((1, 3, 2)[j % 3] + 1) ** 2, 2 * H, d, dtype=torch.bfloat16, device="cuda") for j in range(steps)]
+            work.append((r, dev(r["first"]), lens, outs))
+        torch.cuda.synchronize()
+        for w in work:
+            with torch.cuda.stream(w[0]["stream"] if at_once else torch.cuda.current_stream()):
+                go(*w)
+            if not at_once:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        got.append([(w[1], w[2][-1], w[3]) for w in work])
+    for (p0, l0, o0), (p1, l1, o1) in zip(*got):
+        assert torch.equal(p0, p1) and torch.equal(l0, l1) and l0.tolist() == [L + 4 * (2 + 4 + 3) for L in (700, 13, 0)]
+        assert all(torch.equal(x, y) for x, y in zip(o0, o1))
+
+
 def test_page_moves(B):
     """space_pages_copy takes the 8-bit pool's pages whole or in rows of a page."""
     d, H = 64, 3
