@@ -599,6 +599,8 @@ int space_rope_append(space_ctx* ctx, const space_rope_args* args, void* stream)
  * NaN counts as 0 and an infinity as the largest finite bf16 (SPACE_ST_NONFINITE).  Rows come one after another: e covers
  * the rows that a block has had since its first row was last written, and where a later row raises it the block's earlier
  * codes are rounded once more, to multiples of 2^(e - 9) (all others stay exactly what they were).
+ * (So a page that sequences share is copied before one of them writes into it, space_pager_make_writable: the block's earlier
+ * rows are the others' too.)
  *
  * Bytes of a page, per kv head (head_stride apart), the order of the attention's tensor-core operands:
  *   K codes [d/16][128][16]: channel c of row r in byte (c/16) 2048 + 16 r + c%16
