@@ -626,7 +626,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
         o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
       }
       if (whole) store_row4<DH>(p, b, h, r0 + r, c4, o);
-      else __stcg(reinterpret_cast<float4*>(p.part + (int64_t)slot * SLOT + r * DH) + c4, o);
+      else __stcg(reinterpret_cast<float4*>(p.part + (int64_t)slot * SLOT + r * DH) + c4, held(o));
       if (c4 == 0) {
         float M, l;
         total(r, M, l);

@@ -51,15 +51,21 @@ __device__ __forceinline__ void split4(float a, float b, float c, float d, uint3
   w1 = codes4(a, b, c, d);
 }
 
+// A mean of V rows is a number of their type; weights are rounded, their sum is not, so that a mean of the largest ones would pass
+// them.  (NaN stays.)
+__device__ __forceinline__ float4 held(float4 o) {
+  const float most = 3.3895313892515355e38f;
+  auto one = [&](float v) { return v > most ? most : v < -most ? -most : v; };
+  return make_float4(one(o.x), one(o.y), one(o.z), one(o.w));
+}
+
 // Four channels of a finished row.
 template <int DH>
 __device__ __forceinline__ void store_row4(const Params& p, int b, int h, int r, int c4, float4 o) {
   int i, hq;
   row_of(p, h, r, i, hq);
-  // weights are rounded, their sum is not: a mean of the largest numbers would pass them (NaN stays)
-  const float most = 3.3895313892515355e38f;
-  auto held = [&](float v) { return v > most ? most : v < -most ? -most : v; };
-  const __nv_bfloat162 x = __floats2bfloat162_rn(held(o.x), held(o.y)), y = __floats2bfloat162_rn(held(o.z), held(o.w));
+  o = held(o);
+  const __nv_bfloat162 x = __floats2bfloat162_rn(o.x, o.y), y = __floats2bfloat162_rn(o.z, o.w);
   __nv_bfloat16* dst = p.out + (((int64_t)b * p.n_q + i) * p.H_q + hq) * DH + 4 * c4;
   *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
 }
@@ -70,8 +76,9 @@ __device__ __forceinline__ void store_lse(const Params& p, int b, int h, int r, 
   p.lse[((int64_t)b * p.H_q + hq) * p.n_q + i] = (M + log2f(l)) * 0.6931471805599453f;
 }
 
-// The pieces of an item that was cut over several thread blocks: outputs of their own keys, weighed by l 2^M, always in the
-// same order; called by the block that stored the last of them, by whole warps.  item_at: the item's place in the
+// The pieces of an item that was cut over several thread blocks: outputs of their own keys, weighed by their share l 2^M of all keys,
+// always in the same order (every factor is 1 at most, that of what has been joined so far among them: means of V rows stay as large as
+// those, whatever their sums would be); called by the block that stored the last of them, by whole warps.  item_at: the item's place in the
 // flat list; a block's share can hold the end of one cut item (its second slot) and the start of another (its first one).
 // A thread has four channels of U query rows; the DH / 4 threads of a row look up that many pieces' M and l at
 // once, while BATCH pieces' outputs are on their way.
@@ -122,8 +129,12 @@ __device__ __forceinline__ void join_pieces(const Params& p, const Cut& cut, int
             float sum = w[u];
 #pragma unroll
             for (int k = 1; k < C4; k <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, k);
-            den[u] = fmaf(den[u], down, sum);
-            o[u].x *= down; o[u].y *= down; o[u].z *= down; o[u].w *= down;
+            const float before = den[u] * down;
+            den[u] = before + sum;
+            const float rd = den[u] > 0.f ? 1.f / den[u] : 0.f;                // (a row without keys: zeros; NaN stays)
+            const float f = before * rd;
+            w[u] *= rd;
+            o[u].x *= f; o[u].y *= f; o[u].z *= f; o[u].w *= f;
           }
         }
 #pragma unroll
@@ -139,8 +150,7 @@ __device__ __forceinline__ void join_pieces(const Params& p, const Cut& cut, int
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (idx + tid % 32 + u * threads < n) {
-        const float rd = den[u] > 0.f ? 1.f / den[u] : 0.f;                    // a row without keys: zeros
-        store_row4<DH>(p, b, h, r0 + r[u], c4, make_float4(o[u].x * rd, o[u].y * rd, o[u].z * rd, o[u].w * rd));
+        store_row4<DH>(p, b, h, r0 + r[u], c4, o[u]);
         if (c4 == 0) store_lse(p, b, h, r0 + r[u], M[u], den[u]);
       }
   }

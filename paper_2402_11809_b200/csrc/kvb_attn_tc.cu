@@ -801,7 +801,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
           const int c4 = (hf * (DH / 2) + c0 + c) / 4;
           const float4 o = make_float4(y[0], y[1], y[2], y[3]);
           if (whole) store_row4<DH>(p, b, h, r0 + r, c4, o);
-          else __stcg(reinterpret_cast<float4*>(ps + r * DH) + c4, o);
+          else __stcg(reinterpret_cast<float4*>(ps + r * DH) + c4, held(o));
         }
         soft_sync();
       }
