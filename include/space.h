@@ -596,6 +596,7 @@ int space_rope_append(space_ctx* ctx, const space_rope_args* args, void* stream)
  * Elements are e4m3 numbers (four bits of significance, up to 448); the 32 rows of a block (rows 0..31, 32..63, ..
  * of a page) share a power of two 2^e per kv head, one for K and one for V, and an element stands for code * 2^e:
  *   e = the least whole number with max|x| <= 448 2^e, -100 at least;   code = x / 2^e to the nearest, ties to even.
+ * (At e = 120, where 256 2^e is no bf16 number any more, codes are held to 240.)
  * NaN counts as 0 and an infinity as the largest finite bf16 (SPACE_ST_NONFINITE).  Rows come one after another: e covers
  * the rows that a block has had since its first row was last written, and where a later row raises it the block's earlier
  * codes are rounded once more, to multiples of 2^(e - 9) (all others stay exactly what they were).

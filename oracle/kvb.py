@@ -2,7 +2,7 @@
 
 An element is an e4m3 code times a power of two 2^e that the 32 rows of a block share per kv head: e is the least whole number,
 -100 at least, with max|x| <= 448 2^e; where later rows of a block raise it, the codes of the earlier ones are rounded once
-more.  NaN counts as 0, an infinity as the largest finite bf16.  Plain numpy, from the format's definition
+more.  Codes are held to 240 at e = 120: 256 2^120 is no bf16 number.  NaN counts as 0, an infinity as the largest finite bf16.  Plain numpy, from the format's definition
 (include/space.h, space_kvb_cache).
 """
 import numpy as np
@@ -58,6 +58,7 @@ def append(pool, table, head, L, k, v):
     """Rows k, v [n, d] (64 bits, finite) behind the L rows of a sequence; pool [n_pages, H, head_bytes] is changed.  Pages
     outside the pool are skipped."""
     n, d = k.shape
+    k, v = (np.clip(x, -240 * 2.0 ** 120, 240 * 2.0 ** 120) for x in (k, v))
     for s0 in range(L // BLOCK * BLOCK, L + n, BLOCK):
         page = table[s0 // PAGE]
         if not 0 <= page < pool.shape[0]:

@@ -17,7 +17,9 @@ namespace {
 using namespace kvb;
 
 constexpr int THREADS = 256;
-constexpr float BF16_MAX = 3.3895313892515355e38f;
+// Elements are held to 240 2^120 in magnitude: 256 2^120, to which larger ones would be rounded, is no bf16 number.
+constexpr float ELEMENT_MAX = 0x1.Ep127f;
+constexpr uint32_t ELEMENT_MAX_BITS = 0x7F70u;       // (as bf16)
 
 struct AppendParams {
   Cache cache;
@@ -46,7 +48,11 @@ struct VTile {
   static __device__ __forceinline__ int at(int group, int c) { return group * GROUP + 16 * c + 4 * (c >> 3); }
 };
 
-// Four codes with their scale's power of two raised.
+__device__ __forceinline__ uint32_t held_pair(uint32_t w) {        // two finite bf16
+  return __vminu2(w & 0x7FFF7FFFu, ELEMENT_MAX_BITS * 0x10001u) | (w & 0x80008000u);
+}
+
+// Four codes with their scale's power of two raised.  (From 2^119 to 2^120: 224 at most.)
 __device__ __forceinline__ uint32_t coarser(uint32_t w, float ratio) {
   const uint32_t lo = halves2(w & 0xFFFFu), hi = halves2(w >> 16);
   const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
@@ -131,6 +137,10 @@ __global__ void __launch_bounds__(THREADS, 4) kvb_append_kernel(const __grid_con
         most[which] = kvq::max_bits(v[which][k]);
       }
     }
+    if (most[1] > ELEMENT_MAX_BITS) {                // (K: once it is turned)
+      v[1][k] = make_uint4(held_pair(v[1][k].x), held_pair(v[1][k].y), held_pair(v[1][k].z), held_pair(v[1][k].w));
+      most[1] = ELEMENT_MAX_BITS;
+    }
     top[1] = fmaxf(top[1], __uint_as_float(most[1] << 16));
     if (p.t.table) {
       rope::turn_row<LANES>(p.t, v[0][k], x, u[k], y[k]);
@@ -143,13 +153,13 @@ __global__ void __launch_bounds__(THREADS, 4) kvb_append_kernel(const __grid_con
       top[0] = fmaxf(top[0], __uint_as_float(most[0] << 16));
     }
   }
-  if (top[0] > BF16_MAX) {                           // (two of the largest numbers turned into one can pass the largest)
-    top[0] = BF16_MAX;
+  if (top[0] > ELEMENT_MAX) {                        // (two of the largest numbers turned into one can pass the largest)
+    top[0] = ELEMENT_MAX;
 #pragma unroll
     for (int k = 0; k < PASSES; ++k)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        y[k][j] = rope::pair(fminf(fmaxf(rope::first_of(y[k][j]), -BF16_MAX), BF16_MAX), fminf(fmaxf(rope::second_of(y[k][j]), -BF16_MAX), BF16_MAX));
+        y[k][j] = rope::pair(fminf(fmaxf(rope::first_of(y[k][j]), -ELEMENT_MAX), ELEMENT_MAX), fminf(fmaxf(rope::second_of(y[k][j]), -ELEMENT_MAX), ELEMENT_MAX));
   }
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
