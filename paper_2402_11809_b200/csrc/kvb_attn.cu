@@ -28,6 +28,8 @@ using namespace kvb;
 
 constexpr int WARPS = PAGE_BLOCKS, THREADS = 32 * WARPS;   // a warp per 32-row block of a page
 constexpr float REF_FAR = 0x1p22f;                   // up to this a reference's rounding moves weights by 2^0.25 at most
+constexpr int ROW_LARGE = 58;                        // (of smaller rows no sum of 128 products passes 2^123)
+constexpr float ROW_DOWN = 0x1p-70f;
 
 // NT: query rows of an item in eights.
 template <int DH, int NT>
@@ -476,25 +478,14 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
         vr[i] = make_uint4(0, 0, 0, 0);
         if (key < p.n_q) vr[i] = *(reinterpret_cast<const uint4*>(p.vn + (int64_t)b * p.n_sb + (int64_t)key * p.n_sr + (int64_t)h * p.n_sh) + lane % LANES);
       }
-      float sc[NT][4], kf[2] = {p.c, p.c};
+      float sc[NT][4];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+      // Rows that hold a number of 2^ROW_LARGE or more, keys and queries (whose factors say so), are taken ROW_DOWN times as large: sums of
+      // products stay numbers.
+      uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int j = 0; j < DH / 32; ++j) top = max(top, kvq::max_bits(kr[i][j]));
-        if (__any_sync(0xFFFFFFFFu, top >= 0x7200u)) { // (from 2^101 on: what is not finite, and sums that fp32 would not hold)
-          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-#pragma unroll
-          for (int j = 0; j < DH / 32; ++j) {
-            kvq::make_finite(kr[i][j]);
-            if (top >= 0x7200u) kr[i][j] = kvq::scale_bf16(kr[i][j], 0x1p-64f);
-          }
-          if (top >= 0x7200u) kf[i] = p.c * 0x1p64f;
-        }
-      }
+      for (int j = 0; j < DH / 32; ++j) top = max(top, max(kvq::max_bits(kr[0][j]), kvq::max_bits(kr[1][j])));
 #pragma unroll
       for (int k = 0; k < DH / 32; ++k) {
 #pragma unroll
@@ -503,6 +494,63 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
           mma_bf16(sc[nt], kr[0][k].x, kr[1][k].x, kr[0][k].y, kr[1][k].y, q.x, q.y);
           mma_bf16(sc[nt], kr[0][k].z, kr[1][k].z, kr[0][k].w, kr[1][k].w, q.z, q.w);
         }
+      }
+      // Rows that hold a number of 2^ROW_LARGE or more, keys and queries (their factors say so), or a key one that is not finite: the
+      // products once more, of such rows times ROW_DOWN, so that their sums are numbers.  (Loaded anew: the rows that were there
+      // have given their registers up.)
+      const float f_large = p.c * pow2(ROW_LARGE - 7);
+      constexpr uint32_t BITS_LARGE = (uint32_t)(ROW_LARGE + 127) << 7;        // (as bf16)
+      if (__any_sync(0xFFFFFFFFu, top >= BITS_LARGE || qf[lane % RT] >= f_large)) {
+        const uint4* key_at[2];
+        bool large[2];                               // such a key 8 i + n8
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int key = min(k0 + 8 * i + n8, p.n_q - 1);                     // (one behind the last: nobody sees it)
+          key_at[i] = reinterpret_cast<const uint4*>(p.kn + (int64_t)b * p.n_sb + (int64_t)key * p.n_sr + (int64_t)h * p.n_sh) + t * (DH / 32);
+          top = 0;
+#pragma unroll 1
+          for (int j = 0; j < DH / 32; ++j) {
+            uint4 v = key_at[i][j];
+            top = max(top, kvq::top_bits(v));
+          }
+          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+          large[i] = top >= BITS_LARGE;
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+#pragma unroll 1
+        for (int j = 0; j < DH / 32; ++j) {
+          uint4 v[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            v[i] = key_at[i][j];
+            kvq::make_finite(v[i]);
+            if (large[i]) v[i] = kvq::scale_bf16(v[i], ROW_DOWN);
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            int i, hq;
+            row_of(p, h, min(r0 + 8 * nt + n8, p.n_q * p.G - 1), i, hq);
+            uint4 q = *(reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh) + t * (DH / 32) + j);
+            if (qf[8 * nt + n8] >= f_large) q = kvq::scale_bf16(q, ROW_DOWN);
+            mma_bf16(sc[nt], v[0].x, v[1].x, v[0].y, v[1].y, q.x, q.y);
+            mma_bf16(sc[nt], v[0].z, v[1].z, v[0].w, v[1].w, q.z, q.w);
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const bool large_row = qf[8 * nt + 2 * t + c] >= f_large;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              float x = sc[nt][2 * i + c];
+              if (large[i]) x *= 1.f / ROW_DOWN;
+              if (large_row) x *= 1.f / ROW_DOWN;
+              sc[nt][2 * i + c] = x > 0x1p127f ? 0x1p127f : x < -0x1p127f ? -0x1p127f : x;
+            }
+          }
       }
       __syncwarp();
 #pragma unroll
@@ -526,7 +574,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const bool vis = (see >> (k0 + 8 * i + n8)) & 1ull;
-            const float x = sc[nt][2 * i + c] * kf[i];       // (a row that is not finite: NaN here, and at the end)
+            const float x = sc[nt][2 * i + c] * p.c;         // (a row that is not finite: NaN here, and at the end)
             y[c][i] = vis ? (x > SCORE_MAX ? SCORE_MAX : x < -SCORE_MAX ? -SCORE_MAX : x) : -CUDART_INF_F;
             top = fmaxf(top, y[c][i]);
           }

@@ -120,3 +120,48 @@ def read(B, ctx, pool, table, n, H, d):
     out = torch.empty(1, n, 2, H, d, dtype=torch.bfloat16, device="cuda")
     ctx.space_kvb_read(ctx.kvb_read_args(pool, dev(table), i32([n]), out[:, :, 0], out[:, :, 1]))
     return out
+
+
+# ------------------------------------------------------------------------------------------------ block rows and query rows far from one
+
+@pytest.mark.parametrize("q_up,k_up", [(70, 70), (100, 100), (125, 125), (30, 100), (125, 10), (60, 50)])
+@pytest.mark.parametrize("d,k", FORMS)
+def test_products_beyond_the_largest_number(B, d, k, q_up, k_up):
+    """Query rows times 2^q_up, block rows times 2^k_up, signs of all kinds: scores are held to 2^29 (log2 units), so that the keys
+    above that, or where there are none all of those below -2^29, count the same."""
+    rng = np.random.default_rng(44)
+    n_q = (k + 1) ** 2
+    pool, table = random_cache(rng, [0, 300], 1, d, WIDE if k == 6 else 3)
+    q, kn, vn = bits(rng, 2, n_q, 2, d), bits(rng, 2, n_q, 1, d), bits(rng, 2, n_q, 1, d)
+    q, kn = (f32_to_bf16_bits((bf16_bits_to_f64(x) * 2.0 ** up).astype(np.float32)) for x, up in ((q, q_up), (kn, k_up)))
+    out, lse, status = run(B, q, pool, table, [0, 300], k, kn, vn, 1, d)
+    assert status == [0, 0] and np.isfinite(out).all() and np.isfinite(lse).all()
+    assert np.abs(lse).max() <= (2.0 ** 29 + 16) * math.log(2) * (1 + 2.0 ** -20)
+    q64, k64, v64, see = bf16_bits_to_f64(q)[0], bf16_bits_to_f64(kn)[0, :, 0], bf16_bits_to_f64(vn)[0, :, 0], kvb.visible(k)
+    clear = 0
+    for hq in range(2):                                                  # sequence 0: the block's rows alone
+        s = q64[:, hq] @ k64.T
+        # a score's sign is known where it stands out of what products and their sums are rounded by
+        known = (np.abs(s) > 2.0 ** -8 * (np.abs(q64[:, hq]) @ np.abs(k64).T)) | ~see
+        for i in np.nonzero(known.all(-1))[0]:
+            up = see[i] & (s[i] > 0)
+            want = v64[up if up.any() else see[i]].mean(0)
+            # even weights, each rounded by 2^-8; rows by 2^-17 of their largest; the output by 2^-8 of itself
+            top = np.abs(v64).max()
+            assert (np.abs(out[0, i, hq] - want) <= (2.0 ** -8 + 2.0 ** -17 + 2.0 ** -8) * top).all()
+            clear += 1
+    assert clear > n_q // 2
+
+
+@pytest.mark.parametrize("q_up,k_up", [(64, -64), (-64, 64), (100, -100), (-90, 90), (30, -30)])
+@pytest.mark.parametrize("d,k", FORMS)
+def test_products_of_large_and_small_rows(B, d, k, q_up, k_up):
+    """Ordinary scores between rows that are far from one."""
+    rng = np.random.default_rng(45)
+    n_q = (k + 1) ** 2
+    pool, table = np.zeros((1, 1, kvb.head_bytes(d)), np.uint8), np.full((2, WIDE if k == 6 else 1), -1, np.int32)
+    q, kn, vn = bits(rng, 2, n_q, 2, d), bits(rng, 2, n_q, 1, d), bits(rng, 2, n_q, 1, d)
+    q, kn = (f32_to_bf16_bits((bf16_bits_to_f64(x) * 2.0 ** up).astype(np.float32)) for x, up in ((q, q_up), (kn, k_up)))
+    out, lse, status = run(B, q, pool, table, [0, 0], k, kn, vn, 1, d)
+    check(out, lse, *kvb.attention(bf16_bits_to_f64(q), pool, table, [0, 0], k, 1 / math.sqrt(d), bf16_bits_to_f64(kn), bf16_bits_to_f64(vn)))
+    assert status == [0, 0]
