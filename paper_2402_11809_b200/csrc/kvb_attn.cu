@@ -495,12 +495,13 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
           mma_bf16(sc[nt], kr[0][k].z, kr[1][k].z, kr[0][k].w, kr[1][k].w, q.z, q.w);
         }
       }
-      // Rows that hold a number of 2^ROW_LARGE or more, keys and queries (their factors say so), or a key one that is not finite: the
-      // products once more, of such rows times ROW_DOWN, so that their sums are numbers.  (Loaded anew: the rows that were there
+      // Rows that hold a number of 2^ROW_LARGE or more, keys and queries (their factors say so), or one that is not finite: the
+      // products once more, of such rows times ROW_DOWN, so that their sums are numbers; of a query row that is not finite with zeros, as over the cache: its keys are
+      // known to be there, and it is made NaN at the end.  (Loaded anew: the rows that were there
       // have given their registers up.)
       const float f_large = p.c * pow2(ROW_LARGE - 7);
       constexpr uint32_t BITS_LARGE = (uint32_t)(ROW_LARGE + 127) << 7;        // (as bf16)
-      if (__any_sync(0xFFFFFFFFu, top >= BITS_LARGE || qf[lane % RT] >= f_large)) {
+      if (__any_sync(0xFFFFFFFFu, top >= BITS_LARGE || !(qf[lane % RT] < f_large))) {
         const uint4* key_at[2];
         bool large[2];                               // such a key 8 i + n8
 #pragma unroll
@@ -533,7 +534,9 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
             int i, hq;
             row_of(p, h, min(r0 + 8 * nt + n8, p.n_q * p.G - 1), i, hq);
             uint4 q = *(reinterpret_cast<const uint4*>(p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_sr + (int64_t)hq * p.q_sh) + t * (DH / 32) + j);
-            if (qf[8 * nt + n8] >= f_large) q = kvq::scale_bf16(q, ROW_DOWN);
+            const float of_row = qf[8 * nt + n8];
+            if (of_row >= f_large) q = kvq::scale_bf16(q, ROW_DOWN);
+            if (of_row != of_row) q = make_uint4(0, 0, 0, 0);
             mma_bf16(sc[nt], v[0].x, v[1].x, v[0].y, v[1].y, q.x, q.y);
             mma_bf16(sc[nt], v[0].z, v[1].z, v[0].w, v[1].w, q.z, q.w);
           }
@@ -574,7 +577,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const bool vis = (see >> (k0 + 8 * i + n8)) & 1ull;
-            const float x = sc[nt][2 * i + c] * p.c;         // (a row that is not finite: NaN here, and at the end)
+            const float x = sc[nt][2 * i + c] * p.c;
             y[c][i] = vis ? (x > SCORE_MAX ? SCORE_MAX : x < -SCORE_MAX ? -SCORE_MAX : x) : -CUDART_INF_F;
             top = fmaxf(top, y[c][i]);
           }

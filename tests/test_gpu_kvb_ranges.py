@@ -165,3 +165,21 @@ def test_products_of_large_and_small_rows(B, d, k, q_up, k_up):
     out, lse, status = run(B, q, pool, table, [0, 0], k, kn, vn, 1, d)
     check(out, lse, *kvb.attention(bf16_bits_to_f64(q), pool, table, [0, 0], k, 1 / math.sqrt(d), bf16_bits_to_f64(kn), bf16_bits_to_f64(vn)))
     assert status == [0, 0]
+
+
+@pytest.mark.parametrize("fill", [0x7FC0, 0x7F80, 0xFF80])
+@pytest.mark.parametrize("d,k", FORMS)
+def test_a_query_row_that_is_not_finite_and_sees_the_block_alone(B, d, k, fill):
+    rng = np.random.default_rng(46)
+    n_q = (k + 1) ** 2
+    pool, table = np.zeros((1, 1, kvb.head_bytes(d)), np.uint8), np.full((2, WIDE if k == 6 else 1), -1, np.int32)
+    q, kn, vn = bits(rng, 2, n_q, 2, d), bits(rng, 2, n_q, 1, d), bits(rng, 2, n_q, 1, d)
+    base = run(B, q, pool, table, [0, 0], k, kn, vn, 1, d)
+    for where in (slice(5, 6), slice(0, d)):
+        q2 = q.copy()
+        q2[0, n_q // 2, 1, where] = fill
+        got = run(B, q2, pool, table, [0, 0], k, kn, vn, 1, d)
+        bad = np.zeros((2, n_q, 2), bool)
+        bad[0, n_q // 2, 1] = True
+        assert np.isnan(got[0][bad]).all() and np.isnan(got[1].transpose(0, 2, 1)[bad]).all()
+        assert (got[0][~bad] == base[0][~bad]).all() and (got[1].transpose(0, 2, 1)[~bad] == base[1].transpose(0, 2, 1)[~bad]).all()
