@@ -676,8 +676,9 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
         const float4 x = *reinterpret_cast<const float4*>(sm + w * S::RING + (r * S::O_PITCH + 4 * c4) * 4);
         o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
       }
+      o = held(o);
       if (whole) store_row4<DH>(p, b, h, r0 + r, c4, o);
-      else __stcg(reinterpret_cast<float4*>(p.part + (int64_t)slot * SLOT + r * DH) + c4, held(o));
+      else __stcg(reinterpret_cast<float4*>(p.part + (int64_t)slot * SLOT + r * DH) + c4, o);
       if (c4 == 0) {
         float M, l;
         total(r, M, l);

@@ -51,8 +51,8 @@ __device__ __forceinline__ void split4(float a, float b, float c, float d, uint3
   w1 = codes4(a, b, c, d);
 }
 
-// A mean of V rows is a number of their type; weights are rounded, their sum is not, so that a mean of the largest ones would pass
-// them.  (NaN stays.)
+// Four channels of a row's mean over an item's, or a piece's, keys.  A mean of V rows is a number of their type; weights are rounded, their
+// sum is not, so that a mean of the largest ones would pass them.  (NaN stays.)
 __device__ __forceinline__ float4 held(float4 o) {
   const float most = 3.3895313892515355e38f;
   auto one = [&](float v) { return v > most ? most : v < -most ? -most : v; };
@@ -64,7 +64,6 @@ template <int DH>
 __device__ __forceinline__ void store_row4(const Params& p, int b, int h, int r, int c4, float4 o) {
   int i, hq;
   row_of(p, h, r, i, hq);
-  o = held(o);
   const __nv_bfloat162 x = __floats2bfloat162_rn(o.x, o.y), y = __floats2bfloat162_rn(o.z, o.w);
   __nv_bfloat16* dst = p.out + (((int64_t)b * p.n_q + i) * p.H_q + hq) * DH + 4 * c4;
   *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
@@ -131,7 +130,7 @@ __device__ __forceinline__ void join_pieces(const Params& p, const Cut& cut, int
             for (int k = 1; k < C4; k <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, k);
             const float before = den[u] * down;
             den[u] = before + sum;
-            const float rd = den[u] > 0.f ? 1.f / den[u] : 0.f;                // (a row without keys: zeros; NaN stays)
+            const float rd = den[u] > 0.f ? __fdividef(1.f, den[u]) : 0.f;     // (a row without keys: zeros; NaN stays)
             const float f = before * rd;
             w[u] *= rd;
             o[u].x *= f; o[u].y *= f; o[u].z *= f; o[u].w *= f;

@@ -799,9 +799,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
             for (int k = 0; k < REP; ++k) y[j] += buf[(c + j) * S::PITCH + hf * GROUP + k * RT + r];
           }
           const int c4 = (hf * (DH / 2) + c0 + c) / 4;
-          const float4 o = make_float4(y[0], y[1], y[2], y[3]);
+          const float4 o = held(make_float4(y[0], y[1], y[2], y[3]));
           if (whole) store_row4<DH>(p, b, h, r0 + r, c4, o);
-          else __stcg(reinterpret_cast<float4*>(ps + r * DH) + c4, held(o));
+          else __stcg(reinterpret_cast<float4*>(ps + r * DH) + c4, o);
         }
         soft_sync();
       }
