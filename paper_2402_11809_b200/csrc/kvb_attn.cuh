@@ -32,6 +32,12 @@ struct Params {
   uint64_t mask[SPACE_MAX_ROWS];                     // Eq. 5: bit j of word i: block row i sees block row j
 };
 
+// One decision of several warps after a wait: `all` is a barrier of them that tells each whether all of them were told that it is there.
+// (While another wait runs out, some can be told so and others that it was given up, and a barrier that only some of them reach has no end.)
+#pragma nv_exec_check_disable
+template <class Hold, class All>
+__host__ __device__ __forceinline__ bool all_told(Hold hold, All all) { return all(hold()); }
+
 // Where a kv head's query row r lies: block row and head.  (G is a power of two.)
 __device__ __forceinline__ void row_of(const Params& p, int h, int r, int& i, int& hq) {
   i = r >> p.gsh;

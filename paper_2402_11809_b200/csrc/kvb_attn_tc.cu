@@ -112,6 +112,12 @@ __device__ __forceinline__ float max16(const uint32_t* s) {
 }
 
 __device__ __forceinline__ void pair_sync() { asm volatile("bar.sync 2, 64;" ::: "memory"); }      // the warps that bring own rows
+__device__ __forceinline__ bool pair_all(bool mine) {                                                // (and whether both may)
+  int all;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 2, 64, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+               : "=r"(all) : "r"((int)mine) : "memory");
+  return all != 0;
+}
 __device__ __forceinline__ void prefetch_line(const char* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // The block's own rows as a page, by two warps: row j's K as two e4m3 terms in rows j and 64 + j of the stage, V likewise in sixteens
@@ -447,9 +453,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
       // ---- the block's own rows, an item ahead
       while (wk.next(prefix, seq_len, p.has_new, share0)) {
         if (!p.has_new || wk.L < 0 || wk.t1 <= wk.cached()) continue;
-        bool ok = true;
-        if (own) ok = hold(FREEK + STAGES, own - 1, 19) && hold(FREEV + STAGES, own - 1, 20);
-        if (__any_sync(0xFFFFFFFFu, !ok)) break;
+        const auto place = [&] { return own == 0 || (hold(FREEK + STAGES, own - 1, 19) && hold(FREEV + STAGES, own - 1, 20)); };
+        if (!all_told(place, pair_all)) break;       // (both warps or none: bring_own has barriers of the two)
         bring_own<DH>(p, wk.b, wk.it / p.n_rt, sm + S::K_OFF + STAGES * F::CODES, sm + S::V_OFF + STAGES * F::CODES,
                       reinterpret_cast<float2*>(sm + S::OWN_OFF), BAR(FULLK + STAGES));
         if ((threadIdx.x & 63) == 0) mbar_arrive(BAR(FULLV + STAGES));

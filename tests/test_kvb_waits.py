@@ -1,0 +1,47 @@
+"""Waits of the attention over the 8-bit cache after one of them has run out, on the host: nobody is left behind."""
+import ctypes as C
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2402_11809_b200 import build
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    so = tmp_path_factory.mktemp("waits") / "kvb_waits.so"
+    cmd = [build._nvcc(), "-gencode", "arch=compute_100a,code=compute_100a", "-O0", "-std=c++17", "-shared", "-Xcompiler", "-fPIC",
+           "-cudart", "static", "-Xlinker", "--unresolved-symbols=ignore-all", os.path.join(HERE, "kvb_waits_host.cu"), "-o", str(so)]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr[-2000:]
+    return C.CDLL(str(so), os.RTLD_LAZY)
+
+
+def bring(lib, answers, alone):
+    a, brought = np.ascontiguousarray(answers, np.int32), np.zeros(2, np.int32)
+    p = lambda x: x.ctypes.data_as(C.c_void_p)  # noqa: E731
+    return lib.host_bring_own(p(a), len(a), int(alone), p(brought)), brought.tolist()
+
+
+ANSWERS = [[[1, 1]] * 5, [[1, 1], [0, 1], [1, 1]], [[1, 1], [1, 0], [1, 1]], [[0, 1]], [[1, 0]], [[0, 0], [1, 1]], [[1, 1], [1, 1], [1, 0], [0, 1]]]
+
+
+@pytest.mark.parametrize("answers", ANSWERS)
+def test_both_warps_go_by_both_answers(lib, answers):
+    stuck, brought = bring(lib, answers, False)
+    n = next((i for i, a in enumerate(answers) if not all(a)), len(answers))
+    assert not stuck and brought == [n, n]
+
+
+def test_answers_of_their_own_leave_a_warp_behind(lib):
+    assert bring(lib, [[1, 1], [1, 0], [1, 1]], True)[0] and not bring(lib, [[1, 1]] * 3, True)[0]
+
+
+def test_the_kernel_leaves_with_both_warps_only():
+    text = open(os.path.join(build.CSRC, "kvb_attn_tc.cu")).read()
+    role = text[text.index("// ---- the block's own rows, an item ahead"):text.index("bring_own<DH>(p, wk.b")]
+    assert role.count("break") == 1 and "if (!all_told(place, pair_all)) break;" in role
