@@ -256,8 +256,9 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
     const int c1 = min(t1, Tc);
 
     // this warp's blocks: rows [32 warp, +32) of pages t0 .. c1-1; a sequence's last page may leave it none
-    int n_blk = *abort_flag ? 0 : max(c1 - t0, 0);   // (after a wait that ran out: no more requests, but every item is counted)
-    if (*abort_flag && p.status && threadIdx.x == 0) atomicOr(p.status + b, SPACE_ST_TIMEOUT);
+    const bool over = __any_sync(0xFFFFFFFFu, *abort_flag);
+    int n_blk = over ? 0 : max(c1 - t0, 0);          // (after a wait that ran out: no more requests, but every item is counted)
+    if (over && p.status && threadIdx.x == 0) atomicOr(p.status + b, SPACE_ST_TIMEOUT);
     if (n_blk > 0 && L - (c1 - 1) * SPACE_PAGE_SIZE <= warp * BLOCK_ROWS) --n_blk;
     const int32_t* table = p.cache.page_table + (int64_t)b * p.cache.pages_per_seq;
     // A block's pieces, one a lane: sixteens of K channels, sixteens of V rows, the scales of two blocks.
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(THREADS, Smem<DH, NT>::CTAS) kvb_attn_kernel(c
     for (int j = 0; j < n_blk; ++j, ++step) {
       request(j + STAGES - 1, step + STAGES - 1);
       const uint32_t s = step % STAGES, parity = (step / STAGES) & 1;
-      if (!wait(bar + 8 * s, parity, abort_flag, p.err, 40 + warp)) {
+      if (!warp_wait(bar + 8 * s, parity, abort_flag, p.err, 40 + warp)) {
         if (p.status && lane == 0) atomicOr(p.status + b, SPACE_ST_TIMEOUT);
         // what is on its way has to land before the ring is used for anything else
         const uint32_t issued = step + min(STAGES, n_blk - j);

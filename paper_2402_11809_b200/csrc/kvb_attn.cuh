@@ -10,6 +10,7 @@ using kvq::lds128;
 using kvq::lds64;
 using kvq::mul2;
 using kvq::wait;
+using kvq::warp_wait;
 using kvq::WAIT_NS;
 using namespace tc;
 

@@ -468,10 +468,10 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
     const uint32_t lanes = (uint32_t)(32 * w4) << 16;
     const int key0 = rep * (TILE / REP) + half * KEYS;       // first of this thread's keys of a page
     const uint32_t TM_C = TM_O + lanes + half * (DH / 2);
-    // What is announced of page m.
+    // What is announced of page m, to whole warps: a warp goes round its loop together.
     int next_item, next_page;
     auto look = [&](uint32_t m) {
-      const bool said = hold(SAID + m % RING, m / RING, 12);
+      const bool said = __all_sync(0xFFFFFFFFu, hold(SAID + m % RING, m / RING, 12));
       next_item = said ? desc[m % RING].x : NO_MORE;
       next_page = desc[m % RING].y;
     };

@@ -53,6 +53,12 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
   return true;
 }
 
+// The same by a whole warp: one answer for all of its lanes.  (Each tries for itself: while another wait runs out, some could find the
+// phase there and others the flag, and the lanes of a warp that goes by it would part for good.)
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* err, int site) {
+  return __all_sync(0xFFFFFFFFu, wait(bar, parity, abort_flag, err, site));
+}
+
 __device__ __forceinline__ uint32_t pack_h(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);

@@ -1,6 +1,7 @@
 """Waits of the attention over the 8-bit cache after one of them has run out, on the host: nobody is left behind."""
 import ctypes as C
 import os
+import re
 import subprocess
 
 import numpy as np
@@ -45,3 +46,20 @@ def test_the_kernel_leaves_with_both_warps_only():
     text = open(os.path.join(build.CSRC, "kvb_attn_tc.cu")).read()
     role = text[text.index("// ---- the block's own rows, an item ahead"):text.index("bring_own<DH>(p, wk.b")]
     assert role.count("break") == 1 and "if (!all_told(place, pair_all)) break;" in role
+
+
+@pytest.mark.parametrize("src", ["kvb_attn.cu", "kvq_attn.cu"])
+def test_a_warp_goes_by_one_answer(src):
+    """What a whole warp goes by, how a wait ended and whether one has run out, is voted on by its lanes."""
+    text = open(os.path.join(build.CSRC, src)).read()
+    kernel = text[text.index("__global__"):]
+    assert not re.search(r"(?<!warp_)wait\(bar", kernel) and "if (!warp_wait(bar" in kernel
+    assert "const bool over = __any_sync(0xFFFFFFFFu, *abort_flag);" in kernel and kernel.count("*abort_flag") == 2      # (the other: cleared)
+    header = open(os.path.join(build.CSRC, "kvq_attn.cuh")).read()
+    assert "return __all_sync(0xFFFFFFFFu, wait(" in header[header.index("bool warp_wait("):]
+
+
+def test_the_softmax_goes_by_announcements_together():
+    text = open(os.path.join(build.CSRC, "kvb_attn_tc.cu")).read()
+    look = text[text.index("auto look = [&]"):text.index("next_page = desc[m")]
+    assert "__all_sync(0xFFFFFFFFu, hold(SAID" in look
