@@ -58,7 +58,7 @@ struct Smem {
   static constexpr int TOPS_OFF = XCH_OFF + 2 * SOFT * 8;    // [2][SOFT] largest elements of query rows' halves, by item
   static constexpr int DESC_OFF = TOPS_OFF + 2 * SOFT * 4;   // [RING] {item of the share, page of it}
   static constexpr int BAR_OFF = DESC_OFF + RING * 8;
-  static constexpr int N_BARS = 4 * (STAGES + 1) + RING + 13;
+  static constexpr int N_BARS = 4 * (STAGES + 1) + RING + 14;
   static constexpr int MISC_OFF = BAR_OFF + N_BARS * 8;
   static constexpr int MASK_OFF = (MISC_OFF + 16 + 7) / 8 * 8;
   static constexpr int TABLE_OFF = MASK_OFF + SPACE_MAX_ROWS * 8;    // prefix[max_batch + 1], seq_len[max_batch]
@@ -242,9 +242,9 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
   auto BAR = [&](int i) { return bar0 + 8u * i; };
   // Of a stage: K, V are there / have been used.  SAID: page m is announced and its scales are there.  QREADY: an item's query rows are
   // there.  SDONE (two, by page): scores.  PREADY: weights (and the result before has been added up).  ODONE: a page's result.
-  // XCH, QTOP (by pair of warps): largest scores, elements of both halves.
+  // XCH, QTOP (by pair of warps): largest scores, elements of both halves.  OVER: all products are done.
   constexpr int FULLK = 0, FULLV = STAGES + 1, FREEK = 2 * (STAGES + 1), FREEV = 3 * (STAGES + 1), SAID = 4 * (STAGES + 1), QREADY = SAID + RING,
-                SDONE = QREADY + 1, PREADY = QREADY + 3, ODONE = QREADY + 4, XCH = QREADY + 5, QTOP = QREADY + 9;
+                SDONE = QREADY + 1, PREADY = QREADY + 3, ODONE = QREADY + 4, XCH = QREADY + 5, QTOP = QREADY + 9, OVER = QREADY + 13;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::MISC_OFF);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF + 4);
   volatile int* last_flag = reinterpret_cast<volatile int*>(sm + S::MISC_OFF + 8);
@@ -257,6 +257,7 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
     *abort_flag = 0;
     for (int s = 0; s < 4 * (STAGES + 1) + RING; ++s) mbar_init(BAR(s), 1);
     mbar_init(BAR(QREADY), 8); mbar_init(BAR(SDONE), 1); mbar_init(BAR(SDONE + 1), 1); mbar_init(BAR(PREADY), 8); mbar_init(BAR(ODONE), 1);
+    mbar_init(BAR(OVER), 1);
     for (int i = 0; i < 4; ++i) { mbar_init(BAR(XCH + i), 2); mbar_init(BAR(QTOP + i), 2); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
@@ -430,7 +431,8 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
         tc_commit(BAR(FREEV + s));
         ++m;
       }
-      if (m) hold(ODONE, m - 1, 10);                 // all products done before tensor memory is released
+      tc_commit(BAR(OVER));                          // all products done before tensor memory is released, after a wait that ran out too
+      mbar_drain_bounded(BAR(OVER), 0, WAIT_NS);
     } else if (warp >= 10) {
       // ---- query rows, and the block's own, of all the share's items: out of HBM before somebody waits for them
       Walk ahead = wk;

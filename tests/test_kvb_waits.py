@@ -63,3 +63,15 @@ def test_the_softmax_goes_by_announcements_together():
     text = open(os.path.join(build.CSRC, "kvb_attn_tc.cu")).read()
     look = text[text.index("auto look = [&]"):text.index("next_page = desc[m")]
     assert "__all_sync(0xFFFFFFFFu, hold(SAID" in look
+
+
+def test_products_are_done_before_tensor_memory_is_released():
+    """Whatever has run out: the thread that asked for the products waits for a barrier of its own, without a look at the flag."""
+    text = open(os.path.join(build.CSRC, "kvb_attn_tc.cu")).read()
+    role = text[text.index("// ---- products: scores of page q"):text.index("} else if (warp >= 10) {")]
+    assert role.rstrip().endswith("mbar_drain_bounded(BAR(OVER), 0, WAIT_NS);")
+    assert role.index("tc_commit(BAR(OVER));") > max(role.rindex("mma8_ts("), role.rindex("++m;"))
+    assert text.count("BAR(OVER)") == 3 and "mbar_init(BAR(OVER), 1);" in text
+    drain = open(os.path.join(build.CSRC, "tc_common.cuh")).read()
+    drain = drain[drain.index("void mbar_drain_bounded("):]
+    assert "abort_flag" not in drain[:drain.index("\n}")]
