@@ -600,11 +600,13 @@ __global__ void __launch_bounds__(THREADS, 1) kvb_attn_tc_kernel(const __grid_co
         auto meet = [&]() {
           float2* xch = reinterpret_cast<float2*>(sm + S::XCH_OFF) + (m & 1) * SOFT;
           xch[threadIdx.x] = make_float2(pm, E);
+          if (REP == 4) tc_fence_before();           // (both halves of 32 columns: a half's weights go where the other one's scores were)
           __syncwarp();
           if (lane == 0) mbar_arrive(BAR(XCH + w4));
           look(m + 1);                               // (meanwhile)
           if (pending) add();
           hold(XCH + w4, m, 16);
+          if (REP == 4) tc_fence_after();
           const float2 other = xch[threadIdx.x ^ GROUP];
           top = fmaxf(pm, other.x); lower = pm - top;
           none = top == -CUDART_INF_F;

@@ -75,3 +75,13 @@ def test_products_are_done_before_tensor_memory_is_released():
     drain = open(os.path.join(build.CSRC, "tc_common.cuh")).read()
     drain = drain[drain.index("void mbar_drain_bounded("):]
     assert "abort_flag" not in drain[:drain.index("\n}")]
+
+
+def test_scores_are_read_before_weights_take_their_place():
+    """Where both halves of a row have the same 32 columns, tensor memory changes hands with their largest scores."""
+    text = open(os.path.join(build.CSRC, "kvb_attn_tc.cu")).read()
+    meet = text[text.index("auto meet = [&]"):text.index("auto put = [&]")]
+    at = [meet.index(x) for x in ("if (REP == 4) tc_fence_before();", "mbar_arrive(BAR(XCH + w4))", "hold(XCH + w4, m, 16)", "if (REP == 4) tc_fence_after();", "xch[threadIdx.x ^ GROUP]")]
+    assert at == sorted(at)
+    read = text.index("tmem_ld16(TM_SM + key0, v)")
+    assert read < text.index("tmem_wait_ld();", read) < text.index("auto meet = [&]")
