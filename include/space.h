@@ -660,7 +660,9 @@ int space_kvb_read(space_ctx* ctx, const space_kvb_read_args* args, void* stream
  * exactly, but elements more than 2^8 times smaller than the largest of their row are rounded, by at most 2^-17 of it; so are
  * the block's own rows where a kv head has more than sixteen query rows (else they are bf16 as they are).  Weights are rounded likewise:
  * each to eight bits, and by at most 2^-18 of the largest among the keys that it goes with (32 or 128 of them; there times
- * their V scales).  Scores, in units of log2, are held to +-2^29: of keys beyond that none is preferred.
+ * their V scales).  Scores, in units of log2, are good up to +-2^29: the largest of 32
+ * neighbouring cached keys, and each of the block's own, is held to that (the others of those 32 in proportion), so that keys beyond it
+ * are not told apart for what they are.
  * Asynchronous on `stream`, no allocation; one call at a time per context (scratch of the context).
  * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE (batch or k beyond the context's), UNSUPPORTED (batch * n_kv_heads *
  * ceil(query rows of a kv head / 8) * (pages_per_seq + 4) above 2e9), CUDA. */

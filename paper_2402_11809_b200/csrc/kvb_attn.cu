@@ -18,9 +18,9 @@
 // The pieces of an item that was cut are joined by the block that stores the last of them, always in the same order.
 // Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT and the block drains and exits.
 //
-// What bounds it: 64 sequences of up to 16384 keys, 8 heads of four rows: 229 us, 5.0 TB/s (0.76 of the copy rate), 54 % of the issue slots,
+// What bounds it: 64 sequences of up to 16384 keys, 8 heads of four rows: 227 us, 5.0 TB/s (0.76 of the copy rate), 54 % of the issue slots,
 // the tensor pipe 31 % of its; with sixteen rows the chain of a block (products, maximum over the lanes, weights, products) with two warps
-// to a scheduler.
+// to a scheduler (255 registers a thread, 16 bytes spilled; of up to eight rows 168 and 20).
 #include "kvb_attn.cuh"
 
 namespace {

@@ -85,7 +85,7 @@ __device__ __forceinline__ void store_lse(const Params& p, int b, int h, int r, 
 // The pieces of an item that was cut over several thread blocks: outputs of their own keys, weighed by their share l 2^M of all keys,
 // always in the same order (every factor is 1 at most, that of what has been joined so far among them: means of V rows stay as large as
 // those, whatever their sums would be); called by the block that stored the last of them, by whole warps.  item_at: the item's place in the
-// flat list; a block's share can hold the end of one cut item (its second slot) and the start of another (its first one).
+// flat list; a block's share can hold the end of one cut item (its first slot) and the start of another (its second one).
 // A thread has four channels of U query rows; the DH / 4 threads of a row look up that many pieces' M and l at
 // once, while BATCH pieces' outputs are on their way.
 template <int DH, int RT, int U, int BATCH>

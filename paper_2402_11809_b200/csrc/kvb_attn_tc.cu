@@ -21,13 +21,15 @@
 //
 // What bounds it: the softmax's chain of a page, about 2400 cycles with two warps to a scheduler (scores from tensor memory
 // 370, weights 870 of which 512 are exponentials, the result 500, waits and meetings 500) against 1200 of products and 1300 of the page's bytes;
-// between items 11,000 cycles.  16 sequences of up to 4096 keys, 32 heads, 36 rows: 125 us; 8 of 8192, 8 heads, 392 rows, 128 at a
-// time: 270 us (390 TFLOP/s of the products that the formulas ask for, twice that of e4m3 ones).
+// between items 11,000 cycles.  16 sequences of up to 4096 keys, 32 heads, 36 rows: 127 us; 8 of 8192, 8 heads, 392 rows, 128 at a
+// time: 272 us (387 TFLOP/s of the products that the formulas ask for, twice that of e4m3 ones).  With 128 rows a thread's scores and
+// sums and a page's result are more than its registers: 286 bytes are spilled (with 64 rows 12, with 32 none; head size 128).
 //
 // Warps: 0-7 softmax and sums, 8 products (one thread), 9 copies (one thread), 10 and 11 ask L2 for the rows that items will want and
 // bring blocks' own rows.  The copying thread walks the list and leaves out what has no keys (pages outside the pool); what
 // there is it announces in order, and everybody else goes by that.
-// Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT, no role leaves its loop early, and the block drains and exits.
+// Every wait is bounded; an expired wait sets SPACE_ST_TIMEOUT.  The warps that copy and that bring rows end there (of the latter both or
+// neither), the others go through the rest of the share with waits that return at once, every warp as one; the block drains and exits.
 #include "kvb_attn.cuh"
 
 namespace {

@@ -7,9 +7,10 @@
 // Queries that are to be turned along have thread blocks of their own behind those.
 // Read back: the same way round.
 //
-// What bounds them: 16 prompts of 512 to 4096 rows, 8 kv heads and 32 turned query heads of 128: 172 us, 4.3 TB/s of HBM and 69 % of the issue
+// What bounds them: 16 prompts of 512 to 4096 rows, 8 kv heads and 32 turned query heads of 128: 172 us, 4.3 TB/s of HBM and 68 % of the issue
 // slots (the queries' 600 MB take half; K and V the rest of the instructions: rotation, largest magnitudes, codes, bytes
 // that change places); read back 56 us, 5.0 TB/s.  Accepted rows of 64 sequences: a launch each, 5 us.
+// (64 registers, 36 bytes of a thread spilled, for head size 128: four thread blocks an SM.)
 #include "kvb_common.cuh"
 #include "rope_common.cuh"
 

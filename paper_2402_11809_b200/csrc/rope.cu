@@ -5,7 +5,7 @@
 // head to head by a stride, products are taken in pairs.  4 x 5700 rows of 32 + 8 + 8 heads of 128: 90.5 us, 6.2 TB/s, 0.94 of the copy
 // rate.  (A list of (row, head) pairs, table entries loaded for each: 193 us; a row of heads over a whole thread block, addresses worked
 // out for every head: 125 us, bound by instructions, 175 a 16-byte vector instead of 79.)  16 x 36 rows of 32 + 32 + 32 heads: 7.9 us with eight warps
-// to a row, 13.4 with two rows to a block.  The order is a projection's output's: q, then K, then V heads of a row.
+// to a row, 13.4 with two rows to a block.  (64 registers, 36 bytes of a thread spilled.)  The order is a projection's output's: q, then K, then V heads of a row.
 #include "rope_common.cuh"
 
 namespace {
